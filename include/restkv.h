@@ -359,6 +359,105 @@ restkv_status restkv_prepare_output_projection(restkv_handle* h, int n_q_heads, 
                                                size_t factor_bytes, restkv_stream stream);
 restkv_status restkv_set_output_projection(restkv_handle* h, const void* factor, int n_q_heads, int head_dim);
 
+/*
+ * A paged cache behind an eviction.  (The paper stops at the compacted K', V'; this is what a decoding loop does with them: rows
+ * are appended to pages, attended over and, for the next eviction, read back.)
+ *
+ * The pool has n_pages pages of page_rows rows for K and as many for V (caller-owned, 16-byte aligned, restkv_paged_page_bytes()
+ * each).  A page holds the rows of all n_kv_heads heads, head by head.  table [batch, table_width] (device int32) names the pages
+ * of every sequence in order: row r of sequence b lies in page table[b, r / page_rows].  lengths (device int32, [batch], or
+ * [batch, n_kv_heads] with lengths_per_head, as restkv_evict_budgets leaves them) are the rows of every sequence, in each of the
+ * calls below with the call's own new tokens included, so that one vector serves all layers of a step.
+ *
+ * Formats (restkv_page_format)
+ *   BF16, F32  rows of head_dim elements, [n_pages, n_kv_heads, page_rows, head_dim]; the dtype of the call has to be the same
+ *   INT4       for dtype BF16 and F32.  Blocks of 16 rows, [n_pages, n_kv_heads, page_rows / 16] of 8 * head_dim + 64 * n_groups
+ *              bytes, n_groups = head_dim / group: the codes of the 16 rows, head_dim / 2 bytes each, then 64 bytes for every
+ *              group: for c = 0..3 the steps (bf16) of the block's rows c, c + 4, c + 8, c + 12 and then their offsets (bf16).
+ *              A value is offset + step * code, rounded once to the dtype where it is read back.  The offset is the minimum of the group's values
+ *              rounded down to bf16, the step a fifteenth of the span from there to their maximum rounded up to bf16 (so that no
+ *              value is clipped), a code the nearest one, ties to even; before that a NaN becomes 0 and what lies beyond +-2^120
+ *              is set there.  Within a row of codes, lowest 4 bits first: K's 32-bit word c * (head_dim / 32) + m has the dims
+ *              32 m + 8 c + (0..7), V's 16-bit unit r * (head_dim / 32) + m the dims 32 m + 4 r + (0..3): what one lane of the attention
+ *              kernel needs lies side by side.
+ * head_dim: a multiple of 32, at most 256 (else RESTKV_ERR_UNSUPPORTED).  page_rows: a multiple of 16.  group: 32, 64 or 128, a divisor of head_dim.
+ *
+ * What is only known on the device is checked there: a length below 0 counts as 0; a row past table_width * page_rows, a table
+ * entry outside [0, n_pages) or a position outside the rotation tables is skipped (not written, not seen, read back as 0) and sets
+ * the sticky status: restkv_poll_status() then returns RESTKV_ERR_INVALID_ARG.  No two rows of a call may lie in the same place.
+ */
+typedef enum { RESTKV_PAGES_BF16 = 0, RESTKV_PAGES_F32 = 1, RESTKV_PAGES_INT4 = 2 } restkv_page_format;
+
+typedef struct {
+  int batch, n_q_heads, n_kv_heads, head_dim;
+  restkv_dtype dtype;   /* of the new rows, the queries and the outputs */
+  int page_format;      /* restkv_page_format */
+  int group;            /* INT4: dims that share a step and an offset */
+  int page_rows, n_pages, table_width;
+  int lengths_per_head; /* 0: lengths [batch], 1: lengths [batch, n_kv_heads] */
+  float softmax_scale;  /* 0 => 1/sqrt(head_dim) */
+  float softcap;        /* 0, or c > 0: a scaled logit s becomes c * tanh(s / c) */
+} restkv_paged;
+
+/* Rows [batch, heads, n_tokens, head_dim] on the device: element strides (multiples of 8, head_dim is contiguous, the base
+ * 16-byte aligned); 0,0,0 => contiguous. */
+typedef struct {
+  const void* data;
+  long long stride_b, stride_h, stride_n;
+} restkv_rows;
+
+/* Position rotation: cos, sin device float [n_positions, rotary_dim / 2] (16-byte aligned).  The first rotary_dim dims (a
+ * multiple of 16) of a row at position p turn in pairs: (a, b) -> (a cos[p,i] - b sin[p,i], b cos[p,i] + a sin[p,i]) with
+ * (a, b) = dims (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved. */
+typedef struct {
+  const float *cos, *sin;
+  int n_positions, rotary_dim, interleaved;
+} restkv_rotation;
+
+/* Bytes of one page of K (those of V are as large); 0 on invalid arguments. */
+size_t restkv_paged_page_bytes(const restkv_paged* cache);
+/* Bytes of workspace (256-byte aligned) that restkv_paged_attend needs for n_tokens query tokens; 0 on invalid arguments. */
+size_t restkv_paged_workspace_bytes(const restkv_paged* cache, int n_tokens);
+
+/*
+ * restkv_paged_append -- K_new, V_new [batch, n_kv_heads, n_tokens, head_dim] become the last rows of the sequences: token i of a
+ * sequence with count c goes to row lengths[b] - c + i.
+ *   counts     device int32 [batch]: tokens of every sequence that are there, the first ones (clamped to [0, n_tokens]); NULL: n_tokens
+ *   rotation   NULL, or the rotation of K_new (and Q) on the way, computed in fp32; host pointer, read during the call
+ *   positions  device int32 [batch, n_tokens]; NULL: a token's position is its row (not with lengths_per_head)
+ *   Q, Q_out   NULL, or queries [batch, n_q_heads, n_tokens, head_dim] and where they go rotated, contiguous, dtype (may be Q's
+ *              own memory if that is contiguous); tokens past a count become 0
+ * Rows of a 16-bit or 32-bit page are rounded once, after the rotation; rows of INT4 pages are quantised from fp32.
+ */
+restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, int n_tokens, const restkv_rows* K_new,
+                                  const restkv_rows* V_new, void* K_pages, void* V_pages, const int32_t* lengths,
+                                  const int32_t* table, const int32_t* counts, const int32_t* positions,
+                                  const restkv_rotation* rotation, const restkv_rows* Q, void* Q_out, restkv_stream stream);
+
+/*
+ * restkv_paged_attend -- attention of the last n_tokens tokens of every sequence over its rows: query i of a sequence with count c
+ * sees the rows below lengths - (c - 1 - i), i.e. all that were there and the call's own tokens up to itself.
+ *   Q     [batch, n_q_heads, n_tokens, head_dim], dtype; query head hq reads KV head hq / (n_q_heads / n_kv_heads)
+ *   out   device [batch, n_q_heads, n_tokens, head_dim] contiguous, dtype
+ *   lse   optional device float [batch, n_q_heads, n_tokens]: natural-log sum of exp of the (capped) logits
+ * A query that sees no row, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32;
+ * steps and offsets of 4-bit rows are applied in fp32.  With bf16 the softmax weights are rounded to bf16 before they meet V.
+ * A row that some query of the call sees has to be finite.
+ */
+restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, int n_tokens, const restkv_rows* Q,
+                                  const void* K_pages, const void* V_pages, const int32_t* lengths, const int32_t* table,
+                                  const int32_t* counts, void* out, float* lse, void* workspace, size_t workspace_bytes,
+                                  restkv_stream stream);
+
+/*
+ * restkv_paged_read -- rows back out of the pages, as restkv_evict and the other calls take them: K_out[b,h,i] = row first + i.
+ *   first         device int32, of the shape of lengths; NULL: 0
+ *   K_out, V_out  device [batch, n_kv_heads, n_rows, head_dim] contiguous, dtype; rows past the sequence's length become 0
+ */
+restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, const void* K_pages, const void* V_pages,
+                                const int32_t* lengths, const int32_t* table, const int32_t* first, int n_rows, void* K_out,
+                                void* V_out, restkv_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -27,6 +27,7 @@ EXPORTS = [
     "restkv_set_kernel_path", "restkv_set_profile_events", "restkv_set_wait_limit", "restkv_set_fused_select", "restkv_last_evict_fused_select",
     "restkv_set_variant", "restkv_evict_budgets",
     "restkv_output_projection_bytes", "restkv_prepare_output_projection", "restkv_set_output_projection",
+    "restkv_paged_page_bytes", "restkv_paged_workspace_bytes", "restkv_paged_append", "restkv_paged_attend", "restkv_paged_read",
 ]
 KERNEL_NONE, KERNEL_PASS1, KERNEL_COMBINE, KERNEL_PASS2, KERNEL_POOL, KERNEL_SELECT, KERNEL_COMPACT = range(7)
 
@@ -56,6 +57,28 @@ INDICATOR_RECONSTRUCTION, INDICATOR_ATTENTION, INDICATOR_ATTENTION_VNORM = 0, 1,
 TEMPORAL_EMA, TEMPORAL_MEAN, TEMPORAL_INV_EMA, TEMPORAL_NONE = 0, 1, 2, 3
 SPATIAL_MEAN, SPATIAL_MAX = 0, 1
 GROUP_MEAN, GROUP_MAX = 0, 1
+
+
+PAGES_BF16, PAGES_F32, PAGES_INT4 = 0, 1, 2
+
+
+class Paged(ctypes.Structure):
+    """restkv_paged: a paged cache's shape and format."""
+    _fields_ = [(name, ctypes.c_int) for name in ("batch", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "page_format", "group",
+                                                  "page_rows", "n_pages", "table_width", "lengths_per_head")]
+    _fields_ += [("softmax_scale", ctypes.c_float), ("softcap", ctypes.c_float)]
+
+
+class Rows(ctypes.Structure):
+    """restkv_rows: rows [batch, heads, n_tokens, head_dim] with their element strides."""
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_longlong), ("stride_h", ctypes.c_longlong),
+                ("stride_n", ctypes.c_longlong)]
+
+
+class Rotation(ctypes.Structure):
+    """restkv_rotation: position tables (kept alive by whoever made them, see make_rotation)."""
+    _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_positions", ctypes.c_int), ("rotary_dim", ctypes.c_int),
+                ("interleaved", ctypes.c_int)]
 
 
 class RestKVError(RuntimeError):
@@ -112,6 +135,14 @@ def load_library() -> ctypes.CDLL:
     lib.restkv_output_projection_bytes.restype = sz
     lib.restkv_prepare_output_projection.argtypes = [vp, ci, ci, ci, ci, vp, vp, sz, vp]
     lib.restkv_set_output_projection.argtypes = [vp, vp, ci, ci]
+    cache, rows = ctypes.POINTER(Paged), ctypes.POINTER(Rows)
+    lib.restkv_paged_page_bytes.argtypes = [cache]
+    lib.restkv_paged_page_bytes.restype = sz
+    lib.restkv_paged_workspace_bytes.argtypes = [cache, ci]
+    lib.restkv_paged_workspace_bytes.restype = sz
+    lib.restkv_paged_append.argtypes = [vp, cache, ci, rows, rows, vp, vp, vp, vp, vp, vp, ctypes.POINTER(Rotation), rows, vp, vp]
+    lib.restkv_paged_attend.argtypes = [vp, cache, ci, rows, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.restkv_paged_read.argtypes = [vp, cache, vp, vp, vp, vp, vp, ci, vp, vp, vp]
     _lib = lib
     return lib
 
@@ -132,6 +163,31 @@ def fixed_pool(width: int = 1, shift: int = 0) -> PoolParams:
 
 def adaptive_pool(beta: float, base_width: int, budget: int) -> PoolParams:
     return PoolParams(POOL_ADAPTIVE, 1, 0, beta, base_width, budget)
+
+
+def make_paged(batch, n_q_heads, n_kv_heads, head_dim, page_format, page_rows, n_pages, table_width, group=0, dtype=BF16,
+               lengths_per_head=0, softmax_scale=0.0, softcap=0.0) -> Paged:
+    return Paged(batch, n_q_heads, n_kv_heads, head_dim, dtype, page_format, group, page_rows, n_pages, table_width,
+                 int(lengths_per_head), softmax_scale, softcap)
+
+
+def make_rotation(cos, sin, rotary_dim, interleaved=False) -> Rotation:
+    """Tables cos, sin [n_positions, rotary_dim / 2] (contiguous float32); the result keeps them alive."""
+    for t in (cos, sin):
+        if tuple(t.shape) != (cos.shape[0], rotary_dim // 2) or not t.is_contiguous() or t.element_size() != 4:
+            raise ValueError("cos and sin have to be contiguous float32 tables [n_positions, rotary_dim / 2]")
+    r = Rotation(cos.data_ptr(), sin.data_ptr(), cos.shape[0], int(rotary_dim), int(bool(interleaved)))
+    r.tables = (cos, sin)
+    return r
+
+
+def make_rows(t) -> Rows:
+    """A tensor [batch, heads, n_tokens, head_dim] of any strides with a contiguous last dimension, as restkv_rows."""
+    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+        raise ValueError("rows have to be [batch, heads, n_tokens, head_dim] with a contiguous last dimension")
+    if not any(t.stride()[:3]):   # the C ABI reads three zeros as "contiguous"
+        raise ValueError("rows that are all one row in memory have to be materialised")
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
 
 
 def _ptr(t) -> Optional[int]:
@@ -255,6 +311,33 @@ class Handle:
                                             _ptr(out), _ptr(lse), _ptr(workspace),
                                             workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
                     "restkv_decode")
+
+    def paged_page_bytes(self, cache: Paged) -> int:
+        return int(self._lib.restkv_paged_page_bytes(ctypes.byref(cache)))
+
+    def paged_workspace_bytes(self, cache: Paged, n_tokens: int) -> int:
+        return int(self._lib.restkv_paged_workspace_bytes(ctypes.byref(cache), int(n_tokens)))
+
+    def paged_append(self, cache, n_tokens, K_new, V_new, K_pages, V_pages, lengths, table, counts=None, positions=None, rotation=None,
+                     Q=None, Q_out=None, stream=None):
+        """K_new, V_new, Q: tensors [batch, heads, n_tokens, head_dim] of any row strides."""
+        self._check(self._lib.restkv_paged_append(
+            self._h, ctypes.byref(cache), int(n_tokens), ctypes.byref(make_rows(K_new)), ctypes.byref(make_rows(V_new)), _ptr(K_pages),
+            _ptr(V_pages), _ptr(lengths), _ptr(table), _ptr(counts), _ptr(positions),
+            ctypes.byref(rotation) if rotation is not None else None, ctypes.byref(make_rows(Q)) if Q is not None else None, _ptr(Q_out),
+            _stream_ptr(stream)), "restkv_paged_append")
+
+    def paged_attend(self, cache, n_tokens, Q, K_pages, V_pages, lengths, table, out, workspace, lse=None, counts=None, stream=None):
+        """Q: a tensor [batch, n_q_heads, n_tokens, head_dim] of any row strides."""
+        self._check(self._lib.restkv_paged_attend(
+            self._h, ctypes.byref(cache), int(n_tokens), ctypes.byref(make_rows(Q)), _ptr(K_pages), _ptr(V_pages), _ptr(lengths),
+            _ptr(table), _ptr(counts), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(),
+            _stream_ptr(stream)), "restkv_paged_attend")
+
+    def paged_read(self, cache, K_pages, V_pages, lengths, table, n_rows, K_out, V_out, first=None, stream=None):
+        self._check(self._lib.restkv_paged_read(
+            self._h, ctypes.byref(cache), _ptr(K_pages), _ptr(V_pages), _ptr(lengths), _ptr(table), _ptr(first), int(n_rows), _ptr(K_out),
+            _ptr(V_out), _stream_ptr(stream)), "restkv_paged_read")
 
     def poll_status(self, stream=None) -> int:
         return int(self._lib.restkv_poll_status(self._h, _stream_ptr(stream)))

@@ -1,0 +1,134 @@
+// The paged cache: its description as the kernels get it, where a row lies, and the 4-bit format.
+#pragma once
+
+#include "restkv_common.cuh"
+
+namespace restkv {
+
+constexpr int kBlockRows = 16;   // rows of a block: what one tile of the attention kernels holds, and a 4-bit block's parameters
+
+struct PagedCache {
+  int batch, Hq, Hkv, G, d;
+  int format, group;
+  int page_rows, n_pages, table_width;
+  int per_head;               // lengths [batch, Hkv] instead of [batch]
+  float scale, softcap;       // softcap 0: none
+  int row_bytes;              // of a row of elements, or of a row's codes
+  int block_bytes;            // 16 rows (and their steps and offsets)
+  long long head_bytes;       // one head's rows of a page
+  const int* lengths;
+  const int* table;
+  const int* counts;          // null: every sequence has n_tokens
+  int n_tokens;
+  const uint8_t *K, *V;
+  unsigned int* dev_status;
+
+  __host__ __device__ long long capacity() const { return (long long)table_width * page_rows; }
+};
+
+struct RowsView {   // [batch, heads, n_tokens, d] in element strides
+  const void* data;
+  long long sb, sh, sn;
+};
+
+struct RotationView {
+  const float *cos, *sin;   // null: no rotation
+  int n_positions, half;    // rotary_dim / 2
+  int interleaved;
+};
+
+// Rows of a sequence for one KV head: within the table, and never negative.
+__device__ __forceinline__ int paged_length(const PagedCache& c, int b, int h) {
+  const int n = c.lengths[c.per_head ? b * c.Hkv + h : b];
+  const long long most = c.capacity();
+  return n < 0 ? 0 : (int)(n < most ? n : most);
+}
+// Sets the sticky status if a sequence claims more rows than its table can name.
+__device__ __forceinline__ void check_length(const PagedCache& c, int b, int h) {
+  if (c.lengths[c.per_head ? b * c.Hkv + h : b] > c.capacity()) atomicOr(c.dev_status, kDevBadIndex);
+}
+__device__ __forceinline__ int paged_count(const PagedCache& c, int b) {
+  if (!c.counts) return c.n_tokens;
+  const int n = c.counts[b];
+  return n < 0 ? 0 : n < c.n_tokens ? n : c.n_tokens;
+}
+// Byte offset, in K's pages as in V's, of block `block` of 16 rows of a sequence and head; -1 if the table's entry is out of range.
+__device__ __forceinline__ long long paged_block(const PagedCache& c, int b, int h, int block) {
+  const int per_page = c.page_rows / kBlockRows;
+  const int slot = block / per_page;
+  const int page = c.table[(long long)b * c.table_width + slot];
+  if ((unsigned int)page >= (unsigned int)c.n_pages) return -1;
+  return ((long long)page * c.Hkv + h) * c.head_bytes + (long long)(block - slot * per_page) * c.block_bytes;
+}
+
+// ---- the 4-bit format ----
+// Offset and step of a group are bf16, rounded outward so that offset <= every value <= offset + 15 * step: the codes clip nothing
+// and the error of a value is half a step, also where a group lies far from 0.  (A symmetric grid would spend half its codes on nothing there.)
+__device__ __forceinline__ float bf16_below(float x) {
+  const unsigned int u = __float_as_uint(x), t = u & 0xFFFF0000u;
+  return __uint_as_float(u != t && (int)u < 0 ? t + 0x10000u : t);
+}
+__device__ __forceinline__ float bf16_above(float x) {   // x >= 0
+  const unsigned int u = __float_as_uint(x), t = u & 0xFFFF0000u;
+  return __uint_as_float(u != t ? t + 0x10000u : t);
+}
+__device__ __forceinline__ float int4_input(float x) {   // NaN -> 0; 2^120 keeps the span of a group finite
+  return x == x ? fminf(fmaxf(x, -0x1p120f), 0x1p120f) : 0.f;
+}
+// The nearest code.  The quotient is IEEE's, so that values half-way between two codes (common where the inputs are bf16) go to the even one.
+__device__ __forceinline__ unsigned int int4_code(float x, float lo, float step) {
+  const float q = step > 0.f ? rintf(__fdiv_rn(x - lo, step)) : 0.f;
+  return (unsigned int)fminf(q, 15.f);
+}
+// Byte of a block where row r has the step of group g; its offset lies 8 bytes on.
+__device__ __forceinline__ int int4_params(int d, int g, int r) { return 8 * d + 64 * g + 16 * (r & 3) + 2 * (r >> 2); }
+
+template <typename T> struct Pack8;   // 8 consecutive elements of a row
+template <> struct Pack8<__nv_bfloat16> {
+  uint4 u;
+  __device__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ void get(float* x) const {
+    const unsigned int w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ static void store(__nv_bfloat16* p, const float* x) {
+    uint4 v;
+    unsigned int* w = &v.x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 pair = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const unsigned int*>(&pair);
+    }
+    *reinterpret_cast<uint4*>(p) = v;
+  }
+};
+template <> struct Pack8<float> {
+  float4 a, b;
+  __device__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
+  __device__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ void get(float* x) const {
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+  __device__ static void store(float* p, const float* x) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+  }
+};
+
+// ---- launches ----
+cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K_new, const RowsView& V_new, uint8_t* K_pages,
+                                uint8_t* V_pages, const int* positions, const RotationView& rotation, const RowsView& Q, void* Q_out,
+                                int sm_count, cudaStream_t st);
+cudaError_t launch_paged_read(const PagedCache& c, bool f32, const int* first, int n_rows, void* K_out, void* V_out, cudaStream_t st);
+// fp32 SIMT attention: every dtype, format and head_dim.
+int paged_simt_splits(const PagedCache& c, int sm_count);
+size_t paged_simt_bytes(const PagedCache& c, int splits);
+cudaError_t launch_paged_simt(const PagedCache& c, bool f32, const RowsView& Q, void* out, float* lse, float* part, int splits,
+                              cudaStream_t st);
+
+}  // namespace restkv
