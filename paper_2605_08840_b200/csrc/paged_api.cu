@@ -53,6 +53,15 @@ static restkv_status check_tokens(const PagedCache& c, int n_tokens) {
   return RESTKV_OK;
 }
 
+// The kernels that a call runs on: the tensor pipe for bf16 with the head_dims it has (kernel path 1 keeps off it), else fp32.
+static bool on_tensor_pipe(const PagedCache& c, bool f32) { return !f32 && paged_mma_supported(c); }
+
+static size_t attend_bytes(const PagedCache& c, bool f32, int sm_count) {
+  const size_t simt = paged_simt_bytes(c, paged_simt_splits(c, sm_count));   // what every call can run on
+  const size_t mma = on_tensor_pipe(c, f32) ? paged_mma_bytes(c, sm_count) : 0;
+  return align256(simt > mma ? simt : mma);
+}
+
 static restkv_status make_rows(const restkv_rows* s, int heads, int n, int d, RowsView* out) {
   if (!s || !s->data || !aligned16(s->data)) return RESTKV_ERR_INVALID_ARG;
   *out = RowsView{s->data, s->stride_b, s->stride_h, s->stride_n};
@@ -87,7 +96,7 @@ size_t restkv_paged_workspace_bytes(const restkv_paged* cache, int n_tokens) {
   PagedCache c;
   if (make_cache(cache, &c) != RESTKV_OK || check_tokens(c, n_tokens) != RESTKV_OK) return 0;
   c.n_tokens = n_tokens;
-  return align256(paged_simt_bytes(c, paged_simt_splits(c, device_sms())));
+  return attend_bytes(c, cache->dtype == RESTKV_F32, device_sms());
 }
 
 restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, int n_tokens, const restkv_rows* K_new,
@@ -138,10 +147,16 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
   c.K = (const uint8_t*)K_pages; c.V = (const uint8_t*)V_pages;
   if (!workspace || ((uintptr_t)workspace & 255u) != 0) return RESTKV_ERR_WORKSPACE;
   Call call{h, (cudaStream_t)stream};
-  const int splits = paged_simt_splits(c, h->sm_count);
-  if (workspace_bytes < paged_simt_bytes(c, splits)) return RESTKV_ERR_WORKSPACE;
+  const bool f32 = cache->dtype == RESTKV_F32;
+  if (workspace_bytes < attend_bytes(c, f32, h->sm_count)) return RESTKV_ERR_WORKSPACE;
+  if (on_tensor_pipe(c, f32) && h->tc_state && h->kernel_path != 1) {
+    int launches = 0;
+    RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
+                  launch_paged_mma(h->tc_state, c, q, out, lse, (float*)workspace, h->sm_count, h->wait_limit, call.st, &launches), launches);
+    return RESTKV_OK;
+  }
   RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
-                launch_paged_simt(c, cache->dtype == RESTKV_F32, q, out, lse, (float*)workspace, splits, call.st), 2);
+                launch_paged_simt(c, f32, q, out, lse, (float*)workspace, paged_simt_splits(c, h->sm_count), call.st), 2);
   return RESTKV_OK;
 }
 

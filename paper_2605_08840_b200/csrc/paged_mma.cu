@@ -1,0 +1,817 @@
+// Attention of a few query tokens over the paged cache: bf16 in and out, pages of bf16 or of 4-bit codes, head_dim 64, 128 or 256.
+//
+// What bounds it: every row is read once and meets few query rows (tokens x query heads of a KV head, up to 16 per pass), so the step
+// streams HBM; in 4 bits the instructions that turn codes into operands come close behind.  The design follows from that:
+//   - warps that never wait for one another while they stream: each owns every kWarps-th tile of its CTA's run and a ring of tile
+//     slots that its own lane 0 fills with bulk copies (4 bits: a block of 16 rows lies in one piece, codes and parameters) or TMA
+//     boxes (bf16: 128-byte swizzle for ldmatrix);
+//   - mma.sync m16n8k16: S = Q K^T with the query rows as the 16 rows and 8 cache rows as columns, O^T = V^T P^T with 16 dims as rows
+//     and 8 query rows as columns.  The accumulator layout of S is the operand layout of P^T, so the weights never leave the
+//     registers, and up to 8 query rows cost half of what P V with 16 padded rows does;
+//   - 4-bit rows are laid out for the fragments: a lane's 4 bytes of K are 8 codes of the dims that its operand registers take, its 2
+//     bytes of V 4 dims of one row.  (x & 0x0078) | 0x4180 is 16 + code as bf16, so a pair costs a shift and a logic operation;
+//     steps and offsets are applied in fp32: s += step * (q . code) + offset * sum(q) per group, with the 16 taken out by the
+//     accumulator's start -16 sum(q); o = sum bf16(p step) (code - 8) + sum p (offset + 8 step), where a product with a constant
+//     operand of -24 sums the rounded weights.  (With code instead of code - 8 there the weights' rounding would weigh twice as much.)
+// Work is split in one of two ways:
+//   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
+//     short caches, where latency counts;
+//   - the tiles of all units end to end, an equal share of them per CTA whatever the sequences' lengths, partial results in the
+//     workspace and a second kernel that merges what several CTAs share.
+#include <math.h>
+
+#include <cooperative_groups.h>
+
+#include "paged.cuh"
+#include "tc_common.cuh"
+
+namespace restkv {
+
+namespace {
+
+namespace cg = cooperative_groups;
+
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t* r) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// c[0..1] += x * (column sums of B), for a matrix A of bf16 pairs `xx` = (x, x): all its rows are the same, one is kept.
+__device__ __forceinline__ void mma_column_sums(float* c, uint32_t xx, uint32_t b0, uint32_t b1) {
+  float unused0, unused1;
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %4, %4, %4}, {%5, %6}, {%7, %8, %9, %9};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(unused0), "=f"(unused1)
+               : "r"(xx), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t lds32(uint32_t addr) {
+  uint32_t v;
+  asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds64(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+// kWords consecutive words of shared memory, aligned to as much as is read at once.
+template <int kWords> __device__ __forceinline__ void lds_words(uint32_t addr, uint32_t* w) {
+  if constexpr (kWords == 1) {
+    w[0] = lds32(addr);
+  } else if constexpr (kWords == 2) {
+    const uint2 v = lds64(addr);
+    w[0] = v.x; w[1] = v.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < kWords; i += 4) {
+      const uint4 v = lds128(addr + 4 * i);
+      w[i] = v.x; w[i + 1] = v.y; w[i + 2] = v.z; w[i + 3] = v.w;
+    }
+  }
+}
+// Codes i and i + 4 of a word (those at 4 i of both halves) as a pair of bf16, 16 too large.
+template <int i> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
+  return ((i == 0 ? w << 3 : w >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+}
+__device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+constexpr uint32_t kMinus24 = 0xC1C0C1C0u;
+
+struct PagedMmaArgs {
+  PagedCache c;
+  RowsView Q;
+  __nv_bfloat16* out;
+  float* lse;        // or null
+  float* part;       // [2 * CTAs, rows, d + 2] (m, l, o), without clusters
+  int row_tiles;     // units per KV head
+  int cluster;       // CTAs per unit, 0: tiles of all units end to end
+  long long wait_limit;
+};
+
+// The shape of an instantiation.  kD head_dim, kGroups groups of a 4-bit row (0: bf16), kNT tiles of 8 query rows.
+template <int kD, int kGroups, int kNT> struct Config {
+  static constexpr bool kInt4 = kGroups > 0;
+  static constexpr int kRows = 8 * kNT;
+  static constexpr uint32_t kBlockBytes = kInt4 ? 8u * kD + 64u * kGroups : 32u * kD;   // 16 rows of K, or of V
+  // tiles of two blocks spread the softmax's exchanges and the waits over more rows; at 8 KB and more they cost ring slots
+  static constexpr int kBlocks = kBlockBytes <= 2560 ? 2 : 1;
+  static constexpr int kTileRows = kBlocks * kBlockRows;
+  static constexpr uint32_t kStageBytes = 2 * kBlocks * kBlockBytes;
+  static constexpr int kWarps = !kInt4 && kD == 256 ? 4 : 8;
+  // two CTAs per SM where 128 registers are enough: one streams while the other merges
+  static constexpr int kPerSm = kInt4 && kNT == 1 && kD <= 128 ? 2 : 1;
+  static constexpr int kFit = (int)((kPerSm == 2 ? 110u * 1024u : 220u * 1024u) / (kWarps * kStageBytes));
+  static constexpr int kStages = kFit < 2 ? 2 : kFit > 6 ? 6 : kFit;
+  static constexpr uint32_t kRing = kStages * kStageBytes;
+  static constexpr uint32_t kPartBytes = kRows * kD * 4u;                               // a warp's o in the merge
+  static_assert(kRing >= kPartBytes + (kRows + kWarps - 1) / kWarps * kD * 4u, "the merge needs the ring's space");
+  static constexpr size_t kSmem = (size_t)kWarps * kRing + 1024;
+};
+
+// Where a CTA's run of tiles begins: entry (a sequence, or with lengths per head a KV head of one), unit of the entry, tile of the unit.
+struct Run {
+  long long tiles;          // of all units
+  long long first;          // tile at which `entry` begins
+  int entry;
+};
+
+__device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_rows) {
+  const int n = c.per_head ? paged_length(c, e / c.Hkv, e % c.Hkv) : paged_length(c, e, 0);
+  const int t = (n + tile_rows - 1) / tile_rows;
+  return t > 0 ? t : 1;     // a unit without rows has its outputs written, too
+}
+
+// By a whole warp: the tiles of all units, and the entry that holds tile share(tiles).
+template <typename F>
+__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, F share) {
+  const int lane = threadIdx.x & 31;
+  const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
+  const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
+  Run r{0, 0, 0};
+  long long mine = 0;
+  for (int e = lane; e < entries; e += 32) mine += (long long)entry_tiles(c, e, tile_rows) * units;
+  r.tiles = mine;
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) r.tiles += __shfl_xor_sync(0xffffffffu, r.tiles, off);
+  const long long want = share(r.tiles);
+  for (int base = 0; base < entries; base += 32) {
+    const long long t = base + lane < entries ? (long long)entry_tiles(c, base + lane, tile_rows) * units : 0;
+    long long upto = t;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const long long o = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += o;
+    }
+    const unsigned int past = __ballot_sync(0xffffffffu, r.first + upto > want);
+    if (past) {
+      const int at = __ffs((int)past) - 1;
+      r.entry = base + at;
+      r.first += __shfl_sync(0xffffffffu, upto - t, at);
+      return r;
+    }
+    r.first += __shfl_sync(0xffffffffu, upto, 31);
+  }
+  r.entry = entries;
+  return r;
+}
+
+template <int kD, int kGroups, int kNT>
+__global__ void __launch_bounds__(Config<kD, kGroups, kNT>::kWarps * 32, Config<kD, kGroups, kNT>::kPerSm)
+paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PagedMmaArgs a) {
+  using C = Config<kD, kGroups, kNT>;
+  constexpr bool kInt4 = C::kInt4;
+  constexpr int kW = C::kWarps, kStages = C::kStages, kRows = C::kRows, kBlocks = C::kBlocks, kWords = kD / 32;
+  constexpr int kG = kInt4 ? kGroups : 1;
+  constexpr int kPerGroup = kWords / kG;       // 32-dim blocks of a group
+  const PagedCache& c = a.c;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) uint64_t full[kW][kStages];
+  __shared__ float w_ml[kW][kRows][2];
+  __shared__ float w_lo[kW][kRows][kG];        // 4 bits: sum of p (offset + 8 step) per group
+  __shared__ float c_ml[kRows][2];
+  __shared__ int abort_flag;
+  __shared__ long long run_s[2];
+  __shared__ int run_entry;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q4 = lane & 3;
+  const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  uint8_t* rings = smem_raw + (smem_base - smem_u32(smem_raw));
+  uint8_t* ring = rings + warp * C::kRing;
+  const uint32_t ring_addr = smem_base + (uint32_t)warp * C::kRing;
+  const int R = c.n_tokens * c.G;
+
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (lane == 0) {
+    for (int s = 0; s < kStages; ++s) mbar_init(&full[warp][s], 1);
+    fence_mbar_init();
+    if (!kInt4) {
+      prefetch_tensormap(&tmK);
+      prefetch_tensormap(&tmV);
+    }
+  }
+  grid_dependency_wait();
+  grid_dependency_launch();
+
+  long long tile = 0, end = 0, first = 0;      // of the CTA's run, without clusters
+  int entry = 0;
+  if (!a.cluster) {
+    if (warp == 0) {
+      const Run run = find_run(c, a.row_tiles, C::kTileRows, [&](long long t) { return t * blockIdx.x / gridDim.x; });
+      if (lane == 0) { run_s[0] = run.tiles; run_s[1] = run.first; run_entry = run.entry; }
+    }
+    __syncthreads();
+    tile = run_s[0] * blockIdx.x / gridDim.x;
+    end = run_s[0] * (blockIdx.x + 1) / gridDim.x;
+    first = run_s[1];
+    entry = run_entry;
+    if (tile >= end) return;
+  } else {
+    __syncthreads();
+  }
+
+  int used = 0;                                // tiles that this warp has taken from its ring
+  bool ok = true;
+  for (int piece = 0;; ++piece) {
+    // ---- the unit and the run of its tiles ----
+    int unit, t0, t1, whole;                   // whole: no other CTA has tiles of the unit
+    int cluster_rank = 0;
+    if (a.cluster) {
+      unit = (int)(blockIdx.x / (unsigned int)a.cluster);
+      cluster_rank = (int)(blockIdx.x % (unsigned int)a.cluster);
+      const int bh = unit / a.row_tiles;
+      const int tiles = entry_tiles(c, c.per_head ? bh : bh / c.Hkv, C::kTileRows);
+      t0 = (int)((long long)tiles * cluster_rank / a.cluster);
+      t1 = (int)((long long)tiles * (cluster_rank + 1) / a.cluster);
+      whole = 0;
+    } else {
+      const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles;
+      int tiles = entry_tiles(c, entry, C::kTileRows);
+      if (tile >= first + (long long)tiles * units) {      // the next entry
+        first += (long long)tiles * units;
+        ++entry;
+        tiles = entry_tiles(c, entry, C::kTileRows);
+      }
+      const int k = (int)((tile - first) / tiles);
+      const long long begin = first + (long long)k * tiles;
+      unit = entry * units + k;
+      t0 = (int)(tile - begin);
+      t1 = (int)((end - begin < tiles) ? end - begin : tiles);
+      whole = t0 == 0 && t1 == tiles;
+    }
+    const int bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
+    const int n = paged_length(c, b, h), count = paged_count(c, b);
+    if (t0 == 0 && threadIdx.x == 0) check_length(c, b, h);
+    const int blocks = (n + kBlockRows - 1) / kBlockRows;
+    const int mine = t1 - t0 > warp ? (t1 - t0 - warp + kW - 1) / kW : 0;   // tiles t0 + warp + kW * i
+
+    // ---- requests: the blocks' places are looked up 32 / kBlocks tiles at a time, one lane each ----
+    long long place = -1;
+    unsigned int absent = 0;                   // bit slot * kBlocks + block: nothing was loaded there
+    auto request = [&](int i) {                // by the whole warp
+      constexpr int kAhead = 32 / kBlocks;
+      if (i % kAhead == 0) {
+        const int t = t0 + warp + (i + lane / kBlocks) * kW;
+        const int block = t * kBlocks + lane % kBlocks;
+        place = -1;
+        if (t < t1 && block < blocks) {
+          place = paged_block(c, b, h, block);
+          if (place < 0) atomicOr(c.dev_status, kDevBadIndex);
+        }
+      }
+      const int s = (used + i) % kStages;
+      long long at[kBlocks];
+      int there = 0;
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k) {
+        at[k] = __shfl_sync(0xffffffffu, place, (i % kAhead) * kBlocks + k);
+        there += at[k] >= 0;
+        const unsigned int bit = 1u << (s * kBlocks + k);
+        absent = at[k] >= 0 ? absent & ~bit : absent | bit;
+      }
+      if (lane == 0) {
+        uint8_t* dst = ring + (uint32_t)s * C::kStageBytes;
+        uint64_t* bar = &full[warp][s];
+        mbar_arrive_expect_tx(bar, (uint32_t)there * 2 * C::kBlockBytes);
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) {
+          if (at[k] < 0) continue;
+          uint8_t* kd = dst + k * 2 * C::kBlockBytes;
+          if constexpr (kInt4) {
+            bulk_load(kd, c.K + at[k], C::kBlockBytes, bar);
+            bulk_load(kd + C::kBlockBytes, c.V + at[k], C::kBlockBytes, bar);
+          } else {
+            const int row = (int)(at[k] / (2 * kD));
+#pragma unroll
+            for (int x = 0; x < kD / 64; ++x) {
+              tma_load_2d(kd + x * 2048, &tmK, bar, x * 64, row);
+              tma_load_2d(kd + C::kBlockBytes + x * 2048, &tmV, bar, x * 64, row);
+            }
+          }
+        }
+      }
+      __syncwarp();
+    };
+    for (int i = 0; i < mine && i < kStages; ++i) request(i);
+
+    // ---- Q as the A operand: query rows rho0 + r (and + 8), kD / 16 steps; sums of q per group; what each row sees ----
+    uint32_t qa[kD / 16][kNT == 2 ? 4 : 2];
+    float q_sum[kNT][kG];
+    int sees[kNT];
+    int sees_least = n;
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) {
+      const int rho = rho0 + r + 8 * t, i = rho / c.G, g = rho - i * c.G;
+      const bool live = rho < R && i < count;
+      sees[t] = live ? n - (count - 1 - i) : n;
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
+#pragma unroll
+      for (int g2 = 0; g2 < kG; ++g2) q_sum[t][g2] = 0.f;
+#pragma unroll
+      for (int m = 0; m < kWords; ++m) {
+        if constexpr (kInt4) {     // dims 32 m + 8 q4 .. + 7, in the pairs (i, i + 4) that a word's codes come in
+          uint4 u = make_uint4(0u, 0u, 0u, 0u);
+          if (live) u = *reinterpret_cast<const uint4*>(q + 32 * m + 8 * q4);
+          qa[2 * m][t] = __byte_perm(u.x, u.z, 0x5410);
+          qa[2 * m][kNT + t] = __byte_perm(u.x, u.z, 0x7632);
+          qa[2 * m + 1][t] = __byte_perm(u.y, u.w, 0x5410);
+          qa[2 * m + 1][kNT + t] = __byte_perm(u.y, u.w, 0x7632);
+          q_sum[t][m / kPerGroup] += ((lower(u.x) + upper(u.x)) + (lower(u.y) + upper(u.y))) + ((lower(u.z) + upper(u.z)) + (lower(u.w) + upper(u.w)));
+        } else {
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            const int k = 2 * m + s;
+            qa[k][t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
+            qa[k][kNT + t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
+          }
+        }
+      }
+#pragma unroll
+      for (int g2 = 0; g2 < kG; ++g2) {
+        q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 1);
+        q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 2);
+      }
+      sees_least = min(sees_least, sees[t]);
+    }
+    sees_least = __reduce_min_sync(0xffffffffu, sees_least);
+
+    const float to_log2 = c.scale * kLog2e, cap_log2 = c.softcap * kLog2e;
+    const float cap_in = c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : 0.f;
+    float m[kNT], l[kNT];                      // log2 units; l: this lane's share of the row's sum
+    float o[kD / 16][kNT][4];                  // dims of the 16-dim tile (r, r + 8), query rows 2 q4, 2 q4 + 1 (+ 8 per tile)
+    float z[kG][kNT][2], lo[kG][kNT];          // 4 bits: -24 sum bf16(p step); this lane's share of sum p (offset + 8 step)
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) {
+      m[t] = -INFINITY;
+      l[t] = 0.f;
+#pragma unroll
+      for (int k = 0; k < kD / 16; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[k][t][e] = 0.f;
+#pragma unroll
+      for (int g = 0; g < kG; ++g) { z[g][t][0] = z[g][t][1] = 0.f; lo[g][t] = 0.f; }
+    }
+
+    for (int i = 0; i < mine; ++i) {
+      const int s = (used + i) % kStages;
+      ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][s], (uint32_t)((used + i) / kStages) & 1u, &abort_flag, c.dev_status, kDevTimeout,
+                                             a.wait_limit));
+      if (!ok) {
+        if (lane == 0)   // nothing may still be on its way into shared memory when the CTA returns
+          for (int j = i; j < mine && j < i + kStages; ++j) wait_issued(&full[warp][(used + j) % kStages], (uint32_t)((used + j) / kStages));
+        break;
+      }
+      const uint32_t stage = ring_addr + (uint32_t)s * C::kStageBytes;
+      const int row0 = (t0 + warp + i * kW) * C::kTileRows;
+      const unsigned int gone = absent >> (s * kBlocks) & ((1u << kBlocks) - 1u);
+      const bool edge = row0 + C::kTileRows > sees_least || gone != 0;
+      // rows of the lane's four columns in a block: 4 bits q4 + 4 j, which is the order of the parameters; bf16 2 q4 + (j & 1) + 8 (j / 2)
+      auto column = [&](int j) { return kInt4 ? q4 + 4 * j : 2 * q4 + (j & 1) + 8 * (j >> 1); };
+      float sc[kBlocks][kNT][4];
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k) {
+        const uint32_t kt = stage + k * 2 * C::kBlockBytes;
+        if constexpr (kInt4) {
+          float p0[kG][4], p1[kG][4];          // steps and offsets of the four rows
+#pragma unroll
+          for (int g = 0; g < kG; ++g) {
+            const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * q4);
+            p0[g][0] = lower(u.x); p0[g][1] = upper(u.x); p0[g][2] = lower(u.y); p0[g][3] = upper(u.y);
+            p1[g][0] = lower(u.z); p1[g][1] = upper(u.z); p1[g][2] = lower(u.w); p1[g][3] = upper(u.w);
+          }
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            uint32_t w[kWords];
+            lds_words<kWords>(kt + (uint32_t)(8 * half + (r >> 1) + 4 * (r & 1)) * (kD / 2) + q4 * (kD / 8), w);
+#pragma unroll
+            for (int g = 0; g < kG; ++g) {
+              float acc[4];
+              acc[0] = acc[1] = -16.f * q_sum[0][g];
+              acc[2] = acc[3] = kNT == 2 ? -16.f * q_sum[kNT - 1][g] : 0.f;
+#pragma unroll
+              for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x) {
+                const uint32_t a0[4] = {qa[2 * x][0], kNT == 2 ? qa[2 * x][1] : 0u, qa[2 * x][kNT], kNT == 2 ? qa[2 * x][kNT + kNT - 1] : 0u};
+                const uint32_t a1[4] = {qa[2 * x + 1][0], kNT == 2 ? qa[2 * x + 1][1] : 0u, qa[2 * x + 1][kNT],
+                                        kNT == 2 ? qa[2 * x + 1][kNT + kNT - 1] : 0u};
+                mma16816(acc, a0, code_pair<0>(w[x]), code_pair<1>(w[x]));
+                mma16816(acc, a1, code_pair<2>(w[x]), code_pair<3>(w[x]));
+              }
+#pragma unroll
+              for (int t = 0; t < kNT; ++t)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  const int j = 2 * half + e;
+                  const float add = p1[g][j] * q_sum[t][g];
+                  sc[k][t][j] = g == 0 ? fmaf(p0[g][j], acc[2 * t + e], add) : fmaf(p0[g][j], acc[2 * t + e], sc[k][t][j] + add);
+                }
+            }
+          }
+        } else {
+          float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+          const int mat = lane >> 3, mr = lane & 7;
+#pragma unroll
+          for (int x = 0; x < kD / 16; ++x) {
+            uint32_t w[4];
+            ldsm4(kt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), w);
+            const uint32_t a0[4] = {qa[x][0], kNT == 2 ? qa[x][1] : 0u, qa[x][kNT], kNT == 2 ? qa[x][kNT + kNT - 1] : 0u};
+            mma16816(acc[0], a0, w[0], w[1]);
+            mma16816(acc[1], a0, w[2], w[3]);
+          }
+#pragma unroll
+          for (int t = 0; t < kNT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[k][t][j] = acc[j >> 1][2 * t + (j & 1)];
+        }
+      }
+      // logits in log2 units; columns that a row does not see weigh nothing
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+        for (int t = 0; t < kNT; ++t)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
+            if (c.softcap > 0.f) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j] * cap_in)), cap_log2);
+            else sc[k][t][j] *= to_log2;
+          }
+      if (edge) {
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int t = 0; t < kNT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (row0 + k * kBlockRows + column(j) >= sees[t] || (gone >> k & 1u)) sc[k][t][j] = -INFINITY;
+      }
+      float f[kNT];
+      bool grown = false;
+#pragma unroll
+      for (int t = 0; t < kNT; ++t) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) mx = fmaxf(mx, fmaxf(fmaxf(sc[k][t][0], sc[k][t][1]), fmaxf(sc[k][t][2], sc[k][t][3])));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+        f[t] = 1.f;
+        if (mx > m[t]) {
+          f[t] = ex2_approx(m[t] - mx);        // m = -inf gives 0
+          m[t] = mx;
+          l[t] *= f[t];
+          grown = true;
+        }
+        const float m_use = m[t] == -INFINITY ? 0.f : m[t];   // only logits of -inf so far: they weigh nothing
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) sc[k][t][j] = ex2_approx(sc[k][t][j] - m_use);
+          l[t] += (sc[k][t][0] + sc[k][t][1]) + (sc[k][t][2] + sc[k][t][3]);
+        }
+      }
+      if (__any_sync(0xffffffffu, grown)) {
+#pragma unroll
+        for (int t = 0; t < kNT; ++t) {
+          // the factors of the rows that o's columns stand for
+          const float f0 = __shfl_sync(0xffffffffu, f[t], 8 * q4), f1 = __shfl_sync(0xffffffffu, f[t], 8 * q4 + 4);
+#pragma unroll
+          for (int k = 0; k < kD / 16; ++k) {
+            o[k][t][0] *= f0; o[k][t][1] *= f1;
+            o[k][t][2] *= f0; o[k][t][3] *= f1;
+          }
+          if (kInt4) {
+#pragma unroll
+            for (int g = 0; g < kG; ++g) { z[g][t][0] *= f0; z[g][t][1] *= f1; lo[g][t] *= f[t]; }
+          }
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k) {
+        const uint32_t vt = stage + k * 2 * C::kBlockBytes + C::kBlockBytes;
+        // rows past the cache hold anything: their bits are cleared, so that a weight of 0 finds a number there
+        uint32_t keep01 = 0xFFFFFFFFu, keep23 = 0xFFFFFFFFu;
+        if (edge) {
+          const int left = (gone >> k & 1u) ? 0 : n - (row0 + k * kBlockRows);
+          keep01 = (column(0) < left ? 0xFFFFu : 0u) | (column(1) < left ? 0xFFFF0000u : 0u);
+          keep23 = (column(2) < left ? 0xFFFFu : 0u) | (column(3) < left ? 0xFFFF0000u : 0u);
+        }
+        if constexpr (kInt4) {
+          uint32_t w[4][(kWords + 1) / 2];     // the units of rows q4, q4 + 4, q4 + 8, q4 + 12
+#pragma unroll
+          for (int j = 0; j < 4; ++j) lds_words<kWords / 2>(vt + (uint32_t)(q4 + 4 * j) * (kD / 2) + r * (kD / 16), w[j]);
+          uint32_t pb[kNT][2];
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) {
+            if (x % kPerGroup == 0) {
+              const int g = x / kPerGroup;
+              uint4 u = lds128(vt + 8 * kD + 64 * g + 16 * q4);
+              if (edge) { u.x &= keep01; u.y &= keep23; u.z &= keep01; u.w &= keep23; }
+              const float s0 = lower(u.x), s1 = upper(u.x), s2 = lower(u.y), s3 = upper(u.y);
+              const float mid0 = fmaf(8.f, s0, lower(u.z)), mid1 = fmaf(8.f, s1, upper(u.z)), mid2 = fmaf(8.f, s2, lower(u.w)),
+                          mid3 = fmaf(8.f, s3, upper(u.w));
+#pragma unroll
+              for (int t = 0; t < kNT; ++t) {
+                const float* p = sc[k][t];
+                lo[g][t] = fmaf(p[0], mid0, fmaf(p[1], mid1, fmaf(p[2], mid2, fmaf(p[3], mid3, lo[g][t]))));
+                pb[t][0] = pack_bf16x2(p[0] * s0, p[1] * s1);
+                pb[t][1] = pack_bf16x2(p[2] * s2, p[3] * s3);
+                mma_column_sums(z[g][t], kMinus24, pb[t][0], pb[t][1]);
+              }
+            }
+            const uint32_t y0 = __byte_perm(w[0][x >> 1], w[1][x >> 1], x & 1 ? 0x7632 : 0x5410);
+            const uint32_t y1 = __byte_perm(w[2][x >> 1], w[3][x >> 1], x & 1 ? 0x7632 : 0x5410);
+            const uint32_t va[4] = {code_pair<0>(y0), code_pair<1>(y0), code_pair<0>(y1), code_pair<1>(y1)};
+            const uint32_t vb[4] = {code_pair<2>(y0), code_pair<3>(y0), code_pair<2>(y1), code_pair<3>(y1)};
+#pragma unroll
+            for (int t = 0; t < kNT; ++t) {
+              mma16816(o[2 * x][t], va, pb[t][0], pb[t][1]);
+              mma16816(o[2 * x + 1][t], vb, pb[t][0], pb[t][1]);
+            }
+          }
+        } else {
+          uint32_t pb[kNT][2];
+#pragma unroll
+          for (int t = 0; t < kNT; ++t) {
+            pb[t][0] = pack_bf16x2(sc[k][t][0], sc[k][t][1]);
+            pb[t][1] = pack_bf16x2(sc[k][t][2], sc[k][t][3]);
+          }
+          const int mat = lane >> 3, mr = lane & 7;
+#pragma unroll
+          for (int x = 0; x < kD / 16; ++x) {
+            uint32_t va[4];
+            ldsm4_t(vt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), va);
+            if (edge) { va[0] &= keep01; va[1] &= keep01; va[2] &= keep23; va[3] &= keep23; }
+#pragma unroll
+            for (int t = 0; t < kNT; ++t) mma16816(o[x][t], va, pb[t][0], pb[t][1]);
+          }
+        }
+      }
+      __syncwarp();   // every lane has read the slot
+      if (i + kStages < mine) request(i + kStages);
+    }
+    used += mine;
+
+    // ---- merge, in a fixed order: the warps of the CTA through their (idle) rings ----
+    __syncwarp();
+    float* w_o = reinterpret_cast<float*>(ring);   // [rows][kD]
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) {
+      l[t] += __shfl_xor_sync(0xffffffffu, l[t], 1);
+      l[t] += __shfl_xor_sync(0xffffffffu, l[t], 2);
+      if (q4 == 0) { w_ml[warp][r + 8 * t][0] = m[t]; w_ml[warp][r + 8 * t][1] = l[t]; }
+      if (kInt4) {
+#pragma unroll
+        for (int g = 0; g < kG; ++g) {
+          lo[g][t] += __shfl_xor_sync(0xffffffffu, lo[g][t], 1);
+          lo[g][t] += __shfl_xor_sync(0xffffffffu, lo[g][t], 2);
+          if (q4 == 0) w_lo[warp][r + 8 * t][g] = lo[g][t];
+        }
+      }
+      if (mine > 0) {
+        float* row = w_o + (2 * q4 + 8 * t) * kD;
+        if constexpr (kInt4) {
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) {   // dims 32 x + 4 r + (0..3)
+            const float z0 = z[x / kPerGroup][t][0], z1 = z[x / kPerGroup][t][1];
+            *reinterpret_cast<float4*>(row + 32 * x + 4 * r) =
+                make_float4(o[2 * x][t][0] + z0, o[2 * x][t][2] + z0, o[2 * x + 1][t][0] + z0, o[2 * x + 1][t][2] + z0);
+            *reinterpret_cast<float4*>(row + kD + 32 * x + 4 * r) =
+                make_float4(o[2 * x][t][1] + z1, o[2 * x][t][3] + z1, o[2 * x + 1][t][1] + z1, o[2 * x + 1][t][3] + z1);
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < kD / 16; ++x) {
+            row[16 * x + r] = o[x][t][0];
+            row[kD + 16 * x + r] = o[x][t][1];
+            row[16 * x + 8 + r] = o[x][t][2];
+            row[kD + 16 * x + 8 + r] = o[x][t][3];
+          }
+        }
+      }
+    }
+    __syncthreads();
+    const int rows = R - rho0 < kRows ? R - rho0 : kRows;
+    // a row's result: written where the unit is this CTA's (or this cluster's) alone
+    auto finish = [&](int row, int k, float acc, float mm, float ll) {
+      const int rho = rho0 + row, i = rho / c.G, g = rho - i * c.G;
+      const bool some = ll > 0.f && i < count;
+      const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
+      a.out[at * kD + k] = __float2bfloat16(some ? acc / ll : 0.f);
+      if (k == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+    };
+    auto c_o = [&](int row) { return reinterpret_cast<float*>(rings + (row % kW) * C::kRing + C::kPartBytes) + (row / kW) * kD; };
+    for (int e = threadIdx.x; e < rows * kD; e += kW * 32) {
+      const int row = e / kD, k = e % kD;
+      float mm = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) mm = fmaxf(mm, w_ml[w][row][0]);
+      float acc = 0.f, ll = 0.f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        const float mw = w_ml[w][row][0];
+        if (mw == -INFINITY) continue;         // a warp without tiles, or whose tiles this row does not see
+        const float f = ex2_approx(mw - mm);
+        float v = reinterpret_cast<const float*>(rings + w * C::kRing)[row * kD + k];
+        if (kInt4) v += w_lo[w][row][k / (kD / kG)];
+        acc = fmaf(v, f, acc);
+        ll = fmaf(w_ml[w][row][1], f, ll);
+      }
+      if (a.cluster) {
+        c_o(row)[k] = acc;
+        if (k == 0) { c_ml[row][0] = mm; c_ml[row][1] = ll; }
+      } else if (whole) {
+        finish(row, k, acc, mm, ll);
+      } else {
+        float* p = a.part + ((long long)(2 * blockIdx.x + (piece > 0)) * kRows + row) * (kD + 2);
+        p[2 + k] = acc;
+        if (k == 0) { p[0] = mm; p[1] = ll; }
+      }
+    }
+    if (a.cluster) {
+      cg::cluster_group cluster = cg::this_cluster();
+      cluster.sync();
+      for (int e = cluster_rank * kW * 32 + (int)threadIdx.x; e < rows * kD; e += a.cluster * kW * 32) {
+        const int row = e / kD, k = e % kD;
+        float mm = -INFINITY, acc = 0.f, ll = 0.f;
+        float mr[16], lr[16], vr[16];
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          mr[x] = -INFINITY;
+          if (x < a.cluster) {
+            const float* p = cluster.map_shared_rank(&c_ml[row][0], x);
+            mr[x] = p[0];
+            lr[x] = p[1];
+            vr[x] = *cluster.map_shared_rank(c_o(row) + k, x);
+            mm = fmaxf(mm, mr[x]);
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < 16; ++x) {
+          if (mr[x] == -INFINITY) continue;
+          const float f = ex2_approx(mr[x] - mm);
+          acc = fmaf(vr[x], f, acc);
+          ll = fmaf(lr[x], f, ll);
+        }
+        finish(row, k, acc, mm, ll);
+      }
+      cluster.sync();   // shared memory stays alive until every peer has read it
+      return;
+    }
+    tile += t1 - t0;
+    // all of the CTA's warps go on to the next piece or none
+    if (__syncthreads_or(!ok) || tile >= end) return;
+    fence_proxy_async_smem();   // the rings were written by ordinary stores; bulk copies come next
+  }
+}
+
+// grid (units, rows): merges what several CTAs left of a unit.
+template <int kD, int kRows>
+__global__ void __launch_bounds__(kD) paged_mma_combine_kernel(const __grid_constant__ PagedMmaArgs a, int ctas, int tile_rows) {
+  grid_dependency_wait();
+  __shared__ long long run_s[2];
+  const PagedCache& c = a.c;
+  const int unit = blockIdx.x, row = blockIdx.y, bh = unit / a.row_tiles, rho = (unit - bh * a.row_tiles) * kRows + row;
+  if (rho >= c.n_tokens * c.G) return;
+  const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles, entry = unit / units;
+  const int b = bh / c.Hkv, h = bh - b * c.Hkv, i = rho / c.G, g = rho - i * c.G;
+  if (threadIdx.x < 32) {
+    // where the unit's entry begins, by the same sums as in the kernel before
+    long long before = 0, all = 0;
+    const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
+    for (int e = threadIdx.x; e < entries; e += 32) {
+      const long long t = (long long)entry_tiles(c, e, tile_rows) * units;
+      all += t;
+      if (e < entry) before += t;
+    }
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) {
+      all += __shfl_xor_sync(0xffffffffu, all, off);
+      before += __shfl_xor_sync(0xffffffffu, before, off);
+    }
+    if (threadIdx.x == 0) { run_s[0] = all; run_s[1] = before; }
+  }
+  __syncthreads();
+  const long long all = run_s[0];
+  const int tiles = entry_tiles(c, entry, tile_rows);
+  const long long u0 = run_s[1] + (long long)(unit - entry * units) * tiles, u1 = u0 + tiles;
+  // the CTA whose share [all * x / ctas, all * (x + 1) / ctas) holds tile t
+  auto holder = [&](long long t) { return (int)(((t + 1) * ctas - 1) / all); };
+  const int x0 = holder(u0), x1 = holder(u1 - 1);
+  if (x0 == x1) return;                        // it was one CTA's: written
+  auto slot = [&](int x) {
+    const int later = x == x0 && all * x / ctas < u0;      // not the first piece of its CTA
+    return a.part + ((long long)(2 * x + later) * kRows + row) * (kD + 2);
+  };
+  float mm = -INFINITY, ll = 0.f, acc = 0.f;
+  for (int x = x0; x <= x1; ++x)
+    if (all * x / ctas < all * (x + 1) / ctas) mm = fmaxf(mm, slot(x)[0]);
+  for (int x = x0; x <= x1; ++x) {
+    if (all * x / ctas == all * (x + 1) / ctas) continue;  // a CTA without tiles
+    const float* p = slot(x);
+    if (p[0] == -INFINITY) continue;
+    const float f = ex2_approx(p[0] - mm);
+    acc = fmaf(p[2 + threadIdx.x], f, acc);
+    ll = fmaf(p[1], f, ll);
+  }
+  const bool some = ll > 0.f && i < paged_count(c, b);
+  const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
+  a.out[at * kD + threadIdx.x] = __float2bfloat16(some ? acc / ll : 0.f);
+  if (threadIdx.x == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+}
+
+// ---- host: one set of functions per instantiation ----
+struct Variant {
+  void (*kernel)(CUtensorMap, CUtensorMap, PagedMmaArgs);
+  void (*combine)(PagedMmaArgs, int, int);
+  int d, threads, per_sm, rows, tile_rows;
+  size_t smem;
+};
+
+template <int kD, int kGroups, int kNT> Variant variant() {
+  using C = Config<kD, kGroups, kNT>;
+  return Variant{paged_mma_kernel<kD, kGroups, kNT>, paged_mma_combine_kernel<kD, C::kRows>, kD, C::kWarps * 32, C::kPerSm, C::kRows,
+                 C::kTileRows, C::kSmem};
+}
+
+template <int kNT> bool pick_nt(const PagedCache& c, Variant* v) {
+  const int groups = c.format == RESTKV_PAGES_INT4 ? c.d / c.group : 0;
+  switch (c.d * 16 + groups) {
+    case 64 * 16 + 0: *v = variant<64, 0, kNT>(); return true;
+    case 64 * 16 + 1: *v = variant<64, 1, kNT>(); return true;
+    case 64 * 16 + 2: *v = variant<64, 2, kNT>(); return true;
+    case 128 * 16 + 0: *v = variant<128, 0, kNT>(); return true;
+    case 128 * 16 + 1: *v = variant<128, 1, kNT>(); return true;
+    case 128 * 16 + 2: *v = variant<128, 2, kNT>(); return true;
+    case 128 * 16 + 4: *v = variant<128, 4, kNT>(); return true;
+    case 256 * 16 + 0: *v = variant<256, 0, kNT>(); return true;
+    case 256 * 16 + 2: *v = variant<256, 2, kNT>(); return true;
+    case 256 * 16 + 4: *v = variant<256, 4, kNT>(); return true;
+    case 256 * 16 + 8: *v = variant<256, 8, kNT>(); return true;
+    default: return false;
+  }
+}
+
+// Up to 8 query rows go through in one tile of 8; more in tiles of 16, which read the cache once per 16.
+bool pick(const PagedCache& c, Variant* v) {
+  return (long long)c.n_tokens * c.G <= 8 ? pick_nt<1>(c, v) : pick_nt<2>(c, v);
+}
+
+}  // namespace
+
+cudaError_t paged_mma_init() {
+  PagedCache c{};
+  for (int d : {64, 128, 256})
+    for (int group : {0, 32, 64, 128})
+      for (int rows : {1, 16}) {
+        if (group > d) continue;
+        c.d = d; c.group = group; c.G = rows; c.n_tokens = 1;
+        c.format = group ? RESTKV_PAGES_INT4 : RESTKV_PAGES_BF16;
+        Variant v;
+        if (!pick(c, &v)) continue;
+        cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+      }
+  return cudaSuccess;
+}
+
+bool paged_mma_supported(const PagedCache& c) {
+  Variant v;
+  return pick(c, &v);
+}
+
+size_t paged_mma_bytes(const PagedCache& c, int sm_count) {
+  Variant v;
+  if (!pick(c, &v)) return 0;
+  return (size_t)2 * v.per_sm * sm_count * v.rows * (v.d + 2) * sizeof(float);
+}
+
+cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count,
+                             long long wait_limit, cudaStream_t st, int* launches) {
+  Variant v;
+  if (!pick(c, &v)) return cudaErrorInvalidValue;
+  CUtensorMap tmK{}, tmV{};
+  if (c.format == RESTKV_PAGES_BF16) {
+    const cuuint64_t dims[2] = {(cuuint64_t)c.d, (cuuint64_t)c.n_pages * c.Hkv * c.page_rows};
+    const cuuint64_t str[1] = {(cuuint64_t)c.d * 2};
+    if (encode_tiles((TcState*)state, &tmK, c.K, 2, dims, str, kBlockRows) != CUDA_SUCCESS ||
+        encode_tiles((TcState*)state, &tmV, c.V, 2, dims, str, kBlockRows) != CUDA_SUCCESS)
+      return cudaErrorInvalidValue;
+  }
+  PagedMmaArgs a{};
+  a.c = c; a.Q = Q; a.out = (__nv_bfloat16*)out; a.lse = lse; a.part = part; a.wait_limit = wait_limit;
+  a.row_tiles = (c.n_tokens * c.G + v.rows - 1) / v.rows;
+  a.cluster = 0;
+  const int units = c.batch * c.Hkv * a.row_tiles;
+  const int ctas = v.per_sm * sm_count;
+  cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
+  if (e != cudaSuccess) return e;
+  *launches = 2;
+  return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), v.d, 0, st, a, ctas, v.tile_rows);
+}
+
+}  // namespace restkv
