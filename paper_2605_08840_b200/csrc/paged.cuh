@@ -52,13 +52,19 @@ __device__ __forceinline__ int paged_count(const PagedCache& c, int b) {
   const int n = c.counts[b];
   return n < 0 ? 0 : n < c.n_tokens ? n : c.n_tokens;
 }
-// Byte offset, in K's pages as in V's, of block `block` of 16 rows of a sequence and head; -1 if the table's entry is out of range.
-__device__ __forceinline__ long long paged_block(const PagedCache& c, int b, int h, int block) {
+// Block `block` of 16 rows of a sequence and head, counted from the first of the pool, in K's pages as in V's; -1 if the table's entry is
+// out of range.
+__device__ __forceinline__ int paged_block_index(const PagedCache& c, int b, int h, int block) {
   const int per_page = c.page_rows / kBlockRows;
   const int slot = block / per_page;
   const int page = c.table[(long long)b * c.table_width + slot];
   if ((unsigned int)page >= (unsigned int)c.n_pages) return -1;
-  return ((long long)page * c.Hkv + h) * c.head_bytes + (long long)(block - slot * per_page) * c.block_bytes;
+  return (page * c.Hkv + h) * per_page + block - slot * per_page;
+}
+// The same as a byte offset.
+__device__ __forceinline__ long long paged_block(const PagedCache& c, int b, int h, int block) {
+  const int at = paged_block_index(c, b, h, block);
+  return at < 0 ? -1 : (long long)at * c.block_bytes;
 }
 
 // ---- the 4-bit format ----

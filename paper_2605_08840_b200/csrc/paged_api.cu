@@ -39,8 +39,9 @@ static restkv_status make_cache(const restkv_paged* s, PagedCache* out) {
   }
   c.page_rows = s->page_rows; c.n_pages = s->n_pages; c.table_width = s->table_width; c.per_head = s->lengths_per_head;
   c.head_bytes = (long long)(c.page_rows / kBlockRows) * c.block_bytes;
-  // rows are counted in 32 bits; heads of a batch are a grid's second dimension
+  // rows, of a sequence and (16 at a time) of the pool, are counted in 32 bits; heads of a batch are a grid's second dimension
   if (c.capacity() > 0x7FFFFFFFll - kBlockRows) return RESTKV_ERR_UNSUPPORTED;
+  if ((long long)c.n_pages * c.Hkv * c.page_rows > 0x7FFFFFFFll) return RESTKV_ERR_UNSUPPORTED;
   if ((long long)c.batch * c.Hkv > 65535) return RESTKV_ERR_UNSUPPORTED;
   *out = c;
   return RESTKV_OK;

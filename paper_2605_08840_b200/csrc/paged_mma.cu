@@ -9,10 +9,14 @@
 //     and 8 query rows as columns.  The accumulator layout of S is the operand layout of P^T, so the weights never leave the
 //     registers, and up to 8 query rows cost half of what P V with 16 padded rows does;
 //   - 4-bit rows are laid out for the fragments: a lane's 4 bytes of K are 8 codes of the dims that its operand registers take, its 2
-//     bytes of V 4 dims of one row.  (x & 0x0078) | 0x4180 is 16 + code as bf16, so a pair costs a shift and a logic operation;
-//     steps and offsets are applied in fp32: s += step * (q . code) + offset * sum(q) per group, with the 16 taken out by the
-//     accumulator's start -16 sum(q); o = sum bf16(p step) (code - 8) + sum p (offset + 8 step), where a product with a constant
-//     operand of -24 sums the rounded weights.  (With code instead of code - 8 there the weights' rounding would weigh twice as much.)
+//     bytes of V 4 dims of one row.
+//     K: a byte c of 0..15 is 2^-9 c as e4m3, so that K's codes are operands of m16n8k32 as they stand, 4 of them for three logic
+//     operations on 8.  q is split for it: scaled by a power of two per query row, e4m3 of that, and 16 times what is left; both parts
+//     together hold all 8 bits of a bf16 down to 2^-14 of the row's largest element (2^-22 of that is lost below), products and sums
+//     are exact in the fp32 accumulator.  s = step * (q . code) + offset * sum(q) per group, in fp32.
+//     V: (x & 0x0078) | 0x4180 is 16 + code as bf16, a shift and a logic operation for a pair.  o = sum bf16(p step) (code - 8)
+//     + sum p (offset + 8 step), where a product with a constant operand of -24 sums the rounded weights.  (With code instead of
+//     code - 8 there the weights' rounding would weigh twice as much; e4m3 has not the range that p needs.)
 // Work is split in one of two ways:
 //   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
 //     short caches, where latency counts;
@@ -21,6 +25,7 @@
 #include <math.h>
 
 #include <cooperative_groups.h>
+#include <cuda_fp16.h>
 
 #include "paged.cuh"
 #include "tc_common.cuh"
@@ -43,6 +48,29 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// d = A B for e4m3 operands, 32 of them deep.
+__device__ __forceinline__ void mma16832(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// Four values as e4m3 (hi), and 16 times the rest of each (lo).
+__device__ __forceinline__ void split_e4m3(const float* x, uint32_t* hi, uint32_t* lo) {
+  uint32_t h[2], l[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    uint16_t b;
+    uint32_t back;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(x[2 * k + 1]), "f"(x[2 * k]));
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(b));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
+    h[k] = b;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(16.f * (x[2 * k + 1] - f.y)), "f"(16.f * (x[2 * k] - f.x)));
+    l[k] = b;
+  }
+  *hi = h[0] | h[1] << 16;
+  *lo = l[0] | l[1] << 16;
 }
 // c[0..1] += x * (column sums of B), for a matrix A of bf16 pairs `xx` = (x, x): all its rows are the same, one is kept.
 __device__ __forceinline__ void mma_column_sums(float* c, uint32_t xx, uint32_t b0, uint32_t b1) {
@@ -90,7 +118,7 @@ struct PagedMmaArgs {
   RowsView Q;
   __nv_bfloat16* out;
   float* lse;        // or null
-  float* part;       // [2 * CTAs, rows, d + 2] (m, l, o), without clusters
+  float* part;       // per CTA two of: o [rows, d], (m, l) [rows]; without clusters
   int row_tiles;     // units per KV head
   int cluster;       // CTAs per unit, 0: tiles of all units end to end
   long long wait_limit;
@@ -203,15 +231,18 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   int entry = 0;
   if (!a.cluster) {
     if (warp == 0) {
-      const Run run = find_run(c, a.row_tiles, C::kTileRows, [&](long long t) { return t * blockIdx.x / gridDim.x; });
+      const Run run = find_run(c, a.row_tiles, C::kTileRows, [&](long long t) {
+        return blockIdx.x < t ? t * blockIdx.x / (t < gridDim.x ? t : gridDim.x) : 0;
+      });
       if (lane == 0) { run_s[0] = run.tiles; run_s[1] = run.first; run_entry = run.entry; }
     }
     __syncthreads();
-    tile = run_s[0] * blockIdx.x / gridDim.x;
-    end = run_s[0] * (blockIdx.x + 1) / gridDim.x;
+    const long long ctas = run_s[0] < gridDim.x ? run_s[0] : gridDim.x;     // of them each has a tile
+    if (blockIdx.x >= ctas) return;
+    tile = run_s[0] * blockIdx.x / ctas;
+    end = run_s[0] * (blockIdx.x + 1) / ctas;
     first = run_s[1];
     entry = run_entry;
-    if (tile >= end) return;
   } else {
     __syncthreads();
   }
@@ -252,7 +283,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     const int mine = t1 - t0 > warp ? (t1 - t0 - warp + kW - 1) / kW : 0;   // tiles t0 + warp + kW * i
 
     // ---- requests: the blocks' places are looked up 32 / kBlocks tiles at a time, one lane each ----
-    long long place = -1;
+    int place = -1;
     unsigned int absent = 0;                   // bit slot * kBlocks + block: nothing was loaded there
     auto request = [&](int i) {                // by the whole warp
       constexpr int kAhead = 32 / kBlocks;
@@ -261,12 +292,12 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         const int block = t * kBlocks + lane % kBlocks;
         place = -1;
         if (t < t1 && block < blocks) {
-          place = paged_block(c, b, h, block);
+          place = paged_block_index(c, b, h, block);
           if (place < 0) atomicOr(c.dev_status, kDevBadIndex);
         }
       }
       const int s = (used + i) % kStages;
-      long long at[kBlocks];
+      int at[kBlocks];
       int there = 0;
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
@@ -279,19 +310,27 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         uint8_t* dst = ring + (uint32_t)s * C::kStageBytes;
         uint64_t* bar = &full[warp][s];
         mbar_arrive_expect_tx(bar, (uint32_t)there * 2 * C::kBlockBytes);
-#pragma unroll
-        for (int k = 0; k < kBlocks; ++k) {
-          if (at[k] < 0) continue;
-          uint8_t* kd = dst + k * 2 * C::kBlockBytes;
-          if constexpr (kInt4) {
-            bulk_load(kd, c.K + at[k], C::kBlockBytes, bar);
-            bulk_load(kd + C::kBlockBytes, c.V + at[k], C::kBlockBytes, bar);
+        if constexpr (kInt4) {
+          // K's blocks, then V's; two that follow one another in a page come in one piece
+          if (kBlocks == 2 && at[0] >= 0 && at[kBlocks - 1] == at[0] + 1) {
+            bulk_load(dst, c.K + (long long)at[0] * C::kBlockBytes, 2 * C::kBlockBytes, bar);
+            bulk_load(dst + 2 * C::kBlockBytes, c.V + (long long)at[0] * C::kBlockBytes, 2 * C::kBlockBytes, bar);
           } else {
-            const int row = (int)(at[k] / (2 * kD));
+#pragma unroll
+            for (int k = 0; k < kBlocks; ++k) {
+              if (at[k] < 0) continue;
+              bulk_load(dst + k * C::kBlockBytes, c.K + (long long)at[k] * C::kBlockBytes, C::kBlockBytes, bar);
+              bulk_load(dst + (kBlocks + k) * C::kBlockBytes, c.V + (long long)at[k] * C::kBlockBytes, C::kBlockBytes, bar);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < kBlocks; ++k) {
+            if (at[k] < 0) continue;
 #pragma unroll
             for (int x = 0; x < kD / 64; ++x) {
-              tma_load_2d(kd + x * 2048, &tmK, bar, x * 64, row);
-              tma_load_2d(kd + C::kBlockBytes + x * 2048, &tmV, bar, x * 64, row);
+              tma_load_2d(dst + k * C::kBlockBytes + x * 2048, &tmK, bar, x * 64, at[k] * kBlockRows);
+              tma_load_2d(dst + (kBlocks + k) * C::kBlockBytes + x * 2048, &tmV, bar, x * 64, at[k] * kBlockRows);
             }
           }
         }
@@ -300,9 +339,11 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     };
     for (int i = 0; i < mine && i < kStages; ++i) request(i);
 
-    // ---- Q as the A operand: query rows rho0 + r (and + 8), kD / 16 steps; sums of q per group; what each row sees ----
-    uint32_t qa[kD / 16][kNT == 2 ? 4 : 2];
-    float q_sum[kNT][kG];
+    // ---- Q as the A operand: query rows rho0 + r (and + 8); what each row sees ----
+    // bf16: kD / 16 steps.  4 bits: kD / 32 steps with the upper parts of 8 rows as rows 0..7 and the lower ones as rows 8..15; sums of q
+    // per group; all in units of 2^-exponent, which the logits' factor takes out again.
+    uint32_t qa[kInt4 ? kWords : kD / 16][kInt4 ? 4 * kNT : 2 * kNT];
+    float q_sum[kNT][kG], unscale[kNT];
     int sees[kNT];
     int sees_least = n;
 #pragma unroll
@@ -310,39 +351,59 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       const int rho = rho0 + r + 8 * t, i = rho / c.G, g = rho - i * c.G;
       const bool live = rho < R && i < count;
       sees[t] = live ? n - (count - 1 - i) : n;
+      sees_least = min(sees_least, sees[t]);
+      unscale[t] = 1.f;
       const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
+      if constexpr (kInt4) {
+        uint4 u[kWords];                       // dims 32 m + 8 q4 .. + 7
+        float top = 0.f;
 #pragma unroll
-      for (int g2 = 0; g2 < kG; ++g2) q_sum[t][g2] = 0.f;
+        for (int m = 0; m < kWords; ++m) {
+          u[m] = live ? *reinterpret_cast<const uint4*>(q + 32 * m + 8 * q4) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-      for (int m = 0; m < kWords; ++m) {
-        if constexpr (kInt4) {     // dims 32 m + 8 q4 .. + 7, in the pairs (i, i + 4) that a word's codes come in
-          uint4 u = make_uint4(0u, 0u, 0u, 0u);
-          if (live) u = *reinterpret_cast<const uint4*>(q + 32 * m + 8 * q4);
-          qa[2 * m][t] = __byte_perm(u.x, u.z, 0x5410);
-          qa[2 * m][kNT + t] = __byte_perm(u.x, u.z, 0x7632);
-          qa[2 * m + 1][t] = __byte_perm(u.y, u.w, 0x5410);
-          qa[2 * m + 1][kNT + t] = __byte_perm(u.y, u.w, 0x7632);
-          q_sum[t][m / kPerGroup] += ((lower(u.x) + upper(u.x)) + (lower(u.y) + upper(u.y))) + ((lower(u.z) + upper(u.z)) + (lower(u.w) + upper(u.w)));
-        } else {
+          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(fabsf(lower((&u[m].x)[x])), fabsf(upper((&u[m].x)[x]))));
+        }
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // 2^e top in [128, 256), for top of 2^-100 .. 2^100; an infinite one makes the row's logits NaN
+        int e = 134 - (int)(__float_as_uint(top) >> 23);
+        e = e < -100 ? -100 : e > 100 ? 100 : e;
+        const float scale = top < INFINITY ? __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7FFFFFFFu);
+        unscale[t] = __uint_as_float((uint32_t)(127 + 9 - e) << 23);   // with the codes' 2^-9
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            const int k = 2 * m + s;
-            qa[k][t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
-            qa[k][kNT + t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
+        for (int g2 = 0; g2 < kG; ++g2) q_sum[t][g2] = 0.f;
+#pragma unroll
+        for (int m = 0; m < kWords; ++m) {
+          float v[8];                          // even dims, then odd ones: the order of a word's codes split by bytes
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            v[x] = lower((&u[m].x)[x]) * scale;
+            v[4 + x] = upper((&u[m].x)[x]) * scale;
           }
+          split_e4m3(v, &qa[m][4 * t], &qa[m][4 * t + 1]);
+          split_e4m3(v + 4, &qa[m][4 * t + 2], &qa[m][4 * t + 3]);
+          q_sum[t][m / kPerGroup] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        }
+#pragma unroll
+        for (int g2 = 0; g2 < kG; ++g2) {
+          q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 1);
+          q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 2);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kD / 16; ++k) {
+          qa[k][t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
+          qa[k][kNT + t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
         }
       }
-#pragma unroll
-      for (int g2 = 0; g2 < kG; ++g2) {
-        q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 1);
-        q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 2);
-      }
-      sees_least = min(sees_least, sees[t]);
     }
     sees_least = __reduce_min_sync(0xffffffffu, sees_least);
 
-    const float to_log2 = c.scale * kLog2e, cap_log2 = c.softcap * kLog2e;
-    const float cap_in = c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : 0.f;
+    const float cap_log2 = c.softcap * kLog2e;
+    float to_log2[kNT];                        // what a row's sums are multiplied with: to log2 units, or to the cap's exponent
+#pragma unroll
+    for (int t = 0; t < kNT; ++t)
+      to_log2[t] = (c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : c.scale * kLog2e) * unscale[t];
     float m[kNT], l[kNT];                      // log2 units; l: this lane's share of the row's sum
     float o[kD / 16][kNT][4];                  // dims of the 16-dim tile (r, r + 8), query rows 2 q4, 2 q4 + 1 (+ 8 per tile)
     float z[kG][kNT][2], lo[kG][kNT];          // 4 bits: -24 sum bf16(p step); this lane's share of sum p (offset + 8 step)
@@ -376,41 +437,34 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       float sc[kBlocks][kNT][4];
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
-        const uint32_t kt = stage + k * 2 * C::kBlockBytes;
+        const uint32_t kt = stage + k * C::kBlockBytes;
         if constexpr (kInt4) {
-          float p0[kG][4], p1[kG][4];          // steps and offsets of the four rows
+          uint32_t w[2][kWords];               // rows r / 2 + 4 (r % 2) (+ 8): columns r of the two tiles of 8 columns
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
+            lds_words<kWords>(kt + (uint32_t)(8 * half + (r >> 1) + 4 * (r & 1)) * (kD / 2) + q4 * (kD / 8), w[half]);
 #pragma unroll
           for (int g = 0; g < kG; ++g) {
-            const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * q4);
-            p0[g][0] = lower(u.x); p0[g][1] = upper(u.x); p0[g][2] = lower(u.y); p0[g][3] = upper(u.y);
-            p1[g][0] = lower(u.z); p1[g][1] = upper(u.z); p1[g][2] = lower(u.w); p1[g][3] = upper(u.w);
-          }
+            float acc[2][kNT][4];              // upper parts of rows (columns 2 q4, 2 q4 + 1), lower parts
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t w[kWords];
-            lds_words<kWords>(kt + (uint32_t)(8 * half + (r >> 1) + 4 * (r & 1)) * (kD / 2) + q4 * (kD / 8), w);
+            for (int half = 0; half < 2; ++half)
 #pragma unroll
-            for (int g = 0; g < kG; ++g) {
-              float acc[4];
-              acc[0] = acc[1] = -16.f * q_sum[0][g];
-              acc[2] = acc[3] = kNT == 2 ? -16.f * q_sum[kNT - 1][g] : 0.f;
+              for (int t = 0; t < kNT; ++t) {
+                acc[half][t][0] = acc[half][t][1] = acc[half][t][2] = acc[half][t][3] = 0.f;
 #pragma unroll
-              for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x) {
-                const uint32_t a0[4] = {qa[2 * x][0], kNT == 2 ? qa[2 * x][1] : 0u, qa[2 * x][kNT], kNT == 2 ? qa[2 * x][kNT + kNT - 1] : 0u};
-                const uint32_t a1[4] = {qa[2 * x + 1][0], kNT == 2 ? qa[2 * x + 1][1] : 0u, qa[2 * x + 1][kNT],
-                                        kNT == 2 ? qa[2 * x + 1][kNT + kNT - 1] : 0u};
-                mma16816(acc, a0, code_pair<0>(w[x]), code_pair<1>(w[x]));
-                mma16816(acc, a1, code_pair<2>(w[x]), code_pair<3>(w[x]));
+                for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x)
+                  mma16832(acc[half][t], &qa[x][4 * t], w[half][x] & 0x0F0F0F0Fu, w[half][x] >> 4 & 0x0F0F0F0Fu);
               }
+            const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * q4);
+            const float step[4] = {lower(u.x), upper(u.x), lower(u.y), upper(u.y)}, off[4] = {lower(u.z), upper(u.z), lower(u.w), upper(u.w)};
 #pragma unroll
-              for (int t = 0; t < kNT; ++t)
+            for (int t = 0; t < kNT; ++t)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                  const int j = 2 * half + e;
-                  const float add = p1[g][j] * q_sum[t][g];
-                  sc[k][t][j] = g == 0 ? fmaf(p0[g][j], acc[2 * t + e], add) : fmaf(p0[g][j], acc[2 * t + e], sc[k][t][j] + add);
-                }
-            }
+              for (int j = 0; j < 4; ++j) {
+                const float dot = fmaf(0.0625f, acc[j >> 1][t][2 + (j & 1)], acc[j >> 1][t][j & 1]);
+                const float add = off[j] * (q_sum[t][g] * 0x1p-9f);
+                sc[k][t][j] = fmaf(step[j], dot, g == 0 ? add : sc[k][t][j] + add);
+              }
           }
         } else {
           float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -437,8 +491,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
-            if (c.softcap > 0.f) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j] * cap_in)), cap_log2);
-            else sc[k][t][j] *= to_log2;
+            if (c.softcap > 0.f) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j] * to_log2[t])), cap_log2);
+            else sc[k][t][j] *= to_log2[t];
           }
       if (edge) {
 #pragma unroll
@@ -459,7 +513,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         f[t] = 1.f;
-        if (mx > m[t]) {
+        if (mx > m[t] + kRescaleThreshold) {   // weights of up to 2^8 do no harm: o is rescaled when they would grow past that
           f[t] = ex2_approx(m[t] - mx);        // m = -inf gives 0
           m[t] = mx;
           l[t] *= f[t];
@@ -491,7 +545,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
-        const uint32_t vt = stage + k * 2 * C::kBlockBytes + C::kBlockBytes;
+        const uint32_t vt = stage + (kBlocks + k) * C::kBlockBytes;
         // rows past the cache hold anything: their bits are cleared, so that a weight of 0 finds a number there
         uint32_t keep01 = 0xFFFFFFFFu, keep23 = 0xFFFFFFFFu;
         if (edge) {
@@ -626,9 +680,9 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       } else if (whole) {
         finish(row, k, acc, mm, ll);
       } else {
-        float* p = a.part + ((long long)(2 * blockIdx.x + (piece > 0)) * kRows + row) * (kD + 2);
-        p[2 + k] = acc;
-        if (k == 0) { p[0] = mm; p[1] = ll; }
+        float* p = a.part + (long long)(2 * blockIdx.x + (piece > 0)) * kRows * (kD + 2);
+        p[row * kD + k] = acc;
+        if (k == 0) { p[kRows * kD + 2 * row] = mm; p[kRows * kD + 2 * row + 1] = ll; }
       }
     }
     if (a.cluster) {
@@ -668,9 +722,11 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   }
 }
 
-// grid (units, rows): merges what several CTAs left of a unit.
+// grid (units, rows), block 2 kD: merges what several CTAs left of a unit, 8 pieces at a time (kD / 4 threads each).
+constexpr int kMaxCtas = 512;
+
 template <int kD, int kRows>
-__global__ void __launch_bounds__(kD) paged_mma_combine_kernel(const __grid_constant__ PagedMmaArgs a, int ctas, int tile_rows) {
+__global__ void __launch_bounds__(2 * kD) paged_mma_combine_kernel(const __grid_constant__ PagedMmaArgs a, int ctas, int tile_rows) {
   grid_dependency_wait();
   __shared__ long long run_s[2];
   const PagedCache& c = a.c;
@@ -698,28 +754,59 @@ __global__ void __launch_bounds__(kD) paged_mma_combine_kernel(const __grid_cons
   const long long all = run_s[0];
   const int tiles = entry_tiles(c, entry, tile_rows);
   const long long u0 = run_s[1] + (long long)(unit - entry * units) * tiles, u1 = u0 + tiles;
+  if (ctas > all) ctas = (int)all;
   // the CTA whose share [all * x / ctas, all * (x + 1) / ctas) holds tile t
   auto holder = [&](long long t) { return (int)(((t + 1) * ctas - 1) / all); };
   const int x0 = holder(u0), x1 = holder(u1 - 1);
   if (x0 == x1) return;                        // it was one CTA's: written
-  auto slot = [&](int x) {
-    const int later = x == x0 && all * x / ctas < u0;      // not the first piece of its CTA
-    return a.part + ((long long)(2 * x + later) * kRows + row) * (kD + 2);
-  };
-  float mm = -INFINITY, ll = 0.f, acc = 0.f;
-  for (int x = x0; x <= x1; ++x)
-    if (all * x / ctas < all * (x + 1) / ctas) mm = fmaxf(mm, slot(x)[0]);
-  for (int x = x0; x <= x1; ++x) {
-    if (all * x / ctas == all * (x + 1) / ctas) continue;  // a CTA without tiles
-    const float* p = slot(x);
-    if (p[0] == -INFINITY) continue;
-    const float f = ex2_approx(p[0] - mm);
-    acc = fmaf(p[2 + threadIdx.x], f, acc);
-    ll = fmaf(p[1], f, ll);
+  // a CTA's first piece lies in its first slot, its last in the second; x0's is a later one where the unit begins inside its share
+  constexpr long long kSlot = kRows * (kD + 2);
+  const bool later = all * x0 / ctas < u0;
+  const int pieces = x1 - x0 + 1;
+  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0 && later)) * kSlot; };
+  __shared__ float factor[kMaxCtas];
+  __shared__ float of_warp[2][2 * kD / 32];
+  __shared__ float4 acc_s[8][kD / 4];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  float mm = -INFINITY;
+  for (int x = threadIdx.x; x < pieces; x += 2 * kD) mm = fmaxf(mm, piece(x)[kRows * kD + 2 * row]);
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+  if (lane == 0) of_warp[0][warp] = mm;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 2 * kD / 32; ++w) mm = fmaxf(mm, of_warp[0][w]);
+  float ll = 0.f;
+  for (int x = threadIdx.x; x < pieces; x += 2 * kD) {
+    const float* ml = piece(x) + kRows * kD + 2 * row;
+    const float f = ml[0] == -INFINITY ? 0.f : ex2_approx(ml[0] - mm);
+    factor[x] = f;
+    ll = fmaf(ml[1], f, ll);
   }
+#pragma unroll
+  for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
+  if (lane == 0) of_warp[1][warp] = ll;
+  __syncthreads();
+  ll = 0.f;
+#pragma unroll
+  for (int w = 0; w < 2 * kD / 32; ++w) ll += of_warp[1][w];
+  const int sub = threadIdx.x / (kD / 4), v = threadIdx.x % (kD / 4);
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+  for (int x = sub; x < pieces; x += 8) {
+    const float4 o = reinterpret_cast<const float4*>(piece(x) + row * kD)[v];
+    const float f = factor[x];
+    acc.x = fmaf(o.x, f, acc.x); acc.y = fmaf(o.y, f, acc.y); acc.z = fmaf(o.z, f, acc.z); acc.w = fmaf(o.w, f, acc.w);
+  }
+  acc_s[sub][v] = acc;
+  __syncthreads();
+  if (threadIdx.x >= kD) return;
+  float sum = 0.f;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) sum += reinterpret_cast<const float*>(acc_s[x])[threadIdx.x];
   const bool some = ll > 0.f && i < paged_count(c, b);
   const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
-  a.out[at * kD + threadIdx.x] = __float2bfloat16(some ? acc / ll : 0.f);
+  a.out[at * kD + threadIdx.x] = __float2bfloat16(some ? sum / ll : 0.f);
   if (threadIdx.x == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
 }
 
@@ -807,11 +894,11 @@ cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q
   a.row_tiles = (c.n_tokens * c.G + v.rows - 1) / v.rows;
   a.cluster = 0;
   const int units = c.batch * c.Hkv * a.row_tiles;
-  const int ctas = v.per_sm * sm_count;
+  const int ctas = v.per_sm * sm_count < kMaxCtas ? v.per_sm * sm_count : kMaxCtas;
   cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
   *launches = 2;
-  return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), v.d, 0, st, a, ctas, v.tile_rows);
+  return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), 2 * v.d, 0, st, a, ctas, v.tile_rows);
 }
 
 }  // namespace restkv
