@@ -10,19 +10,20 @@
 //     registers, and up to 8 query rows cost half of what P V with 16 padded rows does;
 //   - 4-bit rows are laid out for the fragments: a lane's 4 bytes of K are 8 codes of the dims that its operand registers take, its 2
 //     bytes of V 4 dims of one row.
-//     K: a byte c of 0..15 is 2^-9 c as e4m3, so that K's codes are operands of m16n8k32 as they stand, 4 of them for three logic
-//     operations on 8.  q is split for it: scaled by a power of two per query row, e4m3 of that, and 16 times what is left; both parts
-//     together hold all 8 bits of a bf16 down to 2^-14 of the row's largest element (2^-22 of that is lost below), products and sums
-//     are exact in the fp32 accumulator.  s = step * (q . code) + offset * sum(q) per group, in fp32.
-//     V: (x & 0x0078) | 0x4180 is 16 + code as bf16, a shift and a logic operation for a pair.  o = sum bf16(p step) (code - 8)
-//     + sum p (offset + 8 step), where a product with a constant operand of -24 sums the rounded weights.  (With code instead of
-//     code - 8 there the weights' rounding would weigh twice as much; e4m3 has not the range that p needs.)
+//     A nibble is an operand as it stands: the 16 bits c << 4k are the f16 subnormal 2^(4k - 24) c for k = 0, 1, products with it are
+//     exact in the fp32 accumulator, and a shift and four logic operations make 4 operand registers of 8 codes.  q is f16 scaled by a
+//     power of two per query row (exact down to 2^-28 of the row's largest element).  s = step * (q . code) + offset * sum(q) per
+//     group, o = sum f16(p step) code + sum p offset, all sums in fp32.
+//     (bf16 16 + code: two operations per register, and the weights' rounding weighs twice as much unless 8 is taken off the codes:
+//     60 us for 131072 rows.  e4m3 codes: m16n8k32 is carried out as conversions and f16 products here, 60 us, too.)
 // Work is split in one of two ways:
 //   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
 //     short caches, where latency counts;
 //   - the tiles of all units end to end, an equal share of them per CTA whatever the sequences' lengths, partial results in the
 //     workspace and a second kernel that merges what several CTAs share.
 #include <math.h>
+
+#include <type_traits>
 
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
@@ -49,35 +50,25 @@ __device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// d = A B for e4m3 operands, 32 of them deep.
-__device__ __forceinline__ void mma16832(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+__device__ __forceinline__ void mma16816_f16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// Four values as e4m3 (hi), and 16 times the rest of each (lo).
-__device__ __forceinline__ void split_e4m3(const float* x, uint32_t* hi, uint32_t* lo) {
-  uint32_t h[2], l[2];
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    uint16_t b;
-    uint32_t back;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(x[2 * k + 1]), "f"(x[2 * k]));
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(back) : "h"(b));
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&back));
-    h[k] = b;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(b) : "f"(16.f * (x[2 * k + 1] - f.y)), "f"(16.f * (x[2 * k] - f.x)));
-    l[k] = b;
-  }
-  *hi = h[0] | h[1] << 16;
-  *lo = l[0] | l[1] << 16;
+__device__ __forceinline__ void mma16816_f16_start(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {   // c = A B
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+               : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
-// c[0..1] += x * (column sums of B), for a matrix A of bf16 pairs `xx` = (x, x): all its rows are the same, one is kept.
-__device__ __forceinline__ void mma_column_sums(float* c, uint32_t xx, uint32_t b0, uint32_t b1) {
-  float unused0, unused1;
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %4, %4, %4}, {%5, %6}, {%7, %8, %9, %9};"
-               : "=f"(c[0]), "=f"(c[1]), "=f"(unused0), "=f"(unused1)
-               : "r"(xx), "r"(b0), "r"(b1), "f"(c[0]), "f"(c[1]), "f"(0.f));
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float lg2_approx(float x) {
+  float y;
+  asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
 }
 __device__ __forceinline__ uint32_t lds32(uint32_t addr) {
   uint32_t v;
@@ -104,14 +95,12 @@ template <int kWords> __device__ __forceinline__ void lds_words(uint32_t addr, u
     }
   }
 }
-// Codes i and i + 4 of a word (those at 4 i of both halves) as a pair of bf16, 16 too large.
+// The codes at 4 i of both halves of a word as a pair of f16 subnormals: 2^-24 code for even i, 2^-20 code for odd i.
 template <int i> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
-  return ((i == 0 ? w << 3 : w >> (4 * i - 3)) & 0x00780078u) | 0x41804180u;
+  return (i >= 2 ? w >> 8 : w) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
 }
 __device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-constexpr uint32_t kMinus24 = 0xC1C0C1C0u;
 
 struct PagedMmaArgs {
   PagedCache c;
@@ -128,6 +117,8 @@ struct PagedMmaArgs {
 template <int kD, int kGroups, int kNT> struct Config {
   static constexpr bool kInt4 = kGroups > 0;
   static constexpr int kRows = 8 * kNT;
+  // log2 of the largest weight that a rescaling leaves, and of what it may grow to before the next one (in 4 bits times the step, in f16)
+  static constexpr float kStart = kInt4 ? 5.f : 0.f, kSlack = kInt4 ? 13.f : 8.f;
   static constexpr uint32_t kBlockBytes = kInt4 ? 8u * kD + 64u * kGroups : 32u * kD;   // 16 rows of K, or of V
   // tiles of two blocks spread the softmax's exchanges and the waits over more rows; at 8 KB and more they cost ring slots
   static constexpr int kBlocks = kBlockBytes <= 2560 ? 2 : 1;
@@ -197,13 +188,14 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   using C = Config<kD, kGroups, kNT>;
   constexpr bool kInt4 = C::kInt4;
   constexpr int kW = C::kWarps, kStages = C::kStages, kRows = C::kRows, kBlocks = C::kBlocks, kWords = kD / 32;
+  constexpr float kStart = C::kStart, kSlack = C::kSlack;
   constexpr int kG = kInt4 ? kGroups : 1;
   constexpr int kPerGroup = kWords / kG;       // 32-dim blocks of a group
   const PagedCache& c = a.c;
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[kW][kStages];
   __shared__ float w_ml[kW][kRows][2];
-  __shared__ float w_lo[kW][kRows][kG];        // 4 bits: sum of p (offset + 8 step) per group
+  __shared__ float w_lo[kW][kRows][kG];        // 4 bits: sum of p offset per group
   __shared__ float c_ml[kRows][2];
   __shared__ int abort_flag;
   __shared__ long long run_s[2];
@@ -247,7 +239,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     __syncthreads();
   }
 
-  int used = 0;                                // tiles that this warp has taken from its ring
+  int slot = 0;                                // of the warp's ring: the next tile's, and the parity it completes with
+  uint32_t parity = 0;
   bool ok = true;
   for (int piece = 0;; ++piece) {
     // ---- the unit and the run of its tiles ----
@@ -285,7 +278,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     // ---- requests: the blocks' places are looked up 32 / kBlocks tiles at a time, one lane each ----
     int place = -1;
     unsigned int absent = 0;                   // bit slot * kBlocks + block: nothing was loaded there
-    auto request = [&](int i) {                // by the whole warp
+    auto request = [&](int i, int s) {         // tile i into slot s, by the whole warp
       constexpr int kAhead = 32 / kBlocks;
       if (i % kAhead == 0) {
         const int t = t0 + warp + (i + lane / kBlocks) * kW;
@@ -296,7 +289,6 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           if (place < 0) atomicOr(c.dev_status, kDevBadIndex);
         }
       }
-      const int s = (used + i) % kStages;
       int at[kBlocks];
       int there = 0;
 #pragma unroll
@@ -337,12 +329,14 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
       __syncwarp();
     };
-    for (int i = 0; i < mine && i < kStages; ++i) request(i);
+#pragma unroll
+    for (int i = 0; i < kStages; ++i)
+      if (i < mine) request(i, slot + i < kStages ? slot + i : slot + i - kStages);
 
-    // ---- Q as the A operand: query rows rho0 + r (and + 8); what each row sees ----
-    // bf16: kD / 16 steps.  4 bits: kD / 32 steps with the upper parts of 8 rows as rows 0..7 and the lower ones as rows 8..15; sums of q
-    // per group; all in units of 2^-exponent, which the logits' factor takes out again.
-    uint32_t qa[kInt4 ? kWords : kD / 16][kInt4 ? 4 * kNT : 2 * kNT];
+    // ---- Q as the A operand: query rows rho0 + r (and + 8), kD / 16 steps; what each row sees ----
+    // 4 bits: in f16, scaled by a power of two per row (and 2^-4 where the codes come 16 times too large); sums of q per group in the
+    // codes' and that scale, which the logits' factor takes out again.
+    uint32_t qa[kD / 16][2 * kNT];
     float q_sum[kNT][kG], unscale[kNT];
     int sees[kNT];
     int sees_least = n;
@@ -365,29 +359,33 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         }
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // 2^e top in [128, 256), for top of 2^-100 .. 2^100; an infinite one makes the row's logits NaN
-        int e = 134 - (int)(__float_as_uint(top) >> 23);
+        // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
+        int e = 141 - (int)(__float_as_uint(top) >> 23);
         e = e < -100 ? -100 : e > 100 ? 100 : e;
         const float scale = top < INFINITY ? __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7FFFFFFFu);
-        unscale[t] = __uint_as_float((uint32_t)(127 + 9 - e) << 23);   // with the codes' 2^-9
+        unscale[t] = __uint_as_float((uint32_t)(127 + 24 - e) << 23);
 #pragma unroll
         for (int g2 = 0; g2 < kG; ++g2) q_sum[t][g2] = 0.f;
 #pragma unroll
         for (int m = 0; m < kWords; ++m) {
-          float v[8];                          // even dims, then odd ones: the order of a word's codes split by bytes
+          float v[8];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            v[x] = lower((&u[m].x)[x]) * scale;
-            v[4 + x] = upper((&u[m].x)[x]) * scale;
+            v[2 * x] = lower((&u[m].x)[x]) * scale;
+            v[2 * x + 1] = upper((&u[m].x)[x]) * scale;
           }
-          split_e4m3(v, &qa[m][4 * t], &qa[m][4 * t + 1]);
-          split_e4m3(v + 4, &qa[m][4 * t + 2], &qa[m][4 * t + 3]);
+          // the pairs (i, i + 4) that a word's codes come in
+          qa[2 * m][t] = pack_f16x2(v[0], v[4]);
+          qa[2 * m][kNT + t] = pack_f16x2(0x1p-4f * v[1], 0x1p-4f * v[5]);
+          qa[2 * m + 1][t] = pack_f16x2(v[2], v[6]);
+          qa[2 * m + 1][kNT + t] = pack_f16x2(0x1p-4f * v[3], 0x1p-4f * v[7]);
           q_sum[t][m / kPerGroup] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
 #pragma unroll
         for (int g2 = 0; g2 < kG; ++g2) {
           q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 1);
           q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 2);
+          q_sum[t][g2] *= 0x1p-24f;
         }
       } else {
 #pragma unroll
@@ -404,34 +402,24 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
     for (int t = 0; t < kNT; ++t)
       to_log2[t] = (c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : c.scale * kLog2e) * unscale[t];
-    float m[kNT], l[kNT];                      // log2 units; l: this lane's share of the row's sum
+    float ref[kNT], l[kNT];                    // weights are 2^(logit - ref); l: this lane's share of the row's sum
     float o[kD / 16][kNT][4];                  // dims of the 16-dim tile (r, r + 8), query rows 2 q4, 2 q4 + 1 (+ 8 per tile)
-    float z[kG][kNT][2], lo[kG][kNT];          // 4 bits: -24 sum bf16(p step); this lane's share of sum p (offset + 8 step)
+    float lo[kG][kNT];                         // 4 bits: this lane's share of sum p offset
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
-      m[t] = -INFINITY;
+      ref[t] = -INFINITY;
       l[t] = 0.f;
 #pragma unroll
       for (int k = 0; k < kD / 16; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[k][t][e] = 0.f;
 #pragma unroll
-      for (int g = 0; g < kG; ++g) { z[g][t][0] = z[g][t][1] = 0.f; lo[g][t] = 0.f; }
+      for (int g = 0; g < kG; ++g) lo[g][t] = 0.f;
     }
 
-    for (int i = 0; i < mine; ++i) {
-      const int s = (used + i) % kStages;
-      ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][s], (uint32_t)((used + i) / kStages) & 1u, &abort_flag, c.dev_status, kDevTimeout,
-                                             a.wait_limit));
-      if (!ok) {
-        if (lane == 0)   // nothing may still be on its way into shared memory when the CTA returns
-          for (int j = i; j < mine && j < i + kStages; ++j) wait_issued(&full[warp][(used + j) % kStages], (uint32_t)((used + j) / kStages));
-        break;
-      }
-      const uint32_t stage = ring_addr + (uint32_t)s * C::kStageBytes;
-      const int row0 = (t0 + warp + i * kW) * C::kTileRows;
-      const unsigned int gone = absent >> (s * kBlocks) & ((1u << kBlocks) - 1u);
-      const bool edge = row0 + C::kTileRows > sees_least || gone != 0;
+    // One tile; kEdge: some of its rows are not there, or not for every query row.
+    auto take = [&](auto edge, uint32_t stage, int row0, unsigned int gone) {
+      constexpr bool kEdge = decltype(edge)::value;
       // rows of the lane's four columns in a block: 4 bits q4 + 4 j, which is the order of the parameters; bf16 2 q4 + (j & 1) + 8 (j / 2)
       auto column = [&](int j) { return kInt4 ? q4 + 4 * j : 2 * q4 + (j & 1) + 8 * (j >> 1); };
       float sc[kBlocks][kNT][4];
@@ -445,26 +433,25 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             lds_words<kWords>(kt + (uint32_t)(8 * half + (r >> 1) + 4 * (r & 1)) * (kD / 2) + q4 * (kD / 8), w[half]);
 #pragma unroll
           for (int g = 0; g < kG; ++g) {
-            float acc[2][kNT][4];              // upper parts of rows (columns 2 q4, 2 q4 + 1), lower parts
+            float acc[2][4];                   // rows r, r + 8; columns 2 q4, 2 q4 + 1
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-              for (int t = 0; t < kNT; ++t) {
-                acc[half][t][0] = acc[half][t][1] = acc[half][t][2] = acc[half][t][3] = 0.f;
-#pragma unroll
-                for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x)
-                  mma16832(acc[half][t], &qa[x][4 * t], w[half][x] & 0x0F0F0F0Fu, w[half][x] >> 4 & 0x0F0F0F0Fu);
+              for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x) {
+                const uint32_t a0[4] = {qa[2 * x][0], kNT == 2 ? qa[2 * x][1] : 0u, qa[2 * x][kNT], kNT == 2 ? qa[2 * x][kNT + kNT - 1] : 0u};
+                const uint32_t a1[4] = {qa[2 * x + 1][0], kNT == 2 ? qa[2 * x + 1][1] : 0u, qa[2 * x + 1][kNT],
+                                        kNT == 2 ? qa[2 * x + 1][kNT + kNT - 1] : 0u};
+                if (x == g * kPerGroup) mma16816_f16_start(acc[half], a0, code_pair<0>(w[half][x]), code_pair<1>(w[half][x]));
+                else mma16816_f16(acc[half], a0, code_pair<0>(w[half][x]), code_pair<1>(w[half][x]));
+                mma16816_f16(acc[half], a1, code_pair<2>(w[half][x]), code_pair<3>(w[half][x]));
               }
             const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * q4);
             const float step[4] = {lower(u.x), upper(u.x), lower(u.y), upper(u.y)}, off[4] = {lower(u.z), upper(u.z), lower(u.w), upper(u.w)};
 #pragma unroll
             for (int t = 0; t < kNT; ++t)
 #pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const float dot = fmaf(0.0625f, acc[j >> 1][t][2 + (j & 1)], acc[j >> 1][t][j & 1]);
-                const float add = off[j] * (q_sum[t][g] * 0x1p-9f);
-                sc[k][t][j] = fmaf(step[j], dot, g == 0 ? add : sc[k][t][j] + add);
-              }
+              for (int j = 0; j < 4; ++j)
+                sc[k][t][j] = fmaf(step[j], acc[j >> 1][2 * t + (j & 1)], g == 0 ? off[j] * q_sum[t][g] : fmaf(off[j], q_sum[t][g], sc[k][t][j]));
           }
         } else {
           float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
@@ -489,12 +476,17 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
         for (int t = 0; t < kNT; ++t)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
-            if (c.softcap > 0.f) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j] * to_log2[t])), cap_log2);
-            else sc[k][t][j] *= to_log2[t];
-          }
-      if (edge) {
+          for (int j = 0; j < 4; ++j) sc[k][t][j] *= to_log2[t];
+      if (cap_log2 > 0.f) {
+        // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int t = 0; t < kNT; ++t)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j])), cap_log2);
+      }
+      if constexpr (kEdge) {
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
@@ -503,6 +495,34 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             for (int j = 0; j < 4; ++j)
               if (row0 + k * kBlockRows + column(j) >= sees[t] || (gone >> k & 1u)) sc[k][t][j] = -INFINITY;
       }
+      // bits of the rows of V that are there
+      uint32_t keep01[kBlocks], keep23[kBlocks];
+#pragma unroll
+      for (int k = 0; k < kBlocks; ++k) {
+        keep01[k] = keep23[k] = 0xFFFFFFFFu;
+        if constexpr (kEdge) {
+          // rows past the cache hold anything: their bits are cleared, so that a weight of 0 finds a number there
+          const int left = (gone >> k & 1u) ? 0 : n - (row0 + k * kBlockRows);
+          keep01[k] = (column(0) < left ? 0xFFFFu : 0u) | (column(1) < left ? 0xFFFF0000u : 0u);
+          keep23[k] = (column(2) < left ? 0xFFFFu : 0u) | (column(3) < left ? 0xFFFF0000u : 0u);
+        }
+      }
+      // 4 bits: p step is to fit f16 whatever the steps are, so that the reference grows with the largest of them, too
+      uint2 v_step[kBlocks][kG];
+      float most = 0.f;
+      if constexpr (kInt4) {
+        uint32_t top = 0x2B802B80u;            // 2^-40 at least: weights stay well within fp32
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int g = 0; g < kG; ++g) {
+            v_step[k][g] = lds64(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * q4);
+            v_step[k][g].x &= keep01[k];
+            v_step[k][g].y &= keep23[k];
+            top = __vmaxu2(top, __vmaxu2(v_step[k][g].x, v_step[k][g].y));   // steps are not negative: ordered as integers
+          }
+        most = lg2_approx(__uint_as_float(max(top & 0xFFFF0000u, top << 16)));
+      }
       float f[kNT];
       bool grown = false;
 #pragma unroll
@@ -510,16 +530,17 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         float mx = -INFINITY;
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k) mx = fmaxf(mx, fmaxf(fmaxf(sc[k][t][0], sc[k][t][1]), fmaxf(sc[k][t][2], sc[k][t][3])));
+        mx += most;
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
         f[t] = 1.f;
-        if (mx > m[t] + kRescaleThreshold) {   // weights of up to 2^8 do no harm: o is rescaled when they would grow past that
-          f[t] = ex2_approx(m[t] - mx);        // m = -inf gives 0
-          m[t] = mx;
+        if (mx > ref[t] + kSlack) {            // o is rescaled only when the weights would grow past 2^kSlack
+          f[t] = ex2_approx(ref[t] - (mx - kStart));   // ref = -inf gives 0
+          ref[t] = mx - kStart;
           l[t] *= f[t];
           grown = true;
         }
-        const float m_use = m[t] == -INFINITY ? 0.f : m[t];   // only logits of -inf so far: they weigh nothing
+        const float m_use = ref[t] == -INFINITY ? 0.f : ref[t];   // only logits of -inf so far: they weigh nothing
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k) {
 #pragma unroll
@@ -539,20 +560,13 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           }
           if (kInt4) {
 #pragma unroll
-            for (int g = 0; g < kG; ++g) { z[g][t][0] *= f0; z[g][t][1] *= f1; lo[g][t] *= f[t]; }
+            for (int g = 0; g < kG; ++g) lo[g][t] *= f[t];
           }
         }
       }
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
         const uint32_t vt = stage + (kBlocks + k) * C::kBlockBytes;
-        // rows past the cache hold anything: their bits are cleared, so that a weight of 0 finds a number there
-        uint32_t keep01 = 0xFFFFFFFFu, keep23 = 0xFFFFFFFFu;
-        if (edge) {
-          const int left = (gone >> k & 1u) ? 0 : n - (row0 + k * kBlockRows);
-          keep01 = (column(0) < left ? 0xFFFFu : 0u) | (column(1) < left ? 0xFFFF0000u : 0u);
-          keep23 = (column(2) < left ? 0xFFFFu : 0u) | (column(3) < left ? 0xFFFF0000u : 0u);
-        }
         if constexpr (kInt4) {
           uint32_t w[4][(kWords + 1) / 2];     // the units of rows q4, q4 + 4, q4 + 8, q4 + 12
 #pragma unroll
@@ -562,18 +576,15 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           for (int x = 0; x < kWords; ++x) {
             if (x % kPerGroup == 0) {
               const int g = x / kPerGroup;
-              uint4 u = lds128(vt + 8 * kD + 64 * g + 16 * q4);
-              if (edge) { u.x &= keep01; u.y &= keep23; u.z &= keep01; u.w &= keep23; }
-              const float s0 = lower(u.x), s1 = upper(u.x), s2 = lower(u.y), s3 = upper(u.y);
-              const float mid0 = fmaf(8.f, s0, lower(u.z)), mid1 = fmaf(8.f, s1, upper(u.z)), mid2 = fmaf(8.f, s2, lower(u.w)),
-                          mid3 = fmaf(8.f, s3, upper(u.w));
+              uint2 u = lds64(vt + 8 * kD + 64 * g + 16 * q4 + 8);
+              if constexpr (kEdge) { u.x &= keep01[k]; u.y &= keep23[k]; }
+              const float s0 = lower(v_step[k][g].x), s1 = upper(v_step[k][g].x), s2 = lower(v_step[k][g].y), s3 = upper(v_step[k][g].y);
 #pragma unroll
               for (int t = 0; t < kNT; ++t) {
                 const float* p = sc[k][t];
-                lo[g][t] = fmaf(p[0], mid0, fmaf(p[1], mid1, fmaf(p[2], mid2, fmaf(p[3], mid3, lo[g][t]))));
-                pb[t][0] = pack_bf16x2(p[0] * s0, p[1] * s1);
-                pb[t][1] = pack_bf16x2(p[2] * s2, p[3] * s3);
-                mma_column_sums(z[g][t], kMinus24, pb[t][0], pb[t][1]);
+                lo[g][t] = fmaf(p[0], lower(u.x), fmaf(p[1], upper(u.x), fmaf(p[2], lower(u.y), fmaf(p[3], upper(u.y), lo[g][t]))));
+                pb[t][0] = pack_f16x2(p[0] * s0, p[1] * s1);
+                pb[t][1] = pack_f16x2(p[2] * s2, p[3] * s3);
               }
             }
             const uint32_t y0 = __byte_perm(w[0][x >> 1], w[1][x >> 1], x & 1 ? 0x7632 : 0x5410);
@@ -582,8 +593,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             const uint32_t vb[4] = {code_pair<2>(y0), code_pair<3>(y0), code_pair<2>(y1), code_pair<3>(y1)};
 #pragma unroll
             for (int t = 0; t < kNT; ++t) {
-              mma16816(o[2 * x][t], va, pb[t][0], pb[t][1]);
-              mma16816(o[2 * x + 1][t], vb, pb[t][0], pb[t][1]);
+              mma16816_f16(o[2 * x][t], va, pb[t][0], pb[t][1]);
+              mma16816_f16(o[2 * x + 1][t], vb, pb[t][0], pb[t][1]);
             }
           }
         } else {
@@ -598,16 +609,33 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           for (int x = 0; x < kD / 16; ++x) {
             uint32_t va[4];
             ldsm4_t(vt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), va);
-            if (edge) { va[0] &= keep01; va[1] &= keep01; va[2] &= keep23; va[3] &= keep23; }
+            if constexpr (kEdge) { va[0] &= keep01[k]; va[1] &= keep01[k]; va[2] &= keep23[k]; va[3] &= keep23[k]; }
 #pragma unroll
             for (int t = 0; t < kNT; ++t) mma16816(o[x][t], va, pb[t][0], pb[t][1]);
           }
         }
       }
+    };
+
+    for (int i = 0; i < mine; ++i) {
+      ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit));
+      if (!ok) {
+        if (lane == 0)   // nothing may still be on its way into shared memory when the CTA returns
+          for (int j = 0; j < kStages && i + j < mine; ++j) {
+            const int s = slot + j < kStages ? slot + j : slot + j - kStages;
+            wait_issued(&full[warp][s], s < slot ? parity ^ 1u : parity);
+          }
+        break;
+      }
+      const uint32_t stage = ring_addr + (uint32_t)slot * C::kStageBytes;
+      const int row0 = (t0 + warp + i * kW) * C::kTileRows;
+      const unsigned int gone = absent >> (slot * kBlocks) & ((1u << kBlocks) - 1u);
+      if (row0 + C::kTileRows > sees_least || gone != 0) take(std::true_type{}, stage, row0, gone);
+      else take(std::false_type{}, stage, row0, 0u);
       __syncwarp();   // every lane has read the slot
-      if (i + kStages < mine) request(i + kStages);
+      if (i + kStages < mine) request(i + kStages, slot);
+      if (++slot == kStages) { slot = 0; parity ^= 1u; }
     }
-    used += mine;
 
     // ---- merge, in a fixed order: the warps of the CTA through their (idle) rings ----
     __syncwarp();
@@ -616,7 +644,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     for (int t = 0; t < kNT; ++t) {
       l[t] += __shfl_xor_sync(0xffffffffu, l[t], 1);
       l[t] += __shfl_xor_sync(0xffffffffu, l[t], 2);
-      if (q4 == 0) { w_ml[warp][r + 8 * t][0] = m[t]; w_ml[warp][r + 8 * t][1] = l[t]; }
+      if (q4 == 0) { w_ml[warp][r + 8 * t][0] = ref[t]; w_ml[warp][r + 8 * t][1] = l[t]; }
       if (kInt4) {
 #pragma unroll
         for (int g = 0; g < kG; ++g) {
@@ -630,11 +658,9 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         if constexpr (kInt4) {
 #pragma unroll
           for (int x = 0; x < kWords; ++x) {   // dims 32 x + 4 r + (0..3)
-            const float z0 = z[x / kPerGroup][t][0], z1 = z[x / kPerGroup][t][1];
-            *reinterpret_cast<float4*>(row + 32 * x + 4 * r) =
-                make_float4(o[2 * x][t][0] + z0, o[2 * x][t][2] + z0, o[2 * x + 1][t][0] + z0, o[2 * x + 1][t][2] + z0);
-            *reinterpret_cast<float4*>(row + kD + 32 * x + 4 * r) =
-                make_float4(o[2 * x][t][1] + z1, o[2 * x][t][3] + z1, o[2 * x + 1][t][1] + z1, o[2 * x + 1][t][3] + z1);
+            const float *e = o[2 * x][t], *f = o[2 * x + 1][t];
+            *reinterpret_cast<float4*>(row + 32 * x + 4 * r) = make_float4(e[0] * 0x1p24f, e[2] * 0x1p20f, f[0] * 0x1p24f, f[2] * 0x1p20f);
+            *reinterpret_cast<float4*>(row + kD + 32 * x + 4 * r) = make_float4(e[1] * 0x1p24f, e[3] * 0x1p20f, f[1] * 0x1p24f, f[3] * 0x1p20f);
           }
         } else {
 #pragma unroll
