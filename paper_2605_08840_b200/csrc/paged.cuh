@@ -137,10 +137,10 @@ size_t paged_simt_bytes(const PagedCache& c, int splits);
 cudaError_t launch_paged_simt(const PagedCache& c, bool f32, const RowsView& Q, void* out, float* lse, float* part, int splits,
                               cudaStream_t st);
 // bf16 with head_dim 64, 128 or 256 on the tensor pipe, up to 16 query rows per pass over the cache.
-cudaError_t paged_mma_init();
+cudaError_t paged_mma_init(int (*clusters_of)[5]);
 bool paged_mma_supported(const PagedCache& c);
 size_t paged_mma_bytes(const PagedCache& c, int sm_count);
 cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count,
-                             long long wait_limit, cudaStream_t st, int* launches);
+                             const int (*clusters_of)[5], long long wait_limit, cudaStream_t st, int* launches);
 
 }  // namespace restkv

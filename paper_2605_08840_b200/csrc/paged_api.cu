@@ -153,7 +153,8 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
   if (on_tensor_pipe(c, f32) && h->tc_state && h->kernel_path != 1) {
     int launches = 0;
     RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
-                  launch_paged_mma(h->tc_state, c, q, out, lse, (float*)workspace, h->sm_count, h->wait_limit, call.st, &launches), launches);
+                  launch_paged_mma(h->tc_state, c, q, out, lse, (float*)workspace, h->sm_count, h->paged_clusters,
+                                   h->wait_limit, call.st, &launches), launches);
     return RESTKV_OK;
   }
   RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,

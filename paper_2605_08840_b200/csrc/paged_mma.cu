@@ -20,7 +20,8 @@
 //   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
 //     short caches, where latency counts;
 //   - the tiles of all units end to end, an equal share of them per CTA whatever the sequences' lengths, partial results in the
-//     workspace and a second kernel that merges what several CTAs share.
+//     workspace and a second kernel that merges them.  (The last CTA of a unit to arrive at a counter merging them instead: 4 us more at
+//     131072 rows, where one CTA reads what 37 left; at 8 x 2176 rows 3 us more.)
 #include <math.h>
 
 #include <type_traits>
@@ -102,6 +103,12 @@ template <int i> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
 __device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
+constexpr int kMaxCtas = 512;
+#ifndef KCR
+#define KCR 4096
+#endif
+constexpr int kClusterRows = KCR;
+
 struct PagedMmaArgs {
   PagedCache c;
   RowsView Q;
@@ -131,58 +138,133 @@ template <int kD, int kGroups, int kNT> struct Config {
   static constexpr int kStages = kFit < 2 ? 2 : kFit > 6 ? 6 : kFit;
   static constexpr uint32_t kRing = kStages * kStageBytes;
   static constexpr uint32_t kPartBytes = kRows * kD * 4u;                               // a warp's o in the merge
-  static_assert(kRing >= kPartBytes + (kRows + kWarps - 1) / kWarps * kD * 4u, "the merge needs the ring's space");
   static constexpr size_t kSmem = (size_t)kWarps * kRing + 1024;
+  // in clusters: two slots per warp, and what the peers push
+  static constexpr uint32_t kPushBytes = kRows * kD * 4u + 256u + 16u * kRows * 8u;
+  static constexpr size_t kClusterSmem = (size_t)kWarps * 2 * kStageBytes + kPushBytes + 1024;
+  static_assert(2 * kStageBytes >= kPartBytes, "the merge needs the ring's space");
 };
 
-// Where a CTA's run of tiles begins: entry (a sequence, or with lengths per head a KV head of one), unit of the entry, tile of the unit.
-struct Run {
-  long long tiles;          // of all units
-  long long first;          // tile at which `entry` begins
-  int entry;
+// Tiles dealt out end to end: CTA x of `ctas` has those from boundary x to boundary x + 1.  A boundary is start(x) = all * x / ctas, but
+// moved to the near end of its unit where that is at most `snap` tiles away: a CTA that ends one unit and begins another pays for
+// prologue and merge twice, 5 us, in which it would go through some 24 tiles.
+struct Deal {
+  int ctas, each, more, snap;
+  __device__ __forceinline__ Deal(int all, int grid) : ctas(all < grid ? all : grid), each(all / ctas), more(all - each * ctas) {
+    snap = (each - 1) / 2 < 24 ? (each - 1) / 2 : 24;   // less than half a share: no share vanishes
+  }
+  __device__ __forceinline__ int start(int x) const { return x * each + x * more / ctas; }
+  // tile `at` of a unit of `tiles`: where a boundary there goes, as tile of the unit
+  __device__ __forceinline__ int moved(int at, int tiles) const {
+    const int left = tiles - at;
+    return at <= snap && at <= left ? 0 : left <= snap ? tiles : at;
+  }
+  // the last CTA whose start is not past `tile`
+  __device__ __forceinline__ int last(int tile) const {
+    int x = (int)((float)tile / ((float)each + (float)more / (float)ctas));
+    x = x < ctas ? x : ctas - 1;
+    while (x > 0 && start(x) > tile) --x;
+    while (x + 1 < ctas && start(x + 1) <= tile) ++x;
+    return x;
+  }
+  // the CTAs that have tiles of the unit [u0, u0 + tiles): the first of them its beginning
+  __device__ __forceinline__ int first_of(int u0, int tiles) const { return last(u0 + (snap < tiles / 2 ? snap : tiles / 2)); }
+  __device__ __forceinline__ int last_of(int u0, int tiles) const {
+    return last(u0 + tiles - 1 - (snap < (tiles - 1) / 2 ? snap : (tiles - 1) / 2));
+  }
 };
 
+// Entries: sequences, or with lengths per head the KV heads of all sequences; each has `units` units of as many tiles.
 __device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_rows) {
   const int n = c.per_head ? paged_length(c, e / c.Hkv, e % c.Hkv) : paged_length(c, e, 0);
   const int t = (n + tile_rows - 1) / tile_rows;
   return t > 0 ? t : 1;     // a unit without rows has its outputs written, too
 }
 
-// By a whole warp: the tiles of all units, and the entry that holds tile share(tiles).
-template <typename F>
-__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, F share) {
+// By a whole warp: a CTA's run of tiles [tile, end), the entry that `tile` lies in, the entry's first tile and tiles per unit.
+struct Run {
+  int tile, end, entry, first, tiles;
+};
+__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int x, int grid) {
   const int lane = threadIdx.x & 31;
   const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
   const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
-  Run r{0, 0, 0};
-  long long mine = 0;
-  for (int e = lane; e < entries; e += 32) mine += (long long)entry_tiles(c, e, tile_rows) * units;
-  r.tiles = mine;
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) r.tiles += __shfl_xor_sync(0xffffffffu, r.tiles, off);
-  const long long want = share(r.tiles);
+  const int t0 = lane < entries ? entry_tiles(c, lane, tile_rows) : 0;
+  int sum = t0 * units;
+  for (int e = 32 + lane; e < entries; e += 32) sum += entry_tiles(c, e, tile_rows) * units;
+  const int all = __reduce_add_sync(0xffffffffu, sum);
+  const Deal deal(all, grid);
+  Run r{0, 0, 0, 0, 1};
+  if (x >= deal.ctas) return r;
+  r.tile = r.end = all;
+  int want = deal.start(x), before = 0;
+  bool have = false;
   for (int base = 0; base < entries; base += 32) {
-    const long long t = base + lane < entries ? (long long)entry_tiles(c, base + lane, tile_rows) * units : 0;
-    long long upto = t;
+    const int t = base == 0 ? t0 : base + lane < entries ? entry_tiles(c, base + lane, tile_rows) : 0;
+    int upto = t * units;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-      const long long o = __shfl_up_sync(0xffffffffu, upto, off);
+      const int o = __shfl_up_sync(0xffffffffu, upto, off);
       if (lane >= off) upto += o;
     }
-    const unsigned int past = __ballot_sync(0xffffffffu, r.first + upto > want);
-    if (past) {
+    for (;;) {             // both boundaries of the CTA may lie in these entries
+      const unsigned int past = __ballot_sync(0xffffffffu, before + upto > want);
+      if (!past) break;
       const int at = __ffs((int)past) - 1;
-      r.entry = base + at;
-      r.first += __shfl_sync(0xffffffffu, upto - t, at);
-      return r;
+      const int tiles = __shfl_sync(0xffffffffu, t, at), first = before + __shfl_sync(0xffffffffu, upto, at) - tiles * units;
+      const int unit0 = first + (want - first) / tiles * tiles, boundary = unit0 + deal.moved(want - unit0, tiles);
+      if (!have) {
+        have = true;
+        r = Run{boundary, all, base + at, first, tiles};
+        if (x + 1 == deal.ctas) return r;
+        want = deal.start(x + 1);
+      } else {
+        r.end = boundary;
+        return r;
+      }
     }
-    r.first += __shfl_sync(0xffffffffu, upto, 31);
+    before += __shfl_sync(0xffffffffu, upto, 31);
   }
-  r.entry = entries;
   return r;
 }
 
-template <int kD, int kGroups, int kNT>
+// Dims 4 v .. 4 v + 3 of a query row's result.
+template <int kD>
+__device__ __forceinline__ void write_row(const PagedMmaArgs& a, int b, int h, int rho, int count, int v, float4 acc, float mm, float ll) {
+  const PagedCache& c = a.c;
+  const int i = rho / c.G, g = rho - i * c.G;
+  const bool some = ll > 0.f && i < count;
+  const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
+  const float f = some ? 1.f / ll : 0.f;
+  uint2 w = make_uint2(0u, 0u);
+  if (some) w = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
+  reinterpret_cast<uint2*>(a.out + at * kD)[v] = w;
+  if (v == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+}
+__device__ __forceinline__ void fma4(float4& acc, float4 x, float f) {
+  acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
+}
+
+// What a CTA works on without clusters, in shared memory: it is needed before the tiles and after them, and registers are short between.
+struct Piece {
+  Run run;
+  int unit, t0, t1;        // tiles [t0, t1) of the unit
+  int whole;               // no other CTA has tiles of it
+  __device__ __forceinline__ void cut(const PagedCache& c, int row_tiles, int tile_rows) {   // at run.tile
+    const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
+    if (run.tile >= run.first + run.tiles * units) {     // the next entry
+      run.first += run.tiles * units;
+      run.tiles = entry_tiles(c, ++run.entry, tile_rows);
+    }
+    const int k = (run.tile - run.first) / run.tiles, begin = run.first + k * run.tiles;
+    unit = run.entry * units + k;
+    t0 = run.tile - begin;
+    t1 = run.end - begin < run.tiles ? run.end - begin : run.tiles;
+    whole = t0 == 0 && t1 == run.tiles;
+  }
+};
+
+template <int kD, int kGroups, int kNT, bool kCluster>
 __global__ void __launch_bounds__(Config<kD, kGroups, kNT>::kWarps * 32, Config<kD, kGroups, kNT>::kPerSm)
 paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ PagedMmaArgs a) {
   using C = Config<kD, kGroups, kNT>;
@@ -196,15 +278,17 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   __shared__ __align__(8) uint64_t full[kW][kStages];
   __shared__ float w_ml[kW][kRows][2];
   __shared__ float w_lo[kW][kRows][kG];        // 4 bits: sum of p offset per group
-  __shared__ float c_ml[kRows][2];
+  __shared__ float w_factor[kW][kRows];
+  __shared__ float2 c_ml[kRows];
   __shared__ int abort_flag;
-  __shared__ long long run_s[2];
-  __shared__ int run_entry;
+  __shared__ Piece piece_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q4 = lane & 3;
   const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   uint8_t* rings = smem_raw + (smem_base - smem_u32(smem_raw));
-  uint8_t* ring = rings + warp * C::kRing;
-  const uint32_t ring_addr = smem_base + (uint32_t)warp * C::kRing;
+  constexpr int stages = kCluster ? 2 : kStages;
+  constexpr uint32_t ring_bytes = (uint32_t)stages * C::kStageBytes;
+  uint8_t* ring = rings + warp * ring_bytes;
+  const uint32_t ring_addr = smem_base + (uint32_t)warp * ring_bytes;
   const int R = c.n_tokens * c.G;
 
   if (threadIdx.x == 0) abort_flag = 0;
@@ -216,77 +300,96 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       prefetch_tensormap(&tmV);
     }
   }
+  __syncwarp();
+  if (kCluster) cluster_arrive();             // peers push into shared memory once all have begun
   grid_dependency_wait();
   grid_dependency_launch();
 
-  long long tile = 0, end = 0, first = 0;      // of the CTA's run, without clusters
-  int entry = 0;
-  if (!a.cluster) {
+  if constexpr (!kCluster) {
     if (warp == 0) {
-      const Run run = find_run(c, a.row_tiles, C::kTileRows, [&](long long t) {
-        return blockIdx.x < t ? t * blockIdx.x / (t < gridDim.x ? t : gridDim.x) : 0;
-      });
-      if (lane == 0) { run_s[0] = run.tiles; run_s[1] = run.first; run_entry = run.entry; }
+      const Run run = find_run(c, a.row_tiles, C::kTileRows, blockIdx.x, gridDim.x);
+      if (lane == 0) {
+        piece_s.run = run;
+        if (run.tile < run.end) piece_s.cut(c, a.row_tiles, C::kTileRows);
+      }
     }
     __syncthreads();
-    const long long ctas = run_s[0] < gridDim.x ? run_s[0] : gridDim.x;     // of them each has a tile
-    if (blockIdx.x >= ctas) return;
-    tile = run_s[0] * blockIdx.x / ctas;
-    end = run_s[0] * (blockIdx.x + 1) / ctas;
-    first = run_s[1];
-    entry = run_entry;
+    if (piece_s.run.tile >= piece_s.run.end) return;
   } else {
     __syncthreads();
   }
 
   int slot = 0;                                // of the warp's ring: the next tile's, and the parity it completes with
   uint32_t parity = 0;
-  bool ok = true;
-  for (int piece = 0;; ++piece) {
+  for (;;) {
+    bool ok = true;                            // false: a wait ran out
     // ---- the unit and the run of its tiles ----
-    int unit, t0, t1, whole;                   // whole: no other CTA has tiles of the unit
+    int next, t1;                              // the warp's first tile; its tiles are `stride` apart and below t1
     int cluster_rank = 0;
-    if (a.cluster) {
-      unit = (int)(blockIdx.x / (unsigned int)a.cluster);
+    const volatile Piece& piece = piece_s;     // read again where it is needed
+    const int stride = kCluster ? a.cluster * kW : kW;
+    auto unit_of_cta = [&]() { return kCluster ? (int)(blockIdx.x / (unsigned int)a.cluster) : piece.unit; };
+    if (kCluster) {
+      // every CTA of the cluster takes tiles all over the unit, so that its warps' first blocks are known before the length is
       cluster_rank = (int)(blockIdx.x % (unsigned int)a.cluster);
-      const int bh = unit / a.row_tiles;
-      const int tiles = entry_tiles(c, c.per_head ? bh : bh / c.Hkv, C::kTileRows);
-      t0 = (int)((long long)tiles * cluster_rank / a.cluster);
-      t1 = (int)((long long)tiles * (cluster_rank + 1) / a.cluster);
-      whole = 0;
+      next = cluster_rank * kW + warp;
+      t1 = 0;
     } else {
-      const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles;
-      int tiles = entry_tiles(c, entry, C::kTileRows);
-      if (tile >= first + (long long)tiles * units) {      // the next entry
-        first += (long long)tiles * units;
-        ++entry;
-        tiles = entry_tiles(c, entry, C::kTileRows);
-      }
-      const int k = (int)((tile - first) / tiles);
-      const long long begin = first + (long long)k * tiles;
-      unit = entry * units + k;
-      t0 = (int)(tile - begin);
-      t1 = (int)((end - begin < tiles) ? end - begin : tiles);
-      whole = t0 == 0 && t1 == tiles;
+      next = piece.t0 + warp;
+      t1 = piece.t1;
     }
-    const int bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
-    const int n = paged_length(c, b, h), count = paged_count(c, b);
-    if (t0 == 0 && threadIdx.x == 0) check_length(c, b, h);
-    const int blocks = (n + kBlockRows - 1) / kBlockRows;
-    const int mine = t1 - t0 > warp ? (t1 - t0 - warp + kW - 1) / kW : 0;   // tiles t0 + warp + kW * i
+    const int unit = unit_of_cta(), bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
 
-    // ---- requests: the blocks' places are looked up 32 / kBlocks tiles at a time, one lane each ----
-    int place = -1;
+    // ---- the places of the warp's blocks, looked up for 32 / kBlocks tiles at a time, a block per lane ----
+    int place = -1, block_of_lane;
+    const int per_page = c.page_rows / kBlockRows;
+    auto look_up = [&](int i) {                // the page is only looked at once everything that is loaded beside it is on its way
+      block_of_lane = (next + (i + lane / kBlocks) * stride) * kBlocks + lane % kBlocks;
+      const int at = block_of_lane / per_page;
+      place = at < c.table_width ? c.table[(long long)b * c.table_width + at] : -1;
+    };
+    look_up(0);
+    const int n = paged_length(c, b, h), count = paged_count(c, b);
+    if (kCluster) t1 = (n + C::kTileRows - 1) / C::kTileRows;
+    if (threadIdx.x == 0 && (kCluster ? cluster_rank : piece.t0) == 0) check_length(c, b, h);
+    const int blocks = (n + kBlockRows - 1) / kBlockRows;
+    const int mine = t1 > next ? (t1 - next + stride - 1) / stride : 0;
+
+    // ---- the query rows rho0 + r (and + 8): loaded before the first blocks are asked for, behind which they would have to wait ----
+    // bf16: in the order of the A operand.  4 bits: dims 32 m + 8 q4 .. + 7 in words 4 m .. 4 m + 3.
+    uint32_t q_raw[kNT][kD / 8];
+#pragma unroll
+    for (int t = 0; t < kNT; ++t) {
+      const int rho = rho0 + r + 8 * t, i = rho / c.G, g = rho - i * c.G;
+      const bool live = rho < R;
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
+      if constexpr (kInt4) {
+#pragma unroll
+        for (int m = 0; m < kWords; ++m) {
+          const uint4 u = live ? *reinterpret_cast<const uint4*>(q + 32 * m + 8 * q4) : make_uint4(0u, 0u, 0u, 0u);
+          q_raw[t][4 * m] = u.x; q_raw[t][4 * m + 1] = u.y; q_raw[t][4 * m + 2] = u.z; q_raw[t][4 * m + 3] = u.w;
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < kD / 16; ++k) {
+          q_raw[t][2 * k] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
+          q_raw[t][2 * k + 1] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
+        }
+      }
+    }
+
     unsigned int absent = 0;                   // bit slot * kBlocks + block: nothing was loaded there
     auto request = [&](int i, int s) {         // tile i into slot s, by the whole warp
       constexpr int kAhead = 32 / kBlocks;
       if (i % kAhead == 0) {
-        const int t = t0 + warp + (i + lane / kBlocks) * kW;
-        const int block = t * kBlocks + lane % kBlocks;
-        place = -1;
-        if (t < t1 && block < blocks) {
-          place = paged_block_index(c, b, h, block);
-          if (place < 0) atomicOr(c.dev_status, kDevBadIndex);
+        if (i > 0) look_up(i);
+        if (block_of_lane / kBlocks >= t1 || block_of_lane >= blocks) {
+          place = -1;
+        } else if ((unsigned int)place >= (unsigned int)c.n_pages) {
+          place = -1;
+          atomicOr(c.dev_status, kDevBadIndex);
+        } else {
+          place = (place * c.Hkv + h) * per_page + block_of_lane % per_page;
         }
       }
       int at[kBlocks];
@@ -331,9 +434,9 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     };
 #pragma unroll
     for (int i = 0; i < kStages; ++i)
-      if (i < mine) request(i, slot + i < kStages ? slot + i : slot + i - kStages);
+      if (i < mine && i < stages) request(i, slot + i < stages ? slot + i : slot + i - stages);
 
-    // ---- Q as the A operand: query rows rho0 + r (and + 8), kD / 16 steps; what each row sees ----
+    // ---- Q as the A operand, kD / 16 steps; what each row sees ----
     // 4 bits: in f16, scaled by a power of two per row (and 2^-4 where the codes come 16 times too large); sums of q per group in the
     // codes' and that scale, which the logits' factor takes out again.
     uint32_t qa[kD / 16][2 * kNT];
@@ -342,21 +445,14 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     int sees_least = n;
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
-      const int rho = rho0 + r + 8 * t, i = rho / c.G, g = rho - i * c.G;
-      const bool live = rho < R && i < count;
-      sees[t] = live ? n - (count - 1 - i) : n;
+      const int rho = rho0 + r + 8 * t, i = rho / c.G;
+      sees[t] = rho < R && i < count ? n - (count - 1 - i) : n;
       sees_least = min(sees_least, sees[t]);
       unscale[t] = 1.f;
-      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
       if constexpr (kInt4) {
-        uint4 u[kWords];                       // dims 32 m + 8 q4 .. + 7
         float top = 0.f;
 #pragma unroll
-        for (int m = 0; m < kWords; ++m) {
-          u[m] = live ? *reinterpret_cast<const uint4*>(q + 32 * m + 8 * q4) : make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-          for (int x = 0; x < 4; ++x) top = fmaxf(top, fmaxf(fabsf(lower((&u[m].x)[x])), fabsf(upper((&u[m].x)[x]))));
-        }
+        for (int x = 0; x < kD / 8; ++x) top = fmaxf(top, fmaxf(fabsf(lower(q_raw[t][x])), fabsf(upper(q_raw[t][x]))));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
         top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
         // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
@@ -371,8 +467,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           float v[8];
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            v[2 * x] = lower((&u[m].x)[x]) * scale;
-            v[2 * x + 1] = upper((&u[m].x)[x]) * scale;
+            v[2 * x] = lower(q_raw[t][4 * m + x]) * scale;
+            v[2 * x + 1] = upper(q_raw[t][4 * m + x]) * scale;
           }
           // the pairs (i, i + 4) that a word's codes come in
           qa[2 * m][t] = pack_f16x2(v[0], v[4]);
@@ -390,8 +486,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       } else {
 #pragma unroll
         for (int k = 0; k < kD / 16; ++k) {
-          qa[k][t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 2 * q4) : 0u;
-          qa[k][kNT + t] = live ? *reinterpret_cast<const uint32_t*>(q + 16 * k + 8 + 2 * q4) : 0u;
+          qa[k][t] = q_raw[t][2 * k];
+          qa[k][kNT + t] = q_raw[t][2 * k + 1];
         }
       }
     }
@@ -508,7 +604,6 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         }
       }
       // 4 bits: p step is to fit f16 whatever the steps are, so that the reference grows with the largest of them, too
-      uint2 v_step[kBlocks][kG];
       float most = 0.f;
       if constexpr (kInt4) {
         uint32_t top = 0x2B802B80u;            // 2^-40 at least: weights stay well within fp32
@@ -516,10 +611,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
           for (int g = 0; g < kG; ++g) {
-            v_step[k][g] = lds64(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * q4);
-            v_step[k][g].x &= keep01[k];
-            v_step[k][g].y &= keep23[k];
-            top = __vmaxu2(top, __vmaxu2(v_step[k][g].x, v_step[k][g].y));   // steps are not negative: ordered as integers
+            const uint2 u = lds64(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * q4);
+            top = __vmaxu2(top, __vmaxu2(u.x & keep01[k], u.y & keep23[k]));   // steps are not negative: ordered as integers
           }
         most = lg2_approx(__uint_as_float(max(top & 0xFFFF0000u, top << 16)));
       }
@@ -576,13 +669,13 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           for (int x = 0; x < kWords; ++x) {
             if (x % kPerGroup == 0) {
               const int g = x / kPerGroup;
-              uint2 u = lds64(vt + 8 * kD + 64 * g + 16 * q4 + 8);
-              if constexpr (kEdge) { u.x &= keep01[k]; u.y &= keep23[k]; }
-              const float s0 = lower(v_step[k][g].x), s1 = upper(v_step[k][g].x), s2 = lower(v_step[k][g].y), s3 = upper(v_step[k][g].y);
+              uint4 u = lds128(vt + 8 * kD + 64 * g + 16 * q4);
+              if constexpr (kEdge) { u.x &= keep01[k]; u.y &= keep23[k]; u.z &= keep01[k]; u.w &= keep23[k]; }
+              const float s0 = lower(u.x), s1 = upper(u.x), s2 = lower(u.y), s3 = upper(u.y);
 #pragma unroll
               for (int t = 0; t < kNT; ++t) {
                 const float* p = sc[k][t];
-                lo[g][t] = fmaf(p[0], lower(u.x), fmaf(p[1], upper(u.x), fmaf(p[2], lower(u.y), fmaf(p[3], upper(u.y), lo[g][t]))));
+                lo[g][t] = fmaf(p[0], lower(u.z), fmaf(p[1], upper(u.z), fmaf(p[2], lower(u.w), fmaf(p[3], upper(u.w), lo[g][t]))));
                 pb[t][0] = pack_f16x2(p[0] * s0, p[1] * s1);
                 pb[t][1] = pack_f16x2(p[2] * s2, p[3] * s3);
               }
@@ -621,25 +714,28 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit));
       if (!ok) {
         if (lane == 0)   // nothing may still be on its way into shared memory when the CTA returns
-          for (int j = 0; j < kStages && i + j < mine; ++j) {
-            const int s = slot + j < kStages ? slot + j : slot + j - kStages;
+          for (int j = 0; j < stages && i + j < mine; ++j) {
+            const int s = slot + j < stages ? slot + j : slot + j - stages;
             wait_issued(&full[warp][s], s < slot ? parity ^ 1u : parity);
           }
         break;
       }
       const uint32_t stage = ring_addr + (uint32_t)slot * C::kStageBytes;
-      const int row0 = (t0 + warp + i * kW) * C::kTileRows;
+      const int row0 = (next + i * stride) * C::kTileRows;
       const unsigned int gone = absent >> (slot * kBlocks) & ((1u << kBlocks) - 1u);
       if (row0 + C::kTileRows > sees_least || gone != 0) take(std::true_type{}, stage, row0, gone);
       else take(std::false_type{}, stage, row0, 0u);
       __syncwarp();   // every lane has read the slot
-      if (i + kStages < mine) request(i + kStages, slot);
-      if (++slot == kStages) { slot = 0; parity ^= 1u; }
+      if (i + stages < mine) request(i + stages, slot);
+      if (++slot == stages) { slot = 0; parity ^= 1u; }
     }
 
     // ---- merge, in a fixed order: the warps of the CTA through their (idle) rings ----
     __syncwarp();
-    float* w_o = reinterpret_cast<float*>(ring);   // [rows][kD]
+    // w_o [rows][kD / 4] float4, a row's order such that the four rows that lanes store side by side go to different banks
+    auto w_o = [&](int w, int row, int v) {
+      return reinterpret_cast<float4*>(rings + w * ring_bytes) + row * (kD / 4) + (v ^ ((row >> 1 & 3) << 1));
+    };
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
       l[t] += __shfl_xor_sync(0xffffffffu, l[t], 1);
@@ -654,200 +750,196 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         }
       }
       if (mine > 0) {
-        float* row = w_o + (2 * q4 + 8 * t) * kD;
+        const int row = 2 * q4 + 8 * t;
         if constexpr (kInt4) {
 #pragma unroll
           for (int x = 0; x < kWords; ++x) {   // dims 32 x + 4 r + (0..3)
             const float *e = o[2 * x][t], *f = o[2 * x + 1][t];
-            *reinterpret_cast<float4*>(row + 32 * x + 4 * r) = make_float4(e[0] * 0x1p24f, e[2] * 0x1p20f, f[0] * 0x1p24f, f[2] * 0x1p20f);
-            *reinterpret_cast<float4*>(row + kD + 32 * x + 4 * r) = make_float4(e[1] * 0x1p24f, e[3] * 0x1p20f, f[1] * 0x1p24f, f[3] * 0x1p20f);
+            *w_o(warp, row, 8 * x + r) = make_float4(e[0] * 0x1p24f, e[2] * 0x1p20f, f[0] * 0x1p24f, f[2] * 0x1p20f);
+            *w_o(warp, row + 1, 8 * x + r) = make_float4(e[1] * 0x1p24f, e[3] * 0x1p20f, f[1] * 0x1p24f, f[3] * 0x1p20f);
           }
         } else {
 #pragma unroll
-          for (int x = 0; x < kD / 16; ++x) {
-            row[16 * x + r] = o[x][t][0];
-            row[kD + 16 * x + r] = o[x][t][1];
-            row[16 * x + 8 + r] = o[x][t][2];
-            row[kD + 16 * x + 8 + r] = o[x][t][3];
+          for (int x = 0; x < kD / 16; ++x) {  // dims 16 x + r, 16 x + 8 + r
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              reinterpret_cast<float*>(w_o(warp, row + (e & 1), 4 * x + 2 * (e >> 1) + (r >> 2)))[r & 3] = o[x][t][e];
           }
         }
       }
     }
     __syncthreads();
-    const int rows = R - rho0 < kRows ? R - rho0 : kRows;
-    // a row's result: written where the unit is this CTA's (or this cluster's) alone
-    auto finish = [&](int row, int k, float acc, float mm, float ll) {
-      const int rho = rho0 + row, i = rho / c.G, g = rho - i * c.G;
-      const bool some = ll > 0.f && i < count;
-      const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
-      a.out[at * kD + k] = __float2bfloat16(some ? acc / ll : 0.f);
-      if (k == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
-    };
-    auto c_o = [&](int row) { return reinterpret_cast<float*>(rings + (row % kW) * C::kRing + C::kPartBytes) + (row / kW) * kD; };
-    for (int e = threadIdx.x; e < rows * kD; e += kW * 32) {
-      const int row = e / kD, k = e % kD;
-      float mm = -INFINITY;
+    const int unit_now = unit_of_cta(), bh_now = unit_now / a.row_tiles, rho_now = (unit_now - bh_now * a.row_tiles) * kRows;
+    const int b_now = bh_now / c.Hkv, h_now = bh_now - b_now * c.Hkv, rows = R - rho_now < kRows ? R - rho_now : kRows;
+    if (threadIdx.x < kRows * kW) {            // a warp's factor for each row, and the CTA's (reference, sum)
+      const int row = threadIdx.x / kW, w = threadIdx.x % kW;
+      const float mw = w_ml[w][row][0];
+      float mm = mw;
 #pragma unroll
-      for (int w = 0; w < kW; ++w) mm = fmaxf(mm, w_ml[w][row][0]);
-      float acc = 0.f, ll = 0.f;
+      for (int off = kW / 2; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+      const float f = mw == -INFINITY ? 0.f : ex2_approx(mw - mm);   // without tiles, or with none that the row sees
+      float ll = w_ml[w][row][1] * f;
+#pragma unroll
+      for (int off = kW / 2; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
+      w_factor[w][row] = f;
+      if (w == 0) c_ml[row] = make_float2(mm, ll);
+    }
+    __syncthreads();
+    const int items = rows * (kD / 4);         // four dims of a row
+    // of the units that it shares, a CTA has the beginning of one at most and none of that of another: a slot for each
+    float* const part = a.part + (long long)(2 * blockIdx.x + (piece.t0 == 0)) * kRows * (kD + 2);
+    // in clusters the results of item x are merged by CTA x % cluster
+    uint8_t* const push = rings + kW * ring_bytes;
+    float2* const push_ml = reinterpret_cast<float2*>(push);                                // [cluster][kRows]
+    float4* const push_o = reinterpret_cast<float4*>(push + 16 * kRows * sizeof(float2));   // [cluster][items / cluster, rounded up]
+    const int per_cta = kCluster ? (items + a.cluster - 1) / a.cluster : 0;
+    const int whole = kCluster ? 0 : piece.whole, count_now = paged_count(c, b_now);
+    if (kCluster) cluster_wait();
+    for (int x = threadIdx.x; x < items; x += kW * 32) {
+      const int row = x / (kD / 4), v = x % (kD / 4);
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int w = 0; w < kW; ++w) {
-        const float mw = w_ml[w][row][0];
-        if (mw == -INFINITY) continue;         // a warp without tiles, or whose tiles this row does not see
-        const float f = ex2_approx(mw - mm);
-        float v = reinterpret_cast<const float*>(rings + w * C::kRing)[row * kD + k];
-        if (kInt4) v += w_lo[w][row][k / (kD / kG)];
-        acc = fmaf(v, f, acc);
-        ll = fmaf(w_ml[w][row][1], f, ll);
+        const float f = w_factor[w][row];
+        if (f == 0.f) continue;
+        float4 o4 = *w_o(w, row, v);
+        if (kInt4) {
+          const float add = w_lo[w][row][v / (kD / 4 / kG)];
+          o4.x += add; o4.y += add; o4.z += add; o4.w += add;
+        }
+        fma4(acc, o4, f);
       }
-      if (a.cluster) {
-        c_o(row)[k] = acc;
-        if (k == 0) { c_ml[row][0] = mm; c_ml[row][1] = ll; }
+      if (kCluster) {
+        const int to = x % a.cluster;
+        *cg::this_cluster().map_shared_rank(push_o + cluster_rank * per_cta + x / a.cluster, to) = acc;
       } else if (whole) {
-        finish(row, k, acc, mm, ll);
+        write_row<kD>(a, b_now, h_now, rho_now + row, count_now, v, acc, c_ml[row].x, c_ml[row].y);
       } else {
-        float* p = a.part + (long long)(2 * blockIdx.x + (piece > 0)) * kRows * (kD + 2);
-        p[row * kD + k] = acc;
-        if (k == 0) { p[kRows * kD + 2 * row] = mm; p[kRows * kD + 2 * row + 1] = ll; }
+        reinterpret_cast<float4*>(part)[row * (kD / 4) + v] = acc;
+        if (v == 0) reinterpret_cast<float2*>(part + kRows * kD)[row] = c_ml[row];
       }
     }
-    if (a.cluster) {
-      cg::cluster_group cluster = cg::this_cluster();
-      cluster.sync();
-      for (int e = cluster_rank * kW * 32 + (int)threadIdx.x; e < rows * kD; e += a.cluster * kW * 32) {
-        const int row = e / kD, k = e % kD;
-        float mm = -INFINITY, acc = 0.f, ll = 0.f;
-        float mr[16], lr[16], vr[16];
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          mr[x] = -INFINITY;
-          if (x < a.cluster) {
-            const float* p = cluster.map_shared_rank(&c_ml[row][0], x);
-            mr[x] = p[0];
-            lr[x] = p[1];
-            vr[x] = *cluster.map_shared_rank(c_o(row) + k, x);
-            mm = fmaxf(mm, mr[x]);
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          if (mr[x] == -INFINITY) continue;
-          const float f = ex2_approx(mr[x] - mm);
-          acc = fmaf(vr[x], f, acc);
-          ll = fmaf(lr[x], f, ll);
-        }
-        finish(row, k, acc, mm, ll);
+    if constexpr (kCluster) {
+      for (int x = threadIdx.x; x < rows * a.cluster; x += kW * 32) {
+        const int to = x / rows, row = x - to * rows;
+        *cg::this_cluster().map_shared_rank(push_ml + cluster_rank * kRows + row, to) = c_ml[row];
       }
-      cluster.sync();   // shared memory stays alive until every peer has read it
+      __syncwarp();
+      cluster_arrive();
+      cluster_wait();
+      // a.cluster threads side by side hold an item's parts
+      const int from = threadIdx.x & (a.cluster - 1);
+      for (int y = threadIdx.x / a.cluster; y - (int)((threadIdx.x & 31) / a.cluster) < per_cta; y += kW * 32 / a.cluster) {   // whole warps stay
+        const int x = y * a.cluster + cluster_rank;
+        const bool there = y < per_cta && x < items;
+        const int row = there ? x / (kD / 4) : 0, v = x % (kD / 4);
+        const float2 ml = push_ml[from * kRows + row];
+        float4 acc = there ? push_o[from * per_cta + y] : make_float4(0.f, 0.f, 0.f, 0.f);
+        float mm = ml.x;
+        for (int off = a.cluster / 2; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
+        const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - mm);
+        float ll = ml.y * f;
+        acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
+        for (int off = a.cluster / 2; off > 0; off >>= 1) {
+          ll += __shfl_xor_sync(0xffffffffu, ll, off);
+          acc.x += __shfl_xor_sync(0xffffffffu, acc.x, off);
+          acc.y += __shfl_xor_sync(0xffffffffu, acc.y, off);
+          acc.z += __shfl_xor_sync(0xffffffffu, acc.z, off);
+          acc.w += __shfl_xor_sync(0xffffffffu, acc.w, off);
+        }
+        if (there && from == 0) write_row<kD>(a, b_now, h_now, rho_now + row, count_now, v, acc, mm, ll);
+      }
       return;
     }
-    tile += t1 - t0;
     // all of the CTA's warps go on to the next piece or none
-    if (__syncthreads_or(!ok) || tile >= end) return;
+    if (__syncthreads_or(!ok)) return;
+    if (threadIdx.x == 0) {
+      piece_s.run.tile += piece_s.t1 - piece_s.t0;
+      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, C::kTileRows);
+    }
+    __syncthreads();
+    if (piece_s.run.tile >= piece_s.run.end) return;
     fence_proxy_async_smem();   // the rings were written by ordinary stores; bulk copies come next
   }
 }
 
 // grid (units, rows), block 2 kD: merges what several CTAs left of a unit, 8 pieces at a time (kD / 4 threads each).
-constexpr int kMaxCtas = 512;
-
 template <int kD, int kRows>
-__global__ void __launch_bounds__(2 * kD) paged_mma_combine_kernel(const __grid_constant__ PagedMmaArgs a, int ctas, int tile_rows) {
+__global__ void __launch_bounds__(2 * kD) paged_mma_combine_kernel(const __grid_constant__ PagedMmaArgs a, int grid, int tile_rows) {
   grid_dependency_wait();
-  __shared__ long long run_s[2];
+  grid_dependency_launch();
+  __shared__ int run_s[2];
+  __shared__ float2 ml_s[kMaxCtas];
+  __shared__ float4 acc_s[8][kD / 4];
   const PagedCache& c = a.c;
   const int unit = blockIdx.x, row = blockIdx.y, bh = unit / a.row_tiles, rho = (unit - bh * a.row_tiles) * kRows + row;
   if (rho >= c.n_tokens * c.G) return;
   const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles, entry = unit / units;
-  const int b = bh / c.Hkv, h = bh - b * c.Hkv, i = rho / c.G, g = rho - i * c.G;
+  const int b = bh / c.Hkv, h = bh - b * c.Hkv, lane = threadIdx.x & 31;
   if (threadIdx.x < 32) {
     // where the unit's entry begins, by the same sums as in the kernel before
-    long long before = 0, all = 0;
+    int before = 0, all = 0;
     const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
     for (int e = threadIdx.x; e < entries; e += 32) {
-      const long long t = (long long)entry_tiles(c, e, tile_rows) * units;
+      const int t = entry_tiles(c, e, tile_rows) * units;
       all += t;
       if (e < entry) before += t;
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-      all += __shfl_xor_sync(0xffffffffu, all, off);
-      before += __shfl_xor_sync(0xffffffffu, before, off);
-    }
+    all = __reduce_add_sync(0xffffffffu, all);
+    before = __reduce_add_sync(0xffffffffu, before);
     if (threadIdx.x == 0) { run_s[0] = all; run_s[1] = before; }
   }
+  const int tiles = entry_tiles(c, entry, tile_rows), count = paged_count(c, b);
   __syncthreads();
-  const long long all = run_s[0];
-  const int tiles = entry_tiles(c, entry, tile_rows);
-  const long long u0 = run_s[1] + (long long)(unit - entry * units) * tiles, u1 = u0 + tiles;
-  if (ctas > all) ctas = (int)all;
-  // the CTA whose share [all * x / ctas, all * (x + 1) / ctas) holds tile t
-  auto holder = [&](long long t) { return (int)(((t + 1) * ctas - 1) / all); };
-  const int x0 = holder(u0), x1 = holder(u1 - 1);
-  if (x0 == x1) return;                        // it was one CTA's: written
-  // a CTA's first piece lies in its first slot, its last in the second; x0's is a later one where the unit begins inside its share
-  constexpr long long kSlot = kRows * (kD + 2);
-  const bool later = all * x0 / ctas < u0;
-  const int pieces = x1 - x0 + 1;
-  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0 && later)) * kSlot; };
-  __shared__ float factor[kMaxCtas];
-  __shared__ float of_warp[2][2 * kD / 32];
-  __shared__ float4 acc_s[8][kD / 4];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float mm = -INFINITY;
-  for (int x = threadIdx.x; x < pieces; x += 2 * kD) mm = fmaxf(mm, piece(x)[kRows * kD + 2 * row]);
+  const Deal deal(run_s[0], grid);
+  const int u0 = run_s[1] + (unit - entry * units) * tiles;
+  const int x0 = deal.first_of(u0, tiles), pieces = deal.last_of(u0, tiles) - x0 + 1;
+  if (pieces == 1) return;                     // it was one CTA's: written
+  constexpr int kSlot = kRows * (kD + 2);
+  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0)) * kSlot; };
+  const int sub = threadIdx.x / (kD / 4), v = threadIdx.x % (kD / 4);
+  constexpr int kAhead = 5;                    // requested before the factors are known
+  float4 o[kAhead];
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (sub + 8 * k < pieces) o[k] = __ldcg(reinterpret_cast<const float4*>(piece(sub + 8 * k) + row * kD) + v);
+  for (int x = threadIdx.x; x < pieces; x += 2 * kD) ml_s[x] = __ldcg(reinterpret_cast<const float2*>(piece(x) + kRows * kD) + row);
+  __syncthreads();
+  float mm = -INFINITY, ll = 0.f;
+  for (int x = lane; x < pieces; x += 32) mm = fmaxf(mm, ml_s[x].x);
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-  if (lane == 0) of_warp[0][warp] = mm;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < 2 * kD / 32; ++w) mm = fmaxf(mm, of_warp[0][w]);
-  float ll = 0.f;
-  for (int x = threadIdx.x; x < pieces; x += 2 * kD) {
-    const float* ml = piece(x) + kRows * kD + 2 * row;
-    const float f = ml[0] == -INFINITY ? 0.f : ex2_approx(ml[0] - mm);
-    factor[x] = f;
-    ll = fmaf(ml[1], f, ll);
-  }
+  auto factor = [&](int x) { return ml_s[x].x == -INFINITY ? 0.f : ex2_approx(ml_s[x].x - mm); };
+  for (int x = lane; x < pieces; x += 32) ll = fmaf(ml_s[x].y, factor(x), ll);
 #pragma unroll
   for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
-  if (lane == 0) of_warp[1][warp] = ll;
-  __syncthreads();
-  ll = 0.f;
-#pragma unroll
-  for (int w = 0; w < 2 * kD / 32; ++w) ll += of_warp[1][w];
-  const int sub = threadIdx.x / (kD / 4), v = threadIdx.x % (kD / 4);
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-  for (int x = sub; x < pieces; x += 8) {
-    const float4 o = reinterpret_cast<const float4*>(piece(x) + row * kD)[v];
-    const float f = factor[x];
-    acc.x = fmaf(o.x, f, acc.x); acc.y = fmaf(o.y, f, acc.y); acc.z = fmaf(o.z, f, acc.z); acc.w = fmaf(o.w, f, acc.w);
-  }
+#pragma unroll
+  for (int k = 0; k < kAhead; ++k)
+    if (sub + 8 * k < pieces) fma4(acc, o[k], factor(sub + 8 * k));
+  for (int x = sub + 8 * kAhead; x < pieces; x += 8) fma4(acc, __ldcg(reinterpret_cast<const float4*>(piece(x) + row * kD) + v), factor(x));
   acc_s[sub][v] = acc;
   __syncthreads();
-  if (threadIdx.x >= kD) return;
-  float sum = 0.f;
+  if (sub != 0) return;
 #pragma unroll
-  for (int x = 0; x < 8; ++x) sum += reinterpret_cast<const float*>(acc_s[x])[threadIdx.x];
-  const bool some = ll > 0.f && i < paged_count(c, b);
-  const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
-  a.out[at * kD + threadIdx.x] = __float2bfloat16(some ? sum / ll : 0.f);
-  if (threadIdx.x == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+  for (int k = 1; k < 8; ++k) fma4(acc, acc_s[k][v], 1.f);
+  write_row<kD>(a, b, h, rho, count, v, acc, mm, ll);
 }
 
 // ---- host: one set of functions per instantiation ----
 struct Variant {
   void (*kernel)(CUtensorMap, CUtensorMap, PagedMmaArgs);
+  void (*in_clusters)(CUtensorMap, CUtensorMap, PagedMmaArgs);
   void (*combine)(PagedMmaArgs, int, int);
   int d, threads, per_sm, rows, tile_rows;
-  size_t smem;
+  size_t smem, cluster_smem;
+  long long max_tiles(const PagedCache& c, long long units) const { return (c.capacity() / tile_rows + 1) * units; }
 };
 
 template <int kD, int kGroups, int kNT> Variant variant() {
   using C = Config<kD, kGroups, kNT>;
-  return Variant{paged_mma_kernel<kD, kGroups, kNT>, paged_mma_combine_kernel<kD, C::kRows>, kD, C::kWarps * 32, C::kPerSm, C::kRows,
-                 C::kTileRows, C::kSmem};
+  return Variant{paged_mma_kernel<kD, kGroups, kNT, false>, paged_mma_kernel<kD, kGroups, kNT, true>, paged_mma_combine_kernel<kD, C::kRows>, kD, C::kWarps * 32, C::kPerSm, C::kRows,
+                 C::kTileRows, C::kSmem, C::kClusterSmem};
 }
 
 template <int kNT> bool pick_nt(const PagedCache& c, Variant* v) {
@@ -873,9 +965,18 @@ bool pick(const PagedCache& c, Variant* v) {
   return (long long)c.n_tokens * c.G <= 8 ? pick_nt<1>(c, v) : pick_nt<2>(c, v);
 }
 
+// CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units.
+int paged_mma_cluster(const PagedCache& c, const Variant& v, long long units, const int* clusters_of) {
+  int i = 4;
+  while (i >= 0 && units > clusters_of[i]) --i;
+  if (i < 1) return 0;
+  return c.capacity() <= kClusterRows ? 1 << i : 0;
+}
+
 }  // namespace
 
-cudaError_t paged_mma_init() {
+// clusters_of[p][i]: clusters of 2^i CTAs that the device holds at once of kernels with p + 1 CTAs per SM.
+cudaError_t paged_mma_init(int (*clusters_of)[5]) {
   PagedCache c{};
   for (int d : {64, 128, 256})
     for (int group : {0, 32, 64, 128})
@@ -886,15 +987,37 @@ cudaError_t paged_mma_init() {
         Variant v;
         if (!pick(c, &v)) continue;
         cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(v.in_clusters, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.cluster_smem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(v.in_clusters, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
+        if (d != 128 || rows != 1 || (group != 0 && group != 64)) continue;
+        for (int i = 0; i < 5; ++i) {
+          cudaLaunchConfig_t cfg = {};
+          cfg.gridDim = dim3(16);
+          cfg.blockDim = dim3((unsigned int)v.threads);
+          cfg.dynamicSmemBytes = v.cluster_smem;
+          cudaLaunchAttribute attr[1];
+          attr[0].id = cudaLaunchAttributeClusterDimension;
+          attr[0].val.clusterDim.x = 1u << i;
+          attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+          cfg.attrs = attr;
+          cfg.numAttrs = 1;
+          int* held = &clusters_of[v.per_sm - 1][i];
+          *held = 0;
+          if (cudaOccupancyMaxActiveClusters(held, v.in_clusters, &cfg) != cudaSuccess) {
+            (void)cudaGetLastError();   // a size this device does not take: it holds none of them
+            *held = 0;
+          }
+        }
       }
   return cudaSuccess;
 }
 
 bool paged_mma_supported(const PagedCache& c) {
   Variant v;
-  return pick(c, &v);
+  if (!pick(c, &v)) return false;
+  const long long units = (long long)c.batch * c.Hkv * ((c.n_tokens * (long long)c.G + v.rows - 1) / v.rows);
+  return v.max_tiles(c, units) <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }
 
 size_t paged_mma_bytes(const PagedCache& c, int sm_count) {
@@ -904,7 +1027,7 @@ size_t paged_mma_bytes(const PagedCache& c, int sm_count) {
 }
 
 cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count,
-                             long long wait_limit, cudaStream_t st, int* launches) {
+                             const int (*clusters_of)[5], long long wait_limit, cudaStream_t st, int* launches) {
   Variant v;
   if (!pick(c, &v)) return cudaErrorInvalidValue;
   CUtensorMap tmK{}, tmV{};
@@ -918,10 +1041,28 @@ cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q
   PagedMmaArgs a{};
   a.c = c; a.Q = Q; a.out = (__nv_bfloat16*)out; a.lse = lse; a.part = part; a.wait_limit = wait_limit;
   a.row_tiles = (c.n_tokens * c.G + v.rows - 1) / v.rows;
-  a.cluster = 0;
-  const int units = c.batch * c.Hkv * a.row_tiles;
-  const int ctas = v.per_sm * sm_count < kMaxCtas ? v.per_sm * sm_count : kMaxCtas;
-  cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
+  const long long units = (long long)c.batch * c.Hkv * a.row_tiles;
+  a.cluster = paged_mma_cluster(c, v, units, clusters_of[v.per_sm - 1]);
+  *launches = 1;
+  if (a.cluster) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned int)(units * a.cluster));
+    cfg.blockDim = dim3((unsigned int)v.threads);
+    cfg.dynamicSmemBytes = v.cluster_smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned int)a.cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, v.in_clusters, tmK, tmV, a);
+  }
+  int ctas = v.per_sm * sm_count;
+  if (ctas > kMaxCtas) ctas = kMaxCtas;
+  const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
   *launches = 2;
   return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), 2 * v.d, 0, st, a, ctas, v.tile_rows);

@@ -13,6 +13,7 @@ struct restkv_handle {
   void* tc_state;
   int select_clusters[4];     // clusters of 1, 2, 4, 8 CTAs of the select kernel that the device holds at once
   int decode_clusters[5];     // clusters of 1, 2, 4, 8, 16 CTAs of the decode kernel that the device holds at once
+  int paged_clusters[2][5];   // the same of the paged attention kernels with one and with two CTAs per SM
   long long launches;
   int last_cuda_error;
   int kernel_path;            // 0 auto, 1 SIMT, 2 tensor core required, 3 tensor core in its head-sequential form

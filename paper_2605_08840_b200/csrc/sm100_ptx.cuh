@@ -14,6 +14,10 @@ __device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepco
 // Lets such a successor be scheduled as soon as the SMs have room for it.
 __device__ __forceinline__ void grid_dependency_launch() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
+// Barrier of a cluster in two halves: what a CTA wrote before its arrival, peers see after their wait.
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 
 // One thread of a converged warp, the same one each time.  What issues tcgen05.mma stands behind this and not behind lane == 0: the

@@ -711,3 +711,34 @@ def test_refusals_enqueue_nothing(handle):
     assert handle.launch_count() == launches
     torch.cuda.synchronize()
     assert torch.equal(cache.K, stale) and torch.all(out == 7.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_attend_many_sequences(handle, fmt, per_head):
+    """More units of work than the device keeps counters for, and than it has SMs; lengths that share no pattern."""
+    rng = np.random.default_rng(11)
+    b, Hkv = 90, 3
+    cache = Cache(rng, b, 2 * Hkv, Hkv, 64, fmt, 16, 12, 32 if fmt == "int4" else 0, per_head=per_head)
+    lengths = rng.integers(0, 190, (b, Hkv) if per_head else (b,))
+    lengths.flat[3] = 0
+    lengths.flat[5] = 192
+    cache.fill(handle, rng, lengths)
+    check_attention(handle, rng, cache, lengths, None, 1)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("steps", [2.0 ** -30, 2.0 ** -12, 2.0 ** 12, 2.0 ** 40])
+@pytest.mark.parametrize("t", [1, 40])
+def test_attend_values_of_any_size(handle, fmt, steps, t):
+    """V far from 1, and in one cache rows that are 2^20 times larger than the rest, which carry little weight or all of it."""
+    rng = np.random.default_rng(12)
+    cache = Cache(rng, 1, 4, 1, 128, fmt, 16, 40, 64 if fmt == "int4" else 0)
+    K = rng.standard_normal((1, 1, 600, 128))
+    V = rng.standard_normal((1, 1, 600, 128)) * steps
+    V[:, :, 17::100] *= 2.0 ** 20
+    V[:, :, 400:432] = 0.0
+    handle.paged_append(cache.desc, 600, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([600]), cache.table)
+    check_attention(handle, rng, cache, [600], None, t, q_scale=3.0)
