@@ -5,9 +5,8 @@
 //   - warps that never wait for one another while they stream: each owns every kWarps-th tile of its CTA's run and a ring of tile
 //     slots that its own lane 0 fills with bulk copies (4 bits: a block of 16 rows lies in one piece, codes and parameters) or TMA
 //     boxes (bf16: 128-byte swizzle for ldmatrix);
-//   - mma.sync m16n8k16: S = Q K^T with the query rows as the 16 rows and 8 cache rows as columns, O^T = V^T P^T with 16 dims as rows
-//     and 8 query rows as columns.  The accumulator layout of S is the operand layout of P^T, so the weights never leave the
-//     registers, and up to 8 query rows cost half of what P V with 16 padded rows does;
+//   - mma.sync m16n8k16: S^T = K Q^T with 16 cache rows as rows and 8 query rows as columns, O^T = V^T P^T with 16 dims as rows.  Up to 8
+//     query rows cost no padding; the weights get from one layout to the other by a transposition of 8 x 8 blocks in registers;
 //   - 4-bit rows are laid out for the fragments: a lane's 4 bytes of K are 8 codes of the dims that its operand registers take, its 2
 //     bytes of V 4 dims of one row.
 //     A nibble is an operand as it stands: the 16 bits c << 4k are the f16 subnormal 2^(4k - 24) c for k = 0, 1, products with it are
@@ -65,6 +64,11 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {   // of 16-bit elements, a row per four lanes
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
 }
 __device__ __forceinline__ float lg2_approx(float x) {
   float y;
@@ -277,7 +281,6 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   extern __shared__ uint8_t smem_raw[];
   __shared__ __align__(8) uint64_t full[kW][kStages];
   __shared__ float w_ml[kW][kRows][2];
-  __shared__ float w_lo[kW][kRows][kG];        // 4 bits: sum of p offset per group
   __shared__ float w_factor[kW][kRows];
   __shared__ float2 c_ml[kRows];
   __shared__ int abort_flag;
@@ -436,19 +439,23 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     for (int i = 0; i < kStages; ++i)
       if (i < mine && i < stages) request(i, slot + i < stages ? slot + i : slot + i - stages);
 
-    // ---- Q as the A operand, kD / 16 steps; what each row sees ----
+    // ---- Q^T as the B operand, kD / 16 steps; what the query rows of the lane's columns 2 q4, 2 q4 + 1 see ----
     // 4 bits: in f16, scaled by a power of two per row (and 2^-4 where the codes come 16 times too large); sums of q per group in the
     // codes' and that scale, which the logits' factor takes out again.
-    uint32_t qa[kD / 16][2 * kNT];
-    float q_sum[kNT][kG], unscale[kNT];
-    int sees[kNT];
+    uint32_t qb[kD / 16][kNT][2];
+    float q_sum[kNT][kG][2], to_log2[kNT][2];  // to log2 units, or to the cap's exponent
+    int sees[kNT][2];
     int sees_least = n;
+    const float factor = c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : c.scale * kLog2e;
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
-      const int rho = rho0 + r + 8 * t, i = rho / c.G;
-      sees[t] = rho < R && i < count ? n - (count - 1 - i) : n;
-      sees_least = min(sees_least, sees[t]);
-      unscale[t] = 1.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int rho = rho0 + 2 * q4 + e + 8 * t, i = rho / c.G;
+        sees[t][e] = rho < R && i < count ? n - (count - 1 - i) : n;
+        sees_least = min(sees_least, sees[t][e]);
+        to_log2[t][e] = factor;
+      }
       if constexpr (kInt4) {
         float top = 0.f;
 #pragma unroll
@@ -459,9 +466,12 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         int e = 141 - (int)(__float_as_uint(top) >> 23);
         e = e < -100 ? -100 : e > 100 ? 100 : e;
         const float scale = top < INFINITY ? __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7FFFFFFFu);
-        unscale[t] = __uint_as_float((uint32_t)(127 + 24 - e) << 23);
+        const float unscale = __uint_as_float((uint32_t)(127 + 24 - e) << 23) * factor;
+        to_log2[t][0] = __shfl_sync(0xffffffffu, unscale, 8 * q4);
+        to_log2[t][1] = __shfl_sync(0xffffffffu, unscale, 8 * q4 + 4);
+        float sum[kG];
 #pragma unroll
-        for (int g2 = 0; g2 < kG; ++g2) q_sum[t][g2] = 0.f;
+        for (int g = 0; g < kG; ++g) sum[g] = 0.f;
 #pragma unroll
         for (int m = 0; m < kWords; ++m) {
           float v[8];
@@ -471,108 +481,110 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             v[2 * x + 1] = upper(q_raw[t][4 * m + x]) * scale;
           }
           // the pairs (i, i + 4) that a word's codes come in
-          qa[2 * m][t] = pack_f16x2(v[0], v[4]);
-          qa[2 * m][kNT + t] = pack_f16x2(0x1p-4f * v[1], 0x1p-4f * v[5]);
-          qa[2 * m + 1][t] = pack_f16x2(v[2], v[6]);
-          qa[2 * m + 1][kNT + t] = pack_f16x2(0x1p-4f * v[3], 0x1p-4f * v[7]);
-          q_sum[t][m / kPerGroup] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+          qb[2 * m][t][0] = pack_f16x2(v[0], v[4]);
+          qb[2 * m][t][1] = pack_f16x2(0x1p-4f * v[1], 0x1p-4f * v[5]);
+          qb[2 * m + 1][t][0] = pack_f16x2(v[2], v[6]);
+          qb[2 * m + 1][t][1] = pack_f16x2(0x1p-4f * v[3], 0x1p-4f * v[7]);
+          sum[m / kPerGroup] += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
         }
 #pragma unroll
-        for (int g2 = 0; g2 < kG; ++g2) {
-          q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 1);
-          q_sum[t][g2] += __shfl_xor_sync(0xffffffffu, q_sum[t][g2], 2);
-          q_sum[t][g2] *= 0x1p-24f;
+        for (int g = 0; g < kG; ++g) {
+          sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 1);
+          sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], 2);
+          sum[g] *= 0x1p-24f;
+          q_sum[t][g][0] = __shfl_sync(0xffffffffu, sum[g], 8 * q4);
+          q_sum[t][g][1] = __shfl_sync(0xffffffffu, sum[g], 8 * q4 + 4);
         }
       } else {
 #pragma unroll
         for (int k = 0; k < kD / 16; ++k) {
-          qa[k][t] = q_raw[t][2 * k];
-          qa[k][kNT + t] = q_raw[t][2 * k + 1];
+          qb[k][t][0] = q_raw[t][2 * k];
+          qb[k][t][1] = q_raw[t][2 * k + 1];
         }
       }
     }
     sees_least = __reduce_min_sync(0xffffffffu, sees_least);
 
     const float cap_log2 = c.softcap * kLog2e;
-    float to_log2[kNT];                        // what a row's sums are multiplied with: to log2 units, or to the cap's exponent
-#pragma unroll
-    for (int t = 0; t < kNT; ++t)
-      to_log2[t] = (c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : c.scale * kLog2e) * unscale[t];
-    float ref[kNT], l[kNT];                    // weights are 2^(logit - ref); l: this lane's share of the row's sum
+    float ref[kNT][2], l[kNT][2];              // of the lane's columns: weights are 2^(logit - ref); this lane's share of the sum
     float o[kD / 16][kNT][4];                  // dims of the 16-dim tile (r, r + 8), query rows 2 q4, 2 q4 + 1 (+ 8 per tile)
-    float lo[kG][kNT];                         // 4 bits: this lane's share of sum p offset
+    float lo[kG][kNT][2];                      // 4 bits: this lane's share of sum p offset
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
-      ref[t] = -INFINITY;
-      l[t] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        ref[t][e] = -INFINITY;
+        l[t][e] = 0.f;
+#pragma unroll
+        for (int g = 0; g < kG; ++g) lo[g][t][e] = 0.f;
+      }
 #pragma unroll
       for (int k = 0; k < kD / 16; ++k)
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[k][t][e] = 0.f;
-#pragma unroll
-      for (int g = 0; g < kG; ++g) lo[g][t] = 0.f;
     }
 
     // One tile; kEdge: some of its rows are not there, or not for every query row.
     auto take = [&](auto edge, uint32_t stage, int row0, unsigned int gone) {
       constexpr bool kEdge = decltype(edge)::value;
-      // rows of the lane's four columns in a block: 4 bits q4 + 4 j, which is the order of the parameters; bf16 2 q4 + (j & 1) + 8 (j / 2)
-      auto column = [&](int j) { return kInt4 ? q4 + 4 * j : 2 * q4 + (j & 1) + 8 * (j >> 1); };
+      // Rows m, m + 8 of S^T are rows of the block: m itself in bf16; in 4 bits m / 2 + 4 (m % 2), so that the k indices 2 q4, 2 q4 + 1,
+      // 2 q4 + 8, 2 q4 + 9 of O^T = V^T P^T are the rows q4 + 4 j, whose codes of V lie a warp's load side by side.
+      const int own = kInt4 ? (r >> 1) + 4 * (r & 1) : r;
+      // sc[.][.][2 i + e]: row own + 8 i, query row 2 q4 + e
       float sc[kBlocks][kNT][4];
+      const uint32_t pick = r & 1 ? 0x3244u : 0x1044u;   // one of a pair of bf16 as fp32
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k) {
         const uint32_t kt = stage + k * C::kBlockBytes;
         if constexpr (kInt4) {
-          uint32_t w[2][kWords];               // rows r / 2 + 4 (r % 2) (+ 8): columns r of the two tiles of 8 columns
+          uint32_t w[2][kWords];
 #pragma unroll
-          for (int half = 0; half < 2; ++half)
-            lds_words<kWords>(kt + (uint32_t)(8 * half + (r >> 1) + 4 * (r & 1)) * (kD / 2) + q4 * (kD / 8), w[half]);
+          for (int half = 0; half < 2; ++half) lds_words<kWords>(kt + (uint32_t)(own + 8 * half) * (kD / 2) + q4 * (kD / 8), w[half]);
 #pragma unroll
           for (int g = 0; g < kG; ++g) {
-            float acc[2][4];                   // rows r, r + 8; columns 2 q4, 2 q4 + 1
+            float acc[kNT][4];
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
+            for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x) {
+              const uint32_t a0[4] = {code_pair<0>(w[0][x]), code_pair<0>(w[1][x]), code_pair<1>(w[0][x]), code_pair<1>(w[1][x])};
+              const uint32_t a1[4] = {code_pair<2>(w[0][x]), code_pair<2>(w[1][x]), code_pair<3>(w[0][x]), code_pair<3>(w[1][x])};
 #pragma unroll
-              for (int x = g * kPerGroup; x < (g + 1) * kPerGroup; ++x) {
-                const uint32_t a0[4] = {qa[2 * x][0], kNT == 2 ? qa[2 * x][1] : 0u, qa[2 * x][kNT], kNT == 2 ? qa[2 * x][kNT + kNT - 1] : 0u};
-                const uint32_t a1[4] = {qa[2 * x + 1][0], kNT == 2 ? qa[2 * x + 1][1] : 0u, qa[2 * x + 1][kNT],
-                                        kNT == 2 ? qa[2 * x + 1][kNT + kNT - 1] : 0u};
-                if (x == g * kPerGroup) mma16816_f16_start(acc[half], a0, code_pair<0>(w[half][x]), code_pair<1>(w[half][x]));
-                else mma16816_f16(acc[half], a0, code_pair<0>(w[half][x]), code_pair<1>(w[half][x]));
-                mma16816_f16(acc[half], a1, code_pair<2>(w[half][x]), code_pair<3>(w[half][x]));
+              for (int t = 0; t < kNT; ++t) {
+                if (x == g * kPerGroup) mma16816_f16_start(acc[t], a0, qb[2 * x][t][0], qb[2 * x][t][1]);
+                else mma16816_f16(acc[t], a0, qb[2 * x][t][0], qb[2 * x][t][1]);
+                mma16816_f16(acc[t], a1, qb[2 * x + 1][t][0], qb[2 * x + 1][t][1]);
               }
-            const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * q4);
-            const float step[4] = {lower(u.x), upper(u.x), lower(u.y), upper(u.y)}, off[4] = {lower(u.z), upper(u.z), lower(u.w), upper(u.w)};
+            }
+            const uint4 u = lds128(kt + 8 * kD + 64 * g + 16 * (r >> 1));
+            const float step[2] = {__uint_as_float(__byte_perm(u.x, 0u, pick)), __uint_as_float(__byte_perm(u.y, 0u, pick))};
+            const float off[2] = {__uint_as_float(__byte_perm(u.z, 0u, pick)), __uint_as_float(__byte_perm(u.w, 0u, pick))};
 #pragma unroll
             for (int t = 0; t < kNT; ++t)
 #pragma unroll
-              for (int j = 0; j < 4; ++j)
-                sc[k][t][j] = fmaf(step[j], acc[j >> 1][2 * t + (j & 1)], g == 0 ? off[j] * q_sum[t][g] : fmaf(off[j], q_sum[t][g], sc[k][t][j]));
+              for (int x = 0; x < 4; ++x) {
+                const float q = q_sum[t][g][x & 1];
+                sc[k][t][x] = fmaf(step[x >> 1], acc[t][x], g == 0 ? off[x >> 1] * q : fmaf(off[x >> 1], q, sc[k][t][x]));
+              }
           }
         } else {
-          float acc[2][4] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+          for (int t = 0; t < kNT; ++t) sc[k][t][0] = sc[k][t][1] = sc[k][t][2] = sc[k][t][3] = 0.f;
           const int mat = lane >> 3, mr = lane & 7;
 #pragma unroll
           for (int x = 0; x < kD / 16; ++x) {
             uint32_t w[4];
-            ldsm4(kt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), w);
-            const uint32_t a0[4] = {qa[x][0], kNT == 2 ? qa[x][1] : 0u, qa[x][kNT], kNT == 2 ? qa[x][kNT + kNT - 1] : 0u};
-            mma16816(acc[0], a0, w[0], w[1]);
-            mma16816(acc[1], a0, w[2], w[3]);
+            ldsm4(kt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat & 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat >> 1)) ^ (uint32_t)mr) << 4), w);
+#pragma unroll
+            for (int t = 0; t < kNT; ++t) mma16816(sc[k][t], w, qb[x][t][0], qb[x][t][1]);
           }
-#pragma unroll
-          for (int t = 0; t < kNT; ++t)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) sc[k][t][j] = acc[j >> 1][2 * t + (j & 1)];
         }
       }
-      // logits in log2 units; columns that a row does not see weigh nothing
+      // logits in log2 units; rows that a query row does not see weigh nothing
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
         for (int t = 0; t < kNT; ++t)
 #pragma unroll
-          for (int j = 0; j < 4; ++j) sc[k][t][j] *= to_log2[t];
+          for (int x = 0; x < 4; ++x) sc[k][t][x] *= to_log2[t][x & 1];
       if (cap_log2 > 0.f) {
         // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
 #pragma unroll
@@ -580,7 +592,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
           for (int t = 0; t < kNT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sc[k][t][j] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][j])), cap_log2);
+            for (int x = 0; x < 4; ++x) sc[k][t][x] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][x])), cap_log2);
       }
       if constexpr (kEdge) {
 #pragma unroll
@@ -588,72 +600,71 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
           for (int t = 0; t < kNT; ++t)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (row0 + k * kBlockRows + column(j) >= sees[t] || (gone >> k & 1u)) sc[k][t][j] = -INFINITY;
-      }
-      // bits of the rows of V that are there
-      uint32_t keep01[kBlocks], keep23[kBlocks];
-#pragma unroll
-      for (int k = 0; k < kBlocks; ++k) {
-        keep01[k] = keep23[k] = 0xFFFFFFFFu;
-        if constexpr (kEdge) {
-          // rows past the cache hold anything: their bits are cleared, so that a weight of 0 finds a number there
-          const int left = (gone >> k & 1u) ? 0 : n - (row0 + k * kBlockRows);
-          keep01[k] = (column(0) < left ? 0xFFFFu : 0u) | (column(1) < left ? 0xFFFF0000u : 0u);
-          keep23[k] = (column(2) < left ? 0xFFFFu : 0u) | (column(3) < left ? 0xFFFF0000u : 0u);
-        }
+            for (int x = 0; x < 4; ++x)
+              if (row0 + k * kBlockRows + own + 8 * (x >> 1) >= sees[t][x & 1] || (gone >> k & 1u)) sc[k][t][x] = -INFINITY;
       }
       // 4 bits: p step is to fit f16 whatever the steps are, so that the reference grows with the largest of them, too
+      float v_step[kBlocks][kG][2], v_off[kBlocks][kG][2];
       float most = 0.f;
       if constexpr (kInt4) {
-        uint32_t top = 0x2B802B80u;            // 2^-40 at least: weights stay well within fp32
+        float top = 0x1p-40f;                  // at least: weights stay well within fp32
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
           for (int g = 0; g < kG; ++g) {
-            const uint2 u = lds64(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * q4);
-            top = __vmaxu2(top, __vmaxu2(u.x & keep01[k], u.y & keep23[k]));   // steps are not negative: ordered as integers
+            const uint4 u = lds128(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * (r >> 1));
+            v_step[k][g][0] = __uint_as_float(__byte_perm(u.x, 0u, pick));
+            v_step[k][g][1] = __uint_as_float(__byte_perm(u.y, 0u, pick));
+            v_off[k][g][0] = __uint_as_float(__byte_perm(u.z, 0u, pick));
+            v_off[k][g][1] = __uint_as_float(__byte_perm(u.w, 0u, pick));
+            if constexpr (kEdge) {
+              // a row past the cache holds anything: a weight of 0 is to find a number there
+#pragma unroll
+              for (int x = 0; x < 2; ++x)
+                if (row0 + k * kBlockRows + own + 8 * x >= n || (gone >> k & 1u)) v_step[k][g][x] = v_off[k][g][x] = 0.f;
+            }
+            top = fmax3(top, v_step[k][g][0], v_step[k][g][1]);
           }
-        most = lg2_approx(__uint_as_float(max(top & 0xFFFF0000u, top << 16)));
+        most = lg2_approx(top);
       }
-      float f[kNT];
+      float f[kNT][2];
       bool grown = false;
 #pragma unroll
-      for (int t = 0; t < kNT; ++t) {
-        float mx = -INFINITY;
+      for (int t = 0; t < kNT; ++t)
 #pragma unroll
-        for (int k = 0; k < kBlocks; ++k) mx = fmaxf(mx, fmaxf(fmaxf(sc[k][t][0], sc[k][t][1]), fmaxf(sc[k][t][2], sc[k][t][3])));
-        mx += most;
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        f[t] = 1.f;
-        if (mx > ref[t] + kSlack) {            // o is rescaled only when the weights would grow past 2^kSlack
-          f[t] = ex2_approx(ref[t] - (mx - kStart));   // ref = -inf gives 0
-          ref[t] = mx - kStart;
-          l[t] *= f[t];
-          grown = true;
+        for (int e = 0; e < 2; ++e) {
+          float mx = fmaxf(sc[0][t][e], sc[0][t][2 + e]);
+#pragma unroll
+          for (int k = 1; k < kBlocks; ++k) mx = fmax3(mx, sc[k][t][e], sc[k][t][2 + e]);
+          mx += most;
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+          mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+          f[t][e] = 1.f;
+          if (mx > ref[t][e] + kSlack) {       // o is rescaled only when the weights would grow past 2^kSlack
+            f[t][e] = ex2_approx(ref[t][e] - (mx - kStart));   // ref = -inf gives 0
+            ref[t][e] = mx - kStart;
+            l[t][e] *= f[t][e];
+            grown = true;
+          }
+          const float m_use = ref[t][e] == -INFINITY ? 0.f : ref[t][e];   // only logits of -inf so far: they weigh nothing
+#pragma unroll
+          for (int k = 0; k < kBlocks; ++k) {
+            sc[k][t][e] = ex2_approx(sc[k][t][e] - m_use);
+            sc[k][t][2 + e] = ex2_approx(sc[k][t][2 + e] - m_use);
+            l[t][e] += sc[k][t][e] + sc[k][t][2 + e];
+          }
         }
-        const float m_use = ref[t] == -INFINITY ? 0.f : ref[t];   // only logits of -inf so far: they weigh nothing
-#pragma unroll
-        for (int k = 0; k < kBlocks; ++k) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) sc[k][t][j] = ex2_approx(sc[k][t][j] - m_use);
-          l[t] += (sc[k][t][0] + sc[k][t][1]) + (sc[k][t][2] + sc[k][t][3]);
-        }
-      }
       if (__any_sync(0xffffffffu, grown)) {
 #pragma unroll
         for (int t = 0; t < kNT; ++t) {
-          // the factors of the rows that o's columns stand for
-          const float f0 = __shfl_sync(0xffffffffu, f[t], 8 * q4), f1 = __shfl_sync(0xffffffffu, f[t], 8 * q4 + 4);
 #pragma unroll
-          for (int k = 0; k < kD / 16; ++k) {
-            o[k][t][0] *= f0; o[k][t][1] *= f1;
-            o[k][t][2] *= f0; o[k][t][3] *= f1;
-          }
+          for (int k = 0; k < kD / 16; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][t][e] *= f[t][e & 1];
           if (kInt4) {
 #pragma unroll
-            for (int g = 0; g < kG; ++g) lo[g][t] *= f[t];
+            for (int g = 0; g < kG; ++g) { lo[g][t][0] *= f[t][0]; lo[g][t][1] *= f[t][1]; }
           }
         }
       }
@@ -669,15 +680,14 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           for (int x = 0; x < kWords; ++x) {
             if (x % kPerGroup == 0) {
               const int g = x / kPerGroup;
-              uint4 u = lds128(vt + 8 * kD + 64 * g + 16 * q4);
-              if constexpr (kEdge) { u.x &= keep01[k]; u.y &= keep23[k]; u.z &= keep01[k]; u.w &= keep23[k]; }
-              const float s0 = lower(u.x), s1 = upper(u.x), s2 = lower(u.y), s3 = upper(u.y);
+              const float *step = v_step[k][g], *off = v_off[k][g];
 #pragma unroll
               for (int t = 0; t < kNT; ++t) {
                 const float* p = sc[k][t];
-                lo[g][t] = fmaf(p[0], lower(u.z), fmaf(p[1], upper(u.z), fmaf(p[2], lower(u.w), fmaf(p[3], upper(u.w), lo[g][t]))));
-                pb[t][0] = pack_f16x2(p[0] * s0, p[1] * s1);
-                pb[t][1] = pack_f16x2(p[2] * s2, p[3] * s3);
+                lo[g][t][0] = fmaf(p[0], off[0], fmaf(p[2], off[1], lo[g][t][0]));
+                lo[g][t][1] = fmaf(p[1], off[0], fmaf(p[3], off[1], lo[g][t][1]));
+                pb[t][0] = transpose8x8(pack_f16x2(p[0] * step[0], p[1] * step[0]));
+                pb[t][1] = transpose8x8(pack_f16x2(p[2] * step[1], p[3] * step[1]));
               }
             }
             const uint32_t y0 = __byte_perm(w[0][x >> 1], w[1][x >> 1], x & 1 ? 0x7632 : 0x5410);
@@ -691,18 +701,25 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             }
           }
         } else {
+          // bits of the rows 2 q4, 2 q4 + 1 (+ 8) of V that are there: past the cache is anything, and a weight of 0 is to find a number
+          uint32_t keep0 = 0xFFFFFFFFu, keep1 = 0xFFFFFFFFu;
+          if constexpr (kEdge) {
+            const int left = (gone >> k & 1u) ? 0 : n - (row0 + k * kBlockRows) - 2 * q4;
+            keep0 = (left > 0 ? 0xFFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
+            keep1 = (left > 8 ? 0xFFFFu : 0u) | (left > 9 ? 0xFFFF0000u : 0u);
+          }
           uint32_t pb[kNT][2];
 #pragma unroll
           for (int t = 0; t < kNT; ++t) {
-            pb[t][0] = pack_bf16x2(sc[k][t][0], sc[k][t][1]);
-            pb[t][1] = pack_bf16x2(sc[k][t][2], sc[k][t][3]);
+            pb[t][0] = transpose8x8(pack_bf16x2(sc[k][t][0], sc[k][t][1]));
+            pb[t][1] = transpose8x8(pack_bf16x2(sc[k][t][2], sc[k][t][3]));
           }
           const int mat = lane >> 3, mr = lane & 7;
 #pragma unroll
           for (int x = 0; x < kD / 16; ++x) {
             uint32_t va[4];
             ldsm4_t(vt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), va);
-            if constexpr (kEdge) { va[0] &= keep01[k]; va[1] &= keep01[k]; va[2] &= keep23[k]; va[3] &= keep23[k]; }
+            if constexpr (kEdge) { va[0] &= keep0; va[1] &= keep0; va[2] &= keep1; va[3] &= keep1; }
 #pragma unroll
             for (int t = 0; t < kNT; ++t) mma16816(o[x][t], va, pb[t][0], pb[t][1]);
           }
@@ -738,15 +755,18 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     };
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
-      l[t] += __shfl_xor_sync(0xffffffffu, l[t], 1);
-      l[t] += __shfl_xor_sync(0xffffffffu, l[t], 2);
-      if (q4 == 0) { w_ml[warp][r + 8 * t][0] = ref[t]; w_ml[warp][r + 8 * t][1] = l[t]; }
-      if (kInt4) {
+      auto over_rows = [](float x) {
+        x += __shfl_xor_sync(0xffffffffu, x, 4);
+        x += __shfl_xor_sync(0xffffffffu, x, 8);
+        return x + __shfl_xor_sync(0xffffffffu, x, 16);
+      };
 #pragma unroll
-        for (int g = 0; g < kG; ++g) {
-          lo[g][t] += __shfl_xor_sync(0xffffffffu, lo[g][t], 1);
-          lo[g][t] += __shfl_xor_sync(0xffffffffu, lo[g][t], 2);
-          if (q4 == 0) w_lo[warp][r + 8 * t][g] = lo[g][t];
+      for (int e = 0; e < 2; ++e) {
+        l[t][e] = over_rows(l[t][e]);
+        if (r == 0) { w_ml[warp][2 * q4 + e + 8 * t][0] = ref[t][e]; w_ml[warp][2 * q4 + e + 8 * t][1] = l[t][e]; }
+        if (kInt4) {
+#pragma unroll
+          for (int g = 0; g < kG; ++g) lo[g][t][e] = over_rows(lo[g][t][e]);
         }
       }
       if (mine > 0) {
@@ -754,9 +774,11 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         if constexpr (kInt4) {
 #pragma unroll
           for (int x = 0; x < kWords; ++x) {   // dims 32 x + 4 r + (0..3)
-            const float *e = o[2 * x][t], *f = o[2 * x + 1][t];
-            *w_o(warp, row, 8 * x + r) = make_float4(e[0] * 0x1p24f, e[2] * 0x1p20f, f[0] * 0x1p24f, f[2] * 0x1p20f);
-            *w_o(warp, row + 1, 8 * x + r) = make_float4(e[1] * 0x1p24f, e[3] * 0x1p20f, f[1] * 0x1p24f, f[3] * 0x1p20f);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float *u = &o[2 * x][t][e], *v = &o[2 * x + 1][t][e], add = lo[x / kPerGroup][t][e];
+              *w_o(warp, row + e, 8 * x + r) = make_float4(fmaf(u[0], 0x1p24f, add), fmaf(u[2], 0x1p20f, add), fmaf(v[0], 0x1p24f, add), fmaf(v[2], 0x1p20f, add));
+            }
           }
         } else {
 #pragma unroll
@@ -802,12 +824,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       for (int w = 0; w < kW; ++w) {
         const float f = w_factor[w][row];
         if (f == 0.f) continue;
-        float4 o4 = *w_o(w, row, v);
-        if (kInt4) {
-          const float add = w_lo[w][row][v / (kD / 4 / kG)];
-          o4.x += add; o4.y += add; o4.z += add; o4.w += add;
-        }
-        fma4(acc, o4, f);
+        fma4(acc, *w_o(w, row, v), f);
       }
       if (kCluster) {
         const int to = x % a.cluster;
