@@ -9,8 +9,10 @@
 //     query rows cost no padding; the weights get from one layout to the other by a transposition of 8 x 8 blocks in registers;
 //   - 4-bit rows are laid out for the fragments: a lane's 4 bytes of K are 8 codes of the dims that its operand registers take, its 2
 //     bytes of V 4 dims of one row.
-//     A nibble is an operand as it stands: the 16 bits c << 4k are the f16 subnormal 2^(4k - 24) c for k = 0, 1, products with it are
-//     exact in the fp32 accumulator, and a shift and four logic operations make 4 operand registers of 8 codes.  q is f16 scaled by a
+//     A code is an operand as it stands: 16 bits x < 1024 are the f16 subnormal 2^-24 x, so that a nibble in the lowest or in the next
+//     four bits is 2^-24 or 2^-20 times its code, and products with it are exact in the fp32 accumulator: a shift and four logic
+//     operations make 4 operand registers of 8 codes of K.  For V, whose sums over the upper codes of bytes may as well come out of
+//     those over whole bytes (upper = (byte - lower) / 16), it is one less.  q is f16 scaled by a
 //     power of two per query row (exact down to 2^-28 of the row's largest element).  s = step * (q . code) + offset * sum(q) per
 //     group, o = sum f16(p step) code + sum p offset, all sums in fp32.
 //     (bf16 16 + code: two operations per register, and the weights' rounding weighs twice as much unless 8 is taken off the codes:
@@ -381,9 +383,10 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
     }
 
+    constexpr int kAhead = 32 / kBlocks;       // tiles that are looked up at once
+    unsigned int side_by_side = 0;             // bit per lane: the tile that begins with its block lies in one piece
     unsigned int absent = 0;                   // bit slot * kBlocks + block: nothing was loaded there
     auto request = [&](int i, int s) {         // tile i into slot s, by the whole warp
-      constexpr int kAhead = 32 / kBlocks;
       if (i % kAhead == 0) {
         if (i > 0) look_up(i);
         if (block_of_lane / kBlocks >= t1 || block_of_lane >= blocks) {
@@ -394,41 +397,53 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         } else {
           place = (place * c.Hkv + h) * per_page + block_of_lane % per_page;
         }
+        const int after = __shfl_down_sync(0xffffffffu, place, 1);
+        side_by_side = __ballot_sync(0xffffffffu, place >= 0 && (kBlocks == 1 || after == place + 1));
       }
-      int at[kBlocks];
-      int there = 0;
-#pragma unroll
-      for (int k = 0; k < kBlocks; ++k) {
-        at[k] = __shfl_sync(0xffffffffu, place, (i % kAhead) * kBlocks + k);
-        there += at[k] >= 0;
-        const unsigned int bit = 1u << (s * kBlocks + k);
-        absent = at[k] >= 0 ? absent & ~bit : absent | bit;
-      }
-      if (lane == 0) {
-        uint8_t* dst = ring + (uint32_t)s * C::kStageBytes;
-        uint64_t* bar = &full[warp][s];
-        mbar_arrive_expect_tx(bar, (uint32_t)there * 2 * C::kBlockBytes);
-        if constexpr (kInt4) {
-          // K's blocks, then V's; two that follow one another in a page come in one piece
-          if (kBlocks == 2 && at[0] >= 0 && at[kBlocks - 1] == at[0] + 1) {
-            bulk_load(dst, c.K + (long long)at[0] * C::kBlockBytes, 2 * C::kBlockBytes, bar);
-            bulk_load(dst + 2 * C::kBlockBytes, c.V + (long long)at[0] * C::kBlockBytes, 2 * C::kBlockBytes, bar);
+      const int of = i % kAhead * kBlocks;
+      const int at = __shfl_sync(0xffffffffu, place, of);
+      uint8_t* dst = ring + (uint32_t)s * C::kStageBytes;
+      uint64_t* bar = &full[warp][s];
+      if (side_by_side >> of & 1u) {
+        absent &= ~(((1u << kBlocks) - 1u) << (s * kBlocks));
+        if (elect_one()) {
+          mbar_arrive_expect_tx(bar, C::kStageBytes);
+          if constexpr (kInt4) {               // K's blocks, then V's
+            bulk_load(dst, c.K + (long long)at * C::kBlockBytes, kBlocks * C::kBlockBytes, bar);
+            bulk_load(dst + kBlocks * C::kBlockBytes, c.V + (long long)at * C::kBlockBytes, kBlocks * C::kBlockBytes, bar);
           } else {
 #pragma unroll
-            for (int k = 0; k < kBlocks; ++k) {
-              if (at[k] < 0) continue;
-              bulk_load(dst + k * C::kBlockBytes, c.K + (long long)at[k] * C::kBlockBytes, C::kBlockBytes, bar);
-              bulk_load(dst + (kBlocks + k) * C::kBlockBytes, c.V + (long long)at[k] * C::kBlockBytes, C::kBlockBytes, bar);
-            }
+            for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+              for (int x = 0; x < kD / 64; ++x) {
+                tma_load_2d(dst + k * C::kBlockBytes + x * 2048, &tmK, bar, x * 64, (at + k) * kBlockRows);
+                tma_load_2d(dst + (kBlocks + k) * C::kBlockBytes + x * 2048, &tmV, bar, x * 64, (at + k) * kBlockRows);
+              }
           }
-        } else {
+        }
+      } else {                                 // two pages, or less than a whole tile
+        int one[kBlocks], there = 0;
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k) {
+          one[k] = __shfl_sync(0xffffffffu, place, of + k);
+          there += one[k] >= 0;
+          const unsigned int bit = 1u << (s * kBlocks + k);
+          absent = one[k] >= 0 ? absent & ~bit : absent | bit;
+        }
+        if (elect_one()) {
+          mbar_arrive_expect_tx(bar, (uint32_t)there * 2 * C::kBlockBytes);
 #pragma unroll
           for (int k = 0; k < kBlocks; ++k) {
-            if (at[k] < 0) continue;
+            if (one[k] < 0) continue;
+            if constexpr (kInt4) {
+              bulk_load(dst + k * C::kBlockBytes, c.K + (long long)one[k] * C::kBlockBytes, C::kBlockBytes, bar);
+              bulk_load(dst + (kBlocks + k) * C::kBlockBytes, c.V + (long long)one[k] * C::kBlockBytes, C::kBlockBytes, bar);
+            } else {
 #pragma unroll
-            for (int x = 0; x < kD / 64; ++x) {
-              tma_load_2d(dst + k * C::kBlockBytes + x * 2048, &tmK, bar, x * 64, at[k] * kBlockRows);
-              tma_load_2d(dst + (kBlocks + k) * C::kBlockBytes + x * 2048, &tmV, bar, x * 64, at[k] * kBlockRows);
+              for (int x = 0; x < kD / 64; ++x) {
+                tma_load_2d(dst + k * C::kBlockBytes + x * 2048, &tmK, bar, x * 64, one[k] * kBlockRows);
+                tma_load_2d(dst + (kBlocks + k) * C::kBlockBytes + x * 2048, &tmV, bar, x * 64, one[k] * kBlockRows);
+              }
             }
           }
         }
@@ -692,8 +707,10 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             }
             const uint32_t y0 = __byte_perm(w[0][x >> 1], w[1][x >> 1], x & 1 ? 0x7632 : 0x5410);
             const uint32_t y1 = __byte_perm(w[2][x >> 1], w[3][x >> 1], x & 1 ? 0x7632 : 0x5410);
-            const uint32_t va[4] = {code_pair<0>(y0), code_pair<1>(y0), code_pair<0>(y1), code_pair<1>(y1)};
-            const uint32_t vb[4] = {code_pair<2>(y0), code_pair<3>(y0), code_pair<2>(y1), code_pair<3>(y1)};
+            // rows r: the dim of the lower code of a byte; rows r + 8: the whole byte, from which the merge takes the upper one's
+            const uint32_t w0 = y0 & 0x00FF00FFu, w1 = y1 & 0x00FF00FFu, z0 = __byte_perm(y0, 0u, 0x4341), z1 = __byte_perm(y1, 0u, 0x4341);
+            const uint32_t va[4] = {w0 & 0x000F000Fu, w0, w1 & 0x000F000Fu, w1};
+            const uint32_t vb[4] = {z0 & 0x000F000Fu, z0, z1 & 0x000F000Fu, z1};
 #pragma unroll
             for (int t = 0; t < kNT; ++t) {
               mma16816_f16(o[2 * x][t], va, pb[t][0], pb[t][1]);
@@ -728,7 +745,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     };
 
     for (int i = 0; i < mine; ++i) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit));
+      ok = __all_sync(0xffffffffu, mbar_try_wait(&full[warp][slot], parity));
+      if (!ok) ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit));
       if (!ok) {
         if (lane == 0)   // nothing may still be on its way into shared memory when the CTA returns
           for (int j = 0; j < stages && i + j < mine; ++j) {
@@ -777,7 +795,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
               const float *u = &o[2 * x][t][e], *v = &o[2 * x + 1][t][e], add = lo[x / kPerGroup][t][e];
-              *w_o(warp, row + e, 8 * x + r) = make_float4(fmaf(u[0], 0x1p24f, add), fmaf(u[2], 0x1p20f, add), fmaf(v[0], 0x1p24f, add), fmaf(v[2], 0x1p20f, add));
+              *w_o(warp, row + e, 8 * x + r) = make_float4(fmaf(u[0], 0x1p24f, add), fmaf(u[2] - u[0], 0x1p20f, add), fmaf(v[0], 0x1p24f, add), fmaf(v[2] - v[0], 0x1p20f, add));
             }
           }
         } else {
