@@ -183,11 +183,12 @@ def make_rotation(cos, sin, rotary_dim, interleaved=False) -> Rotation:
 
 def make_rows(t) -> Rows:
     """A tensor [batch, heads, n_tokens, head_dim] of any strides with a contiguous last dimension, as restkv_rows."""
-    if t.dim() != 4 or (t.stride(3) != 1 and t.shape[3] != 1):
+    s = t.stride()
+    if len(s) != 4 or (s[3] != 1 and t.shape[3] != 1):
         raise ValueError("rows have to be [batch, heads, n_tokens, head_dim] with a contiguous last dimension")
-    if not any(t.stride()[:3]):   # the C ABI reads three zeros as "contiguous"
+    if not (s[0] or s[1] or s[2]):   # the C ABI reads three zeros as "contiguous"
         raise ValueError("rows that are all one row in memory have to be materialised")
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    return Rows(t.data_ptr(), s[0], s[1], s[2])
 
 
 def _ptr(t) -> Optional[int]:

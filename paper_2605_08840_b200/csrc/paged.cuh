@@ -94,6 +94,13 @@ template <> struct Pack8<__nv_bfloat16> {
   uint4 u;
   __device__ void load(const __nv_bfloat16* p) { u = *reinterpret_cast<const uint4*>(p); }
   __device__ void zero() { u = make_uint4(0u, 0u, 0u, 0u); }
+  __device__ void put(__nv_bfloat16* p) const { *reinterpret_cast<uint4*>(p) = u; }
+  __device__ void exchange(int lane, float* x) const {   // another lane's, by the whole warp
+    Pack8 o;
+    o.u = make_uint4(__shfl_sync(0xffffffffu, u.x, lane), __shfl_sync(0xffffffffu, u.y, lane), __shfl_sync(0xffffffffu, u.z, lane),
+                     __shfl_sync(0xffffffffu, u.w, lane));
+    o.get(x);
+  }
   __device__ void get(float* x) const {
     const unsigned int w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
@@ -117,6 +124,13 @@ template <> struct Pack8<float> {
   float4 a, b;
   __device__ void load(const float* p) { a = reinterpret_cast<const float4*>(p)[0]; b = reinterpret_cast<const float4*>(p)[1]; }
   __device__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ void put(float* p) const { reinterpret_cast<float4*>(p)[0] = a; reinterpret_cast<float4*>(p)[1] = b; }
+  __device__ void exchange(int lane, float* x) const {
+    float y[8];
+    get(y);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = __shfl_sync(0xffffffffu, y[e], lane);
+  }
   __device__ void get(float* x) const {
     x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
   }

@@ -110,10 +110,6 @@ __device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w <<
 __device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 constexpr int kMaxCtas = 512;
-#ifndef KCR
-#define KCR 4096
-#endif
-constexpr int kClusterRows = KCR;
 
 struct PagedMmaArgs {
   PagedCache c;
@@ -725,12 +721,17 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             keep0 = (left > 0 ? 0xFFFFu : 0u) | (left > 1 ? 0xFFFF0000u : 0u);
             keep1 = (left > 8 ? 0xFFFFu : 0u) | (left > 9 ? 0xFFFF0000u : 0u);
           }
-          uint32_t pb[kNT][2];
+          // the weights as two bf16 parts: the tensor pipe has room for the second product beside HBM, and the outputs keep 16 bits
+          uint32_t pb[kNT][4];
 #pragma unroll
-          for (int t = 0; t < kNT; ++t) {
-            pb[t][0] = transpose8x8(pack_bf16x2(sc[k][t][0], sc[k][t][1]));
-            pb[t][1] = transpose8x8(pack_bf16x2(sc[k][t][2], sc[k][t][3]));
-          }
+          for (int t = 0; t < kNT; ++t)
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+              const float p0 = sc[k][t][2 * x], p1 = sc[k][t][2 * x + 1];
+              const uint32_t hi = pack_bf16x2(p0, p1);
+              pb[t][x] = transpose8x8(hi);
+              pb[t][2 + x] = transpose8x8(pack_bf16x2(p0 - lower(hi), p1 - upper(hi)));
+            }
           const int mat = lane >> 3, mr = lane & 7;
 #pragma unroll
           for (int x = 0; x < kD / 16; ++x) {
@@ -738,7 +739,10 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             ldsm4_t(vt + (uint32_t)(x >> 2) * 2048u + (uint32_t)((mat >> 1) * 8 + mr) * 128u + (((uint32_t)((x & 3) * 2 + (mat & 1)) ^ (uint32_t)mr) << 4), va);
             if constexpr (kEdge) { va[0] &= keep0; va[1] &= keep0; va[2] &= keep1; va[3] &= keep1; }
 #pragma unroll
-            for (int t = 0; t < kNT; ++t) mma16816(o[x][t], va, pb[t][0], pb[t][1]);
+            for (int t = 0; t < kNT; ++t) {
+              mma16816(o[x][t], va, pb[t][0], pb[t][1]);
+              mma16816(o[x][t], va, pb[t][2], pb[t][3]);
+            }
           }
         }
       }
@@ -1000,12 +1004,23 @@ bool pick(const PagedCache& c, Variant* v) {
   return (long long)c.n_tokens * c.G <= 8 ? pick_nt<1>(c, v) : pick_nt<2>(c, v);
 }
 
-// CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units.
+// CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units.  The largest cluster that lets all units run
+// at once; then by the time that each way takes at the longest sequences the table can name, in us: fixed 6 and 12 (the second has
+// another kernel behind it), and the bytes at what its CTAs draw.  A cluster lasts as long as its own sequence, so that sequences of
+// different lengths speak for dealing out: a batch is taken to fill 0.8 of its table.  Measured, 8 KV heads of 4 query heads, clusters
+// against dealt out: 4 bits 2176 rows 7.9 / 13.3, 16384 rows 14.1 / 15.1, 32768 rows 22.2 / 20.1, 8 x 2176 rows 11.4 / 18.9, 8 x 16384
+// 38.6 / 44.6; bf16 2176 rows 7.4 / 12.4, 32768 rows 30.8 / 34.0, 131072 rows 103.5 / 92.0, 8 x 2176 rows 16.6 / 25.9.
 int paged_mma_cluster(const PagedCache& c, const Variant& v, long long units, const int* clusters_of) {
   int i = 4;
   while (i >= 0 && units > clusters_of[i]) --i;
   if (i < 1) return 0;
-  return c.capacity() <= kClusterRows ? 1 << i : 0;
+  const bool int4 = c.format == RESTKV_PAGES_INT4;
+  const double mb = 2e-6 * (double)units * ((double)c.capacity() / kBlockRows) * c.block_bytes;
+  // TB/s; clusters of 16 CTAs of which two share an SM end up on half of the SMs
+  const double together = v.per_sm == 2 ? (i == 4 ? 2.5 : 0.02 * (double)(units << i)) : 0.085 * (double)(units << i);
+  const double fill = c.batch == 1 && !c.per_head ? 1.0 : 0.8;
+  const double in_clusters = 6.0 + mb / fmin(together, 5.5), dealt = 12.0 + fill * mb / (int4 ? 5.5 : 6.1);
+  return in_clusters < dealt ? 1 << i : 0;
 }
 
 }  // namespace
