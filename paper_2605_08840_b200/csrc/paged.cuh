@@ -81,11 +81,6 @@ __device__ __forceinline__ float bf16_above(float x) {   // x >= 0
 __device__ __forceinline__ float int4_input(float x) {   // NaN -> 0; 2^120 keeps the span of a group finite
   return x == x ? fminf(fmaxf(x, -0x1p120f), 0x1p120f) : 0.f;
 }
-// The nearest code.  The quotient is IEEE's, so that values half-way between two codes (common where the inputs are bf16) go to the even one.
-__device__ __forceinline__ unsigned int int4_code(float x, float lo, float step) {
-  const float q = step > 0.f ? rintf(__fdiv_rn(x - lo, step)) : 0.f;
-  return (unsigned int)fminf(q, 15.f);
-}
 // Byte of a block where row r has the step of group g; its offset lies 8 bytes on.
 __device__ __forceinline__ int int4_params(int d, int g, int r) { return 8 * d + 64 * g + 16 * (r & 3) + 2 * (r >> 2); }
 
@@ -144,7 +139,8 @@ template <> struct Pack8<float> {
 cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K_new, const RowsView& V_new, uint8_t* K_pages,
                                 uint8_t* V_pages, const int* positions, const RotationView& rotation, const RowsView& Q, void* Q_out,
                                 int sm_count, cudaStream_t st);
-cudaError_t launch_paged_read(const PagedCache& c, bool f32, const int* first, int n_rows, void* K_out, void* V_out, cudaStream_t st);
+cudaError_t launch_paged_read(const PagedCache& c, bool f32, const int* first, int n_rows, void* K_out, void* V_out, int sm_count,
+                              cudaStream_t st);
 // fp32 SIMT attention: every dtype, format and head_dim.
 int paged_simt_splits(const PagedCache& c, int sm_count);
 size_t paged_simt_bytes(const PagedCache& c, int splits);

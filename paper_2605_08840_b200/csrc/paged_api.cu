@@ -174,7 +174,7 @@ restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, con
   c.K = (const uint8_t*)K_pages; c.V = (const uint8_t*)V_pages;
   Call call{h, (cudaStream_t)stream};
   RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
-                launch_paged_read(c, cache->dtype == RESTKV_F32, first, n_rows, K_out, V_out, call.st), 1);
+                launch_paged_read(c, cache->dtype == RESTKV_F32, first, n_rows, K_out, V_out, h->sm_count, call.st), 1);
   return RESTKV_OK;
 }
 
