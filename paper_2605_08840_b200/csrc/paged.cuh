@@ -152,5 +152,12 @@ bool paged_mma_supported(const PagedCache& c);
 size_t paged_mma_bytes(const PagedCache& c, int sm_count);
 cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count,
                              const int (*clusters_of)[5], long long wait_limit, cudaStream_t st, int* launches);
+// bf16 with head_dim 64 or 128 and at least kChunkRows query rows per KV head on tcgen05, 256 rows per pass.
+constexpr int kChunkRows = 64;
+cudaError_t paged_chunk_init();
+bool paged_chunk_supported(const PagedCache& c);
+size_t paged_chunk_bytes(const PagedCache& c, int sm_count);
+cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count, long long wait_limit,
+                               cudaStream_t st);
 
 }  // namespace restkv

@@ -57,10 +57,13 @@ static restkv_status check_tokens(const PagedCache& c, int n_tokens) {
 // The kernels that a call runs on: the tensor pipe for bf16 with the head_dims it has (kernel path 1 keeps off it), else fp32.
 static bool on_tensor_pipe(const PagedCache& c, bool f32) { return !f32 && paged_mma_supported(c); }
 
+static bool in_chunks(const PagedCache& c, bool f32) { return !f32 && paged_chunk_supported(c); }
+
 static size_t attend_bytes(const PagedCache& c, bool f32, int sm_count) {
   const size_t simt = paged_simt_bytes(c, paged_simt_splits(c, sm_count));   // what every call can run on
   const size_t mma = on_tensor_pipe(c, f32) ? paged_mma_bytes(c, sm_count) : 0;
-  return align256(simt > mma ? simt : mma);
+  const size_t chunk = in_chunks(c, f32) ? paged_chunk_bytes(c, sm_count) : 0;
+  return align256(simt > mma ? (simt > chunk ? simt : chunk) : (mma > chunk ? mma : chunk));
 }
 
 static restkv_status make_rows(const restkv_rows* s, int heads, int n, int d, RowsView* out) {
@@ -150,6 +153,11 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
   Call call{h, (cudaStream_t)stream};
   const bool f32 = cache->dtype == RESTKV_F32;
   if (workspace_bytes < attend_bytes(c, f32, h->sm_count)) return RESTKV_ERR_WORKSPACE;
+  if (in_chunks(c, f32) && h->tc_state && h->kernel_path != 1) {
+    RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
+                  launch_paged_chunk(c, q, out, lse, (float*)workspace, h->sm_count, h->wait_limit, call.st), 2);
+    return RESTKV_OK;
+  }
   if (on_tensor_pipe(c, f32) && h->tc_state && h->kernel_path != 1) {
     int launches = 0;
     RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,

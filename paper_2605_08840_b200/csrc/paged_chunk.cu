@@ -1,0 +1,710 @@
+// Attention of many query tokens over the paged cache (a chunk of prompt): bf16 in and out, pages of bf16 or of 4-bit codes, head_dim 64
+// or 128, on tcgen05.
+//
+// What bounds it: 4 * 128 * 128 * head_dim operations per 128 query rows and 128 cache rows on the tensor pipe, 1024 of its cycles at
+// head_dim 128, beside as many cycles of the special-function unit for the exponentials and the work of turning codes into operands.  So
+//   - a CTA per SM takes 256 query rows (tokens x query heads of a KV head) in two tiles of 128, each with a warpgroup of its own, a
+//     thread per row: while one tile's softmax runs, the other tile's products do, and a tile of K and V serves both;
+//   - S (fp32) and O of both tiles fill the tensor memory's 512 columns at head_dim 128; P (16 bits) takes S's place and is the A operand
+//     of P V there;
+//   - four warps fetch K and V, a row per thread: bf16 by cp.async; codes become f16 operands with one fused operation per pair, the
+//     nibble as it stands being the f16 subnormal 2^-24 code (2^-20 for the upper one of a byte).
+//     K: step * (code - 8), times 2^(a - 24) for a tile's exponent a that just lets its largest step fit f16: at most 11 bits, exact. The
+//     rest, (offset + 8 step) * sum(q) per group, is three more products of f16 parts (22 bits together), another 16 dims for all groups.
+//     V: offset + step * code, rounded once to f16; its tiles' exponents go into the weights'.
+//     (K rounded like V: 10% less of the tensor pipe, but logits lose 2^-12 of their terms.  In both, steps below 2^-8 of the largest of
+//     their 128 rows lose bits.)
+//   - dims within K's operand chunks are in the order in which they come out of a word, and Q's in the same; V's order is undone where O
+//     is written.
+//   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand
+//     (relative error 9.3e-8, minimax), else 1 - 2 / (1 + e^2y) with two trips to the special-function unit.
+// The tiles of all units are dealt out end to end as in the kernel for few tokens; what several CTAs share is merged by a second kernel.
+#include <math.h>
+
+#include <cuda_fp16.h>
+
+#include "paged_deal.cuh"
+
+namespace restkv {
+
+namespace {
+
+constexpr int kChRows = 256;                 // query rows of a unit
+constexpr int kChTile = 128;                 // cache rows of a tile
+constexpr int kSoftmaxWarps = 8, kFetchWarps = 4;
+constexpr int kChThreads = (kSoftmaxWarps + kFetchWarps + 1) * 32;
+constexpr int kFetch = kFetchWarps * 32;
+constexpr int kInfo = 4;                     // tiles whose factors are kept: the fetching warps are two ahead of the softmax at most
+// log2 of the largest weight that a rescaling leaves, and of what it may grow to before the next one
+constexpr float kChStart = 5.f, kChSlack = 13.f;
+
+struct ChunkBarriers {
+  uint64_t q_full[2], s_full[2], p_full[2], pv_done[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+};
+
+// Row `row`, 16-byte chunk `chunk` of a 16-bit operand tile of 128 rows: boxes of [128 rows x 64 elements], 128-byte swizzle.
+__device__ __forceinline__ uint32_t operand_at(uint32_t tile, int row, int chunk) {
+  return tile + (uint32_t)(chunk >> 3) * 16384u + (uint32_t)row * 128u + (uint32_t)(((chunk & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+__device__ __forceinline__ uint32_t hfma2(uint32_t a, uint32_t b, uint32_t c) {
+  uint32_t d;
+  asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(d) : "r"(a), "r"(b), "r"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + (e < -126 ? -126 : e > 127 ? 127 : e)) << 23); }
+__device__ __forceinline__ void fetch_sync() { asm volatile("bar.sync 1, %0;" ::"n"(kFetch) : "memory"); }
+
+// 8 codes of a word as operands: s * 2^-24 code + l, where s16 = s / 16, for the codes in the lower and in the upper half of the word.
+__device__ __forceinline__ void operands_of(uint32_t w, uint32_t s, uint32_t s16, uint32_t l, uint32_t to) {
+  const uint32_t w8 = w >> 8;
+  sts128(to, hfma2(s, w & 0x000F000Fu, l), hfma2(s16, w & 0x00F000F0u, l), hfma2(s, w8 & 0x000F000Fu, l), hfma2(s16, w8 & 0x00F000F0u, l));
+}
+
+// cap * tanh(t / cap) in log2 units, less `m`: t = argument of the tanh, c = cap * log2(e).
+__device__ __forceinline__ f32x2 capped_poly(f32x2 t, f32x2 c, f32x2 minus_m) {
+  const f32x2 z = f2_mul(t, t);
+  f32x2 p = f2_make(0.0154755134f, 0.0154755134f);
+  p = f2_fma(p, z, f2_make(-0.0521015525f, -0.0521015525f));
+  p = f2_fma(p, z, f2_make(0.133101761f, 0.133101761f));
+  p = f2_fma(p, z, f2_make(-0.333323091f, -0.333323091f));
+  p = f2_fma(p, z, f2_make(0.99999994f, 0.99999994f));
+  return f2_fma(f2_mul(p, t), c, minus_m);
+}
+__device__ __forceinline__ float capped(float t, float c) { return fmaf(-2.f * c, rcp_approx(1.f + ex2_approx(t * 2.f * kLog2e)), c); }
+
+// Row `row` of an operand 16 elements deep, without swizzle: 8 rows of 16 bytes together, both halves of a row 128 bytes apart.
+constexpr uint32_t kThinBytes = 128 * 32;
+__device__ __forceinline__ uint32_t thin_at(uint32_t tile, int row) { return tile + (uint32_t)(row >> 3) * 256u + (uint32_t)(row & 7) * 16u; }
+// x as the sum of two f16: in the lower and in the upper half.
+__device__ __forceinline__ uint32_t split_f16(float x) {
+  const __half hi = __float2half_rn(x);
+  return pack_f16x2(__half2float(hi), x - __half2float(hi));
+}
+
+template <int kD, int kGroups> struct ChunkConfig {
+  static constexpr bool kInt4 = kGroups > 0;
+  static constexpr uint32_t kTileBytesD = 128u * kD * 2u;
+  static constexpr size_t kSmem = 6 * (size_t)kTileBytesD + (kInt4 ? 4 * kThinBytes : 0) + 1024;   // two tiles of Q, two of K, two of V
+};
+
+template <int kD, int kGroups>
+__global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid_constant__ PagedMmaArgs a) {
+  using C = ChunkConfig<kD, kGroups>;
+  constexpr bool kInt4 = C::kInt4;
+  constexpr int kWords = kD / 32, kG = kInt4 ? kGroups : 1, kPerGroup = kWords / kG;
+  const PagedCache& c = a.c;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) ChunkBarriers B;
+  __shared__ Piece piece_s;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag;
+  __shared__ float step_max[2][2][kFetchWarps];         // [tile & 1][K, V][warp]
+  __shared__ volatile float k_factor[kInfo], v_shift[kInfo];   // per tile: the logits' factor, log2 of the weights'
+  __shared__ volatile float o_factor[2];                // per piece: what O is multiplied with
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base, k_at = base + 2 * C::kTileBytesD, v_at = base + 4 * C::kTileBytesD;
+  const uint32_t q_thin = base + 6 * C::kTileBytesD, k_thin = q_thin + 2 * kThinBytes;
+  auto wait = [&](uint64_t* bar, int phase) { return mbar_wait(bar, (uint32_t)phase & 1u, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit); };
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&B.q_full[i], 128);
+      mbar_init(&B.s_full[i], 1);
+      mbar_init(&B.p_full[i], 128);
+      mbar_init(&B.pv_done[i], 1);
+      mbar_init(&B.k_full[i], kFetch);
+      mbar_init(&B.k_empty[i], 1);
+      mbar_init(&B.v_full[i], kFetch);
+      mbar_init(&B.v_empty[i], 1);
+    }
+    mbar_init(&B.drained, 1);
+    fence_mbar_init();
+  }
+  if (warp == kSoftmaxWarps + kFetchWarps) {
+    tmem_alloc(&tmem_slot, 512);
+    tmem_relinquish();
+  }
+  grid_dependency_wait();
+  grid_dependency_launch();
+  if (warp == 0) {
+    const Run run = find_run(c, a.row_tiles, kChTile, blockIdx.x, gridDim.x);
+    if (lane == 0) {
+      piece_s.run = run;
+      if (run.tile < run.end) piece_s.cut(c, a.row_tiles, kChTile);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  constexpr uint32_t kO = 256;                          // O of tile w: columns kO + w * kD; S and P: w * 128
+  const volatile Piece& piece = piece_s;
+
+  int done = 0;                                         // tiles of the pieces before: phases of the rings
+  for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
+    const int unit = piece.unit, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kChRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
+    const int R = c.n_tokens * c.G, n = paged_length(c, b, h), count = paged_count(c, b), t0 = piece.t0;
+    // rows that the unit's last query row sees; tiles past them are nobody's business (a unit whose rows see nothing takes one all the same)
+    const int i_last = min(min(R, rho0 + kChRows) - 1, count * c.G - 1) / c.G;
+    const int seen = count > 0 && rho0 < count * c.G ? n - (count - 1 - i_last) : 0;
+    const int t_seen = seen > 0 ? (seen + kChTile - 1) / kChTile : 0;
+    const int tiles = max(0, min(piece.t1, t_seen) - t0);
+    if (threadIdx.x == 0 && t0 == 0) check_length(c, b, h);
+
+    if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kFetchWarps) {
+      // ---------------- fetching K and V: a row per thread ----------------
+      const int r = threadIdx.x - kSoftmaxWarps * 32;
+      const int per_page = c.page_rows / kBlockRows;
+      auto page_of = [&](int j) {                       // of the thread's row of tile j; -1: nothing there
+        const int row = (t0 + j) * kChTile + r;
+        return j < tiles && row < n ? c.table[(long long)b * c.table_width + row / c.page_rows] : -1;
+      };
+      auto place_of = [&](int j, int page) {            // block of the pool, -1
+        const int row = (t0 + j) * kChTile + r;
+        if (j >= tiles || row >= n) return -1;
+        if ((unsigned int)page >= (unsigned int)c.n_pages) {
+          atomicOr(c.dev_status, kDevBadIndex);
+          return -1;
+        }
+        return (page * c.Hkv + h) * per_page + row % c.page_rows / kBlockRows;
+      };
+      bool ok = true;
+      if constexpr (kInt4) {
+        uint32_t kw[4 * kWords], vw[4 * kWords], kp[kG], vp[kG];   // a row's codes; (step, offset) per group
+        auto load = [&](int place) {
+          const bool there = place >= 0;
+          const uint8_t* kb = c.K + (long long)(there ? place : 0) * c.block_bytes;
+          const uint8_t* vb = c.V + (long long)(there ? place : 0) * c.block_bytes;
+          const int q = r & 15;
+#pragma unroll
+          for (int x = 0; x < kWords; ++x) {
+            const uint4 u = there ? reinterpret_cast<const uint4*>(kb + q * (kD / 2))[x] : make_uint4(0u, 0u, 0u, 0u);
+            const uint4 v = there ? reinterpret_cast<const uint4*>(vb + q * (kD / 2))[x] : make_uint4(0u, 0u, 0u, 0u);
+            kw[4 * x] = u.x; kw[4 * x + 1] = u.y; kw[4 * x + 2] = u.z; kw[4 * x + 3] = u.w;
+            vw[4 * x] = v.x; vw[4 * x + 1] = v.y; vw[4 * x + 2] = v.z; vw[4 * x + 3] = v.w;
+          }
+#pragma unroll
+          for (int g = 0; g < kG; ++g) {
+            const unsigned short* k16 = reinterpret_cast<const unsigned short*>(kb + int4_params(kD, g, q));
+            const unsigned short* v16 = reinterpret_cast<const unsigned short*>(vb + int4_params(kD, g, q));
+            kp[g] = there ? k16[0] | (uint32_t)k16[4] << 16 : 0u;
+            vp[g] = there ? v16[0] | (uint32_t)v16[4] << 16 : 0u;
+          }
+        };
+        int page = page_of(0), a_ref = 0;
+        load(place_of(0, page));
+        page = page_of(1);
+        for (int j = 0; j < tiles; ++j) {               // to the end even when a wait ran out: all four warps meet in every round
+          const int at = done + j, s = at & 1;
+          // the tile's exponents: its largest step just below 2^15, its largest offset well within f16
+          float km = 0.f, vm = 0.f;
+#pragma unroll
+          for (int g = 0; g < kG; ++g) {
+            km = fmaxf(km, fmaxf(lower(kp[g]), fabsf(upper(kp[g])) * 0x1p-16f));
+            vm = fmaxf(vm, fmaxf(lower(vp[g]), fabsf(upper(vp[g])) * 0x1p-25f));
+          }
+          const float kx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(km))), vx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vm)));
+          if (lane == 0) {
+            step_max[s][0][warp - kSoftmaxWarps] = kx;
+            step_max[s][1][warp - kSoftmaxWarps] = vx;
+          }
+          fetch_sync();
+          float kt = 0x1p-40f, vt = 0x1p-40f;
+#pragma unroll
+          for (int x = 0; x < kFetchWarps; ++x) { kt = fmaxf(kt, step_max[s][0][x]); vt = fmaxf(vt, step_max[s][1][x]); }
+          const int ka = 141 - (int)(__float_as_uint(kt) >> 23), va = 141 - (int)(__float_as_uint(vt) >> 23);
+          if (j == 0) a_ref = va;
+          if (r == 0) {
+            k_factor[at % kInfo] = power_of_two(24 - ka);
+            v_shift[at % kInfo] = (float)(a_ref - va);
+            if (j == 0) o_factor[nth & 1] = power_of_two(24 - a_ref);
+          }
+          ok = ok && (at < 2 || wait(&B.k_empty[s], (at >> 1) - 1));
+          if (ok) {
+            uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};   // dims 3 g ..: the parts that meet sum(q)'s
+#pragma unroll
+            for (int g = 0; g < kG; ++g) {
+              const float step = lower(kp[g]) * power_of_two(ka);
+              const uint32_t s1 = pack_f16x2(step, step), s16 = pack_f16x2(step * 0.0625f, step * 0.0625f), l = pack_f16x2(step * -0x1p-21f, step * -0x1p-21f);
+#pragma unroll
+              for (int m = g * kPerGroup; m < (g + 1) * kPerGroup; ++m)
+#pragma unroll
+                for (int q = 0; q < 4; ++q)             // word q * kWords + m: dims 32 m + 8 q ..
+                  operands_of(kw[q * kWords + m], s1, s16, l, operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, 4 * m + q));
+              // hi, lo, hi against sum(q)'s hi, hi, lo; times 2^8, as sum(q)'s are times 2^-8
+              const uint32_t mid = split_f16(fmaf(8.f, lower(kp[g]), upper(kp[g])) * power_of_two(ka - 16));
+#pragma unroll
+              for (int x = 0; x < 3; ++x) {
+                const uint32_t part = x == 1 ? mid >> 16 : mid & 0xFFFFu;
+                thin[(3 * g + x) >> 1] |= (3 * g + x) & 1 ? part << 16 : part;
+              }
+            }
+            const uint32_t to = thin_at(k_thin + (uint32_t)s * kThinBytes, r);
+            sts128(to, thin[0], thin[1], thin[2], thin[3]);
+            sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+            fence_proxy_async_smem();
+          }
+          mbar_arrive(&B.k_full[s]);
+          ok = ok && (at < 2 || wait(&B.v_empty[s], (at >> 1) - 1));
+          if (ok) {
+            uint32_t s1[kG], s16[kG], l[kG];
+#pragma unroll
+            for (int g = 0; g < kG; ++g) {
+              const float step = lower(vp[g]) * power_of_two(va), lo = upper(vp[g]) * power_of_two(va - 24);
+              s1[g] = pack_f16x2(step, step);
+              s16[g] = pack_f16x2(step * 0.0625f, step * 0.0625f);
+              l[g] = pack_f16x2(lo, lo);
+            }
+#pragma unroll
+            for (int x = 0; x < 4 * kWords; ++x) {      // word x: dims 32 m + 4 r' + (0..3) in its lower half, 32 (m + 1) + .. in its upper
+              const int g = 2 * (x % (kWords / 2)) / kPerGroup, g1 = (2 * (x % (kWords / 2)) + 1) / kPerGroup;
+              const uint32_t u = g == g1 ? s1[g] : __byte_perm(s1[g], s1[g1], 0x5410), u16 = g == g1 ? s16[g] : __byte_perm(s16[g], s16[g1], 0x5410);
+              operands_of(vw[x], u, u16, g == g1 ? l[g] : __byte_perm(l[g], l[g1], 0x5410), operand_at(v_at + (uint32_t)s * C::kTileBytesD, r, x));
+            }
+            fence_proxy_async_smem();
+          }
+          // the next tile's codes come while the products run
+          load(place_of(j + 1, page));
+          page = page_of(j + 2);
+          mbar_arrive(&B.v_full[s]);
+        }
+      } else {
+        auto fetch = [&](int j, int place) {            // K and V of tile j, a group of copies each
+          const int at = done + j, s = at & 1;
+          const bool there = place >= 0;
+          const long long from = (long long)(there ? place : 0) * c.block_bytes + (r & 15) * (2 * kD);
+          if (at >= 2 && !wait(&B.k_empty[s], (at >> 1) - 1)) return false;
+#pragma unroll
+          for (int x = 0; x < kD / 8; ++x) copy16(operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, x), c.K + from + 16 * x, there);
+          if (at >= 2 && !wait(&B.v_empty[s], (at >> 1) - 1)) return false;
+#pragma unroll
+          for (int x = 0; x < kD / 8; ++x) copy16(operand_at(v_at + (uint32_t)s * C::kTileBytesD, r, x), c.V + from + 16 * x, there);
+          copy16_commit();
+          return true;
+        };
+        int page = page_of(0);
+        if (r == 0) o_factor[nth & 1] = 1.f;
+        if (tiles > 0) ok = fetch(0, place_of(0, page));
+        page = page_of(1);
+        for (int j = 0; j < tiles; ++j) {
+          const int at = done + j, s = at & 1;
+          if (r == 0) { k_factor[at % kInfo] = 1.f; v_shift[at % kInfo] = 0.f; }
+          copy16_wait<0>();
+          fence_proxy_async_smem();
+          mbar_arrive(&B.k_full[s]);
+          mbar_arrive(&B.v_full[s]);
+          // (the slots of the next tile come free only once this one is known to be there)
+          ok = ok && (j + 1 >= tiles || fetch(j + 1, place_of(j + 1, page)));
+          if (!ok) break;
+          page = page_of(j + 2);
+        }
+        copy16_wait<0>();
+      }
+    } else if (warp == kSoftmaxWarps + kFetchWarps) {
+      // ---------------- the products, by one thread ----------------
+      if (elect_one() && tiles > 0) {
+        constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
+        constexpr uint32_t idesc_o = kInt4 ? make_idesc_f16(128, kD, true) : make_idesc_bf16(128, kD, true);
+        auto qk = [&](int w, int s) {
+          const uint64_t a0 = kmajor_desc(q_at + (uint32_t)w * C::kTileBytesD), b0 = kmajor_desc(k_at + (uint32_t)s * C::kTileBytesD);
+#pragma unroll
+          for (int k = 0; k < kD / 16; ++k) {
+            const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
+            umma_ss(tmem + (uint32_t)w * 128u, a0 + step, b0 + step, idesc_s, k > 0);
+          }
+          if constexpr (kInt4)
+            umma_ss(tmem + (uint32_t)w * 128u, make_smem_desc_plain(q_thin + (uint32_t)w * kThinBytes, 128u, 256u),
+                    make_smem_desc_plain(k_thin + (uint32_t)s * kThinBytes, 128u, 256u), idesc_s, true);
+          umma_commit(&B.s_full[w]);
+        };
+        bool ok = true;
+        for (int w = 0; w < 2 && ok; ++w) {
+          ok = wait(&B.q_full[w], nth) && (w == 1 || wait(&B.k_full[done & 1], done >> 1));
+          if (!ok) break;
+          tc_fence_after();
+          qk(w, done & 1);
+        }
+        if (ok) umma_commit(&B.k_empty[done & 1]);
+        for (int j = 0; j < tiles && ok; ++j) {
+          const int at = done + j, s = at & 1;
+          for (int w = 0; w < 2; ++w) {
+            ok = wait(&B.p_full[w], at) && (w == 1 || wait(&B.v_full[s], at >> 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < 8; ++k)                 // 16 cache rows: 8 columns of P, 2048 bytes of V
+              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)w * 128u + (uint32_t)k * 8u,
+                      make_smem_desc(v_at + (uint32_t)s * C::kTileBytesD + (uint32_t)k * 2048u, 16384u, 1024u), idesc_o, j > 0 || k > 0);
+            umma_commit(&B.pv_done[w]);
+            if (w == 1) umma_commit(&B.v_empty[s]);
+            if (j + 1 < tiles) {
+              // S of the next tile takes the place of P, which the products just issued still read
+              ok = (w == 1 || wait(&B.k_full[(at + 1) & 1], (at + 1) >> 1)) && wait(&B.pv_done[w], at);
+              if (!ok) break;
+              tc_fence_after();
+              qk(w, (at + 1) & 1);
+              if (w == 1) umma_commit(&B.k_empty[(at + 1) & 1]);
+            }
+          }
+        }
+        if (!ok) {   // nothing may still write tensor memory, or arrive, when the CTA goes
+          umma_commit(&B.drained);
+          wait_issued(&B.drained, 0);
+        }
+      }
+    } else {
+      // ---------------- softmax: a query row per thread ----------------
+      const int w = warp >> 2, r = threadIdx.x & 127, rho = rho0 + w * 128 + r, i = rho / c.G, g = rho - i * c.G;
+      const bool live = rho < R && i < count;
+      const int sees = live ? n - (count - 1 - i) : n;
+      const uint32_t row_lane = (uint32_t)(warp & 3) << 21;          // lanes 32 (warp % 4) .. of tensor memory, in bits 16 up
+      const uint32_t s_tm = tmem + row_lane + (uint32_t)w * 128u, o_tm = tmem + row_lane + kO + (uint32_t)w * kD;
+      float unscale = 1.f;
+      if (tiles > 0) {
+        // the row into shared memory
+        const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
+        uint4 u[kD / 8];
+#pragma unroll
+        for (int x = 0; x < kD / 8; ++x) u[x] = live ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+        const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
+        if constexpr (kInt4) {
+          float top = 0.f;
+#pragma unroll
+          for (int x = 0; x < kD / 8; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) top = fmaxf(top, fmaxf(fabsf(lower((&u[x].x)[y])), fabsf(upper((&u[x].x)[y]))));
+          // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
+          int e = 141 - (int)(__float_as_uint(top) >> 23);
+          e = e < -100 ? -100 : e > 100 ? 100 : e;
+          const float scale = top < INFINITY ? power_of_two(e) : __uint_as_float(0x7FFFFFFFu);
+          unscale = power_of_two(-e);
+          uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int g2 = 0; g2 < kG; ++g2) {
+            float sum = 0.f;
+#pragma unroll
+            for (int x = g2 * (kD / 8 / kG); x < (g2 + 1) * (kD / 8 / kG); ++x) {
+              float v[8];
+#pragma unroll
+              for (int y = 0; y < 4; ++y) {
+                v[2 * y] = lower((&u[x].x)[y]) * scale;
+                v[2 * y + 1] = upper((&u[x].x)[y]) * scale;
+              }
+              // dims in the order of K's operands
+              sts128(operand_at(tile, r, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
+              sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+            const uint32_t parts = split_f16(sum * 0x1p-8f);
+#pragma unroll
+            for (int x = 0; x < 3; ++x) {
+              const uint32_t part = x == 2 ? parts >> 16 : parts & 0xFFFFu;
+              thin[(3 * g2 + x) >> 1] |= (3 * g2 + x) & 1 ? part << 16 : part;
+            }
+          }
+          const uint32_t to = thin_at(q_thin + (uint32_t)w * kThinBytes, r);
+          sts128(to, thin[0], thin[1], thin[2], thin[3]);
+          sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+        } else {
+#pragma unroll
+          for (int x = 0; x < kD / 8; ++x) sts128(operand_at(tile, r, x), u[x].x, u[x].y, u[x].z, u[x].w);
+        }
+        fence_proxy_async_smem();
+      }
+      mbar_arrive(&B.q_full[w]);
+      const bool cap = c.softcap > 0.f;
+      const float cap_log2 = c.softcap * kLog2e;
+      const float factor = (cap ? c.scale / c.softcap : c.scale * kLog2e) * unscale;   // to the tanh's argument, or to log2 units
+      float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
+      const int sees_all = __reduce_min_sync(0xffffffffu, sees);   // what every row of the warp sees
+      bool ok = true;
+      for (int j = 0; j < tiles; ++j) {
+        const int at = done + j;
+        // the waits' verdict is a warp's: tensor memory is read by whole warps
+        ok = __all_sync(0xffffffffu, wait(&B.s_full[w], at));
+        if (!ok) break;
+        tc_fence_after();
+        const float f = factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
+        const int left = sees - (t0 + j) * kChTile;     // columns that the row sees
+        const bool edge = sees_all < (t0 + j + 1) * kChTile;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float v[32];
+          tmem_ld32(s_tm + x * 32, v);
+          tmem_wait_ld();
+          if (edge) {
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (x * 32 + y >= left) v[y] = -INFINITY;
+          }
+          float m0 = v[0], m1 = v[1];
+#pragma unroll
+          for (int y = 2; y < 32; y += 4) {
+            m0 = fmax3(m0, v[y], v[y + 1]);
+            if (y + 2 < 32) m1 = fmax3(m1, v[y + 2], v[y + 3]);
+          }
+          mx = fmax3(mx, m0, m1);
+        }
+        mx *= f;                                        // (the factor is positive: the largest stays the largest)
+        if (cap && mx != -INFINITY) mx = capped(mx, cap_log2);
+        mx += shift;
+        float rescale = 1.f;
+        if (mx > ref + kChSlack) {                      // O is rescaled only when the weights would grow past 2^kChSlack
+          rescale = ex2_approx(ref - (mx - kChStart));  // ref = -inf gives 0
+          ref = mx - kChStart;
+          l *= rescale;
+        }
+        if (j > 0 && __any_sync(0xffffffffu, rescale != 1.f)) {   // (the products of the tile before have ended: S's came after them)
+#pragma unroll
+          for (int x = 0; x < kD / 32; ++x) {
+            float v[32];
+            tmem_ld32(o_tm + x * 32, v);
+            tmem_wait_ld();
+            uint32_t bits[32];
+#pragma unroll
+            for (int y = 0; y < 32; ++y) bits[y] = __float_as_uint(v[y] * rescale);
+            tmem_st16(o_tm + x * 32, bits);
+            tmem_st16(o_tm + x * 32 + 16, bits + 16);
+          }
+        }
+        const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
+        const f32x2 minus_m = f2_make(-m_use, -m_use), ff = f2_make(f, f), cc = f2_make(cap_log2, cap_log2);
+        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          float v[32];
+          tmem_ld32(s_tm + x * 32, v);
+          tmem_wait_ld();
+          if (cap) {
+            float far = 0.f;
+#pragma unroll
+            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(v[y]), fabsf(v[y + 1]));
+            if (__all_sync(0xffffffffu, far * f <= 0.6f)) {
+#pragma unroll
+              for (int y = 0; y < 32; y += 2) {
+                const f32x2 z = capped_poly(f2_mul(f2_make(v[y], v[y + 1]), ff), cc, minus_m);
+                v[y] = f2_lo(z);
+                v[y + 1] = f2_hi(z);
+              }
+            } else {
+#pragma unroll
+              for (int y = 0; y < 32; ++y) v[y] = capped(v[y] * f, cap_log2) - m_use;
+            }
+          } else {
+#pragma unroll
+            for (int y = 0; y < 32; y += 2) {
+              const f32x2 z = f2_fma(f2_make(v[y], v[y + 1]), ff, minus_m);
+              v[y] = f2_lo(z);
+              v[y + 1] = f2_hi(z);
+            }
+          }
+          if (edge) {
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+              if (x * 32 + y >= left) v[y] = -INFINITY;
+          }
+          uint32_t p[16];
+#pragma unroll
+          for (int y = 0; y < 32; y += 4) {
+            const float e0 = ex2_approx(v[y]), e1 = ex2_approx(v[y + 1]), e2 = ex2_approx(v[y + 2]), e3 = ex2_approx(v[y + 3]);
+            sum0 = f2_add(sum0, f2_make(e0, e1));
+            sum1 = f2_add(sum1, f2_make(e2, e3));
+            p[y / 2] = kInt4 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
+            p[y / 2 + 1] = kInt4 ? pack_f16x2(e2, e3) : pack_bf16x2(e2, e3);
+          }
+          tmem_st16(s_tm + x * 16, p);                  // P where S has been read already
+        }
+        sum0 = f2_add(sum0, sum1);
+        l = fmaf(f2_lo(sum0) + f2_hi(sum0), ex2_approx(-shift), l);
+        tmem_wait_st();
+        tc_fence_before();
+        mbar_arrive(&B.p_full[w]);
+      }
+      // ---- the row's result ----
+      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], done + tiles - 1));
+      if (ok) {
+        tc_fence_after();
+        const bool whole = piece.whole != 0, some = l > 0.f && live;
+        const float ofac = tiles > 0 ? o_factor[nth & 1] : 0.f, norm = whole ? (some ? ofac / l : 0.f) : ofac;
+        float* const part = a.part + (long long)(2 * blockIdx.x + (t0 == 0)) * kChRows * (kD + 2) + (w * 128 + r) * kD;
+        const long long row = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
+        auto emit = [&](int dim, float x0, float x1, float x2, float x3) {
+          if (whole) reinterpret_cast<uint2*>(a.out + row * kD + dim)[0] = make_uint2(pack_bf16x2(x0 * norm, x1 * norm), pack_bf16x2(x2 * norm, x3 * norm));
+          else reinterpret_cast<float4*>(part + dim)[0] = make_float4(x0 * norm, x1 * norm, x2 * norm, x3 * norm);
+        };
+#pragma unroll
+        for (int x = 0; x < kD / 32; ++x) {
+          float v[32];
+          if (tiles > 0) {
+            tmem_ld32(o_tm + x * 32, v);
+            tmem_wait_ld();
+          }
+          if (tiles == 0 || (whole && !some)) {
+#pragma unroll
+            for (int y = 0; y < 32; ++y) v[y] = 0.f;
+          }
+          if (rho < R) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float* o = v + 8 * y;
+              if constexpr (kInt4) {                    // chunk k of V's operand: dims 32 m + 4 r' + (0..3) and 32 (m + 1) + 4 r' + (0..3) in turn
+                const int k = 4 * x + y, dim = 4 * (k / (kWords / 2)) + 64 * (k % (kWords / 2));
+                emit(dim, o[0], o[2], o[4], o[6]);
+                emit(dim + 32, o[1], o[3], o[5], o[7]);
+              } else {
+                emit(32 * x + 8 * y, o[0], o[1], o[2], o[3]);
+                emit(32 * x + 8 * y + 4, o[4], o[5], o[6], o[7]);
+              }
+            }
+          }
+        }
+        if (rho < R) {
+          if (whole) {
+            if (a.lse) a.lse[row] = some ? fmaf(ref, 0.6931471805599453f, logf(l)) : -INFINITY;
+          } else {
+            reinterpret_cast<float2*>(a.part + (long long)(2 * blockIdx.x + (t0 == 0)) * kChRows * (kD + 2) + kChRows * kD)[w * 128 + r] = make_float2(ref, l);
+          }
+        }
+        tc_fence_before();
+      }
+    }
+    __syncwarp();
+    // all go on to the next piece, or none
+    const bool stop = __syncthreads_or(abort_flag) != 0;
+    tc_fence_after();
+    done += tiles;
+    if (threadIdx.x == 0) {
+      piece_s.run.tile += piece_s.t1 - piece_s.t0;
+      if (stop) piece_s.run.tile = piece_s.run.end;
+      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, kChTile);
+    }
+    __syncthreads();
+  }
+  if (warp == kSoftmaxWarps + kFetchWarps) tmem_dealloc(tmem, 512);
+}
+
+// grid (units, 8), block 256: merges what several CTAs left of a unit, 32 rows per block, a row per kD / 4 threads at a time.
+template <int kD>
+__global__ void __launch_bounds__(256) paged_chunk_combine_kernel(const __grid_constant__ PagedMmaArgs a, int grid) {
+  grid_dependency_wait();
+  grid_dependency_launch();
+  __shared__ int run_s[2];
+  const PagedCache& c = a.c;
+  const int unit = blockIdx.x, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kChRows + (int)blockIdx.y * 32, R = c.n_tokens * c.G;
+  if (rho0 >= R) return;
+  const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles, entry = unit / units, b = bh / c.Hkv, h = bh - b * c.Hkv;
+  if (threadIdx.x < 32) {
+    int before = 0, all = 0;
+    const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
+    for (int e = threadIdx.x; e < entries; e += 32) {
+      const int t = entry_tiles(c, e, kChTile) * units;
+      all += t;
+      if (e < entry) before += t;
+    }
+    all = __reduce_add_sync(0xffffffffu, all);
+    before = __reduce_add_sync(0xffffffffu, before);
+    if (threadIdx.x == 0) { run_s[0] = all; run_s[1] = before; }
+  }
+  const int tiles = entry_tiles(c, entry, kChTile), count = paged_count(c, b);
+  __syncthreads();
+  const Deal deal(run_s[0], grid);
+  const int u0 = run_s[1] + (unit - entry * units) * tiles;
+  const int x0 = deal.first_of(u0, tiles), pieces = deal.last_of(u0, tiles) - x0 + 1;
+  if (pieces == 1) return;
+  constexpr long long kSlot = kChRows * (kD + 2);
+  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0)) * kSlot; };
+  const int v = threadIdx.x % (kD / 4);
+  for (int k = threadIdx.x / (kD / 4); k < 32 && rho0 + k < R; k += 256 / (kD / 4)) {
+    const int row = (int)blockIdx.y * 32 + k;
+    float mm = -INFINITY, ll = 0.f;
+    for (int x = 0; x < pieces; ++x) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(piece(x) + kChRows * kD) + row).x);
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+    for (int x = 0; x < pieces; ++x) {
+      const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(x) + kChRows * kD) + row);
+      const float4 o = __ldcg(reinterpret_cast<const float4*>(piece(x) + row * kD) + v);
+      if (ml.x == -INFINITY) continue;
+      const float f = ex2_approx(ml.x - mm);
+      fma4(acc, o, f);
+      ll = fmaf(ml.y, f, ll);
+    }
+    write_row<kD>(a, b, h, rho0 + k, count, v, acc, mm, ll);
+  }
+}
+
+struct ChunkVariant {
+  void (*kernel)(PagedMmaArgs);
+  void (*combine)(PagedMmaArgs, int);
+  size_t smem;
+};
+template <int kD, int kGroups> ChunkVariant chunk_variant() {
+  return ChunkVariant{paged_chunk_kernel<kD, kGroups>, paged_chunk_combine_kernel<kD>, ChunkConfig<kD, kGroups>::kSmem};
+}
+bool pick_chunk(const PagedCache& c, ChunkVariant* v) {
+  const int groups = c.format == RESTKV_PAGES_INT4 ? c.d / c.group : 0;
+  switch (c.d * 16 + groups) {
+    case 64 * 16 + 0: *v = chunk_variant<64, 0>(); return true;
+    case 64 * 16 + 1: *v = chunk_variant<64, 1>(); return true;
+    case 64 * 16 + 2: *v = chunk_variant<64, 2>(); return true;
+    case 128 * 16 + 0: *v = chunk_variant<128, 0>(); return true;
+    case 128 * 16 + 1: *v = chunk_variant<128, 1>(); return true;
+    case 128 * 16 + 2: *v = chunk_variant<128, 2>(); return true;
+    case 128 * 16 + 4: *v = chunk_variant<128, 4>(); return true;
+    default: return false;
+  }
+}
+int chunk_ctas(int sm_count) { return sm_count < kMaxCtas ? sm_count : kMaxCtas; }
+
+}  // namespace
+
+cudaError_t paged_chunk_init() {
+  PagedCache c{};
+  for (int d : {64, 128})
+    for (int group : {0, 32, 64, 128}) {
+      c.d = d; c.group = group;
+      c.format = group ? RESTKV_PAGES_INT4 : RESTKV_PAGES_BF16;
+      ChunkVariant v;
+      if (group > d || !pick_chunk(c, &v)) continue;
+      const cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
+      if (e != cudaSuccess) return e;
+    }
+  return cudaSuccess;
+}
+
+bool paged_chunk_supported(const PagedCache& c) {
+  ChunkVariant v;
+  const long long rows = (long long)c.n_tokens * c.G;
+  if (rows < kChunkRows || !pick_chunk(c, &v)) return false;
+  const long long units = (long long)c.batch * c.Hkv * ((rows + kChRows - 1) / kChRows);
+  return (c.capacity() / kChTile + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
+}
+
+size_t paged_chunk_bytes(const PagedCache& c, int sm_count) {
+  return (size_t)2 * chunk_ctas(sm_count) * kChRows * (c.d + 2) * sizeof(float);
+}
+
+cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count, long long wait_limit,
+                               cudaStream_t st) {
+  ChunkVariant v;
+  if (!pick_chunk(c, &v)) return cudaErrorInvalidValue;
+  PagedMmaArgs a{};
+  a.c = c; a.Q = Q; a.out = (__nv_bfloat16*)out; a.lse = lse; a.part = part; a.wait_limit = wait_limit;
+  a.row_tiles = (int)(((long long)c.n_tokens * c.G + kChRows - 1) / kChRows);
+  const long long units = (long long)c.batch * c.Hkv * a.row_tiles;
+  const int ctas = chunk_ctas(sm_count);
+  const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), kChThreads, v.smem, st, a);
+  if (e != cudaSuccess) return e;
+  return launch_chained(v.combine, dim3((unsigned int)units, kChRows / 32), 256, 0, st, a, ctas);
+}
+
+}  // namespace restkv

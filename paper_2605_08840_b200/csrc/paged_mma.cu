@@ -30,8 +30,7 @@
 #include <cooperative_groups.h>
 #include <cuda_fp16.h>
 
-#include "paged.cuh"
-#include "tc_common.cuh"
+#include "paged_deal.cuh"
 
 namespace restkv {
 
@@ -106,21 +105,6 @@ template <int kWords> __device__ __forceinline__ void lds_words(uint32_t addr, u
 template <int i> __device__ __forceinline__ uint32_t code_pair(uint32_t w) {
   return (i >= 2 ? w >> 8 : w) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
 }
-__device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-
-constexpr int kMaxCtas = 512;
-
-struct PagedMmaArgs {
-  PagedCache c;
-  RowsView Q;
-  __nv_bfloat16* out;
-  float* lse;        // or null
-  float* part;       // per CTA two of: o [rows, d], (m, l) [rows]; without clusters
-  int row_tiles;     // units per KV head
-  int cluster;       // CTAs per unit, 0: tiles of all units end to end
-  long long wait_limit;
-};
 
 // The shape of an instantiation.  kD head_dim, kGroups groups of a 4-bit row (0: bf16), kNT tiles of 8 query rows.
 template <int kD, int kGroups, int kNT> struct Config {
@@ -145,125 +129,6 @@ template <int kD, int kGroups, int kNT> struct Config {
   static constexpr uint32_t kPushBytes = kRows * kD * 4u + 256u + 16u * kRows * 8u;
   static constexpr size_t kClusterSmem = (size_t)kWarps * 2 * kStageBytes + kPushBytes + 1024;
   static_assert(2 * kStageBytes >= kPartBytes, "the merge needs the ring's space");
-};
-
-// Tiles dealt out end to end: CTA x of `ctas` has those from boundary x to boundary x + 1.  A boundary is start(x) = all * x / ctas, but
-// moved to the near end of its unit where that is at most `snap` tiles away: a CTA that ends one unit and begins another pays for
-// prologue and merge twice, 5 us, in which it would go through some 24 tiles.
-struct Deal {
-  int ctas, each, more, snap;
-  __device__ __forceinline__ Deal(int all, int grid) : ctas(all < grid ? all : grid), each(all / ctas), more(all - each * ctas) {
-    snap = (each - 1) / 2 < 24 ? (each - 1) / 2 : 24;   // less than half a share: no share vanishes
-  }
-  __device__ __forceinline__ int start(int x) const { return x * each + x * more / ctas; }
-  // tile `at` of a unit of `tiles`: where a boundary there goes, as tile of the unit
-  __device__ __forceinline__ int moved(int at, int tiles) const {
-    const int left = tiles - at;
-    return at <= snap && at <= left ? 0 : left <= snap ? tiles : at;
-  }
-  // the last CTA whose start is not past `tile`
-  __device__ __forceinline__ int last(int tile) const {
-    int x = (int)((float)tile / ((float)each + (float)more / (float)ctas));
-    x = x < ctas ? x : ctas - 1;
-    while (x > 0 && start(x) > tile) --x;
-    while (x + 1 < ctas && start(x + 1) <= tile) ++x;
-    return x;
-  }
-  // the CTAs that have tiles of the unit [u0, u0 + tiles): the first of them its beginning
-  __device__ __forceinline__ int first_of(int u0, int tiles) const { return last(u0 + (snap < tiles / 2 ? snap : tiles / 2)); }
-  __device__ __forceinline__ int last_of(int u0, int tiles) const {
-    return last(u0 + tiles - 1 - (snap < (tiles - 1) / 2 ? snap : (tiles - 1) / 2));
-  }
-};
-
-// Entries: sequences, or with lengths per head the KV heads of all sequences; each has `units` units of as many tiles.
-__device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_rows) {
-  const int n = c.per_head ? paged_length(c, e / c.Hkv, e % c.Hkv) : paged_length(c, e, 0);
-  const int t = (n + tile_rows - 1) / tile_rows;
-  return t > 0 ? t : 1;     // a unit without rows has its outputs written, too
-}
-
-// By a whole warp: a CTA's run of tiles [tile, end), the entry that `tile` lies in, the entry's first tile and tiles per unit.
-struct Run {
-  int tile, end, entry, first, tiles;
-};
-__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int x, int grid) {
-  const int lane = threadIdx.x & 31;
-  const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
-  const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
-  const int t0 = lane < entries ? entry_tiles(c, lane, tile_rows) : 0;
-  int sum = t0 * units;
-  for (int e = 32 + lane; e < entries; e += 32) sum += entry_tiles(c, e, tile_rows) * units;
-  const int all = __reduce_add_sync(0xffffffffu, sum);
-  const Deal deal(all, grid);
-  Run r{0, 0, 0, 0, 1};
-  if (x >= deal.ctas) return r;
-  r.tile = r.end = all;
-  int want = deal.start(x), before = 0;
-  bool have = false;
-  for (int base = 0; base < entries; base += 32) {
-    const int t = base == 0 ? t0 : base + lane < entries ? entry_tiles(c, base + lane, tile_rows) : 0;
-    int upto = t * units;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int o = __shfl_up_sync(0xffffffffu, upto, off);
-      if (lane >= off) upto += o;
-    }
-    for (;;) {             // both boundaries of the CTA may lie in these entries
-      const unsigned int past = __ballot_sync(0xffffffffu, before + upto > want);
-      if (!past) break;
-      const int at = __ffs((int)past) - 1;
-      const int tiles = __shfl_sync(0xffffffffu, t, at), first = before + __shfl_sync(0xffffffffu, upto, at) - tiles * units;
-      const int unit0 = first + (want - first) / tiles * tiles, boundary = unit0 + deal.moved(want - unit0, tiles);
-      if (!have) {
-        have = true;
-        r = Run{boundary, all, base + at, first, tiles};
-        if (x + 1 == deal.ctas) return r;
-        want = deal.start(x + 1);
-      } else {
-        r.end = boundary;
-        return r;
-      }
-    }
-    before += __shfl_sync(0xffffffffu, upto, 31);
-  }
-  return r;
-}
-
-// Dims 4 v .. 4 v + 3 of a query row's result.
-template <int kD>
-__device__ __forceinline__ void write_row(const PagedMmaArgs& a, int b, int h, int rho, int count, int v, float4 acc, float mm, float ll) {
-  const PagedCache& c = a.c;
-  const int i = rho / c.G, g = rho - i * c.G;
-  const bool some = ll > 0.f && i < count;
-  const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
-  const float f = some ? 1.f / ll : 0.f;
-  uint2 w = make_uint2(0u, 0u);
-  if (some) w = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
-  reinterpret_cast<uint2*>(a.out + at * kD)[v] = w;
-  if (v == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
-}
-__device__ __forceinline__ void fma4(float4& acc, float4 x, float f) {
-  acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
-}
-
-// What a CTA works on without clusters, in shared memory: it is needed before the tiles and after them, and registers are short between.
-struct Piece {
-  Run run;
-  int unit, t0, t1;        // tiles [t0, t1) of the unit
-  int whole;               // no other CTA has tiles of it
-  __device__ __forceinline__ void cut(const PagedCache& c, int row_tiles, int tile_rows) {   // at run.tile
-    const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
-    if (run.tile >= run.first + run.tiles * units) {     // the next entry
-      run.first += run.tiles * units;
-      run.tiles = entry_tiles(c, ++run.entry, tile_rows);
-    }
-    const int k = (run.tile - run.first) / run.tiles, begin = run.first + k * run.tiles;
-    unit = run.entry * units + k;
-    t0 = run.tile - begin;
-    t1 = run.end - begin < run.tiles ? run.end - begin : run.tiles;
-    whole = t0 == 0 && t1 == run.tiles;
-  }
 };
 
 template <int kD, int kGroups, int kNT, bool kCluster>

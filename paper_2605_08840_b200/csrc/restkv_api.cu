@@ -268,7 +268,7 @@ restkv_status restkv_create(restkv_handle** out) {
   h->counter_turn[0] = h->counter_turn[1] = 0u;
   h->tc_state = nullptr;
   if (tc_init(&h->tc_state) != cudaSuccess || tc_fused_init() != cudaSuccess ||
-      decode_mma_init(h->decode_clusters) != cudaSuccess || paged_mma_init(h->paged_clusters) != cudaSuccess)
+      decode_mma_init(h->decode_clusters) != cudaSuccess || paged_mma_init(h->paged_clusters) != cudaSuccess || paged_chunk_init() != cudaSuccess)
     h->tc_state = nullptr;
   h->wait_limit = 2000000000ll;
   h->fused_select = true;
