@@ -7,7 +7,7 @@
 //     thread per row: while one tile's softmax runs, the other tile's products do, and a tile of K and V serves both;
 //   - S (fp32) and O of both tiles fill the tensor memory's 512 columns at head_dim 128; P (16 bits) takes S's place and is the A operand
 //     of P V there;
-//   - four warps fetch K and V, a row per thread: bf16 by cp.async; codes become f16 operands with one fused operation per pair, the
+//   - seven warps fetch K and V, half a row per thread: bf16 by cp.async; codes become f16 operands with one fused operation per pair, the
 //     nibble as it stands being the f16 subnormal 2^-24 code (2^-20 for the upper one of a byte).
 //     K: step * (code - 8), times 2^(a - 24) for a tile's exponent a that just lets its largest step fit f16: at most 11 bits, exact. The
 //     rest, (offset + 8 step) * sum(q) per group, is three more products of f16 parts (22 bits together), another 16 dims for all groups.
@@ -31,7 +31,7 @@ namespace {
 
 constexpr int kChRows = 256;                 // query rows of a unit
 constexpr int kChTile = 128;                 // cache rows of a tile
-constexpr int kSoftmaxWarps = 8, kFetchWarps = 4;
+constexpr int kSoftmaxWarps = 8, kFetchWarps = 7;   // and one for the products: four warps per scheduler, 128 registers
 constexpr int kChThreads = (kSoftmaxWarps + kFetchWarps + 1) * 32;
 constexpr int kFetch = kFetchWarps * 32;
 constexpr int kInfo = 4;                     // tiles whose factors are kept: the fetching warps are two ahead of the softmax at most
@@ -150,8 +150,13 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   constexpr uint32_t kO = 256;                          // O of tile w: columns kO + w * kD; S and P: w * 128
   const volatile Piece& piece = piece_s;
 
-  int done = 0;                                         // tiles of the pieces before: phases of the rings
-  for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
+  struct Unit {
+    int b, h, rho0, n, count, t0, tiles, done, nth;     // done: tiles of the pieces before, phases of the rings; nth: pieces before
+  };
+  // A role's part of every piece.  All roles go from piece to piece together.
+  auto each_piece = [&](auto&& part) {
+    int done = 0;
+    for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
     const int unit = piece.unit, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kChRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
     const int R = c.n_tokens * c.G, n = paged_length(c, b, h), count = paged_count(c, b), t0 = piece.t0;
     // rows that the unit's last query row sees; tiles past them are nobody's business (a unit whose rows see nothing takes one all the same)
@@ -160,18 +165,41 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     const int t_seen = seen > 0 ? (seen + kChTile - 1) / kChTile : 0;
     const int tiles = max(0, min(piece.t1, t_seen) - t0);
     if (threadIdx.x == 0 && t0 == 0) check_length(c, b, h);
+    part(Unit{b, h, rho0, n, count, t0, tiles, done, nth});
+    __syncwarp();
+    // all go on to the next piece, or none
+    const bool stop = __syncthreads_or(abort_flag) != 0;
+    tc_fence_after();
+    done += tiles;
+    if (threadIdx.x == 0) {
+      piece_s.run.tile += piece_s.t1 - piece_s.t0;
+      if (stop) piece_s.run.tile = piece_s.run.end;
+      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, kChTile);
+    }
+    __syncthreads();
+    }
+  };
 
-    if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kFetchWarps) {
-      // ---------------- fetching K and V: a row per thread ----------------
-      const int r = threadIdx.x - kSoftmaxWarps * 32;
+  if (warp >= kSoftmaxWarps && warp < kSoftmaxWarps + kFetchWarps) {
+    each_piece([&](const Unit& u) {
+      // ---------------- fetching K and V, half a row per thread ----------------
+      // Pieces 0 .. 7 are K's: 32 rows, half of their words each; 8 .. 15 V's.  Warp f takes f, f + 7, f + 14.
+      const int b = u.b, h = u.h, n = u.n, t0 = u.t0, tiles = u.tiles, done = u.done, nth = u.nth;
+      const int fw = warp - kSoftmaxWarps;
+      const bool first = threadIdx.x == kSoftmaxWarps * 32;
+      constexpr int kPieces = (16 + kFetchWarps - 1) / kFetchWarps, kHalf = 2 * kWords;   // 32-bit words of codes of half a row
       const int per_page = c.page_rows / kBlockRows;
-      auto page_of = [&](int j) {                       // of the thread's row of tile j; -1: nothing there
-        const int row = (t0 + j) * kChTile + r;
-        return j < tiles && row < n ? c.table[(long long)b * c.table_width + row / c.page_rows] : -1;
+      auto row_of = [&](int x) { return ((fw + x * kFetchWarps) >> 1 & 3) * 32 + lane; };
+      auto half_of = [&](int x) { return (fw + x * kFetchWarps) & 1; };
+      auto is_v = [&](int x) { return fw + x * kFetchWarps >= 8; };
+      auto has = [&](int x) { return fw + x * kFetchWarps < 16; };
+      auto page_of = [&](int j, int x) {                // of the thread's row of tile j; -1: nothing there
+        const int row = (t0 + j) * kChTile + row_of(x);
+        return has(x) && j < tiles && row < n ? c.table[(long long)b * c.table_width + row / c.page_rows] : -1;
       };
-      auto place_of = [&](int j, int page) {            // block of the pool, -1
-        const int row = (t0 + j) * kChTile + r;
-        if (j >= tiles || row >= n) return -1;
+      auto place_of = [&](int j, int x, int page) {     // block of the pool, -1
+        const int row = (t0 + j) * kChTile + row_of(x);
+        if (!has(x) || j >= tiles || row >= n) return -1;
         if ((unsigned int)page >= (unsigned int)c.n_pages) {
           atomicOr(c.dev_status, kDevBadIndex);
           return -1;
@@ -179,44 +207,49 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         return (page * c.Hkv + h) * per_page + row % c.page_rows / kBlockRows;
       };
       bool ok = true;
+      int page[kPieces];
+#pragma unroll
+      for (int x = 0; x < kPieces; ++x) page[x] = page_of(0, x);
       if constexpr (kInt4) {
-        uint32_t kw[4 * kWords], vw[4 * kWords], kp[kG], vp[kG];   // a row's codes; (step, offset) per group
-        auto load = [&](int place) {
-          const bool there = place >= 0;
-          const uint8_t* kb = c.K + (long long)(there ? place : 0) * c.block_bytes;
-          const uint8_t* vb = c.V + (long long)(there ? place : 0) * c.block_bytes;
-          const int q = r & 15;
+        uint32_t codes[kPieces][kHalf], params[kPieces][kG];   // half a row's codes; (step, offset) per group
+        int a_ref = 0;
+        auto load = [&](int j) {                        // tile j's, and the next one's pages
 #pragma unroll
-          for (int x = 0; x < kWords; ++x) {
-            const uint4 u = there ? reinterpret_cast<const uint4*>(kb + q * (kD / 2))[x] : make_uint4(0u, 0u, 0u, 0u);
-            const uint4 v = there ? reinterpret_cast<const uint4*>(vb + q * (kD / 2))[x] : make_uint4(0u, 0u, 0u, 0u);
-            kw[4 * x] = u.x; kw[4 * x + 1] = u.y; kw[4 * x + 2] = u.z; kw[4 * x + 3] = u.w;
-            vw[4 * x] = v.x; vw[4 * x + 1] = v.y; vw[4 * x + 2] = v.z; vw[4 * x + 3] = v.w;
+          for (int x = 0; x < kPieces; ++x) {
+            const int place = place_of(j, x, page[x]), q = lane & 15;
+            const bool there = place >= 0;
+            const uint8_t* block = (is_v(x) ? c.V : c.K) + (long long)(there ? place : 0) * c.block_bytes;
+#pragma unroll
+            for (int y = 0; y < kHalf / 4; ++y) {
+              const uint4 w = there ? reinterpret_cast<const uint4*>(block + q * (kD / 2) + half_of(x) * (kD / 4))[y] : make_uint4(0u, 0u, 0u, 0u);
+              codes[x][4 * y] = w.x; codes[x][4 * y + 1] = w.y; codes[x][4 * y + 2] = w.z; codes[x][4 * y + 3] = w.w;
+            }
+#pragma unroll
+            for (int g = 0; g < kG; ++g) {
+              const unsigned short* p = reinterpret_cast<const unsigned short*>(block + int4_params(kD, g, q));
+              params[x][g] = there ? p[0] | (uint32_t)p[4] << 16 : 0u;
+            }
           }
 #pragma unroll
-          for (int g = 0; g < kG; ++g) {
-            const unsigned short* k16 = reinterpret_cast<const unsigned short*>(kb + int4_params(kD, g, q));
-            const unsigned short* v16 = reinterpret_cast<const unsigned short*>(vb + int4_params(kD, g, q));
-            kp[g] = there ? k16[0] | (uint32_t)k16[4] << 16 : 0u;
-            vp[g] = there ? v16[0] | (uint32_t)v16[4] << 16 : 0u;
-          }
+          for (int x = 0; x < kPieces; ++x) page[x] = page_of(j + 1, x);
         };
-        int page = page_of(0), a_ref = 0;
-        load(place_of(0, page));
-        page = page_of(1);
-        for (int j = 0; j < tiles; ++j) {               // to the end even when a wait ran out: all four warps meet in every round
+        load(0);
+        for (int j = 0; j < tiles; ++j) {               // to the end even when a wait ran out: the warps meet in every round
           const int at = done + j, s = at & 1;
           // the tile's exponents: its largest step just below 2^15, its largest offset well within f16
-          float km = 0.f, vm = 0.f;
+          float most[2] = {0.f, 0.f};
 #pragma unroll
-          for (int g = 0; g < kG; ++g) {
-            km = fmaxf(km, fmaxf(lower(kp[g]), fabsf(upper(kp[g])) * 0x1p-16f));
-            vm = fmaxf(vm, fmaxf(lower(vp[g]), fabsf(upper(vp[g])) * 0x1p-25f));
-          }
-          const float kx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(km))), vx = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(vm)));
-          if (lane == 0) {
-            step_max[s][0][warp - kSoftmaxWarps] = kx;
-            step_max[s][1][warp - kSoftmaxWarps] = vx;
+          for (int x = 0; x < kPieces; ++x)
+#pragma unroll
+            for (int g = 0; g < kG; ++g) {
+              const float m = fmaxf(lower(params[x][g]), fabsf(upper(params[x][g])) * (is_v(x) ? 0x1p-25f : 0x1p-16f));
+              if (is_v(x)) most[1] = fmaxf(most[1], m);
+              else most[0] = fmaxf(most[0], m);
+            }
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const float m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(most[x])));
+            if (lane == 0) step_max[s][x][fw] = m;
           }
           fetch_sync();
           float kt = 0x1p-40f, vt = 0x1p-40f;
@@ -224,95 +257,112 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           for (int x = 0; x < kFetchWarps; ++x) { kt = fmaxf(kt, step_max[s][0][x]); vt = fmaxf(vt, step_max[s][1][x]); }
           const int ka = 141 - (int)(__float_as_uint(kt) >> 23), va = 141 - (int)(__float_as_uint(vt) >> 23);
           if (j == 0) a_ref = va;
-          if (r == 0) {
+          if (first) {
             k_factor[at % kInfo] = power_of_two(24 - ka);
             v_shift[at % kInfo] = (float)(a_ref - va);
             if (j == 0) o_factor[nth & 1] = power_of_two(24 - a_ref);
           }
           ok = ok && (at < 2 || wait(&B.k_empty[s], (at >> 1) - 1));
-          if (ok) {
-            uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};   // dims 3 g ..: the parts that meet sum(q)'s
+          bool v_free = false;
 #pragma unroll
-            for (int g = 0; g < kG; ++g) {
-              const float step = lower(kp[g]) * power_of_two(ka);
-              const uint32_t s1 = pack_f16x2(step, step), s16 = pack_f16x2(step * 0.0625f, step * 0.0625f), l = pack_f16x2(step * -0x1p-21f, step * -0x1p-21f);
+          for (int x = 0; x < kPieces; ++x) {
+            if (!has(x)) continue;
+            const int r = row_of(x);
+            if (!is_v(x)) {
+              if (!ok) continue;
+              uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};   // dims 3 g ..: the parts that meet sum(q)'s
 #pragma unroll
-              for (int m = g * kPerGroup; m < (g + 1) * kPerGroup; ++m)
+              for (int g = 0; g < kG; ++g) {
+                const float step = lower(params[x][g]) * power_of_two(ka);
+                const uint32_t s1 = pack_f16x2(step, step), s16 = pack_f16x2(step * 0.0625f, step * 0.0625f), l = pack_f16x2(step * -0x1p-21f, step * -0x1p-21f);
 #pragma unroll
-                for (int q = 0; q < 4; ++q)             // word q * kWords + m: dims 32 m + 8 q ..
-                  operands_of(kw[q * kWords + m], s1, s16, l, operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, 4 * m + q));
-              // hi, lo, hi against sum(q)'s hi, hi, lo; times 2^8, as sum(q)'s are times 2^-8
-              const uint32_t mid = split_f16(fmaf(8.f, lower(kp[g]), upper(kp[g])) * power_of_two(ka - 16));
+                for (int m = g * kPerGroup; m < (g + 1) * kPerGroup; ++m)
 #pragma unroll
-              for (int x = 0; x < 3; ++x) {
-                const uint32_t part = x == 1 ? mid >> 16 : mid & 0xFFFFu;
-                thin[(3 * g + x) >> 1] |= (3 * g + x) & 1 ? part << 16 : part;
+                  for (int q = 0; q < 2; ++q)           // word (2 half + q) * kWords + m of the row: dims 32 m + 8 (2 half + q) ..
+                    operands_of(codes[x][q * kWords + m], s1, s16, l, operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, 4 * m + 2 * half_of(x) + q));
+                // hi, lo, hi against sum(q)'s hi, hi, lo; times 2^8, as sum(q)'s are times 2^-8
+                const uint32_t mid = split_f16(fmaf(8.f, lower(params[x][g]), upper(params[x][g])) * power_of_two(ka - 16));
+#pragma unroll
+                for (int y = 0; y < 3; ++y) {
+                  const uint32_t part = y == 1 ? mid >> 16 : mid & 0xFFFFu;
+                  thin[(3 * g + y) >> 1] |= (3 * g + y) & 1 ? part << 16 : part;
+                }
+              }
+              if (half_of(x) == 0) {
+                const uint32_t to = thin_at(k_thin + (uint32_t)s * kThinBytes, r);
+                sts128(to, thin[0], thin[1], thin[2], thin[3]);
+                sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+              }
+            } else {
+              if (!v_free) {                            // the first of V's: K's are done
+                fence_proxy_async_smem();
+                mbar_arrive(&B.k_full[s]);
+                ok = ok && (at < 2 || wait(&B.v_empty[s], (at >> 1) - 1));
+                v_free = true;
+              }
+              if (!ok) continue;
+              uint32_t s1[kG], s16[kG], l[kG];
+#pragma unroll
+              for (int g = 0; g < kG; ++g) {
+                const float step = lower(params[x][g]) * power_of_two(va), lo = upper(params[x][g]) * power_of_two(va - 24);
+                s1[g] = pack_f16x2(step, step);
+                s16[g] = pack_f16x2(step * 0.0625f, step * 0.0625f);
+                l[g] = pack_f16x2(lo, lo);
+              }
+#pragma unroll
+              for (int y = 0; y < kHalf; ++y) {         // word y: dims 32 m + 4 r' + (0..3) in its lower half, 32 (m + 1) + .. in its upper
+                const int g = 2 * (y % (kWords / 2)) / kPerGroup, g1 = (2 * (y % (kWords / 2)) + 1) / kPerGroup;
+                const uint32_t t1 = g == g1 ? s1[g] : __byte_perm(s1[g], s1[g1], 0x5410), t16 = g == g1 ? s16[g] : __byte_perm(s16[g], s16[g1], 0x5410);
+                operands_of(codes[x][y], t1, t16, g == g1 ? l[g] : __byte_perm(l[g], l[g1], 0x5410),
+                            operand_at(v_at + (uint32_t)s * C::kTileBytesD, r, half_of(x) * kHalf + y));
               }
             }
-            const uint32_t to = thin_at(k_thin + (uint32_t)s * kThinBytes, r);
-            sts128(to, thin[0], thin[1], thin[2], thin[3]);
-            sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
-            fence_proxy_async_smem();
           }
-          mbar_arrive(&B.k_full[s]);
-          ok = ok && (at < 2 || wait(&B.v_empty[s], (at >> 1) - 1));
-          if (ok) {
-            uint32_t s1[kG], s16[kG], l[kG];
-#pragma unroll
-            for (int g = 0; g < kG; ++g) {
-              const float step = lower(vp[g]) * power_of_two(va), lo = upper(vp[g]) * power_of_two(va - 24);
-              s1[g] = pack_f16x2(step, step);
-              s16[g] = pack_f16x2(step * 0.0625f, step * 0.0625f);
-              l[g] = pack_f16x2(lo, lo);
-            }
-#pragma unroll
-            for (int x = 0; x < 4 * kWords; ++x) {      // word x: dims 32 m + 4 r' + (0..3) in its lower half, 32 (m + 1) + .. in its upper
-              const int g = 2 * (x % (kWords / 2)) / kPerGroup, g1 = (2 * (x % (kWords / 2)) + 1) / kPerGroup;
-              const uint32_t u = g == g1 ? s1[g] : __byte_perm(s1[g], s1[g1], 0x5410), u16 = g == g1 ? s16[g] : __byte_perm(s16[g], s16[g1], 0x5410);
-              operands_of(vw[x], u, u16, g == g1 ? l[g] : __byte_perm(l[g], l[g1], 0x5410), operand_at(v_at + (uint32_t)s * C::kTileBytesD, r, x));
-            }
-            fence_proxy_async_smem();
-          }
-          // the next tile's codes come while the products run
-          load(place_of(j + 1, page));
-          page = page_of(j + 2);
+          fence_proxy_async_smem();
+          if (!v_free) mbar_arrive(&B.k_full[s]);
           mbar_arrive(&B.v_full[s]);
+          load(j + 1);                                  // the next tile's codes come while the products run
         }
       } else {
-        auto fetch = [&](int j, int place) {            // K and V of tile j, a group of copies each
+        if (first) o_factor[nth & 1] = 1.f;
+        // a side of tile j as a group of copies; `page` is that of tile j
+        auto fetch = [&](int j, bool v) {
           const int at = done + j, s = at & 1;
-          const bool there = place >= 0;
-          const long long from = (long long)(there ? place : 0) * c.block_bytes + (r & 15) * (2 * kD);
-          if (at >= 2 && !wait(&B.k_empty[s], (at >> 1) - 1)) return false;
+          if (j < tiles && at >= 2 && !wait(v ? &B.v_empty[s] : &B.k_empty[s], (at >> 1) - 1)) return false;
 #pragma unroll
-          for (int x = 0; x < kD / 8; ++x) copy16(operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, x), c.K + from + 16 * x, there);
-          if (at >= 2 && !wait(&B.v_empty[s], (at >> 1) - 1)) return false;
+          for (int x = 0; x < kPieces; ++x) {
+            if (!has(x) || is_v(x) != v || j >= tiles) continue;
+            const int place = place_of(j, x, page[x]);
+            const uint8_t* from = (v ? c.V : c.K) + (long long)(place >= 0 ? place : 0) * c.block_bytes + (lane & 15) * (2 * kD) + half_of(x) * kD;
+            const uint32_t to = (v ? v_at : k_at) + (uint32_t)s * C::kTileBytesD;
 #pragma unroll
-          for (int x = 0; x < kD / 8; ++x) copy16(operand_at(v_at + (uint32_t)s * C::kTileBytesD, r, x), c.V + from + 16 * x, there);
+            for (int y = 0; y < kD / 16; ++y) copy16(operand_at(to, row_of(x), half_of(x) * (kD / 16) + y), from + 16 * y, place >= 0);
+            page[x] = page_of(j + 1, x);
+          }
           copy16_commit();
           return true;
         };
-        int page = page_of(0);
-        if (r == 0) o_factor[nth & 1] = 1.f;
-        if (tiles > 0) ok = fetch(0, place_of(0, page));
-        page = page_of(1);
-        for (int j = 0; j < tiles; ++j) {
+        ok = fetch(0, false) && fetch(0, true);
+        for (int j = 0; j < tiles && ok; ++j) {
           const int at = done + j, s = at & 1;
-          if (r == 0) { k_factor[at % kInfo] = 1.f; v_shift[at % kInfo] = 0.f; }
-          copy16_wait<0>();
+          if (first) { k_factor[at % kInfo] = 1.f; v_shift[at % kInfo] = 0.f; }
+          copy16_wait<1>();
           fence_proxy_async_smem();
           mbar_arrive(&B.k_full[s]);
+          ok = fetch(j + 1, false);                     // (its slot comes free only once this tile is known to be there)
+          copy16_wait<1>();
+          fence_proxy_async_smem();
           mbar_arrive(&B.v_full[s]);
-          // (the slots of the next tile come free only once this one is known to be there)
-          ok = ok && (j + 1 >= tiles || fetch(j + 1, place_of(j + 1, page)));
-          if (!ok) break;
-          page = page_of(j + 2);
+          ok = ok && fetch(j + 1, true);
         }
         copy16_wait<0>();
       }
-    } else if (warp == kSoftmaxWarps + kFetchWarps) {
+    });
+  } else if (warp >= kSoftmaxWarps + kFetchWarps) {
+    each_piece([&](const Unit& u) {
       // ---------------- the products, by one thread ----------------
-      if (elect_one() && tiles > 0) {
+      const int tiles = u.tiles, done = u.done, nth = u.nth;
+      if (warp == kSoftmaxWarps + kFetchWarps && tiles > 0 && elect_one()) {
         constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
         constexpr uint32_t idesc_o = kInt4 ? make_idesc_f16(128, kD, true) : make_idesc_bf16(128, kD, true);
         auto qk = [&](int w, int s) {
@@ -362,8 +412,11 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           wait_issued(&B.drained, 0);
         }
       }
-    } else {
+    });
+  } else {
+    each_piece([&](const Unit& u) {
       // ---------------- softmax: a query row per thread ----------------
+      const int b = u.b, h = u.h, rho0 = u.rho0, n = u.n, count = u.count, t0 = u.t0, tiles = u.tiles, done = u.done, nth = u.nth, R = c.n_tokens * c.G;
       const int w = warp >> 2, r = threadIdx.x & 127, rho = rho0 + w * 128 + r, i = rho / c.G, g = rho - i * c.G;
       const bool live = rho < R && i < count;
       const int sees = live ? n - (count - 1 - i) : n;
@@ -373,16 +426,16 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       if (tiles > 0) {
         // the row into shared memory
         const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
-        uint4 u[kD / 8];
+        uint4 raw[kD / 8];
 #pragma unroll
-        for (int x = 0; x < kD / 8; ++x) u[x] = live ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+        for (int x = 0; x < kD / 8; ++x) raw[x] = live ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
         const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
         if constexpr (kInt4) {
           float top = 0.f;
 #pragma unroll
           for (int x = 0; x < kD / 8; ++x)
 #pragma unroll
-            for (int y = 0; y < 4; ++y) top = fmaxf(top, fmaxf(fabsf(lower((&u[x].x)[y])), fabsf(upper((&u[x].x)[y]))));
+            for (int y = 0; y < 4; ++y) top = fmaxf(top, fmaxf(fabsf(lower((&raw[x].x)[y])), fabsf(upper((&raw[x].x)[y]))));
           // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
           int e = 141 - (int)(__float_as_uint(top) >> 23);
           e = e < -100 ? -100 : e > 100 ? 100 : e;
@@ -397,8 +450,8 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
               float v[8];
 #pragma unroll
               for (int y = 0; y < 4; ++y) {
-                v[2 * y] = lower((&u[x].x)[y]) * scale;
-                v[2 * y + 1] = upper((&u[x].x)[y]) * scale;
+                v[2 * y] = lower((&raw[x].x)[y]) * scale;
+                v[2 * y + 1] = upper((&raw[x].x)[y]) * scale;
               }
               // dims in the order of K's operands
               sts128(operand_at(tile, r, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
@@ -416,7 +469,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
         } else {
 #pragma unroll
-          for (int x = 0; x < kD / 8; ++x) sts128(operand_at(tile, r, x), u[x].x, u[x].y, u[x].z, u[x].w);
+          for (int x = 0; x < kD / 8; ++x) sts128(operand_at(tile, r, x), raw[x].x, raw[x].y, raw[x].z, raw[x].w);
         }
         fence_proxy_async_smem();
       }
@@ -436,10 +489,10 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         const float f = factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
         const int left = sees - (t0 + j) * kChTile;     // columns that the row sees
         const bool edge = sees_all < (t0 + j + 1) * kChTile;
+        float v[32];
         float mx = -INFINITY;
-#pragma unroll
+#pragma unroll 1
         for (int x = 0; x < 4; ++x) {
-          float v[32];
           tmem_ld32(s_tm + x * 32, v);
           tmem_wait_ld();
           if (edge) {
@@ -449,11 +502,11 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           }
           float m0 = v[0], m1 = v[1];
 #pragma unroll
-          for (int y = 2; y < 32; y += 4) {
+          for (int y = 2; y < 30; y += 4) {
             m0 = fmax3(m0, v[y], v[y + 1]);
-            if (y + 2 < 32) m1 = fmax3(m1, v[y + 2], v[y + 3]);
+            m1 = fmax3(m1, v[y + 2], v[y + 3]);
           }
-          mx = fmax3(mx, m0, m1);
+          mx = fmax3(mx, fmax3(m0, v[30], v[31]), m1);
         }
         mx *= f;                                        // (the factor is positive: the largest stays the largest)
         if (cap && mx != -INFINITY) mx = capped(mx, cap_log2);
@@ -480,43 +533,43 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
         const f32x2 minus_m = f2_make(-m_use, -m_use), ff = f2_make(f, f), cc = f2_make(cap_log2, cap_log2);
         f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
-#pragma unroll
+#pragma unroll 1
         for (int x = 0; x < 4; ++x) {
-          float v[32];
+          float* const u = v;
           tmem_ld32(s_tm + x * 32, v);
           tmem_wait_ld();
           if (cap) {
             float far = 0.f;
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(v[y]), fabsf(v[y + 1]));
-            if (__all_sync(0xffffffffu, far * f <= 0.6f)) {
+            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(u[y]), fabsf(u[y + 1]));
+            if (!edge && __all_sync(0xffffffffu, far * f <= 0.6f)) {
 #pragma unroll
               for (int y = 0; y < 32; y += 2) {
-                const f32x2 z = capped_poly(f2_mul(f2_make(v[y], v[y + 1]), ff), cc, minus_m);
-                v[y] = f2_lo(z);
-                v[y + 1] = f2_hi(z);
+                const f32x2 z = capped_poly(f2_mul(f2_make(u[y], u[y + 1]), ff), cc, minus_m);
+                u[y] = f2_lo(z);
+                u[y + 1] = f2_hi(z);
               }
             } else {
 #pragma unroll
-              for (int y = 0; y < 32; ++y) v[y] = capped(v[y] * f, cap_log2) - m_use;
+              for (int y = 0; y < 32; ++y) u[y] = capped(u[y] * f, cap_log2) - m_use;
             }
           } else {
 #pragma unroll
             for (int y = 0; y < 32; y += 2) {
-              const f32x2 z = f2_fma(f2_make(v[y], v[y + 1]), ff, minus_m);
-              v[y] = f2_lo(z);
-              v[y + 1] = f2_hi(z);
+              const f32x2 z = f2_fma(f2_make(u[y], u[y + 1]), ff, minus_m);
+              u[y] = f2_lo(z);
+              u[y + 1] = f2_hi(z);
             }
           }
           if (edge) {
 #pragma unroll
             for (int y = 0; y < 32; ++y)
-              if (x * 32 + y >= left) v[y] = -INFINITY;
+              if (x * 32 + y >= left) u[y] = -INFINITY;
           }
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 4) {
-            const float e0 = ex2_approx(v[y]), e1 = ex2_approx(v[y + 1]), e2 = ex2_approx(v[y + 2]), e3 = ex2_approx(v[y + 3]);
+            const float e0 = ex2_approx(u[y]), e1 = ex2_approx(u[y + 1]), e2 = ex2_approx(u[y + 2]), e3 = ex2_approx(u[y + 3]);
             sum0 = f2_add(sum0, f2_make(e0, e1));
             sum1 = f2_add(sum1, f2_make(e2, e3));
             p[y / 2] = kInt4 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
@@ -577,19 +630,9 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         }
         tc_fence_before();
       }
-    }
-    __syncwarp();
-    // all go on to the next piece, or none
-    const bool stop = __syncthreads_or(abort_flag) != 0;
-    tc_fence_after();
-    done += tiles;
-    if (threadIdx.x == 0) {
-      piece_s.run.tile += piece_s.t1 - piece_s.t0;
-      if (stop) piece_s.run.tile = piece_s.run.end;
-      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, kChTile);
-    }
-    __syncthreads();
+    });
   }
+  __syncthreads();
   if (warp == kSoftmaxWarps + kFetchWarps) tmem_dealloc(tmem, 512);
 }
 
