@@ -68,15 +68,15 @@ __device__ __forceinline__ void operands_of(uint32_t w, uint32_t s, uint32_t s16
   sts128(to, hfma2(s, w & 0x000F000Fu, l), hfma2(s16, w & 0x00F000F0u, l), hfma2(s, w8 & 0x000F000Fu, l), hfma2(s16, w8 & 0x00F000F0u, l));
 }
 
-// cap * tanh(t / cap) in log2 units, less `m`: t = argument of the tanh, c = cap * log2(e).
-__device__ __forceinline__ f32x2 capped_poly(f32x2 t, f32x2 c, f32x2 minus_m) {
+// cap * tanh(t) in log2 units: c = cap * log2(e).
+__device__ __forceinline__ f32x2 capped_poly(f32x2 t, f32x2 c) {
   const f32x2 z = f2_mul(t, t);
   f32x2 p = f2_make(0.0154755134f, 0.0154755134f);
   p = f2_fma(p, z, f2_make(-0.0521015525f, -0.0521015525f));
   p = f2_fma(p, z, f2_make(0.133101761f, 0.133101761f));
   p = f2_fma(p, z, f2_make(-0.333323091f, -0.333323091f));
   p = f2_fma(p, z, f2_make(0.99999994f, 0.99999994f));
-  return f2_fma(f2_mul(p, t), c, minus_m);
+  return f2_mul(f2_mul(p, t), c);
 }
 __device__ __forceinline__ float capped(float t, float c) { return fmaf(-2.f * c, rcp_approx(1.f + ex2_approx(t * 2.f * kLog2e)), c); }
 
@@ -87,6 +87,41 @@ __device__ __forceinline__ uint32_t thin_at(uint32_t tile, int row) { return til
 __device__ __forceinline__ uint32_t split_f16(float x) {
   const __half hi = __float2half_rn(x);
   return pack_f16x2(__half2float(hi), x - __half2float(hi));
+}
+
+// `columns` fp32 columns of the thread's row of tensor memory times f.  By whole warps.
+__device__ __noinline__ void rescale(uint32_t at, int columns, float f) {
+  for (int x = 0; x < columns; x += 16) {
+    float v[16];
+    tmem_ld16(at + x, v);
+    tmem_wait_ld();
+    uint32_t w[16];
+#pragma unroll
+    for (int y = 0; y < 16; ++y) w[y] = __float_as_uint(v[y] * f);
+    tmem_st16(at + x, w);
+  }
+  tmem_wait_st();
+}
+// The same for `chunks` chunks of 16 columns of f16 or bf16 pairs; f is a power of two, or 0.
+template <bool kF16> __device__ __noinline__ void rescale_pairs(uint32_t at, int chunks, float f) {
+  tmem_wait_st();            // they have just been written
+  for (int x = 0; x < chunks; ++x) {
+    float v[16];
+    tmem_ld16(at + x * 16, v);
+    tmem_wait_ld();
+    uint32_t w[16];
+#pragma unroll
+    for (int y = 0; y < 16; ++y) {
+      const uint32_t u = __float_as_uint(v[y]);
+      if (kF16) {
+        const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&u));
+        w[y] = pack_f16x2(e.x * f, e.y * f);
+      } else {
+        w[y] = pack_bf16x2(lower(u) * f, upper(u) * f);
+      }
+    }
+    tmem_st16(at + x * 16, w);
+  }
 }
 
 template <int kD, int kGroups> struct ChunkConfig {
@@ -332,11 +367,15 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
 #pragma unroll
           for (int x = 0; x < kPieces; ++x) {
             if (!has(x) || is_v(x) != v || j >= tiles) continue;
-            const int place = place_of(j, x, page[x]);
-            const uint8_t* from = (v ? c.V : c.K) + (long long)(place >= 0 ? place : 0) * c.block_bytes + (lane & 15) * (2 * kD) + half_of(x) * kD;
+            // a row's half in kD / 16 threads side by side; the places are those of the rows' own threads
+            const int own = place_of(j, x, page[x]), per_row = kD / 16, y = half_of(x) * per_row + lane % per_row;
             const uint32_t to = (v ? v_at : k_at) + (uint32_t)s * C::kTileBytesD;
 #pragma unroll
-            for (int y = 0; y < kD / 16; ++y) copy16(operand_at(to, row_of(x), half_of(x) * (kD / 16) + y), from + 16 * y, place >= 0);
+            for (int z = 0; z < per_row; ++z) {
+              const int r = z * (32 / per_row) + lane / per_row, place = __shfl_sync(0xffffffffu, own, r);
+              copy16(operand_at(to, row_of(x) - lane + r, y), (v ? c.V : c.K) + (long long)(place >= 0 ? place : 0) * c.block_bytes + (r & 15) * (2 * kD) + 16 * y,
+                     place >= 0);
+            }
             page[x] = page_of(j + 1, x);
           }
           copy16_commit();
@@ -365,16 +404,18 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       if (warp == kSoftmaxWarps + kFetchWarps && tiles > 0 && elect_one()) {
         constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
         constexpr uint32_t idesc_o = kInt4 ? make_idesc_f16(128, kD, true) : make_idesc_bf16(128, kD, true);
+        // descriptors count 16-byte units
+        const uint64_t q0 = kmajor_desc(q_at), k0 = kmajor_desc(k_at), v0 = make_smem_desc(v_at, 16384u, 1024u);
+        const uint64_t qt = make_smem_desc_plain(q_thin, 128u, 256u), kt = make_smem_desc_plain(k_thin, 128u, 256u);
         auto qk = [&](int w, int s) {
-          const uint64_t a0 = kmajor_desc(q_at + (uint32_t)w * C::kTileBytesD), b0 = kmajor_desc(k_at + (uint32_t)s * C::kTileBytesD);
+          const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4));
 #pragma unroll
           for (int k = 0; k < kD / 16; ++k) {
             const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
             umma_ss(tmem + (uint32_t)w * 128u, a0 + step, b0 + step, idesc_s, k > 0);
           }
           if constexpr (kInt4)
-            umma_ss(tmem + (uint32_t)w * 128u, make_smem_desc_plain(q_thin + (uint32_t)w * kThinBytes, 128u, 256u),
-                    make_smem_desc_plain(k_thin + (uint32_t)s * kThinBytes, 128u, 256u), idesc_s, true);
+            umma_ss(tmem + (uint32_t)w * 128u, qt + (uint64_t)(w * (kThinBytes >> 4)), kt + (uint64_t)(s * (kThinBytes >> 4)), idesc_s, true);
           umma_commit(&B.s_full[w]);
         };
         bool ok = true;
@@ -391,10 +432,10 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             ok = wait(&B.p_full[w], at) && (w == 1 || wait(&B.v_full[s], at >> 1));
             if (!ok) break;
             tc_fence_after();
+            const uint64_t b0 = v0 + (uint64_t)(s * (C::kTileBytesD >> 4));
 #pragma unroll
             for (int k = 0; k < 8; ++k)                 // 16 cache rows: 8 columns of P, 2048 bytes of V
-              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)w * 128u + (uint32_t)k * 8u,
-                      make_smem_desc(v_at + (uint32_t)s * C::kTileBytesD + (uint32_t)k * 2048u, 16384u, 1024u), idesc_o, j > 0 || k > 0);
+              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)w * 128u + (uint32_t)k * 8u, b0 + (uint64_t)(k * 128), idesc_o, j > 0 || k > 0);
             umma_commit(&B.pv_done[w]);
             if (w == 1) umma_commit(&B.v_empty[s]);
             if (j + 1 < tiles) {
@@ -489,12 +530,32 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         const float f = factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
         const int left = sees - (t0 + j) * kChTile;     // columns that the row sees
         const bool edge = sees_all < (t0 + j + 1) * kChTile;
+        // One pass: the weights of 32 columns at a time by the reference as it stands.  Where a row's logits have outgrown it, its sums, O and
+        // what this tile has of P so far are scaled down first (the first tile's reference comes about so, too).
+        const f32x2 ff = f2_make(f, f), cc = f2_make(cap_log2, cap_log2);
+        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
+        const float to_l = ex2_approx(-shift);
         float v[32];
-        float mx = -INFINITY;
 #pragma unroll 1
         for (int x = 0; x < 4; ++x) {
           tmem_ld32(s_tm + x * 32, v);
           tmem_wait_ld();
+          if (cap) {
+            float far = 0.f;
+#pragma unroll
+            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(v[y]), fabsf(v[y + 1]));
+            if (__all_sync(0xffffffffu, far * f <= 0.6f)) {
+#pragma unroll
+              for (int y = 0; y < 32; y += 2) {
+                const f32x2 z = capped_poly(f2_mul(f2_make(v[y], v[y + 1]), ff), cc);
+                v[y] = f2_lo(z);
+                v[y + 1] = f2_hi(z);
+              }
+            } else {
+#pragma unroll
+              for (int y = 0; y < 32; ++y) v[y] = capped(v[y] * f, cap_log2);
+            }
+          }
           if (edge) {
 #pragma unroll
             for (int y = 0; y < 32; ++y)
@@ -506,70 +567,27 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             m0 = fmax3(m0, v[y], v[y + 1]);
             m1 = fmax3(m1, v[y + 2], v[y + 3]);
           }
-          mx = fmax3(mx, fmax3(m0, v[30], v[31]), m1);
-        }
-        mx *= f;                                        // (the factor is positive: the largest stays the largest)
-        if (cap && mx != -INFINITY) mx = capped(mx, cap_log2);
-        mx += shift;
-        float rescale = 1.f;
-        if (mx > ref + kChSlack) {                      // O is rescaled only when the weights would grow past 2^kChSlack
-          rescale = ex2_approx(ref - (mx - kChStart));  // ref = -inf gives 0
-          ref = mx - kChStart;
-          l *= rescale;
-        }
-        if (j > 0 && __any_sync(0xffffffffu, rescale != 1.f)) {   // (the products of the tile before have ended: S's came after them)
-#pragma unroll
-          for (int x = 0; x < kD / 32; ++x) {
-            float v[32];
-            tmem_ld32(o_tm + x * 32, v);
-            tmem_wait_ld();
-            uint32_t bits[32];
-#pragma unroll
-            for (int y = 0; y < 32; ++y) bits[y] = __float_as_uint(v[y] * rescale);
-            tmem_st16(o_tm + x * 32, bits);
-            tmem_st16(o_tm + x * 32 + 16, bits + 16);
-          }
-        }
-        const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
-        const f32x2 minus_m = f2_make(-m_use, -m_use), ff = f2_make(f, f), cc = f2_make(cap_log2, cap_log2);
-        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
-#pragma unroll 1
-        for (int x = 0; x < 4; ++x) {
-          float* const u = v;
-          tmem_ld32(s_tm + x * 32, v);
-          tmem_wait_ld();
-          if (cap) {
-            float far = 0.f;
-#pragma unroll
-            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(u[y]), fabsf(u[y + 1]));
-            if (!edge && __all_sync(0xffffffffu, far * f <= 0.6f)) {
-#pragma unroll
-              for (int y = 0; y < 32; y += 2) {
-                const f32x2 z = capped_poly(f2_mul(f2_make(u[y], u[y + 1]), ff), cc, minus_m);
-                u[y] = f2_lo(z);
-                u[y + 1] = f2_hi(z);
-              }
-            } else {
-#pragma unroll
-              for (int y = 0; y < 32; ++y) u[y] = capped(u[y] * f, cap_log2) - m_use;
+          const float mx = fmaf(fmaxf(fmax3(m0, v[30], v[31]), m1), cap ? 1.f : f, shift);   // (the factor is positive)
+          if (__any_sync(0xffffffffu, mx > ref + kChSlack)) {
+            float down = 1.f;
+            if (mx > ref + kChSlack) {
+              const float next = ceilf(mx) - kChStart;
+              down = ex2_approx(ref - next);            // ref = -inf gives 0
+              ref = next;
             }
-          } else {
-#pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-              const f32x2 z = f2_fma(f2_make(u[y], u[y + 1]), ff, minus_m);
-              u[y] = f2_lo(z);
-              u[y + 1] = f2_hi(z);
-            }
+            l *= down;
+            sum0 = f2_mul(sum0, f2_make(down, down));
+            sum1 = f2_mul(sum1, f2_make(down, down));
+            rescale(o_tm, j > 0 ? kD : 0, down);        // (the products of the tile before have ended: S's came after them)
+            rescale_pairs<kInt4>(s_tm, x, down);
           }
-          if (edge) {
-#pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (x * 32 + y >= left) u[y] = -INFINITY;
-          }
+          const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
+          const f32x2 minus_m = f2_make(-m_use, -m_use), f1 = cap ? f2_make(1.f, 1.f) : ff;
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 4) {
-            const float e0 = ex2_approx(u[y]), e1 = ex2_approx(u[y + 1]), e2 = ex2_approx(u[y + 2]), e3 = ex2_approx(u[y + 3]);
+            const f32x2 a0 = f2_fma(f2_make(v[y], v[y + 1]), f1, minus_m), a1 = f2_fma(f2_make(v[y + 2], v[y + 3]), f1, minus_m);
+            const float e0 = ex2_approx(f2_lo(a0)), e1 = ex2_approx(f2_hi(a0)), e2 = ex2_approx(f2_lo(a1)), e3 = ex2_approx(f2_hi(a1));
             sum0 = f2_add(sum0, f2_make(e0, e1));
             sum1 = f2_add(sum1, f2_make(e2, e3));
             p[y / 2] = kInt4 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
@@ -578,7 +596,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           tmem_st16(s_tm + x * 16, p);                  // P where S has been read already
         }
         sum0 = f2_add(sum0, sum1);
-        l = fmaf(f2_lo(sum0) + f2_hi(sum0), ex2_approx(-shift), l);
+        l = fmaf(f2_lo(sum0) + f2_hi(sum0), to_l, l);
         tmem_wait_st();
         tc_fence_before();
         mbar_arrive(&B.p_full[w]);
