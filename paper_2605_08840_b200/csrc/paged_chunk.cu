@@ -39,7 +39,7 @@ constexpr int kInfo = 4;                     // tiles whose factors are kept: th
 constexpr float kChStart = 5.f, kChSlack = 13.f;
 
 struct ChunkBarriers {
-  uint64_t q_full[2], s_full[2], p_full[2], pv_done[2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
+  uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
 };
 
 // Row `row`, 16-byte chunk `chunk` of a 16-bit operand tile of 128 rows: boxes of [128 rows x 64 elements], 128-byte swizzle.
@@ -68,17 +68,17 @@ __device__ __forceinline__ void operands_of(uint32_t w, uint32_t s, uint32_t s16
   sts128(to, hfma2(s, w & 0x000F000Fu, l), hfma2(s16, w & 0x00F000F0u, l), hfma2(s, w8 & 0x000F000Fu, l), hfma2(s16, w8 & 0x00F000F0u, l));
 }
 
-// cap * tanh(t) in log2 units: c = cap * log2(e).
-__device__ __forceinline__ f32x2 capped_poly(f32x2 t, f32x2 c) {
+// tanh(t) for |t| <= 0.6.
+__device__ __forceinline__ f32x2 tanh_near(f32x2 t) {
   const f32x2 z = f2_mul(t, t);
   f32x2 p = f2_make(0.0154755134f, 0.0154755134f);
   p = f2_fma(p, z, f2_make(-0.0521015525f, -0.0521015525f));
   p = f2_fma(p, z, f2_make(0.133101761f, 0.133101761f));
   p = f2_fma(p, z, f2_make(-0.333323091f, -0.333323091f));
   p = f2_fma(p, z, f2_make(0.99999994f, 0.99999994f));
-  return f2_mul(f2_mul(p, t), c);
+  return f2_mul(p, t);
 }
-__device__ __forceinline__ float capped(float t, float c) { return fmaf(-2.f * c, rcp_approx(1.f + ex2_approx(t * 2.f * kLog2e)), c); }
+__device__ __forceinline__ float tanh_any(float t) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(t * 2.f * kLog2e)), 1.f); }
 
 // Row `row` of an operand 16 elements deep, without swizzle: 8 rows of 16 bytes together, both halves of a row 128 bytes apart.
 constexpr uint32_t kThinBytes = 128 * 32;
@@ -154,9 +154,11 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(&B.q_full[i], 128);
-      mbar_init(&B.s_full[i], 1);
-      mbar_init(&B.p_full[i], 128);
-      mbar_init(&B.pv_done[i], 1);
+      for (int half = 0; half < 2; ++half) {
+        mbar_init(&B.s_full[i][half], 1);
+        mbar_init(&B.p_full[i][half], 128);
+        mbar_init(&B.pv_done[i][half], 1);
+      }
       mbar_init(&B.k_full[i], kFetch);
       mbar_init(&B.k_empty[i], 1);
       mbar_init(&B.v_full[i], kFetch);
@@ -402,50 +404,52 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       // ---------------- the products, by one thread ----------------
       const int tiles = u.tiles, done = u.done, nth = u.nth;
       if (warp == kSoftmaxWarps + kFetchWarps && tiles > 0 && elect_one()) {
-        constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 128, false) : make_idesc_bf16(128, 128, false);
+        constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 64, false) : make_idesc_bf16(128, 64, false);
         constexpr uint32_t idesc_o = kInt4 ? make_idesc_f16(128, kD, true) : make_idesc_bf16(128, kD, true);
         // descriptors count 16-byte units
         const uint64_t q0 = kmajor_desc(q_at), k0 = kmajor_desc(k_at), v0 = make_smem_desc(v_at, 16384u, 1024u);
         const uint64_t qt = make_smem_desc_plain(q_thin, 128u, 256u), kt = make_smem_desc_plain(k_thin, 128u, 256u);
-        auto qk = [&](int w, int s) {
-          const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4));
+        auto qk = [&](int w, int half, int s) {
+          const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4) + half * (8192 >> 4));
+          const uint32_t to = tmem + (uint32_t)(w * 128 + half * 64);
 #pragma unroll
           for (int k = 0; k < kD / 16; ++k) {
             const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
-            umma_ss(tmem + (uint32_t)w * 128u, a0 + step, b0 + step, idesc_s, k > 0);
+            umma_ss(to, a0 + step, b0 + step, idesc_s, k > 0);
           }
           if constexpr (kInt4)
-            umma_ss(tmem + (uint32_t)w * 128u, qt + (uint64_t)(w * (kThinBytes >> 4)), kt + (uint64_t)(s * (kThinBytes >> 4)), idesc_s, true);
-          umma_commit(&B.s_full[w]);
+            umma_ss(to, qt + (uint64_t)(w * (kThinBytes >> 4)), kt + (uint64_t)(s * (kThinBytes >> 4) + half * (2048 >> 4)), idesc_s, true);
+          umma_commit(&B.s_full[w][half]);
         };
         bool ok = true;
-        for (int w = 0; w < 2 && ok; ++w) {
-          ok = wait(&B.q_full[w], nth) && (w == 1 || wait(&B.k_full[done & 1], done >> 1));
+        for (int x = 0; x < 4 && ok; ++x) {
+          if (x < 2) ok = wait(&B.q_full[x], nth) && (x == 1 || wait(&B.k_full[done & 1], done >> 1));
           if (!ok) break;
           tc_fence_after();
-          qk(w, done & 1);
+          qk(x & 1, x >> 1, done & 1);
         }
         if (ok) umma_commit(&B.k_empty[done & 1]);
-        for (int j = 0; j < tiles && ok; ++j) {
-          const int at = done + j, s = at & 1;
-          for (int w = 0; w < 2; ++w) {
-            ok = wait(&B.p_full[w], at) && (w == 1 || wait(&B.v_full[s], at >> 1));
+        // Steps x = 4 j + 2 half + w: P V of step x, then S of step x + 3, in whose place are the weights that step x - 1 reads.
+        for (int x = 0; x <= 4 * tiles && ok; ++x) {
+          if (x < 4 * tiles) {
+            const int w = x & 1, half = x >> 1 & 1, at = done + (x >> 2), s = at & 1;
+            ok = wait(&B.p_full[w][half], at) && ((x & 3) > 0 || wait(&B.v_full[s], at >> 1));
             if (!ok) break;
             tc_fence_after();
-            const uint64_t b0 = v0 + (uint64_t)(s * (C::kTileBytesD >> 4));
+            const uint64_t b0 = v0 + (uint64_t)(s * (C::kTileBytesD >> 4) + half * 512);
 #pragma unroll
-            for (int k = 0; k < 8; ++k)                 // 16 cache rows: 8 columns of P, 2048 bytes of V
-              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)w * 128u + (uint32_t)k * 8u, b0 + (uint64_t)(k * 128), idesc_o, j > 0 || k > 0);
-            umma_commit(&B.pv_done[w]);
-            if (w == 1) umma_commit(&B.v_empty[s]);
-            if (j + 1 < tiles) {
-              // S of the next tile takes the place of P, which the products just issued still read
-              ok = (w == 1 || wait(&B.k_full[(at + 1) & 1], (at + 1) >> 1)) && wait(&B.pv_done[w], at);
-              if (!ok) break;
-              tc_fence_after();
-              qk(w, (at + 1) & 1);
-              if (w == 1) umma_commit(&B.k_empty[(at + 1) & 1]);
-            }
+            for (int k = 0; k < 4; ++k)                 // 16 cache rows: 8 columns of P, 2048 bytes of V
+              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)(w * 128 + half * 64 + k * 8), b0 + (uint64_t)(k * 128), idesc_o, x > 1 || k > 0);
+            umma_commit(&B.pv_done[w][half]);
+            if ((x & 3) == 3) umma_commit(&B.v_empty[s]);
+          }
+          const int y = x - 1, at1 = done + (y >> 2) + 1;
+          if (y >= 0 && y < 4 * (tiles - 1)) {
+            ok = ((y & 3) > 0 || wait(&B.k_full[at1 & 1], at1 >> 1)) && wait(&B.pv_done[y & 1][y >> 1 & 1], at1 - 1);
+            if (!ok) break;
+            tc_fence_after();
+            qk(y & 1, y >> 1 & 1, at1 & 1);
+            if ((y & 3) == 3) umma_commit(&B.k_empty[at1 & 1]);
           }
         }
         if (!ok) {   // nothing may still write tensor memory, or arrive, when the CTA goes
@@ -516,29 +520,30 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       }
       mbar_arrive(&B.q_full[w]);
       const bool cap = c.softcap > 0.f;
-      const float cap_log2 = c.softcap * kLog2e;
       const float factor = (cap ? c.scale / c.softcap : c.scale * kLog2e) * unscale;   // to the tanh's argument, or to log2 units
       float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
       const int sees_all = __reduce_min_sync(0xffffffffu, sees);   // what every row of the warp sees
       bool ok = true;
-      for (int j = 0; j < tiles; ++j) {
-        const int at = done + j;
+      for (int j2 = 0; j2 < 2 * tiles; ++j2) {
+        const int j = j2 >> 1, half = j2 & 1, at = done + j;
         // the waits' verdict is a warp's: tensor memory is read by whole warps
-        ok = __all_sync(0xffffffffu, wait(&B.s_full[w], at));
+        ok = ok && __all_sync(0xffffffffu, wait(&B.s_full[w][half], at));
         if (!ok) break;
         tc_fence_after();
+        const uint32_t s_half = s_tm + (uint32_t)half * 64u;
         const float f = factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
-        const int left = sees - (t0 + j) * kChTile;     // columns that the row sees
-        const bool edge = sees_all < (t0 + j + 1) * kChTile;
+        const int left = sees - (t0 + j) * kChTile - half * 64;     // columns that the row sees
+        const bool edge = sees_all < (t0 + j) * kChTile + half * 64 + 64;
         // One pass: the weights of 32 columns at a time by the reference as it stands.  Where a row's logits have outgrown it, its sums, O and
-        // what this tile has of P so far are scaled down first (the first tile's reference comes about so, too).
-        const f32x2 ff = f2_make(f, f), cc = f2_make(cap_log2, cap_log2);
+        // what this half has of P so far are scaled down first (the first tile's reference comes about so, too).
+        const float to_log2 = cap ? c.softcap * kLog2e : f;
+        const f32x2 ff = f2_make(f, f), f1 = f2_make(to_log2, to_log2);
         f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
         const float to_l = ex2_approx(-shift);
         float v[32];
 #pragma unroll 1
-        for (int x = 0; x < 4; ++x) {
-          tmem_ld32(s_tm + x * 32, v);
+        for (int x = 0; x < 2; ++x) {
+          tmem_ld32(s_half + x * 32, v);
           tmem_wait_ld();
           if (cap) {
             float far = 0.f;
@@ -547,13 +552,13 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             if (__all_sync(0xffffffffu, far * f <= 0.6f)) {
 #pragma unroll
               for (int y = 0; y < 32; y += 2) {
-                const f32x2 z = capped_poly(f2_mul(f2_make(v[y], v[y + 1]), ff), cc);
+                const f32x2 z = tanh_near(f2_mul(f2_make(v[y], v[y + 1]), ff));
                 v[y] = f2_lo(z);
                 v[y + 1] = f2_hi(z);
               }
             } else {
 #pragma unroll
-              for (int y = 0; y < 32; ++y) v[y] = capped(v[y] * f, cap_log2);
+              for (int y = 0; y < 32; ++y) v[y] = tanh_any(v[y] * f);
             }
           }
           if (edge) {
@@ -567,7 +572,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             m0 = fmax3(m0, v[y], v[y + 1]);
             m1 = fmax3(m1, v[y + 2], v[y + 3]);
           }
-          const float mx = fmaf(fmaxf(fmax3(m0, v[30], v[31]), m1), cap ? 1.f : f, shift);   // (the factor is positive)
+          const float mx = fmaf(fmaxf(fmax3(m0, v[30], v[31]), m1), to_log2, shift);   // (the factor is positive)
           if (__any_sync(0xffffffffu, mx > ref + kChSlack)) {
             float down = 1.f;
             if (mx > ref + kChSlack) {
@@ -578,11 +583,15 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             l *= down;
             sum0 = f2_mul(sum0, f2_make(down, down));
             sum1 = f2_mul(sum1, f2_make(down, down));
-            rescale(o_tm, j > 0 ? kD : 0, down);        // (the products of the tile before have ended: S's came after them)
-            rescale_pairs<kInt4>(s_tm, x, down);
+            if (j2 > 0) {                               // the products of the half before may still be adding to O
+              ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][half ^ 1], half ? at : at - 1));
+              tc_fence_after();
+              if (ok) rescale(o_tm, kD, down);
+            }
+            rescale_pairs<kInt4>(s_half, x, down);
           }
           const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
-          const f32x2 minus_m = f2_make(-m_use, -m_use), f1 = cap ? f2_make(1.f, 1.f) : ff;
+          const f32x2 minus_m = f2_make(-m_use, -m_use);
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 4) {
@@ -593,16 +602,16 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             p[y / 2] = kInt4 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
             p[y / 2 + 1] = kInt4 ? pack_f16x2(e2, e3) : pack_bf16x2(e2, e3);
           }
-          tmem_st16(s_tm + x * 16, p);                  // P where S has been read already
+          tmem_st16(s_half + x * 16, p);                // P where S has been read already
         }
         sum0 = f2_add(sum0, sum1);
         l = fmaf(f2_lo(sum0) + f2_hi(sum0), to_l, l);
         tmem_wait_st();
         tc_fence_before();
-        mbar_arrive(&B.p_full[w]);
+        mbar_arrive(&B.p_full[w][half]);
       }
       // ---- the row's result ----
-      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], done + tiles - 1));
+      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][1], done + tiles - 1));
       if (ok) {
         tc_fence_after();
         const bool whole = piece.whole != 0, some = l > 0.f && live;
