@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
 #pragma unroll
             for (int z = 0; z < per_row; ++z) {
               const int r = z * (32 / per_row) + lane / per_row, place = __shfl_sync(0xffffffffu, own, r);
-              copy16(operand_at(to, row_of(x) - lane + r, y), (v ? c.V : c.K) + (long long)(place >= 0 ? place : 0) * c.block_bytes + (r & 15) * (2 * kD) + 16 * y,
+              copy16(operand_at(to, row_of(x) - lane + r, y), (v ? c.V : c.K) + (size_t)(unsigned int)(place >= 0 ? place : 0) * (32u * kD) + (r & 15) * (2 * kD) + 16 * y,
                      place >= 0);
             }
             page[x] = page_of(j + 1, x);
@@ -542,7 +542,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         const float to_l = ex2_approx(-shift);
         float v[32];
 #pragma unroll 1
-        for (int x = 0; x < 2; ++x) {
+        for (int x = 0; x < 2;) {
           tmem_ld32(s_half + x * 32, v);
           tmem_wait_ld();
           if (cap) {
@@ -589,6 +589,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
               if (ok) rescale(o_tm, kD, down);
             }
             rescale_pairs<kInt4>(s_half, x, down);
+            continue;                                   // (the logits again: kept across the calls, each would be copied every time)
           }
           const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
           const f32x2 minus_m = f2_make(-m_use, -m_use);
@@ -603,6 +604,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             p[y / 2 + 1] = kInt4 ? pack_f16x2(e2, e3) : pack_bf16x2(e2, e3);
           }
           tmem_st16(s_half + x * 16, p);                // P where S has been read already
+          ++x;
         }
         sum0 = f2_add(sum0, sum1);
         l = fmaf(f2_lo(sum0) + f2_hi(sum0), to_l, l);
