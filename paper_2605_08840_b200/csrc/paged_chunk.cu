@@ -249,22 +249,28 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       for (int x = 0; x < kPieces; ++x) page[x] = page_of(0, x);
       if constexpr (kInt4) {
         uint32_t codes[kPieces][kHalf], params[kPieces][kG];   // half a row's codes; (step, offset) per group
+        unsigned short step_of[kPieces][kG], offset_of[kPieces][kG];
+        bool there[kPieces];
         int a_ref = 0;
         auto load = [&](int j) {                        // tile j's, and the next one's pages
 #pragma unroll
           for (int x = 0; x < kPieces; ++x) {
+            // Rows that are not there read block 0 in their place and have no steps: nothing here waits for what it loads, which a
+            // branch around the loads, or steps and offsets put together here, would do once per piece.
             const int place = place_of(j, x, page[x]), q = lane & 15;
-            const bool there = place >= 0;
-            const uint8_t* block = (is_v(x) ? c.V : c.K) + (long long)(there ? place : 0) * c.block_bytes;
+            there[x] = place >= 0;
+            const bool v = is_v(x);
+            const uint8_t* block = (v ? c.V : c.K) + (size_t)(unsigned int)max(place, 0) * (unsigned int)c.block_bytes;
 #pragma unroll
             for (int y = 0; y < kHalf / 4; ++y) {
-              const uint4 w = there ? reinterpret_cast<const uint4*>(block + q * (kD / 2) + half_of(x) * (kD / 4))[y] : make_uint4(0u, 0u, 0u, 0u);
+              const uint4 w = reinterpret_cast<const uint4*>(block + q * (kD / 2) + half_of(x) * (kD / 4))[y];
               codes[x][4 * y] = w.x; codes[x][4 * y + 1] = w.y; codes[x][4 * y + 2] = w.z; codes[x][4 * y + 3] = w.w;
             }
 #pragma unroll
             for (int g = 0; g < kG; ++g) {
               const unsigned short* p = reinterpret_cast<const unsigned short*>(block + int4_params(kD, g, q));
-              params[x][g] = there ? p[0] | (uint32_t)p[4] << 16 : 0u;
+              step_of[x][g] = p[0];
+              offset_of[x][g] = p[4];
             }
           }
 #pragma unroll
@@ -279,6 +285,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           for (int x = 0; x < kPieces; ++x)
 #pragma unroll
             for (int g = 0; g < kG; ++g) {
+              params[x][g] = there[x] ? step_of[x][g] | (uint32_t)offset_of[x][g] << 16 : 0u;
               const float m = fmaxf(lower(params[x][g]), fabsf(upper(params[x][g])) * (is_v(x) ? 0x1p-25f : 0x1p-16f));
               if (is_v(x)) most[1] = fmaxf(most[1], m);
               else most[0] = fmaxf(most[0], m);
@@ -307,7 +314,6 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             const int r = row_of(x);
             if (!is_v(x)) {
               if (!ok) continue;
-              uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};   // dims 3 g ..: the parts that meet sum(q)'s
 #pragma unroll
               for (int g = 0; g < kG; ++g) {
                 const float step = lower(params[x][g]) * power_of_two(ka);
@@ -317,15 +323,18 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
 #pragma unroll
                   for (int q = 0; q < 2; ++q)           // word (2 half + q) * kWords + m of the row: dims 32 m + 8 (2 half + q) ..
                     operands_of(codes[x][q * kWords + m], s1, s16, l, operand_at(k_at + (uint32_t)s * C::kTileBytesD, r, 4 * m + 2 * half_of(x) + q));
-                // hi, lo, hi against sum(q)'s hi, hi, lo; times 2^8, as sum(q)'s are times 2^-8
-                const uint32_t mid = split_f16(fmaf(8.f, lower(params[x][g]), upper(params[x][g])) * power_of_two(ka - 16));
-#pragma unroll
-                for (int y = 0; y < 3; ++y) {
-                  const uint32_t part = y == 1 ? mid >> 16 : mid & 0xFFFFu;
-                  thin[(3 * g + y) >> 1] |= (3 * g + y) & 1 ? part << 16 : part;
-                }
               }
               if (half_of(x) == 0) {
+                uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};   // dims 3 g ..: hi, lo, hi against sum(q)'s hi, hi, lo
+#pragma unroll
+                for (int g = 0; g < kG; ++g) {          // times 2^8, as sum(q)'s are times 2^-8
+                  const uint32_t mid = split_f16(fmaf(8.f, lower(params[x][g]), upper(params[x][g])) * power_of_two(ka - 16));
+#pragma unroll
+                  for (int y = 0; y < 3; ++y) {
+                    const uint32_t part = y == 1 ? mid >> 16 : mid & 0xFFFFu;
+                    thin[(3 * g + y) >> 1] |= (3 * g + y) & 1 ? part << 16 : part;
+                  }
+                }
                 const uint32_t to = thin_at(k_thin + (uint32_t)s * kThinBytes, r);
                 sts128(to, thin[0], thin[1], thin[2], thin[3]);
                 sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
@@ -538,73 +547,74 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         // what this half has of P so far are scaled down first (the first tile's reference comes about so, too).
         const float to_log2 = cap ? c.softcap * kLog2e : f;
         const f32x2 ff = f2_make(f, f), f1 = f2_make(to_log2, to_log2);
-        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
         const float to_l = ex2_approx(-shift);
-        float v[32];
-#pragma unroll 1
-        for (int x = 0; x < 2;) {
-          tmem_ld32(s_half + x * 32, v);
+        float v[64];
+        for (;;) {
+          tmem_ld32(s_half, v);
+          tmem_ld32(s_half + 32u, v + 32);
           tmem_wait_ld();
           if (cap) {
-            float far = 0.f;
+            float far0 = 0.f, far1 = 0.f;
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) far = fmax3(far, fabsf(v[y]), fabsf(v[y + 1]));
-            if (__all_sync(0xffffffffu, far * f <= 0.6f)) {
+            for (int y = 0; y < 64; y += 4) {
+              far0 = fmax3(far0, fabsf(v[y]), fabsf(v[y + 1]));
+              far1 = fmax3(far1, fabsf(v[y + 2]), fabsf(v[y + 3]));
+            }
+            if (__all_sync(0xffffffffu, fmaxf(far0, far1) * f <= 0.6f)) {
 #pragma unroll
-              for (int y = 0; y < 32; y += 2) {
+              for (int y = 0; y < 64; y += 2) {
                 const f32x2 z = tanh_near(f2_mul(f2_make(v[y], v[y + 1]), ff));
                 v[y] = f2_lo(z);
                 v[y + 1] = f2_hi(z);
               }
             } else {
 #pragma unroll
-              for (int y = 0; y < 32; ++y) v[y] = tanh_any(v[y] * f);
+              for (int y = 0; y < 64; ++y) v[y] = tanh_any(v[y] * f);
             }
           }
           if (edge) {
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-              if (x * 32 + y >= left) v[y] = -INFINITY;
+            for (int y = 0; y < 64; ++y)
+              if (y >= left) v[y] = -INFINITY;
           }
-          float m0 = v[0], m1 = v[1];
+          float m[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-          for (int y = 2; y < 30; y += 4) {
-            m0 = fmax3(m0, v[y], v[y + 1]);
-            m1 = fmax3(m1, v[y + 2], v[y + 3]);
+          for (int y = 4; y < 60; y += 8)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) m[z] = fmax3(m[z], v[y + 2 * z], v[y + 2 * z + 1]);
+          m[0] = fmax3(m[0], v[60], v[61]);
+          m[1] = fmax3(m[1], v[62], v[63]);
+          const float mx = fmaf(fmaxf(fmax3(m[0], m[1], m[2]), m[3]), to_log2, shift);   // (the factor is positive)
+          if (!__any_sync(0xffffffffu, mx > ref + kChSlack)) break;
+          float down = 1.f;
+          if (mx > ref + kChSlack) {
+            const float next = ceilf(mx) - kChStart;
+            down = ex2_approx(ref - next);              // ref = -inf gives 0
+            ref = next;
           }
-          const float mx = fmaf(fmaxf(fmax3(m0, v[30], v[31]), m1), to_log2, shift);   // (the factor is positive)
-          if (__any_sync(0xffffffffu, mx > ref + kChSlack)) {
-            float down = 1.f;
-            if (mx > ref + kChSlack) {
-              const float next = ceilf(mx) - kChStart;
-              down = ex2_approx(ref - next);            // ref = -inf gives 0
-              ref = next;
-            }
-            l *= down;
-            sum0 = f2_mul(sum0, f2_make(down, down));
-            sum1 = f2_mul(sum1, f2_make(down, down));
-            if (j2 > 0) {                               // the products of the half before may still be adding to O
-              ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][half ^ 1], half ? at : at - 1));
-              tc_fence_after();
-              if (ok) rescale(o_tm, kD, down);
-            }
-            rescale_pairs<kInt4>(s_half, x, down);
-            continue;                                   // (the logits again: kept across the calls, each would be copied every time)
-          }
-          const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
-          const f32x2 minus_m = f2_make(-m_use, -m_use);
+          l *= down;
+          if (j2 > 0) {                                 // the products of the half before may still be adding to O
+            ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][half ^ 1], half ? at : at - 1));
+            tc_fence_after();
+            if (ok) rescale(o_tm, kD, down);
+          }                                             // (then the logits again: kept across the call, each would be copied every time)
+        }
+        const float m_use = (ref == -INFINITY ? 0.f : ref) - shift;   // only logits of -inf so far: they weigh nothing
+        const f32x2 minus_m = f2_make(-m_use, -m_use);
+        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+        for (int x = 0; x < 64; x += 32) {
           uint32_t p[16];
 #pragma unroll
           for (int y = 0; y < 32; y += 4) {
-            const f32x2 a0 = f2_fma(f2_make(v[y], v[y + 1]), f1, minus_m), a1 = f2_fma(f2_make(v[y + 2], v[y + 3]), f1, minus_m);
+            const f32x2 a0 = f2_fma(f2_make(v[x + y], v[x + y + 1]), f1, minus_m), a1 = f2_fma(f2_make(v[x + y + 2], v[x + y + 3]), f1, minus_m);
             const float e0 = ex2_approx(f2_lo(a0)), e1 = ex2_approx(f2_hi(a0)), e2 = ex2_approx(f2_lo(a1)), e3 = ex2_approx(f2_hi(a1));
             sum0 = f2_add(sum0, f2_make(e0, e1));
             sum1 = f2_add(sum1, f2_make(e2, e3));
             p[y / 2] = kInt4 ? pack_f16x2(e0, e1) : pack_bf16x2(e0, e1);
             p[y / 2 + 1] = kInt4 ? pack_f16x2(e2, e3) : pack_bf16x2(e2, e3);
           }
-          tmem_st16(s_half + x * 16, p);                // P where S has been read already
-          ++x;
+          tmem_st16(s_half + x / 2, p);                 // P where S has been read already
         }
         sum0 = f2_add(sum0, sum1);
         l = fmaf(f2_lo(sum0) + f2_hi(sum0), to_l, l);
