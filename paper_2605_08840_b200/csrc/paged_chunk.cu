@@ -36,6 +36,11 @@ constexpr int kChThreads = (kSoftmaxWarps + kFetchWarps + 1) * 32;
 constexpr int kFetch = kFetchWarps * 32;
 constexpr int kInfo = 4;                     // tiles whose factors are kept: the fetching warps are two ahead of the softmax at most
 // log2 of the largest weight that a rescaling leaves, and of what it may grow to before the next one
+// tiles' worth of a CTA's beginning another unit
+#ifndef SNAP
+#define SNAP 2
+#endif
+constexpr int kChSnap = SNAP;
 constexpr float kChStart = 5.f, kChSlack = 13.f;
 
 struct ChunkBarriers {
@@ -124,6 +129,15 @@ template <bool kF16> __device__ __noinline__ void rescale_pairs(uint32_t at, int
   }
 }
 
+// Tiles that the last query row of a unit sees: those past them are nobody's business.
+__device__ __forceinline__ int unit_tiles(const PagedCache& c, int row_tiles, int unit) {
+  const int bh = unit / row_tiles, rho0 = (unit - bh * row_tiles) * kChRows, b = bh / c.Hkv, count = paged_count(c, b);
+  if (rho0 >= count * c.G) return 0;
+  const int i_last = (min(rho0 + kChRows, count * c.G) - 1) / c.G;
+  const int seen = paged_length(c, b, bh - b * c.Hkv) - (count - 1 - i_last);
+  return seen > 0 ? (seen + kChTile - 1) / kChTile : 0;
+}
+
 template <int kD, int kGroups> struct ChunkConfig {
   static constexpr bool kInt4 = kGroups > 0;
   static constexpr uint32_t kTileBytesD = 128u * kD * 2u;
@@ -140,7 +154,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   __shared__ __align__(8) ChunkBarriers B;
   __shared__ Piece piece_s;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_flag;
+  __shared__ int abort_flag, counted[kChThreads / 32];
   __shared__ float step_max[2][2][kFetchWarps];         // [tile & 1][K, V][warp]
   __shared__ volatile float k_factor[kInfo], v_shift[kInfo];   // per tile: the logits' factor, log2 of the weights'
   __shared__ volatile float o_factor[2];                // per piece: what O is multiplied with
@@ -173,11 +187,57 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   }
   grid_dependency_wait();
   grid_dependency_launch();
-  if (warp == 0) {
-    const Run run = find_run(c, a.row_tiles, kChTile, blockIdx.x, gridDim.x);
-    if (lane == 0) {
-      piece_s.run = run;
-      if (run.tile < run.end) piece_s.cut(c, a.row_tiles, kChTile);
+  auto tiles_of = [&](int unit) { return max(1, unit_tiles(c, a.row_tiles, unit)); };   // a unit without rows has its outputs written, too
+  {
+    // The CTA's run of tiles: every thread counts those of some units; the threads in whose units the run begins and ends say where.
+    const int units = c.batch * c.Hkv * a.row_tiles, per = (units + kChThreads - 1) / kChThreads;
+    const int u0 = min((int)threadIdx.x * per, units), u1 = min(u0 + per, units);
+    int sum = 0;
+    for (int u = u0; u < u1; ++u) sum += tiles_of(u);
+    int upto = sum, all = 0, first = 0;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += o;
+    }
+    if (lane == 31) counted[warp] = upto;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kChThreads / 32; ++x) {
+      first += x < warp ? counted[x] : 0;
+      all += counted[x];
+    }
+    first += upto - sum;
+    const Deal deal(all, gridDim.x, kChSnap);
+    const int x = blockIdx.x;
+    if (threadIdx.x == 0) {
+      if (x >= deal.ctas) piece_s.run = Run{0, 0, 0, 0, 1};
+      else if (x + 1 == deal.ctas) piece_s.run.end = all;
+    }
+    for (int k = 0; k < 2; ++k) {
+      if (x + k >= deal.ctas) break;
+      const int want = deal.start(x + k);
+      if (want < first || want >= first + sum) continue;
+      int u = u0, f = first, t = tiles_of(u);
+      while (want >= f + t) {
+        f += t;
+        t = tiles_of(++u);
+      }
+      const int boundary = f + deal.moved(want - f, t);
+      if (k == 1) {
+        piece_s.run.end = boundary;
+      } else {
+        piece_s.run.tile = boundary;
+        piece_s.run.entry = u;
+        piece_s.run.first = f;
+        piece_s.run.tiles = t;
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const Run run = piece_s.run;
+      if (run.tile < run.end) piece_s.cut(1, tiles_of);
+      a.begins[blockIdx.x] = run.tile < run.end ? make_int2(piece_s.unit, piece_s.t0) : make_int2(-1, 0);
     }
   }
   tc_fence_before();
@@ -195,12 +255,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     int done = 0;
     for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
     const int unit = piece.unit, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kChRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
-    const int R = c.n_tokens * c.G, n = paged_length(c, b, h), count = paged_count(c, b), t0 = piece.t0;
-    // rows that the unit's last query row sees; tiles past them are nobody's business (a unit whose rows see nothing takes one all the same)
-    const int i_last = min(min(R, rho0 + kChRows) - 1, count * c.G - 1) / c.G;
-    const int seen = count > 0 && rho0 < count * c.G ? n - (count - 1 - i_last) : 0;
-    const int t_seen = seen > 0 ? (seen + kChTile - 1) / kChTile : 0;
-    const int tiles = max(0, min(piece.t1, t_seen) - t0);
+    const int n = paged_length(c, b, h), count = paged_count(c, b), t0 = piece.t0, tiles = min(piece.t1, unit_tiles(c, a.row_tiles, unit)) - t0;
     if (threadIdx.x == 0 && t0 == 0) check_length(c, b, h);
     part(Unit{b, h, rho0, n, count, t0, tiles, done, nth});
     __syncwarp();
@@ -211,7 +266,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     if (threadIdx.x == 0) {
       piece_s.run.tile += piece_s.t1 - piece_s.t0;
       if (stop) piece_s.run.tile = piece_s.run.end;
-      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, kChTile);
+      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(1, tiles_of);
     }
     __syncthreads();
     }
@@ -478,52 +533,50 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       const uint32_t s_tm = tmem + row_lane + (uint32_t)w * 128u, o_tm = tmem + row_lane + kO + (uint32_t)w * kD;
       float unscale = 1.f;
       if (tiles > 0) {
-        // the row into shared memory
-        const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn;
-        uint4 raw[kD / 8];
-#pragma unroll
-        for (int x = 0; x < kD / 8; ++x) raw[x] = live ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+        // the warp's rows into shared memory, a row in kD / 8 lanes side by side
+        constexpr int kLanes = kD / 8, kRowsAtOnce = 32 / kLanes;
         const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
-        if constexpr (kInt4) {
-          float top = 0.f;
+        const int x = lane % kLanes, row0 = (warp & 3) * 32 + lane / kLanes;
+#pragma unroll 4
+        for (int z = 0; z < 32; z += kRowsAtOnce) {
+          const int row = row0 + z, rho_z = rho0 + w * 128 + row, i_z = rho_z / c.G, g_z = rho_z - i_z * c.G;
+          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g_z) * a.Q.sh + i_z * a.Q.sn;
+          const uint4 raw = rho_z < R && i_z < count ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+          if constexpr (kInt4) {
+            float v[8] = {lower(raw.x), upper(raw.x), lower(raw.y), upper(raw.y), lower(raw.z), upper(raw.z), lower(raw.w), upper(raw.w)};
+            float top = fmaxf(fmaxf(fmax3(fabsf(v[0]), fabsf(v[1]), fabsf(v[2])), fmax3(fabsf(v[3]), fabsf(v[4]), fabsf(v[5]))), fmaxf(fabsf(v[6]), fabsf(v[7])));
 #pragma unroll
-          for (int x = 0; x < kD / 8; ++x)
+            for (int off = 1; off < kLanes; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+            // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
+            int e = 141 - (int)(__float_as_uint(top) >> 23);
+            e = e < -100 ? -100 : e > 100 ? 100 : e;
+            const float scale = top < INFINITY ? power_of_two(e) : __uint_as_float(0x7FFFFFFFu);
+            const float back = __shfl_sync(0xffffffffu, power_of_two(-e), lane % kRowsAtOnce * kLanes);   // that of row z + lane % kRowsAtOnce
+            if (lane / kRowsAtOnce == z / kRowsAtOnce) unscale = back;
 #pragma unroll
-            for (int y = 0; y < 4; ++y) top = fmaxf(top, fmaxf(fabsf(lower((&raw[x].x)[y])), fabsf(upper((&raw[x].x)[y]))));
-          // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
-          int e = 141 - (int)(__float_as_uint(top) >> 23);
-          e = e < -100 ? -100 : e > 100 ? 100 : e;
-          const float scale = top < INFINITY ? power_of_two(e) : __uint_as_float(0x7FFFFFFFu);
-          unscale = power_of_two(-e);
-          uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+            for (int y = 0; y < 8; ++y) v[y] *= scale;
+            // dims in the order of K's operands
+            sts128(operand_at(tile, row, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
+            float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 #pragma unroll
-          for (int g2 = 0; g2 < kG; ++g2) {
-            float sum = 0.f;
+            for (int off = 1; off < kLanes / kG; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+            const uint32_t own = split_f16(sum * 0x1p-8f);
+            uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
 #pragma unroll
-            for (int x = g2 * (kD / 8 / kG); x < (g2 + 1) * (kD / 8 / kG); ++x) {
-              float v[8];
+            for (int g2 = 0; g2 < kG; ++g2) {
+              const uint32_t parts = __shfl_sync(0xffffffffu, own, lane / kLanes * kLanes + g2 * (kLanes / kG));
 #pragma unroll
-              for (int y = 0; y < 4; ++y) {
-                v[2 * y] = lower((&raw[x].x)[y]) * scale;
-                v[2 * y + 1] = upper((&raw[x].x)[y]) * scale;
+              for (int y = 0; y < 3; ++y) {
+                const uint32_t part = y == 2 ? parts >> 16 : parts & 0xFFFFu;
+                thin[(3 * g2 + y) >> 1] |= (3 * g2 + y) & 1 ? part << 16 : part;
               }
-              // dims in the order of K's operands
-              sts128(operand_at(tile, r, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
-              sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
             }
-            const uint32_t parts = split_f16(sum * 0x1p-8f);
-#pragma unroll
-            for (int x = 0; x < 3; ++x) {
-              const uint32_t part = x == 2 ? parts >> 16 : parts & 0xFFFFu;
-              thin[(3 * g2 + x) >> 1] |= (3 * g2 + x) & 1 ? part << 16 : part;
-            }
+            const uint32_t to = thin_at(q_thin + (uint32_t)w * kThinBytes, row);
+            if (x == 0) sts128(to, thin[0], thin[1], thin[2], thin[3]);
+            if (x == 1) sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+          } else {
+            sts128(operand_at(tile, row, x), raw.x, raw.y, raw.z, raw.w);
           }
-          const uint32_t to = thin_at(q_thin + (uint32_t)w * kThinBytes, r);
-          sts128(to, thin[0], thin[1], thin[2], thin[3]);
-          sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
-        } else {
-#pragma unroll
-          for (int x = 0; x < kD / 8; ++x) sts128(operand_at(tile, r, x), raw[x].x, raw[x].y, raw[x].z, raw[x].w);
         }
         fence_proxy_async_smem();
       }
@@ -628,24 +681,35 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         tc_fence_after();
         const bool whole = piece.whole != 0, some = l > 0.f && live;
         const float ofac = tiles > 0 ? o_factor[nth & 1] : 0.f, norm = whole ? (some ? ofac / l : 0.f) : ofac;
-        float* const part = a.part + (long long)(2 * blockIdx.x + (t0 == 0)) * kChRows * (kD + 2) + (w * 128 + r) * kD;
+        const bool nothing = tiles == 0 || (whole && !some);
+        float* const part = a.part + (long long)(2 * blockIdx.x + (t0 == 0)) * kChRows * (kD + 2);
         const long long row = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
-        auto emit = [&](int dim, float x0, float x1, float x2, float x3) {
-          if (whole) reinterpret_cast<uint2*>(a.out + row * kD + dim)[0] = make_uint2(pack_bf16x2(x0 * norm, x1 * norm), pack_bf16x2(x2 * norm, x3 * norm));
-          else reinterpret_cast<float4*>(part + dim)[0] = make_float4(x0 * norm, x1 * norm, x2 * norm, x3 * norm);
-        };
+        // By way of the warp's rows of Q's tile, which no product reads any more, for stores of whole rows: kD values of 16 bits at once,
+        // or fp32 ones in two turns.  16-byte chunk k of row r is at k ^ r.
+        constexpr int kChunks = kD / 8;
+        const uint32_t staged = q_at + (uint32_t)w * C::kTileBytesD + (uint32_t)(warp & 3) * (32u * 2u * kD);
+        const uint32_t mine = staged + (uint32_t)lane * (2u * kD);
+        for (int turn = 0; turn < (whole ? 1 : 2); ++turn) {
+          auto emit = [&](int dim, float x0, float x1, float x2, float x3) {
+            if (nothing) x0 = x1 = x2 = x3 = 0.f;
+            if (whole) {
+              const uint32_t to = mine + (uint32_t)(((dim / 8) ^ (lane & (kChunks - 1))) * 16 + (dim & 4) * 2);
+              asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to), "r"(pack_bf16x2(x0 * norm, x1 * norm)), "r"(pack_bf16x2(x2 * norm, x3 * norm)) : "memory");
+            } else if (dim / (kD / 2) == turn) {
+              sts128(mine + (uint32_t)(((dim % (kD / 2) / 4) ^ (lane & (kChunks - 1))) * 16), __float_as_uint(x0 * norm), __float_as_uint(x1 * norm),
+                     __float_as_uint(x2 * norm), __float_as_uint(x3 * norm));
+            }
+          };
 #pragma unroll
-        for (int x = 0; x < kD / 32; ++x) {
-          float v[32];
-          if (tiles > 0) {
-            tmem_ld32(o_tm + x * 32, v);
-            tmem_wait_ld();
-          }
-          if (tiles == 0 || (whole && !some)) {
+          for (int x = 0; x < kD / 32; ++x) {
+            float v[32];
+            if (tiles > 0) {
+              tmem_ld32(o_tm + x * 32, v);
+              tmem_wait_ld();
+            } else {
 #pragma unroll
-            for (int y = 0; y < 32; ++y) v[y] = 0.f;
-          }
-          if (rho < R) {
+              for (int y = 0; y < 32; ++y) v[y] = 0.f;
+            }
 #pragma unroll
             for (int y = 0; y < 4; ++y) {
               const float* o = v + 8 * y;
@@ -659,6 +723,18 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
               }
             }
           }
+          __syncwarp();
+          const int k = lane % kChunks, in_tile = w * 128 + (warp & 3) * 32;
+#pragma unroll 4
+          for (int z = 0; z < 32; z += 32 / kChunks) {
+            const int at = z + lane / kChunks;
+            const long long to = __shfl_sync(0xffffffffu, row, at);
+            if (rho0 + in_tile + at >= R) continue;
+            const uint4 u = lds128(staged + (uint32_t)at * (2u * kD) + (uint32_t)((k ^ (at & (kChunks - 1))) * 16));
+            if (whole) reinterpret_cast<uint4*>(a.out + to * kD)[k] = u;
+            else reinterpret_cast<uint4*>(part + (in_tile + at) * kD + turn * (kD / 2))[k] = u;
+          }
+          __syncwarp();
         }
         if (rho < R) {
           if (whole) {
@@ -675,58 +751,69 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   if (warp == kSoftmaxWarps + kFetchWarps) tmem_dealloc(tmem, 512);
 }
 
-// grid (units, 8), block 256: merges what several CTAs left of a unit, 32 rows per block, a row per kD / 4 threads at a time.
+// grid (CTAs of the kernel before, 32), block 256: merges what several of them left of a unit, a row per warp.  A unit is merged by the
+// blocks of the first CTA that began inside it.
 template <int kD>
-__global__ void __launch_bounds__(256) paged_chunk_combine_kernel(const __grid_constant__ PagedMmaArgs a, int grid) {
+__global__ void __launch_bounds__(256) paged_chunk_combine_kernel(const __grid_constant__ PagedMmaArgs a) {
   grid_dependency_wait();
   grid_dependency_launch();
-  __shared__ int run_s[2];
   const PagedCache& c = a.c;
-  const int unit = blockIdx.x, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kChRows + (int)blockIdx.y * 32, R = c.n_tokens * c.G;
-  if (rho0 >= R) return;
-  const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles, entry = unit / units, b = bh / c.Hkv, h = bh - b * c.Hkv;
-  if (threadIdx.x < 32) {
-    int before = 0, all = 0;
-    const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
-    for (int e = threadIdx.x; e < entries; e += 32) {
-      const int t = entry_tiles(c, e, kChTile) * units;
-      all += t;
-      if (e < entry) before += t;
-    }
-    all = __reduce_add_sync(0xffffffffu, all);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (threadIdx.x == 0) { run_s[0] = all; run_s[1] = before; }
-  }
-  const int tiles = entry_tiles(c, entry, kChTile), count = paged_count(c, b);
-  __syncthreads();
-  const Deal deal(run_s[0], grid);
-  const int u0 = run_s[1] + (unit - entry * units) * tiles;
-  const int x0 = deal.first_of(u0, tiles), pieces = deal.last_of(u0, tiles) - x0 + 1;
-  if (pieces == 1) return;
+  const int x = blockIdx.x, ctas = gridDim.x, lane = threadIdx.x & 31;
+  const int2 mine = __ldcg(a.begins + x);
+  if (mine.x < 0 || mine.y == 0) return;                // (the first CTA begins a unit: x > 0 from here on)
+  auto inside = [&](int y) {
+    const int2 o = __ldcg(a.begins + y);
+    return o.x == mine.x && o.y > 0;
+  };
+  if (inside(x - 1)) return;
+  const int unit = mine.x, bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv, count = paged_count(c, b);
+  const int row = (int)blockIdx.y * 8 + (threadIdx.x >> 5), rho = (unit - bh * a.row_tiles) * kChRows + row;
+  if (rho >= c.n_tokens * c.G) return;
   constexpr long long kSlot = kChRows * (kD + 2);
-  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0)) * kSlot; };
-  const int v = threadIdx.x % (kD / 4);
-  for (int k = threadIdx.x / (kD / 4); k < 32 && rho0 + k < R; k += 256 / (kD / 4)) {
-    const int row = (int)blockIdx.y * 32 + k;
-    float mm = -INFINITY, ll = 0.f;
-    for (int x = 0; x < pieces; ++x) mm = fmaxf(mm, __ldcg(reinterpret_cast<const float2*>(piece(x) + kChRows * kD) + row).x);
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int x = 0; x < pieces; ++x) {
-      const float2 ml = __ldcg(reinterpret_cast<const float2*>(piece(x) + kChRows * kD) + row);
-      const float4 o = __ldcg(reinterpret_cast<const float4*>(piece(x) + row * kD) + v);
-      if (ml.x == -INFINITY) continue;
-      const float f = ex2_approx(ml.x - mm);
-      fma4(acc, o, f);
-      ll = fmaf(ml.y, f, ll);
+  constexpr int kPer = kD / 32;
+  auto piece = [&](int k) { return a.part + (2ll * (x - 1 + k) + (k == 0)) * kSlot; };   // the CTA before began the unit
+  // 32 pieces at a time, a lane's (reference, sum) each
+  float mm = -INFINITY, ll = 0.f, acc[kPer] = {};
+  for (int base = 0;; base += 32) {
+    const int k = base + lane;
+    const bool some = k == 0 || (x - 1 + k < ctas && inside(x - 1 + k));
+    const int n = __popc(__ballot_sync(0xffffffffu, some));
+    const float2 ml = some ? __ldcg(reinterpret_cast<const float2*>(piece(k) + kChRows * kD) + row) : make_float2(-INFINITY, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    top = fmaxf(top, mm);
+    const float down = mm == -INFINITY ? 0.f : ex2_approx(mm - top), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+    mm = top;
+    float sum = ml.y * f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    ll = fmaf(ll, down, sum);
+#pragma unroll
+    for (int y = 0; y < kPer; ++y) acc[y] *= down;
+#pragma unroll 8
+    for (int y = 0; y < n; ++y) {
+      const float g = __shfl_sync(0xffffffffu, f, y);
+      const float* o = piece(base + y) + row * kD + kPer * lane;
+      float w[kPer];
+      if constexpr (kPer == 4) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+      } else {
+        const float2 u = __ldcg(reinterpret_cast<const float2*>(o));
+        w[0] = u.x; w[1] = u.y;
+      }
+#pragma unroll
+      for (int z = 0; z < kPer; ++z) acc[z] = g > 0.f ? fmaf(w[z], g, acc[z]) : acc[z];
     }
-    write_row<kD>(a, b, h, rho0 + k, count, v, acc, mm, ll);
+    if (n < 32) break;
   }
+  write_row<kD, kPer>(a, b, h, rho, count, lane, acc, mm, ll);
 }
 
 struct ChunkVariant {
   void (*kernel)(PagedMmaArgs);
-  void (*combine)(PagedMmaArgs, int);
+  void (*combine)(PagedMmaArgs);
   size_t smem;
 };
 template <int kD, int kGroups> ChunkVariant chunk_variant() {
@@ -772,7 +859,7 @@ bool paged_chunk_supported(const PagedCache& c) {
 }
 
 size_t paged_chunk_bytes(const PagedCache& c, int sm_count) {
-  return (size_t)2 * chunk_ctas(sm_count) * kChRows * (c.d + 2) * sizeof(float);
+  return (size_t)chunk_ctas(sm_count) * (2 * kChRows * (c.d + 2) * sizeof(float) + sizeof(int2));
 }
 
 cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count, long long wait_limit,
@@ -782,11 +869,11 @@ cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out
   PagedMmaArgs a{};
   a.c = c; a.Q = Q; a.out = (__nv_bfloat16*)out; a.lse = lse; a.part = part; a.wait_limit = wait_limit;
   a.row_tiles = (int)(((long long)c.n_tokens * c.G + kChRows - 1) / kChRows);
-  const long long units = (long long)c.batch * c.Hkv * a.row_tiles;
   const int ctas = chunk_ctas(sm_count);
+  a.begins = reinterpret_cast<int2*>(part + (size_t)2 * ctas * kChRows * (c.d + 2));
   const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), kChThreads, v.smem, st, a);
   if (e != cudaSuccess) return e;
-  return launch_chained(v.combine, dim3((unsigned int)units, kChRows / 32), 256, 0, st, a, ctas);
+  return launch_chained(v.combine, dim3((unsigned int)ctas, kChRows / 8), 256, 0, st, a);
 }
 
 }  // namespace restkv

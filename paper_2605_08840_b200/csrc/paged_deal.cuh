@@ -15,6 +15,7 @@ struct PagedMmaArgs {
   __nv_bfloat16* out;
   float* lse;        // or null
   float* part;       // per CTA two of: o [rows, d], (m, l) [rows]; without clusters
+  int2* begins;      // per CTA: unit and tile of it that it begins with; chunks
   int row_tiles;     // units per KV head
   int cluster;       // CTAs per unit, 0: tiles of all units end to end
   long long wait_limit;
@@ -25,11 +26,11 @@ __device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 
 
 // Tiles dealt out end to end: CTA x of `ctas` has those from boundary x to boundary x + 1.  A boundary is start(x) = all * x / ctas, but
 // moved to the near end of its unit where that is at most `snap` tiles away: a CTA that ends one unit and begins another pays for
-// prologue and merge twice, 5 us, in which it would go through some 24 tiles.
+// prologue and merge twice, in which it would go through as many tiles.
 struct Deal {
   int ctas, each, more, snap;
-  __device__ __forceinline__ Deal(int all, int grid) : ctas(all < grid ? all : grid), each(all / ctas), more(all - each * ctas) {
-    snap = (each - 1) / 2 < 24 ? (each - 1) / 2 : 24;   // less than half a share: no share vanishes
+  __device__ __forceinline__ Deal(int all, int grid, int most) : ctas(all < grid ? all : grid), each(all / ctas), more(all - each * ctas) {
+    snap = (each - 1) / 2 < most ? (each - 1) / 2 : most;   // less than half a share: no share vanishes
   }
   __device__ __forceinline__ int start(int x) const { return x * each + x * more / ctas; }
   // tile `at` of a unit of `tiles`: where a boundary there goes, as tile of the unit
@@ -52,7 +53,9 @@ struct Deal {
   }
 };
 
-// Entries: sequences, or with lengths per head the KV heads of all sequences; each has `units` units of as many tiles.
+// Entries of the kernel for few tokens: sequences, or with lengths per head the KV heads of all sequences; each has units of as many tiles.
+__device__ __forceinline__ int entries_of(const PagedCache& c) { return c.per_head ? c.batch * c.Hkv : c.batch; }
+__device__ __forceinline__ int units_of(const PagedCache& c, int row_tiles) { return c.per_head ? row_tiles : c.Hkv * row_tiles; }
 __device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_rows) {
   const int n = c.per_head ? paged_length(c, e / c.Hkv, e % c.Hkv) : paged_length(c, e, 0);
   const int t = (n + tile_rows - 1) / tile_rows;
@@ -63,15 +66,14 @@ __device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_
 struct Run {
   int tile, end, entry, first, tiles;
 };
-__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int x, int grid) {
+__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int most, int x, int grid) {
   const int lane = threadIdx.x & 31;
-  const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
-  const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
+  const int entries = entries_of(c), units = units_of(c, row_tiles);
   const int t0 = lane < entries ? entry_tiles(c, lane, tile_rows) : 0;
   int sum = t0 * units;
   for (int e = 32 + lane; e < entries; e += 32) sum += entry_tiles(c, e, tile_rows) * units;
   const int all = __reduce_add_sync(0xffffffffu, sum);
-  const Deal deal(all, grid);
+  const Deal deal(all, grid, most);
   Run r{0, 0, 0, 0, 1};
   if (x >= deal.ctas) return r;
   r.tile = r.end = all;
@@ -106,18 +108,26 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int 
   return r;
 }
 
-// Dims 4 v .. 4 v + 3 of a query row's result.
-template <int kD>
-__device__ __forceinline__ void write_row(const PagedMmaArgs& a, int b, int h, int rho, int count, int v, float4 acc, float mm, float ll) {
+// Dims kPer v .. of a query row's result.
+template <int kD, int kPer>
+__device__ __forceinline__ void write_row(const PagedMmaArgs& a, int b, int h, int rho, int count, int v, const float (&acc)[kPer], float mm, float ll) {
   const PagedCache& c = a.c;
   const int i = rho / c.G, g = rho - i * c.G;
   const bool some = ll > 0.f && i < count;
   const long long at = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
   const float f = some ? 1.f / ll : 0.f;
-  uint2 w = make_uint2(0u, 0u);
-  if (some) w = make_uint2(pack_bf16x2(acc.x * f, acc.y * f), pack_bf16x2(acc.z * f, acc.w * f));
-  reinterpret_cast<uint2*>(a.out + at * kD)[v] = w;
+  uint32_t w[kPer / 2];
+#pragma unroll
+  for (int x = 0; x < kPer / 2; ++x) w[x] = some ? pack_bf16x2(acc[2 * x] * f, acc[2 * x + 1] * f) : 0u;
+  __nv_bfloat16* const to = a.out + at * kD + kPer * v;
+  if constexpr (kPer == 4) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint32_t*>(to) = w[0];
   if (v == 0 && a.lse) a.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+}
+template <int kD>
+__device__ __forceinline__ void write_row(const PagedMmaArgs& a, int b, int h, int rho, int count, int v, float4 acc, float mm, float ll) {
+  const float x[4] = {acc.x, acc.y, acc.z, acc.w};
+  write_row<kD, 4>(a, b, h, rho, count, v, x, mm, ll);
 }
 __device__ __forceinline__ void fma4(float4& acc, float4 x, float f) {
   acc.x = fmaf(x.x, f, acc.x); acc.y = fmaf(x.y, f, acc.y); acc.z = fmaf(x.z, f, acc.z); acc.w = fmaf(x.w, f, acc.w);
@@ -128,11 +138,10 @@ struct Piece {
   Run run;
   int unit, t0, t1;        // tiles [t0, t1) of the unit
   int whole;               // no other CTA has tiles of it
-  __device__ __forceinline__ void cut(const PagedCache& c, int row_tiles, int tile_rows) {   // at run.tile
-    const int units = c.per_head ? row_tiles : c.Hkv * row_tiles;
+  template <class TilesOf> __device__ __forceinline__ void cut(int units, TilesOf&& tiles_of) {   // at run.tile
     if (run.tile >= run.first + run.tiles * units) {     // the next entry
       run.first += run.tiles * units;
-      run.tiles = entry_tiles(c, ++run.entry, tile_rows);
+      run.tiles = tiles_of(++run.entry);
     }
     const int k = (run.tile - run.first) / run.tiles, begin = run.first + k * run.tiles;
     unit = run.entry * units + k;

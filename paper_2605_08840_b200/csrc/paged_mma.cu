@@ -38,6 +38,8 @@ namespace {
 
 namespace cg = cooperative_groups;
 
+constexpr int kSnap = 24;   // a CTA that ends one unit and begins another pays 5 us for it: some 24 tiles
+
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -171,12 +173,13 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   grid_dependency_wait();
   grid_dependency_launch();
 
+  auto tiles_of = [&](int entry) { return entry_tiles(c, entry, C::kTileRows); };
   if constexpr (!kCluster) {
     if (warp == 0) {
-      const Run run = find_run(c, a.row_tiles, C::kTileRows, blockIdx.x, gridDim.x);
+      const Run run = find_run(c, a.row_tiles, C::kTileRows, kSnap, blockIdx.x, gridDim.x);
       if (lane == 0) {
         piece_s.run = run;
-        if (run.tile < run.end) piece_s.cut(c, a.row_tiles, C::kTileRows);
+        if (run.tile < run.end) piece_s.cut(units_of(c, a.row_tiles), tiles_of);
       }
     }
     __syncthreads();
@@ -759,7 +762,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     if (__syncthreads_or(!ok)) return;
     if (threadIdx.x == 0) {
       piece_s.run.tile += piece_s.t1 - piece_s.t0;
-      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(c, a.row_tiles, C::kTileRows);
+      if (piece_s.run.tile < piece_s.run.end) piece_s.cut(units_of(c, a.row_tiles), tiles_of);
     }
     __syncthreads();
     if (piece_s.run.tile >= piece_s.run.end) return;
@@ -778,12 +781,12 @@ __global__ void __launch_bounds__(2 * kD) paged_mma_combine_kernel(const __grid_
   const PagedCache& c = a.c;
   const int unit = blockIdx.x, row = blockIdx.y, bh = unit / a.row_tiles, rho = (unit - bh * a.row_tiles) * kRows + row;
   if (rho >= c.n_tokens * c.G) return;
-  const int units = c.per_head ? a.row_tiles : c.Hkv * a.row_tiles, entry = unit / units;
+  const int units = units_of(c, a.row_tiles), entry = unit / units;
   const int b = bh / c.Hkv, h = bh - b * c.Hkv, lane = threadIdx.x & 31;
   if (threadIdx.x < 32) {
     // where the unit's entry begins, by the same sums as in the kernel before
     int before = 0, all = 0;
-    const int entries = c.per_head ? c.batch * c.Hkv : c.batch;
+    const int entries = entries_of(c);
     for (int e = threadIdx.x; e < entries; e += 32) {
       const int t = entry_tiles(c, e, tile_rows) * units;
       all += t;
@@ -795,7 +798,7 @@ __global__ void __launch_bounds__(2 * kD) paged_mma_combine_kernel(const __grid_
   }
   const int tiles = entry_tiles(c, entry, tile_rows), count = paged_count(c, b);
   __syncthreads();
-  const Deal deal(run_s[0], grid);
+  const Deal deal(run_s[0], grid, kSnap);
   const int u0 = run_s[1] + (unit - entry * units) * tiles;
   const int x0 = deal.first_of(u0, tiles), pieces = deal.last_of(u0, tiles) - x0 + 1;
   if (pieces == 1) return;                     // it was one CTA's: written
