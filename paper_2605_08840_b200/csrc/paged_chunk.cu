@@ -537,45 +537,75 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         constexpr int kLanes = kD / 8, kRowsAtOnce = 32 / kLanes;
         const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
         const int x = lane % kLanes, row0 = (warp & 3) * 32 + lane / kLanes;
-#pragma unroll 4
-        for (int z = 0; z < 32; z += kRowsAtOnce) {
-          const int row = row0 + z, rho_z = rho0 + w * 128 + row, i_z = rho_z / c.G, g_z = rho_z - i_z * c.G;
-          const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g_z) * a.Q.sh + i_z * a.Q.sn;
-          const uint4 raw = rho_z < R && i_z < count ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+        // four rows per lane together: what each of them waits for, loads and shuffles, is on its way for all
+#pragma unroll 1
+        for (int z0 = 0; z0 < 32; z0 += 4 * kRowsAtOnce) {
+          uint4 raw[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int rho_z = rho0 + w * 128 + row0 + z0 + y * kRowsAtOnce, i_z = rho_z / c.G, g_z = rho_z - i_z * c.G;
+            const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g_z) * a.Q.sh + i_z * a.Q.sn;
+            raw[y] = rho_z < R && i_z < count ? reinterpret_cast<const uint4*>(q)[x] : make_uint4(0u, 0u, 0u, 0u);
+          }
           if constexpr (kInt4) {
-            float v[8] = {lower(raw.x), upper(raw.x), lower(raw.y), upper(raw.y), lower(raw.z), upper(raw.z), lower(raw.w), upper(raw.w)};
-            float top = fmaxf(fmaxf(fmax3(fabsf(v[0]), fabsf(v[1]), fabsf(v[2])), fmax3(fabsf(v[3]), fabsf(v[4]), fabsf(v[5]))), fmaxf(fabsf(v[6]), fabsf(v[7])));
+            float top[4], sum[4];
 #pragma unroll
-            for (int off = 1; off < kLanes; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-            // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
-            int e = 141 - (int)(__float_as_uint(top) >> 23);
-            e = e < -100 ? -100 : e > 100 ? 100 : e;
-            const float scale = top < INFINITY ? power_of_two(e) : __uint_as_float(0x7FFFFFFFu);
-            const float back = __shfl_sync(0xffffffffu, power_of_two(-e), lane % kRowsAtOnce * kLanes);   // that of row z + lane % kRowsAtOnce
-            if (lane / kRowsAtOnce == z / kRowsAtOnce) unscale = back;
+            for (int y = 0; y < 4; ++y) {
+              const uint32_t* u = &raw[y].x;
+              top[y] = 0.f;
 #pragma unroll
-            for (int y = 0; y < 8; ++y) v[y] *= scale;
-            // dims in the order of K's operands
-            sts128(operand_at(tile, row, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
-            float sum = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-#pragma unroll
-            for (int off = 1; off < kLanes / kG; off <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            const uint32_t own = split_f16(sum * 0x1p-8f);
-            uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int g2 = 0; g2 < kG; ++g2) {
-              const uint32_t parts = __shfl_sync(0xffffffffu, own, lane / kLanes * kLanes + g2 * (kLanes / kG));
-#pragma unroll
-              for (int y = 0; y < 3; ++y) {
-                const uint32_t part = y == 2 ? parts >> 16 : parts & 0xFFFFu;
-                thin[(3 * g2 + y) >> 1] |= (3 * g2 + y) & 1 ? part << 16 : part;
-              }
+              for (int k = 0; k < 4; ++k) top[y] = fmax3(top[y], fabsf(lower(u[k])), fabsf(upper(u[k])));
             }
-            const uint32_t to = thin_at(q_thin + (uint32_t)w * kThinBytes, row);
-            if (x == 0) sts128(to, thin[0], thin[1], thin[2], thin[3]);
-            if (x == 1) sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+#pragma unroll
+            for (int off = 1; off < kLanes; off <<= 1)
+#pragma unroll
+              for (int y = 0; y < 4; ++y) top[y] = fmaxf(top[y], __shfl_xor_sync(0xffffffffu, top[y], off));
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              // 2^e top in [2^14, 2^15), for top of 2^-86 .. 2^100; an infinite one makes the row's logits NaN
+              int e = 141 - (int)(__float_as_uint(top[y]) >> 23);
+              e = e < -100 ? -100 : e > 100 ? 100 : e;
+              const float scale = top[y] < INFINITY ? power_of_two(e) : __uint_as_float(0x7FFFFFFFu);
+              // of the rows that the warp's lanes have in turn, each thread keeps its own's
+              const float back = __shfl_sync(0xffffffffu, power_of_two(-e), lane % kRowsAtOnce * kLanes);
+              if (lane / kRowsAtOnce == z0 / kRowsAtOnce + y) unscale = back;
+              float v[8];
+              const uint32_t* u = &raw[y].x;
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                v[2 * k] = lower(u[k]) * scale;
+                v[2 * k + 1] = upper(u[k]) * scale;
+              }
+              // dims in the order of K's operands
+              sts128(operand_at(tile, row0 + z0 + y * kRowsAtOnce, x), pack_f16x2(v[0], v[4]), pack_f16x2(v[1], v[5]), pack_f16x2(v[2], v[6]), pack_f16x2(v[3], v[7]));
+              sum[y] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+            }
+#pragma unroll
+            for (int off = 1; off < kLanes / kG; off <<= 1)
+#pragma unroll
+              for (int y = 0; y < 4; ++y) sum[y] += __shfl_xor_sync(0xffffffffu, sum[y], off);
+            uint32_t parts[4][kG];
+#pragma unroll
+            for (int g2 = 0; g2 < kG; ++g2)
+#pragma unroll
+              for (int y = 0; y < 4; ++y) parts[y][g2] = split_f16(__shfl_sync(0xffffffffu, sum[y], lane / kLanes * kLanes + g2 * (kLanes / kG)) * 0x1p-8f);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              uint32_t thin[8] = {0u, 0u, 0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+              for (int g2 = 0; g2 < kG; ++g2)
+#pragma unroll
+                for (int k = 0; k < 3; ++k) {
+                  const uint32_t part = k == 2 ? parts[y][g2] >> 16 : parts[y][g2] & 0xFFFFu;
+                  thin[(3 * g2 + k) >> 1] |= (3 * g2 + k) & 1 ? part << 16 : part;
+                }
+              const uint32_t to = thin_at(q_thin + (uint32_t)w * kThinBytes, row0 + z0 + y * kRowsAtOnce);
+              if (x == 0) sts128(to, thin[0], thin[1], thin[2], thin[3]);
+              if (x == 1) sts128(to + 128u, thin[4], thin[5], thin[6], thin[7]);
+            }
           } else {
-            sts128(operand_at(tile, row, x), raw.x, raw.y, raw.z, raw.w);
+#pragma unroll
+            for (int y = 0; y < 4; ++y) sts128(operand_at(tile, row0 + z0 + y * kRowsAtOnce, x), raw[y].x, raw[y].y, raw[y].z, raw[y].w);
           }
         }
         fence_proxy_async_smem();
