@@ -883,7 +883,7 @@ cudaError_t paged_chunk_init() {
 bool paged_chunk_supported(const PagedCache& c) {
   ChunkVariant v;
   const long long rows = (long long)c.n_tokens * c.G;
-  if (rows < kChunkRows || !pick_chunk(c, &v)) return false;
+  if (rows < kChunkRows || rows * c.batch * c.Hkv < kChunkAll || !pick_chunk(c, &v)) return false;
   const long long units = (long long)c.batch * c.Hkv * ((rows + kChRows - 1) / kChRows);
   return (c.capacity() / kChTile + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }

@@ -742,3 +742,120 @@ def test_attend_values_of_any_size(handle, fmt, steps, t):
     V[:, :, 400:432] = 0.0
     handle.paged_append(cache.desc, 600, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([600]), cache.table)
     check_attention(handle, rng, cache, [600], None, t, q_scale=3.0)
+
+
+# Calls of many query rows: enough of them (64 of a KV head, 1536 together) that they go by tiles of 128 against tiles of 128 cache rows.
+IN_CHUNKS = [(2, 4, 4, 64, 16, [270, 3], [200, 3], 200), (1, 8, 2, 64, 32, [700], None, 256), (3, 6, 2, 128, 16, [130, 100, 0], [120, 20, 0], 120),
+             (1, 1, 1, 64, 16, [1700], None, 1600), (1, 12, 4, 128, 48, [129], None, 129), (4, 8, 1, 128, 16, [64, 65, 191, 48], [48, 1, 48, 48], 48)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", IN_CHUNKS)
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_attend_in_chunks(handle, spec, fmt, cap):
+    b, Hq, Hkv, d, R, lengths, counts, t = spec
+    rng = np.random.default_rng(Hq + d + t)
+    for group in [g for g in (32, 64, 128) if d % g == 0] if fmt == "int4" else [0]:
+        cache = Cache(rng, b, Hq, Hkv, d, fmt, R, -(-max(lengths) // R), group, softcap=cap)
+        cache.fill(handle, rng, lengths)
+        check_attention(handle, rng, cache, lengths, counts, t, q_scale=1.5, strided=True, note="group %d" % group)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_attend_in_chunks_lengths_per_head(handle, fmt):
+    rng = np.random.default_rng(13)
+    cache = Cache(rng, 2, 8, 4, 128, fmt, 16, 20, 64 if fmt == "int4" else 0, per_head=True)
+    lengths = np.array([[1, 300, 64, 117], [0, 105, 200, 133]])
+    cache.fill(handle, rng, lengths)
+    check_attention(handle, rng, cache, lengths, None, 100)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("cap", [0.0, 20.0])
+@pytest.mark.parametrize("q_scale", [0.0, 40.0, 1000.0])
+def test_attend_in_chunks_extreme_logits(handle, fmt, cap, q_scale):
+    rng = np.random.default_rng(14)
+    cache = Cache(rng, 1, 8, 2, 128, fmt, 32, 10, 64 if fmt == "int4" else 0, softcap=cap)
+    cache.fill(handle, rng, [310])
+    check_attention(handle, rng, cache, [310], None, 200, q_scale=q_scale)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("t", [1, 3, 400])
+@pytest.mark.parametrize("d", [64, 128])
+def test_attend_logits_that_grow(handle, fmt, t, d):
+    """Every row's key is longer than the one before it, in every dim alike, so that what a row's weights refer to is left behind again
+    and again: by rows with steps of one sign, and with a jump inside a tile."""
+    rng = np.random.default_rng(15)
+    cache = Cache(rng, 1, 4, 1, d, fmt, 16, 45, 32 if fmt == "int4" else 0)
+    n = 700
+    K = np.linspace(0.0, 6.0, n)[None, None, :, None] * np.sign(rng.standard_normal((1, 1, 1, d))) + 0.1 * rng.standard_normal((1, 1, n, d))
+    K[:, :, 333:] *= 2.0
+    V = rng.standard_normal((1, 1, n, d))
+    handle.paged_append(cache.desc, n, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([n]), cache.table)
+    check_attention(handle, rng, cache, [n], None, t, q_scale=4.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("steps", [2.0 ** -30, 2.0 ** -12, 2.0 ** 12, 2.0 ** 40])
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_attend_in_chunks_values_of_any_size(handle, fmt, steps):
+    rng = np.random.default_rng(16)
+    cache = Cache(rng, 1, 4, 1, 128, fmt, 16, 40, 64 if fmt == "int4" else 0)
+    K = rng.standard_normal((1, 1, 600, 128))
+    V = rng.standard_normal((1, 1, 600, 128)) * steps
+    V[:, :, 17::100] *= 2.0 ** 20
+    V[:, :, 400:432] = 0.0
+    handle.paged_append(cache.desc, 600, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([600]), cache.table)
+    check_attention(handle, rng, cache, [600], None, 400, q_scale=3.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_attend_in_chunks_reports_bad_tables(handle, fmt):
+    rng = np.random.default_rng(17)
+    cache = Cache(rng, 1, 4, 1, 128, fmt, 16, 32, 32 if fmt == "int4" else 0)
+    cache.fill(handle, rng, [512])
+    Q = to_dev(rng.standard_normal((1, 4, 400, 128)), torch.bfloat16)
+    ws = torch.empty(handle.paged_workspace_bytes(cache.desc, 400), dtype=torch.uint8, device="cuda")
+    want, out = torch.empty_like(Q), torch.empty_like(Q)
+    handle.paged_attend(cache.desc, 400, Q, cache.K, cache.V, dev_i32([512]), cache.table, want, ws)
+    assert handle.poll_status() == rk.RESTKV_OK
+    handle.paged_attend(cache.desc, 400, Q, cache.K, cache.V, dev_i32([513]), cache.table, out, ws)
+    assert handle.poll_status() == rk.ERR_INVALID_ARG
+    assert torch.equal(out, want)
+    for bad in (cache.n_pages, -1, 2 ** 31 - 1):
+        table = cache.table.clone()
+        table[0, 9] = bad
+        handle.paged_attend(cache.desc, 400, Q, cache.K, cache.V, dev_i32([500]), table, out, ws)
+        assert handle.poll_status() == rk.ERR_INVALID_ARG
+        assert bool(torch.isfinite(out.float()).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_attend_chunk_equals_its_tokens(handle, fmt):
+    """A chunk over a cache, and its tokens one call at a time with the lengths that they see, by the two kernels: both within a rounding
+    of the output and of the weights of the exact result."""
+    rng = np.random.default_rng(18)
+    cache = Cache(rng, 2, 8, 2, 128, fmt, 32, 12, 64 if fmt == "int4" else 0)
+    lengths, t = [380, 210], 128
+    cache.fill(handle, rng, lengths)
+    Q = to_dev(rng.standard_normal((2, 8, t, 128)), torch.bfloat16)
+    ws = torch.empty(handle.paged_workspace_bytes(cache.desc, t), dtype=torch.uint8, device="cuda")
+    whole, lse = torch.empty_like(Q), torch.empty(2, 8, t, device="cuda")
+    handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32(lengths), cache.table, whole, ws, lse=lse)
+    ws1 = torch.empty(handle.paged_workspace_bytes(cache.desc, 1), dtype=torch.uint8, device="cuda")
+    for i in (0, 1, 63, 64, 127):
+        one, l1 = torch.empty(2, 8, 1, 128, dtype=torch.bfloat16, device="cuda"), torch.empty(2, 8, 1, device="cuda")
+        handle.paged_attend(cache.desc, 1, Q[:, :, i:i + 1].contiguous(), cache.K, cache.V, dev_i32([n - (t - 1 - i) for n in lengths]), cache.table, one,
+                            ws1, lse=l1)
+        torch.cuda.synchronize()
+        # values are at most 5 or so, and a weighted mean of them no larger: two roundings of weights and one of each output
+        assert float((one[:, :, 0].float() - whole[:, :, i].float()).abs().max()) <= 5.5 * (2 * 2.0 ** -8 + 2 * 2.0 ** -8)
+        assert float((l1[:, :, 0] - lse[:, :, i]).abs().max()) <= 2.0 ** -12
+    assert handle.poll_status() == rk.RESTKV_OK
