@@ -62,24 +62,6 @@ __device__ __forceinline__ uint32_t int4_codes(const float* x, float lo, float s
   return (uint32_t)sum[0] | (uint32_t)sum[1] << 16;
 }
 
-// Their place in a block: chunk = dim / 8 of row r.
-__device__ __forceinline__ void int4_store(const PagedCache& c, uint8_t* block, int r, int chunk, bool is_key, uint32_t w, float lo, float step) {
-  const int m = chunk >> 2, q = chunk & 3, words = c.d >> 5;
-  uint8_t* row = block + r * c.row_bytes;
-  if (is_key) {
-    reinterpret_cast<unsigned int*>(row)[q * words + m] = w;
-  } else {
-    unsigned short* v = reinterpret_cast<unsigned short*>(row);
-    v[2 * q * words + m] = (unsigned short)(w & 0xFFFFu);
-    v[(2 * q + 1) * words + m] = (unsigned short)(w >> 16);
-  }
-  if ((chunk * 8 & (c.group - 1)) == 0) {
-    unsigned short* p = reinterpret_cast<unsigned short*>(block + int4_params(c.d, chunk * 8 / c.group, r));
-    p[0] = (unsigned short)(__float_as_uint(step) >> 16);
-    p[4] = (unsigned short)(__float_as_uint(lo) >> 16);
-  }
-}
-
 // grid (batch * n_tokens / warps, y): a warp takes a token, or with few tokens the y-th part of its rows, so that where the token goes and
 // its cosines and sines are found once.  A row lies in kLanes threads, 32 / kLanes heads side by side; Q's heads, then K's, then V's,
 // some rounds of them on their way before the first is needed.  What bounds it: HBM (every row is read and written once), in 4 bits
@@ -93,8 +75,10 @@ struct AppendArgs {
   void* Q_out;
 };
 
+// 72 registers, 28 warps per SM: with 80 (24 warps) or 64 (32 warps, some values found again) 2048 tokens into 4 bits take as long and 10%
+// longer, 8 x 4093 tokens into bf16 2% longer and 1%.
 template <typename T, bool kInt4, int kLanes>
-__global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_constant__ AppendArgs a) {
+__global__ void __launch_bounds__(kRowThreads, 7) paged_append_kernel(const __grid_constant__ AppendArgs a) {
   ptx::grid_dependency_wait();
   ptx::grid_dependency_launch();
   constexpr int kAtOnce = 32 / kLanes;
@@ -216,6 +200,19 @@ __global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_
     if (lane == 0 && r1 > q_rounds) atomicOr(c.dev_status, kDevBadIndex);
     return;
   }
+  // where the chunk goes: the block in head 0's pages, and in it the key's and the value's codes, step and offset
+  long long block = 0;
+  int at_key = 0, at_value = 0, at_params = 0;
+  const int m = chunk >> 2, q = chunk & 3, words = c.d >> 5;
+  const bool leads = kInt4 && (chunk * 8 & (c.group - 1)) == 0;
+  auto place = [&]() {
+    block = (long long)page * c.Hkv * c.head_bytes + (long long)block_of_page * c.block_bytes;
+    const int row = row_of_block * c.row_bytes;
+    at_key = row + (kInt4 ? (q * words + m) * 4 : chunk * 8 * (int)sizeof(T));
+    at_value = kInt4 ? row + (2 * q * words + m) * 2 : at_key;
+    if (kInt4) at_params = int4_params(c.d, chunk * 8 / c.group, row_of_block);
+  };
+  if (!c.per_head) place();
   auto store = [&](auto key, Pack8<T>& raw, int h, bool mine) {
     constexpr bool kKey = decltype(key)::value;
     float x[8];
@@ -230,10 +227,26 @@ __global__ void __launch_bounds__(kRowThreads) paged_append_kernel(const __grid_
         if (chunk == 0) atomicOr(c.dev_status, kDevBadIndex);
         return;
       }
+      place();
     }
-    uint8_t* to = (kKey ? a.K_pages : a.V_pages) + ((long long)(page * c.Hkv + h) * per_page + block_of_page) * c.block_bytes;
-    if constexpr (kInt4) int4_store(c, to, row_of_block, chunk, kKey, int4_codes(x, lo, step), lo, step);
-    else Pack8<T>::store(reinterpret_cast<T*>(to + row_of_block * c.row_bytes) + chunk * 8, x);
+    uint8_t* const to = (kKey ? a.K_pages : a.V_pages) + block + h * c.head_bytes;
+    if constexpr (kInt4) {
+      const uint32_t w = int4_codes(x, lo, step);
+      if (kKey) {
+        *reinterpret_cast<unsigned int*>(to + at_key) = w;
+      } else {
+        unsigned short* const v = reinterpret_cast<unsigned short*>(to + at_value);
+        v[0] = (unsigned short)(w & 0xFFFFu);
+        v[words] = (unsigned short)(w >> 16);
+      }
+      if (leads) {
+        unsigned short* const p = reinterpret_cast<unsigned short*>(to + at_params);
+        p[0] = (unsigned short)(__float_as_uint(step) >> 16);
+        p[4] = (unsigned short)(__float_as_uint(lo) >> 16);
+      }
+    } else {
+      Pack8<T>::store(reinterpret_cast<T*>(to + at_key), x);
+    }
   };
   const int k0 = r0 - q_rounds, k1 = r1 - q_rounds, v0 = k0 - kv_rounds, v1 = k1 - kv_rounds;
   const std::integral_constant<int, kAheadKV> few;
@@ -396,6 +409,7 @@ cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K
   const AppendArgs a{c, Kn, Vn, Q, K_pages, V_pages, positions, rot, Q_out};
   const long long blocks = ((long long)c.batch * c.n_tokens + warps - 1) / warps;
   // a warp per token finds its place and its angles once; with few tokens the rows go to warps of their own until there are 16 per SM
+  // (2048 tokens into 4 bits 14.0 us; until there are 32, 64: 14.5, 15.3)
   const int rounds = ((Q.data ? c.Hq : 0) + at_once - 1) / at_once + 2 * ((c.Hkv + at_once - 1) / at_once);
   long long y = (4LL * sm_count + blocks - 1) / blocks;
   if (y > rounds) y = rounds;
