@@ -440,9 +440,17 @@ restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, i
  *   Q     [batch, n_q_heads, n_tokens, head_dim], dtype; query head hq reads KV head hq / (n_q_heads / n_kv_heads)
  *   out   device [batch, n_q_heads, n_tokens, head_dim] contiguous, dtype
  *   lse   optional device float [batch, n_q_heads, n_tokens]: natural-log sum of exp of the (capped) logits
- * A query that sees no row, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32;
- * steps and offsets of 4-bit rows are applied in fp32.  With bf16 the softmax weights are rounded to bf16 before they meet V.
- * A row that some query of the call sees has to be finite.
+ * A query that sees no row, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32.  A
+ * row that some query of the call sees has to be finite.  The result of a call does not depend on other calls, streams or the order
+ * in which its parts end: the same call gives the same bits.
+ * RESTKV_F32, other head_dims than 64, 128 and 256 and restkv_set_kernel_path(1) run in fp32 throughout.  Else the tensor cores do,
+ * and what is rounded for them is this:
+ *   few tokens     K's 4-bit rows are exact (codes meet Q as f16, scaled by a power of two per query; steps and offsets are applied in
+ *                  fp32); weights over bf16 rows are two bf16 parts (16 bits), over 4-bit rows weight * step is one f16 (11 bits)
+ *   many tokens    (head_dim 64 or 128, at least 64 query rows n_tokens * group per KV head and 1536 in the call) K's 4-bit rows as above,
+ *                  but of steps below 2^-8 of the largest of their 128 rows only what is above 2^-16 of that one is kept; V's 4-bit values
+ *                  are rounded to f16 in the range of their 128 rows; weights are one bf16 over bf16 rows, one f16 over 4-bit rows
+ * The workspace holds the parts of sequences that several blocks work on; it does not grow with their lengths.
  */
 restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, int n_tokens, const restkv_rows* Q,
                                   const void* K_pages, const void* V_pages, const int32_t* lengths, const int32_t* table,

@@ -1,10 +1,15 @@
 // Attention of many query tokens over the paged cache (a chunk of prompt): bf16 in and out, pages of bf16 or of 4-bit codes, head_dim 64
 // or 128, on tcgen05.
 //
-// What bounds it: 4 * 128 * 128 * head_dim operations per 128 query rows and 128 cache rows on the tensor pipe, 1024 of its cycles at
-// head_dim 128, beside as many cycles of the special-function unit for the exponentials and the work of turning codes into operands.  So
+// What bounds it: 4 * 128 * 128 * head_dim operations per 128 query rows and 128 cache rows are 1024 cycles of the tensor pipe at head_dim
+// 128, and the exponentials as many of the special-function unit; between the two the softmax's chain of load, maximum, exponential, sum,
+// store, about 1650 cycles per half tile of 64 columns (2500 with a cap), which nothing but another warp's work hides.  So
 //   - a CTA per SM takes 256 query rows (tokens x query heads of a KV head) in two tiles of 128, each with a warpgroup of its own, a
-//     thread per row: while one tile's softmax runs, the other tile's products do, and a tile of K and V serves both;
+//     thread per row; a tile of K and V serves both;
+//   - a tile of logits is two halves of 64 columns, in turn: while a row's thread is at one, the other's weights meet V and its next
+//     logits are made, so that a softmax warp always finds a half ready (whole tiles in turn: 863 us for 815 below, with a cap 1294 for 1095);
+//   - one pass over a half: 64 logits in registers, their maximum against the running reference, the weights.  The reference is moved (sums
+//     and O scaled by a power of two) only where weights would pass 2^13 (a first pass for the maximum: 975 us for 864);
 //   - S (fp32) and O of both tiles fill the tensor memory's 512 columns at head_dim 128; P (16 bits) takes S's place and is the A operand
 //     of P V there;
 //   - seven warps fetch K and V, half a row per thread: bf16 by cp.async; codes become f16 operands with one fused operation per pair, the
@@ -14,11 +19,17 @@
 //     V: offset + step * code, rounded once to f16; its tiles' exponents go into the weights'.
 //     (K rounded like V: 10% less of the tensor pipe, but logits lose 2^-12 of their terms.  In both, steps below 2^-8 of the largest of
 //     their 128 rows lose bits.)
+//   - weights are rounded to f16 (over 4 bits) or bf16 before they meet V, as an output of bf16 is in the end; their sums are fp32 sums of
+//     the weights before that;
 //   - dims within K's operand chunks are in the order in which they come out of a word, and Q's in the same; V's order is undone where O
 //     is written.
 //   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand
 //     (relative error 9.3e-8, minimax), else 1 - 2 / (1 + e^2y) with two trips to the special-function unit.
-// The tiles of all units are dealt out end to end as in the kernel for few tokens; what several CTAs share is merged by a second kernel.
+//     (A part of the exponentials by a polynomial, too: an eighth of them 825 us for 811, a quarter 853.  The chain bounds it, not the unit.)
+// The tiles that a unit's last query row sees, of all units end to end, are dealt out evenly; what several CTAs share is merged by a second
+// kernel.  Measured, 2048 tokens of 32 heads of 128 (8 KV heads) over 18432 rows: bf16 684 us (854 TFLOP/s, tensor pipe 43% busy), 4 bits in
+// groups of 128 678 us, 64 719 us, 32 907 us (the conversion of codes, a step and an offset per row and group, bounds that one), of 128 with
+// a cap 861 us.  2048 tokens and nothing before them 144 us; 48 tokens over 17000 rows 64 us.
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -35,12 +46,10 @@ constexpr int kSoftmaxWarps = 8, kFetchWarps = 7;   // and one for the products:
 constexpr int kChThreads = (kSoftmaxWarps + kFetchWarps + 1) * 32;
 constexpr int kFetch = kFetchWarps * 32;
 constexpr int kInfo = 4;                     // tiles whose factors are kept: the fetching warps are two ahead of the softmax at most
+// Tiles that a CTA could go through while it ends one unit and begins another.  (2048 tokens alone: none 181 us, 2 147, 4 144, 8 136; 300
+// tokens over 8700 rows: 116, 116, 115, 121.)
+constexpr int kChSnap = 4;
 // log2 of the largest weight that a rescaling leaves, and of what it may grow to before the next one
-// tiles' worth of a CTA's beginning another unit
-#ifndef SNAP
-#define SNAP 2
-#endif
-constexpr int kChSnap = SNAP;
 constexpr float kChStart = 5.f, kChSlack = 13.f;
 
 struct ChunkBarriers {
@@ -106,27 +115,6 @@ __device__ __noinline__ void rescale(uint32_t at, int columns, float f) {
     tmem_st16(at + x, w);
   }
   tmem_wait_st();
-}
-// The same for `chunks` chunks of 16 columns of f16 or bf16 pairs; f is a power of two, or 0.
-template <bool kF16> __device__ __noinline__ void rescale_pairs(uint32_t at, int chunks, float f) {
-  tmem_wait_st();            // they have just been written
-  for (int x = 0; x < chunks; ++x) {
-    float v[16];
-    tmem_ld16(at + x * 16, v);
-    tmem_wait_ld();
-    uint32_t w[16];
-#pragma unroll
-    for (int y = 0; y < 16; ++y) {
-      const uint32_t u = __float_as_uint(v[y]);
-      if (kF16) {
-        const float2 e = __half22float2(*reinterpret_cast<const __half2*>(&u));
-        w[y] = pack_f16x2(e.x * f, e.y * f);
-      } else {
-        w[y] = pack_bf16x2(lower(u) * f, upper(u) * f);
-      }
-    }
-    tmem_st16(at + x * 16, w);
-  }
 }
 
 // Tiles that the last query row of a unit sees: those past them are nobody's business.
