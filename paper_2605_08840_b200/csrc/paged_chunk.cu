@@ -25,11 +25,12 @@
 //     is written.
 //   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand
 //     (relative error 9.3e-8, minimax), else 1 - 2 / (1 + e^2y) with two trips to the special-function unit.
-//     (A part of the exponentials by a polynomial, too: an eighth of them 825 us for 811, a quarter 853.  The chain bounds it, not the unit.)
+//     (A part of the exponentials by a polynomial, too: an eighth of them 825 us for 811, a quarter 853; exponentials by turns with the other
+//     tile's: 678 us for 667, with a cap 1031 for 874.  The chain bounds it, not the unit.)
 // The tiles that a unit's last query row sees, of all units end to end, are dealt out evenly; what several CTAs share is merged by a second
-// kernel.  Measured, 2048 tokens of 32 heads of 128 (8 KV heads) over 18432 rows: bf16 684 us (854 TFLOP/s, tensor pipe 43% busy), 4 bits in
-// groups of 128 678 us, 64 719 us, 32 907 us (the conversion of codes, a step and an offset per row and group, bounds that one), of 128 with
-// a cap 861 us.  2048 tokens and nothing before them 144 us; 48 tokens over 17000 rows 64 us.
+// kernel.  Measured, 2048 tokens of 32 heads of 128 (8 KV heads) over 18432 rows: bf16 672 us (869 TFLOP/s, tensor pipe 42% busy), 4 bits in
+// groups of 128 667 us, of 32 803 us (the conversion of codes, a step and an offset per row and group, bounds that one); with a cap 790, 875
+// and 1071 us.  2048 tokens and nothing before them 144 us; 48 tokens over 17000 rows 64 us.
 #include <math.h>
 
 #include <cuda_fp16.h>
@@ -132,7 +133,9 @@ template <int kD, int kGroups> struct ChunkConfig {
   static constexpr size_t kSmem = 6 * (size_t)kTileBytesD + (kInt4 ? 4 * kThinBytes : 0) + 1024;   // two tiles of Q, two of K, two of V
 };
 
-template <int kD, int kGroups>
+// A kernel of its own for capped logits: with the cap in a branch rows in groups of 32 take 905 us for 803 (with a cap 1114 for 1071), others
+// 0.5% more (with a cap bf16 817 for 790, groups of 128 863 for 875).
+template <int kD, int kGroups, bool kCap>
 __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid_constant__ PagedMmaArgs a) {
   using C = ChunkConfig<kD, kGroups>;
   constexpr bool kInt4 = C::kInt4;
@@ -599,8 +602,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         fence_proxy_async_smem();
       }
       mbar_arrive(&B.q_full[w]);
-      const bool cap = c.softcap > 0.f;
-      const float factor = (cap ? c.scale / c.softcap : c.scale * kLog2e) * unscale;   // to the tanh's argument, or to log2 units
+      const float factor = (kCap ? c.scale / c.softcap : c.scale * kLog2e) * unscale;   // to the tanh's argument, or to log2 units
       float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
       const int sees_all = __reduce_min_sync(0xffffffffu, sees);   // what every row of the warp sees
       bool ok = true;
@@ -616,7 +618,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         const bool edge = sees_all < (t0 + j) * kChTile + half * 64 + 64;
         // One pass: the weights of 32 columns at a time by the reference as it stands.  Where a row's logits have outgrown it, its sums, O and
         // what this half has of P so far are scaled down first (the first tile's reference comes about so, too).
-        const float to_log2 = cap ? c.softcap * kLog2e : f;
+        const float to_log2 = kCap ? c.softcap * kLog2e : f;
         const f32x2 ff = f2_make(f, f), f1 = f2_make(to_log2, to_log2);
         const float to_l = ex2_approx(-shift);
         float v[64];
@@ -624,7 +626,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
           tmem_ld32(s_half, v);
           tmem_ld32(s_half + 32u, v + 32);
           tmem_wait_ld();
-          if (cap) {
+          if constexpr (kCap) {
             float far0 = 0.f, far1 = 0.f;
 #pragma unroll
             for (int y = 0; y < 64; y += 4) {
@@ -834,19 +836,19 @@ struct ChunkVariant {
   void (*combine)(PagedMmaArgs);
   size_t smem;
 };
-template <int kD, int kGroups> ChunkVariant chunk_variant() {
-  return ChunkVariant{paged_chunk_kernel<kD, kGroups>, paged_chunk_combine_kernel<kD>, ChunkConfig<kD, kGroups>::kSmem};
+template <int kD, int kGroups> ChunkVariant chunk_variant(bool cap) {
+  return ChunkVariant{cap ? paged_chunk_kernel<kD, kGroups, true> : paged_chunk_kernel<kD, kGroups, false>, paged_chunk_combine_kernel<kD>, ChunkConfig<kD, kGroups>::kSmem};
 }
 bool pick_chunk(const PagedCache& c, ChunkVariant* v) {
   const int groups = c.format == RESTKV_PAGES_INT4 ? c.d / c.group : 0;
   switch (c.d * 16 + groups) {
-    case 64 * 16 + 0: *v = chunk_variant<64, 0>(); return true;
-    case 64 * 16 + 1: *v = chunk_variant<64, 1>(); return true;
-    case 64 * 16 + 2: *v = chunk_variant<64, 2>(); return true;
-    case 128 * 16 + 0: *v = chunk_variant<128, 0>(); return true;
-    case 128 * 16 + 1: *v = chunk_variant<128, 1>(); return true;
-    case 128 * 16 + 2: *v = chunk_variant<128, 2>(); return true;
-    case 128 * 16 + 4: *v = chunk_variant<128, 4>(); return true;
+    case 64 * 16 + 0: *v = chunk_variant<64, 0>(c.softcap > 0.f); return true;
+    case 64 * 16 + 1: *v = chunk_variant<64, 1>(c.softcap > 0.f); return true;
+    case 64 * 16 + 2: *v = chunk_variant<64, 2>(c.softcap > 0.f); return true;
+    case 128 * 16 + 0: *v = chunk_variant<128, 0>(c.softcap > 0.f); return true;
+    case 128 * 16 + 1: *v = chunk_variant<128, 1>(c.softcap > 0.f); return true;
+    case 128 * 16 + 2: *v = chunk_variant<128, 2>(c.softcap > 0.f); return true;
+    case 128 * 16 + 4: *v = chunk_variant<128, 4>(c.softcap > 0.f); return true;
     default: return false;
   }
 }
@@ -856,15 +858,16 @@ int chunk_ctas(int sm_count) { return sm_count < kMaxCtas ? sm_count : kMaxCtas;
 
 cudaError_t paged_chunk_init() {
   PagedCache c{};
-  for (int d : {64, 128})
-    for (int group : {0, 32, 64, 128}) {
-      c.d = d; c.group = group;
-      c.format = group ? RESTKV_PAGES_INT4 : RESTKV_PAGES_BF16;
-      ChunkVariant v;
-      if (group > d || !pick_chunk(c, &v)) continue;
-      const cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
-      if (e != cudaSuccess) return e;
-    }
+  for (float cap : {0.f, 1.f})
+    for (int d : {64, 128})
+      for (int group : {0, 32, 64, 128}) {
+        c.d = d; c.group = group; c.softcap = cap;
+        c.format = group ? RESTKV_PAGES_INT4 : RESTKV_PAGES_BF16;
+        ChunkVariant v;
+        if (group > d || !pick_chunk(c, &v)) continue;
+        const cudaError_t e = cudaFuncSetAttribute(v.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)v.smem);
+        if (e != cudaSuccess) return e;
+      }
   return cudaSuccess;
 }
 
