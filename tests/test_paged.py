@@ -859,3 +859,64 @@ def test_attend_chunk_equals_its_tokens(handle, fmt):
         assert float((one[:, :, 0].float() - whole[:, :, i].float()).abs().max()) <= 5.5 * (2 * 2.0 ** -8 + 2 * 2.0 ** -8)
         assert float((l1[:, :, 0] - lse[:, :, i]).abs().max()) <= 2.0 ** -12
     assert handle.poll_status() == rk.RESTKV_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "int4-bf16", "int4-f32"])
+@pytest.mark.parametrize("spec", [(2, 8, 2, 128, 16, [300, 277], 200), (1, 3, 1, 96, 16, [40], 40), (1, 4, 4, 64, 32, [513], 400), (3, 8, 2, 128, 48, [7, 1, 100], 1),
+                                  (2, 4, 1, 256, 16, [33, 18], 17)])
+def test_no_paged_write_lands_outside_a_buffer(handle, fmt, spec):
+    """Pages, outputs and workspace out of one allocation with 4 KB bands of a pattern between them, which are intact afterwards."""
+    b, Hq, Hkv, d, R, lengths, t = spec
+    rng = np.random.default_rng(19)
+    dtype = "f32" if fmt.endswith("f32") else "bf16"
+    cache = Cache(rng, b, Hq, Hkv, d, fmt.split("-")[0], R, -(-max(lengths) // R), 32 if fmt.startswith("int4") else 0, dtype)
+    size = 4 if dtype == "f32" else 2
+    parts = {"K": cache.K.numel(), "V": cache.V.numel(), "q": b * Hq * t * d * size, "out": b * Hq * t * d * size, "lse": b * Hq * t * 4,
+             "ws": handle.paged_workspace_bytes(cache.desc, t), "Kr": b * Hkv * max(lengths) * d * size, "Vr": b * Hkv * max(lengths) * d * size}
+    at, total = {}, 4096
+    for k, n in parts.items():
+        at[k] = total
+        total = -(-(total + n) // 256) * 256 + 4096
+    memory = torch.full((total,), 0xA5, dtype=torch.uint8, device="cuda")
+    part = {k: memory[at[k]: at[k] + n] for k, n in parts.items()}
+    inside = torch.zeros(total, dtype=torch.bool, device="cuda")
+    for k, n in parts.items():
+        inside[at[k]: at[k] + n] = True
+    new, Q = to_dev(rng.standard_normal((2, b, Hkv, max(lengths), d)), cache.t), to_dev(rng.standard_normal((b, Hq, t, d)), cache.t)
+    angles = torch.arange(max(lengths), device="cuda")[:, None] * torch.linspace(1.0, 0.01, d // 2, device="cuda")
+    rotation = rk.make_rotation(angles.cos().contiguous(), angles.sin().contiguous(), d)
+    n, most = dev_i32(lengths), max(lengths)
+    # the sequences but for the last t rows, then those with their queries, attention, and all of it read back
+    handle.paged_append(cache.desc, most, new[0], new[1], part["K"], part["V"], n, cache.table, counts=n)
+    handle.paged_append(cache.desc, t, new[0, :, :, -t:], new[1, :, :, -t:], part["K"], part["V"], n, cache.table, counts=dev_i32([min(t, x) for x in lengths]),
+                        rotation=rotation, Q=Q, Q_out=part["q"])
+    out = part["q"].view(cache.t).view(b, Hq, t, d)
+    handle.paged_attend(cache.desc, t, out, part["K"], part["V"], n, cache.table, part["out"], part["ws"], lse=part["lse"].view(torch.float32),
+                        counts=dev_i32([min(t, x) for x in lengths]))
+    handle.paged_read(cache.desc, part["K"], part["V"], n, cache.table, most, part["Kr"], part["Vr"])
+    torch.cuda.synchronize()
+    assert handle.poll_status() == rk.RESTKV_OK
+    assert bool((memory[~inside] == 0xA5).all())
+    # and everything that is promised has been written
+    assert bool(torch.isfinite(part["out"].view(cache.t).float()).all())
+    assert bool(torch.isfinite(part["Kr"].view(cache.t).float()).all()) and bool(torch.isfinite(part["Vr"].view(cache.t).float()).all())
+    pages = part["K"].view_as(cache.K)
+    spare = torch.ones(cache.n_pages, dtype=torch.bool)
+    spare[torch.from_numpy(cache.table_np.reshape(-1))] = False
+    assert bool((pages[spare.cuda()] == 0xA5).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+@pytest.mark.parametrize("t", [1, 6, 200])
+def test_attend_in_fp32_throughout(handle, fmt, t):
+    """Kernel path 1: the same call within the bounds of the tensor cores', and within those of fp32 sums and one rounding of the output."""
+    rng = np.random.default_rng(20)
+    cache = Cache(rng, 2, 8, 2, 128, fmt, 16, 20, 64 if fmt == "int4" else 0, softcap=8.0)
+    cache.fill(handle, rng, [310, 205])
+    handle.set_kernel_path(1)
+    try:
+        check_attention(handle, rng, cache, [310, 205], None, t)
+    finally:
+        handle.set_kernel_path(0)
