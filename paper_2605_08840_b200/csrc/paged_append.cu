@@ -65,7 +65,9 @@ __device__ __forceinline__ uint32_t int4_codes(const float* x, float lo, float s
 // grid (batch * n_tokens / warps, y): a warp takes a token, or with few tokens the y-th part of its rows, so that where the token goes and
 // its cosines and sines are found once.  A row lies in kLanes threads, 32 / kLanes heads side by side; Q's heads, then K's, then V's,
 // some rounds of them on their way before the first is needed.  What bounds it: HBM (every row is read and written once), in 4 bits
-// the instructions beside it, or for one token the latency of lengths -> table -> row.
+// the instructions beside it (366 per warp and 256 values, a quarter of them the codes), or for one token the latency of lengths -> table
+// -> row.  Measured, 32 + 8 heads of 128: one token 2.8 us; 8 x up to 4093 tokens, half of the dims rotated, into bf16 112 us (4.5 TB/s);
+// 32768 rotated tokens into 4 bits 219 us (4.1 TB/s).
 struct AppendArgs {
   PagedCache c;
   RowsView K, V, Q;         // Q.data null: no queries
@@ -283,6 +285,7 @@ __device__ __forceinline__ void int4_read(uint32_t w, uint32_t step_hi, uint32_t
 
 // grid (runs of `run` blocks of 16 rows, batch * Hkv / warps): a warp takes such a run of a head, K and V, so that a block's page is
 // looked up once and its loads are on their way together.  Rows first .. first + n_rows of every head.  Bound by HBM (the rows written).
+// Measured, 4-bit rows into bf16: 8 x up to 32749 rows 223 us (5.8 TB/s), 2176 rows 4.1 us.
 // (4 blocks a run: the set-up is a fifth of the instructions.  With few rows 1, until there are 8 warps per SM: 2176 rows 5.0 us, 8.7 in runs
 // of 4.)
 template <typename T, bool kInt4, int kLanes>

@@ -17,6 +17,7 @@
 //     group, o = sum f16(p step) code + sum p offset, all sums in fp32.
 //     (bf16 16 + code: two operations per register, and the weights' rounding weighs twice as much unless 8 is taken off the codes:
 //     60 us for 131072 rows.  e4m3 codes: m16n8k32 is carried out as conversions and f16 products here, 60 us, too.)
+// Measured, 32 query heads of 128 over 8 KV heads: 131072 rows of 4 bits 40 us (3.7 TB/s), of bf16 93 us (5.8 TB/s); 2085 rows of 4 bits 7.8 us.
 // Work is split in one of two ways:
 //   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
 //     short caches, where latency counts;
