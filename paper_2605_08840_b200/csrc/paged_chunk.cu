@@ -26,7 +26,8 @@
 //   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand
 //     (relative error 9.3e-8, minimax), else 1 - 2 / (1 + e^2y) with two trips to the special-function unit.
 //     (A part of the exponentials by a polynomial, too: an eighth of them 825 us for 811, a quarter 853; exponentials by turns with the other
-//     tile's: 678 us for 667, with a cap 1031 for 874.  The chain bounds it, not the unit.)
+//     tile's: 678 us for 667, with a cap 1031 for 874; weights made beside the maximum and made again where it has moved: 707 for 667, with a
+//     cap 828 for 879, but bf16 804 for 789, groups of 32 1104 for 1068.  The chain bounds it, not the unit.)
 // The tiles that a unit's last query row sees, of all units end to end, are dealt out evenly; what several CTAs share is merged by a second
 // kernel.  Measured, 2048 tokens of 32 heads of 128 (8 KV heads) over 18432 rows: bf16 672 us (869 TFLOP/s, tensor pipe 42% busy), 4 bits in
 // groups of 128 667 us, of 32 803 us (the conversion of codes, a step and an offset per row and group, bounds that one); with a cap 790, 875
