@@ -459,8 +459,10 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
 
 /*
  * restkv_paged_read -- rows back out of the pages, as restkv_evict and the other calls take them: K_out[b,h,i] = row first + i.
- *   first         device int32, of the shape of lengths; NULL: 0
- *   K_out, V_out  device [batch, n_kv_heads, n_rows, head_dim] contiguous, dtype; rows past the sequence's length become 0
+ *   first         device int32, of the shape of lengths; NULL: 0.  May be negative: lengths - n_rows gives the last n_rows rows of
+ *                 every sequence, at the end of the output also those of shorter ones
+ *   K_out, V_out  device [batch, n_kv_heads, n_rows, head_dim] contiguous, dtype; rows before row 0 and past the sequence's length
+ *                 become 0
  */
 restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, const void* K_pages, const void* V_pages,
                                 const int32_t* lengths, const int32_t* table, const int32_t* first, int n_rows, void* K_out,

@@ -284,7 +284,7 @@ __device__ __forceinline__ void int4_read(uint32_t w, uint32_t step_hi, uint32_t
 }
 
 // grid (runs of `run` blocks of 16 rows, batch * Hkv / warps): a warp takes such a run of a head, K and V, so that a block's page is
-// looked up once and its loads are on their way together.  Rows first .. first + n_rows of every head.  Bound by HBM (the rows written).
+// looked up once and its loads are on their way together.  Rows first .. first + n_rows of every head; first may be negative.  Bound by HBM (the rows written).
 // Measured, 4-bit rows into bf16: 8 x up to 32749 rows 223 us (5.8 TB/s), 2176 rows 4.1 us.
 // (4 blocks a run: the set-up is a fifth of the instructions.  With few rows 1, until there are 8 warps per SM: 2176 rows 5.0 us, 8.7 in runs
 // of 4.)
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const PagedCach
       if ((unsigned int)page < (unsigned int)c.n_pages) at = (((long long)page * c.Hkv + h) * per_page + within) * c.block_bytes;
       else if (lane == 0) atomicOr(c.dev_status, kDevBadIndex);
     }
-    if (++within == per_page) { within = 0; ++slot; }
+    if (block_row >= 0 && ++within == per_page) { within = 0; ++slot; }   // (a run may begin before row 0, at block 0 of slot 0)
     if (!has) continue;
 #pragma unroll
     for (int side = 0; side < 2; ++side) {

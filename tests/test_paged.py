@@ -920,3 +920,44 @@ def test_attend_in_fp32_throughout(handle, fmt, t):
         check_attention(handle, rng, cache, [310, 205], None, t)
     finally:
         handle.set_kernel_path(0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "int4-bf16", "int4-f32"])
+@pytest.mark.parametrize("page_rows", [16, 48])
+@pytest.mark.parametrize("per_head", [False, True])
+def test_read_from_before_the_first_row(handle, fmt, page_rows, per_head):
+    """Any first row, negative ones among them, in calls small enough for a block of 16 rows per warp and large enough for runs of blocks."""
+    b, Hkv, d = 5, 8, 64
+    rng = np.random.default_rng(21)
+    dtype = "f32" if fmt.endswith("f32") else "bf16"
+    fmt = fmt.split("-")[0]
+    cache = Cache(rng, b, Hkv, Hkv, d, fmt, page_rows, -(-560 // page_rows), 32 if fmt == "int4" else 0, dtype, per_head=per_head)
+    lengths = np.array([540, 37, 0, 512, 301])
+    if per_head:
+        lengths = np.maximum(lengths[:, None] - 13 * np.arange(Hkv), 0)
+    cache.fill(handle, rng, lengths)
+    per = np.broadcast_to(lengths.reshape(b, -1), (b, Hkv))
+    host = {}
+    for is_key, pages in ((True, cache.K), (False, cache.V)):
+        for i in range(b):
+            for h in range(Hkv):
+                x = cache.rows(pages, is_key, i, h, int(per[i, h]))[0].astype(np.float32)
+                host[is_key, i, h] = bf16_round(x) if dtype == "bf16" else x
+    runs_of_blocks = 16 * (-(-32 * torch.cuda.get_device_properties(0).multi_processor_count // (b * Hkv)) + 1)   # 32 blocks per SM and more
+    for n_rows in (40, 571, runs_of_blocks):
+        for first in (lengths - n_rows, rng.integers(-80, 60, lengths.shape), np.full(lengths.shape, -16), np.full(lengths.shape, -n_rows), np.full(lengths.shape, 3)):
+            K, V = (torch.full((b, Hkv, n_rows, d), float("nan"), dtype=cache.t, device="cuda") for _ in range(2))
+            handle.paged_read(cache.desc, cache.K, cache.V, dev_i32(lengths), cache.table, n_rows, K, V, first=dev_i32(first))
+            torch.cuda.synchronize()
+            starts = np.broadcast_to(first.reshape(b, -1), (b, Hkv))
+            for got, is_key in ((K, True), (V, False)):
+                got = got.float().cpu().numpy()
+                for i in range(b):
+                    for h in range(Hkv):
+                        want = np.zeros((n_rows, d), np.float32)
+                        lo, hi = max(0, int(starts[i, h])), min(int(per[i, h]), int(starts[i, h]) + n_rows)
+                        if hi > lo:
+                            want[lo - starts[i, h]:hi - starts[i, h]] = host[is_key, i, h][lo:hi]
+                        assert np.array_equal(got[i, h], want), (n_rows, i, h)
+    assert handle.poll_status() == rk.RESTKV_OK
