@@ -396,7 +396,8 @@ typedef struct {
   int page_rows, n_pages, table_width;
   int lengths_per_head; /* 0: lengths [batch], 1: lengths [batch, n_kv_heads] */
   float softmax_scale;  /* 0 => 1/sqrt(head_dim) */
-  float softcap;        /* 0, or c > 0: a scaled logit s becomes c * tanh(s / c) */
+  float softcap;        /* 0, or c > 0: a scaled logit s becomes c * tanh(s / c), to 2^-20 of itself (with many tokens and c <= 64 to
+                           2^-22 c); c above 2^100 counts as 2^100 */
 } restkv_paged;
 
 /* Rows [batch, heads, n_tokens, head_dim] on the device: element strides (multiples of 8, head_dim is contiguous, the base

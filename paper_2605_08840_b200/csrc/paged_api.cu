@@ -19,7 +19,7 @@ static restkv_status make_cache(const restkv_paged* s, PagedCache* out) {
   c.scale = s->softmax_scale != 0.f ? s->softmax_scale : 1.0f / sqrtf((float)c.d);
   if (!(c.scale > 0.f) || !std::isfinite(c.scale)) return RESTKV_ERR_INVALID_ARG;
   if (c.d % 32 != 0 || c.d > 256) return RESTKV_ERR_UNSUPPORTED;
-  c.softcap = s->softcap;
+  c.softcap = fminf(s->softcap, 0x1p100f);   // so that logits over it keep all their bits in fp32; they would have to pass 2^88 to notice
   c.format = s->page_format;
   switch (s->page_format) {
     case RESTKV_PAGES_BF16:

@@ -23,8 +23,8 @@
 //     the weights before that;
 //   - dims within K's operand chunks are in the order in which they come out of a word, and Q's in the same; V's order is undone where O
 //     is written.
-//   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand
-//     (relative error 9.3e-8, minimax), else 1 - 2 / (1 + e^2y) with two trips to the special-function unit.
+//   - a capped logit's tanh is an odd polynomial on the FMA pipe while |s / cap| <= 0.6 for all rows and columns that a warp has in hand;
+//     else the exponential form with two trips to the special-function unit, under large caps that or the polynomial one by one.
 //     (A part of the exponentials by a polynomial, too: an eighth of them 825 us for 811, a quarter 853; exponentials by turns with the other
 //     tile's: 678 us for 667, with a cap 1031 for 874; weights made beside the maximum and made again where it has moved: 707 for 667, with a
 //     cap 828 for 879, but bf16 804 for 789, groups of 32 1104 for 1068.  The chain bounds it, not the unit.)
@@ -53,6 +53,10 @@ constexpr int kInfo = 4;                     // tiles whose factors are kept: th
 constexpr int kChSnap = 4;
 // log2 of the largest weight that a rescaling leaves, and of what it may grow to before the next one
 constexpr float kChStart = 5.f, kChSlack = 13.f;
+
+// Up to this cap small logits may go by tanh_far, too: 2^-22 of the cap is 2^-16, a thirty-second of what rounds a weight here.  (One by one,
+// logits on both sides of 0.6 of the cap: 18432 rows in groups of 128 1504 us for 1207, bf16 1387 for 1144.)
+constexpr float kTanhFarAlone = 64.f;
 
 struct ChunkBarriers {
   uint64_t q_full[2], s_full[2][2], p_full[2][2], pv_done[2][2], k_full[2], k_empty[2], v_full[2], v_empty[2], drained;
@@ -83,18 +87,6 @@ __device__ __forceinline__ void operands_of(uint32_t w, uint32_t s, uint32_t s16
   const uint32_t w8 = w >> 8;
   sts128(to, hfma2(s, w & 0x000F000Fu, l), hfma2(s16, w & 0x00F000F0u, l), hfma2(s, w8 & 0x000F000Fu, l), hfma2(s16, w8 & 0x00F000F0u, l));
 }
-
-// tanh(t) for |t| <= 0.6.
-__device__ __forceinline__ f32x2 tanh_near(f32x2 t) {
-  const f32x2 z = f2_mul(t, t);
-  f32x2 p = f2_make(0.0154755134f, 0.0154755134f);
-  p = f2_fma(p, z, f2_make(-0.0521015525f, -0.0521015525f));
-  p = f2_fma(p, z, f2_make(0.133101761f, 0.133101761f));
-  p = f2_fma(p, z, f2_make(-0.333323091f, -0.333323091f));
-  p = f2_fma(p, z, f2_make(0.99999994f, 0.99999994f));
-  return f2_mul(p, t);
-}
-__device__ __forceinline__ float tanh_any(float t) { return fmaf(-2.f, rcp_approx(1.f + ex2_approx(t * 2.f * kLog2e)), 1.f); }
 
 // Row `row` of an operand 16 elements deep, without swizzle: 8 rows of 16 bytes together, both halves of a row 128 bytes apart.
 constexpr uint32_t kThinBytes = 128 * 32;
@@ -614,7 +606,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         if (!ok) break;
         tc_fence_after();
         const uint32_t s_half = s_tm + (uint32_t)half * 64u;
-        const float f = factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
+        const float f = kCap ? fminf(factor * k_factor[at % kInfo], 0x1p126f) : factor * k_factor[at % kInfo], shift = v_shift[at % kInfo];
         const int left = sees - (t0 + j) * kChTile - half * 64;     // columns that the row sees
         const bool edge = sees_all < (t0 + j) * kChTile + half * 64 + 64;
         // One pass: the weights of 32 columns at a time by the reference as it stands.  Where a row's logits have outgrown it, its sums, O and
@@ -634,16 +626,23 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
               far0 = fmax3(far0, fabsf(v[y]), fabsf(v[y + 1]));
               far1 = fmax3(far1, fabsf(v[y + 2]), fabsf(v[y + 3]));
             }
-            if (__all_sync(0xffffffffu, fmaxf(far0, far1) * f <= 0.6f)) {
+            if (__all_sync(0xffffffffu, fmaxf(far0, far1) * f <= kTanhNear)) {
 #pragma unroll
               for (int y = 0; y < 64; y += 2) {
                 const f32x2 z = tanh_near(f2_mul(f2_make(v[y], v[y + 1]), ff));
                 v[y] = f2_lo(z);
                 v[y + 1] = f2_hi(z);
               }
+            } else if (c.softcap <= kTanhFarAlone) {
+#pragma unroll
+              for (int y = 0; y < 64; ++y) v[y] = tanh_far(v[y] * f);
             } else {
 #pragma unroll
-              for (int y = 0; y < 64; ++y) v[y] = tanh_any(v[y] * f);
+              for (int y = 0; y < 64; y += 2) {
+                v[y] *= f;
+                v[y + 1] *= f;
+                tanh_any(v[y], v[y + 1]);
+              }
             }
           }
           if (edge) {

@@ -323,10 +323,10 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     // 4 bits: in f16, scaled by a power of two per row (and 2^-4 where the codes come 16 times too large); sums of q per group in the
     // codes' and that scale, which the logits' factor takes out again.
     uint32_t qb[kD / 16][kNT][2];
-    float q_sum[kNT][kG][2], to_log2[kNT][2];  // to log2 units, or to the cap's exponent
+    float q_sum[kNT][kG][2], to_log2[kNT][2];  // to log2 units, or to the cap's
     int sees[kNT][2];
     int sees_least = n;
-    const float factor = c.softcap > 0.f ? 2.f * kLog2e * c.scale / c.softcap : c.scale * kLog2e;
+    const float factor = c.softcap > 0.f ? fminf(c.scale / c.softcap, 0x1p126f) : c.scale * kLog2e;
 #pragma unroll
     for (int t = 0; t < kNT; ++t) {
 #pragma unroll
@@ -346,7 +346,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         int e = 141 - (int)(__float_as_uint(top) >> 23);
         e = e < -100 ? -100 : e > 100 ? 100 : e;
         const float scale = top < INFINITY ? __uint_as_float((uint32_t)(127 + e) << 23) : __uint_as_float(0x7FFFFFFFu);
-        const float unscale = __uint_as_float((uint32_t)(127 + 24 - e) << 23) * factor;
+        const float unscale = fminf(__uint_as_float((uint32_t)(127 + 24 - e) << 23) * factor, 0x1p126f);   // finite: logits of 0 stay 0
         to_log2[t][0] = __shfl_sync(0xffffffffu, unscale, 8 * q4);
         to_log2[t][1] = __shfl_sync(0xffffffffu, unscale, 8 * q4 + 4);
         float sum[kG];
@@ -458,7 +458,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
           }
         }
       }
-      // logits in log2 units; rows that a query row does not see weigh nothing
+      // logits in log2 units (first as parts of the cap); rows that a query row does not see weigh nothing
 #pragma unroll
       for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
@@ -466,13 +466,29 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
 #pragma unroll
           for (int x = 0; x < 4; ++x) sc[k][t][x] *= to_log2[t][x & 1];
       if (cap_log2 > 0.f) {
-        // cap * tanh(x / cap) with tanh(y) = 1 - 2 / (1 + e^2y): 2^-22 of the cap
+        float far = 0.f;
+#pragma unroll
+        for (int k = 0; k < kBlocks; ++k)
+#pragma unroll
+          for (int t = 0; t < kNT; ++t) far = fmax3(fmax3(far, fabsf(sc[k][t][0]), fabsf(sc[k][t][1])), fabsf(sc[k][t][2]), fabsf(sc[k][t][3]));
+        const bool near = __all_sync(0xffffffffu, far <= kTanhNear);
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
           for (int t = 0; t < kNT; ++t)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) sc[k][t][x] = fmaf(-2.f * cap_log2, rcp_approx(1.f + ex2_approx(sc[k][t][x])), cap_log2);
+            for (int x = 0; x < 4; x += 2) {
+              float *u = &sc[k][t][x], *v = &sc[k][t][x + 1];
+              if (near) {
+                const f32x2 z = tanh_near(f2_make(*u, *v));
+                *u = f2_lo(z);
+                *v = f2_hi(z);
+              } else {
+                tanh_any(*u, *v);
+              }
+              *u *= cap_log2;
+              *v *= cap_log2;
+            }
       }
       if constexpr (kEdge) {
 #pragma unroll

@@ -961,3 +961,88 @@ def test_read_from_before_the_first_row(handle, fmt, page_rows, per_head):
                             want[lo - starts[i, h]:hi - starts[i, h]] = host[is_key, i, h][lo:hi]
                         assert np.array_equal(got[i, h], want), (n_rows, i, h)
     assert handle.poll_status() == rk.RESTKV_OK
+
+
+# ---- each attention kernel against the bits that the header states for it --------------------------------------------------------------
+
+def attend_closely(handle, cache, lengths, Q, kernel, hidden=(), tokens=None, note=""):
+    """One call against 64 bits, within what the header says is rounded in that kernel ("few" tokens, "chunk", "fp32") plus fp32 sums and the
+    output's own rounding.  hidden: table slots (sequence, slot) whose page number is bad; tokens: the query tokens that are looked at."""
+    b, Hq, Hkv, d, R, t = cache.batch, cache.Hq, cache.Hkv, cache.d, cache.R, Q.shape[2]
+    G = Hq // Hkv
+    out = torch.full((b, Hq, t, d), float("nan"), dtype=cache.t, device="cuda")
+    lse = torch.full((b, Hq, t), float("nan"), device="cuda")
+    ws = torch.full((handle.paged_workspace_bytes(cache.desc, t),), 255, dtype=torch.uint8, device="cuda")
+    table = cache.table.clone()
+    for i, slot in hidden:
+        table[i, slot] = (-1, cache.n_pages, 2 ** 31 - 1)[slot % 3]
+    handle.set_kernel_path(1 if kernel == "fp32" else 0)
+    try:
+        handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32(lengths), table, out, ws, lse=lse)
+    finally:
+        handle.set_kernel_path(0)
+    torch.cuda.synchronize()
+    assert handle.poll_status() == (rk.ERR_INVALID_ARG if hidden else rk.RESTKV_OK), note
+    got_o, got_l, q64 = np64(out), np64(lse), np64(Q)
+    for i in range(b):
+        n = int(lengths[i])
+        there = np.array([(i, r // R) not in hidden for r in range(n)], bool)
+        for h in range(Hkv):
+            K, k_steps = cache.rows(cache.K, True, i, h, n)
+            V, v_steps = cache.rows(cache.V, False, i, h, n)
+            # what K's products are made of: |K| itself, or offsets and up to 15 steps of a group
+            K_parts = np.abs(K) + 30 * k_steps
+            for hq in range(h * G, h * G + G):
+                for j in range(t) if tokens is None else tokens:
+                    see = np.flatnonzero(there[: max(0, n - (t - 1 - j))])
+                    if len(see) == 0:
+                        assert np.all(got_o[i, hq, j] == 0) and np.isneginf(got_l[i, hq, j]), note
+                        continue
+                    q, v, step = q64[i, hq, j], V[see], v_steps[see]
+                    s = (K[see] @ q) * cache.scale
+                    # fp32 sums of d terms in the tensor cores' order: 2^-19 of their sizes; chunks keep steps of K down to 2^-16 of the
+                    # largest of 128 rows; the cap's tanh has a relative error of 2^-21, or under small caps 2^-22 of the cap
+                    parts = K_parts[see].max(0) if kernel == "chunk" and cache.fmt == "int4" else K_parts[see]
+                    dl = 2.0 ** -19 * (parts @ np.abs(q)).max() * cache.scale + 2.0 ** -20
+                    if kernel == "chunk" and cache.fmt == "int4":
+                        dl += 2.0 ** -16 * (k_steps.max(0) @ np.abs(q)) * cache.scale
+                    if cache.cap:
+                        dl += 2.0 ** -19 * np.abs(s).max()
+                        s = cache.cap * np.tanh(s / cache.cap)
+                    top = s.max()
+                    w = np.exp(s - top)
+                    l = top + math.log(w.sum())
+                    w /= w.sum()
+                    o, mass = w @ v, w @ np.abs(v)
+                    if kernel == "fp32":
+                        bits = 0.0
+                    elif cache.fmt == "bf16":
+                        bits = (2.0 ** -16 if kernel == "few" else 2.0 ** -8) * mass
+                    elif kernel == "few":     # weight * step in f16 meets a code; below 2^-19 of the largest such product (2^5) an f16's last place
+                        bits = 2.0 ** -11 * (w @ (15 * step)) + len(see) * 15 * 2.0 ** -30 * w.max() * step.max()
+                    else:                     # weights and values in f16, both in the range of their tile
+                        bits = 2.0 ** -10 * mass + 2.0 ** -13 * step.max() + len(see) * 2.0 ** -30 * w.max() * np.abs(v).max()
+                    bound = bits + (2.1 * dl + 2.0 ** -18) * mass + (2.0 ** -8 if cache.dtype == "bf16" else 2.0 ** -24) * np.abs(o) + 1e-30
+                    err = np.abs(got_o[i, hq, j] - o)
+                    assert np.all(err <= bound), "%s: out %.3f of the bound (%s)" % (note, float((err / bound).max()), (i, hq, j))
+                    assert abs(got_l[i, hq, j] - l) <= dl + 2.0 ** -20 * abs(l) + 2.0 ** -18, "%s: lse off by %.3g for %.3g" % (note, got_l[i, hq, j] - l, dl)
+    return out
+
+
+CLOSELY = [("few", 1), ("few", 3), ("chunk", 200), ("fp32", 1), ("fp32", 70)]     # kernel, tokens (of 8 query heads over 2 KV heads)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("int4", 32), ("int4", 64), ("int4", 128)])
+@pytest.mark.parametrize("kernel,t", CLOSELY)
+@pytest.mark.parametrize("cap", [0.0, 3.0, 50.0, 1e3, 1e5, 1e6, 1e8, 1e20, 3e38])
+def test_attend_under_caps_of_any_size(handle, fmt, group, kernel, t, cap):
+    """A cap far above the logits leaves them as they are, one near them bends them: in every kernel, logits with and without others near the cap
+    beside them."""
+    rng = np.random.default_rng(22)
+    cache = Cache(rng, 1, 8, 2, 128, fmt, 16, 22, group, softcap=cap)
+    cache.fill(handle, rng, [340])
+    for scale in (0.1, 2.0) + ((cap,) if 1e3 <= cap <= 1e6 else ()):
+        q = rng.standard_normal((1, 8, t, 128))
+        q[:, :1 if scale == cap else 8] *= scale        # or one head's logits reach the cap, in the same tiles as those of the others
+        attend_closely(handle, cache, [340], to_dev(q, cache.t), kernel, tokens=[0, t // 2, t - 1], note="%s, q %g" % (kernel, scale))
