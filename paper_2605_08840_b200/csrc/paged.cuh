@@ -135,6 +135,30 @@ template <> struct Pack8<float> {
   }
 };
 
+// 8 dims of a row of K or V, as fp32.
+template <typename T, bool kInt4>
+__device__ __forceinline__ void load_chunk(const PagedCache& c, const uint8_t* block, int r, int chunk, bool is_key, float* x) {
+  if constexpr (!kInt4) {
+    Pack8<T> p;
+    p.load(reinterpret_cast<const T*>(block + (long long)r * c.row_bytes) + chunk * 8);
+    p.get(x);
+  } else {
+    const int m = chunk >> 2, q = chunk & 3, words = c.d >> 5;
+    const uint8_t* codes = block + r * c.row_bytes;
+    unsigned int w;
+    if (is_key) {
+      w = reinterpret_cast<const unsigned int*>(codes)[q * words + m];
+    } else {
+      const unsigned short* v = reinterpret_cast<const unsigned short*>(codes);
+      w = v[2 * q * words + m] | (unsigned int)v[(2 * q + 1) * words + m] << 16;
+    }
+    const unsigned short* p = reinterpret_cast<const unsigned short*>(block + int4_params(c.d, chunk * 8 / c.group, r));
+    const float step = __uint_as_float((unsigned int)p[0] << 16), lo = __uint_as_float((unsigned int)p[4] << 16);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = fmaf(step, (float)(w >> (4 * e) & 15u), lo);
+  }
+}
+
 // ---- launches ----
 cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K_new, const RowsView& V_new, uint8_t* K_pages,
                                 uint8_t* V_pages, const int* positions, const RotationView& rotation, const RowsView& Q, void* Q_out,

@@ -138,6 +138,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   __shared__ __align__(8) ChunkBarriers B;
   __shared__ Piece piece_s;
   __shared__ uint32_t tmem_slot;
+  __shared__ int bad_pages[2];                          // in units that the CTA begins, in one that it goes on with
   __shared__ int abort_flag, counted[kChThreads / 32];
   __shared__ float step_max[2][2][kFetchWarps];         // [tile & 1][K, V][warp]
   __shared__ volatile float k_factor[kInfo], v_shift[kInfo];   // per tile: the logits' factor, log2 of the weights'
@@ -149,7 +150,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
   auto wait = [&](uint64_t* bar, int phase) { return mbar_wait(bar, (uint32_t)phase & 1u, &abort_flag, c.dev_status, kDevTimeout, a.wait_limit); };
 
   if (threadIdx.x == 0) {
-    abort_flag = 0;
+    abort_flag = bad_pages[0] = bad_pages[1] = 0;
     for (int i = 0; i < 2; ++i) {
       mbar_init(&B.q_full[i], 128);
       for (int half = 0; half < 2; ++half) {
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     if (threadIdx.x == 0) {
       const Run run = piece_s.run;
       if (run.tile < run.end) piece_s.cut(1, tiles_of);
-      a.begins[blockIdx.x] = run.tile < run.end ? make_int2(piece_s.unit, piece_s.t0) : make_int2(-1, 0);
+      a.begins[blockIdx.x] = run.tile < run.end ? make_int4(piece_s.unit, piece_s.t0, 0, 0) : make_int4(-1, 0, 0, 0);
     }
   }
   tc_fence_before();
@@ -451,6 +452,17 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     each_piece([&](const Unit& u) {
       // ---------------- the products, by one thread ----------------
       const int tiles = u.tiles, done = u.done, nth = u.nth;
+      {
+        // While the others fetch: are all of the piece's pages there?  If not, the merge makes the unit's rows anew.  (Rows left out in the
+        // softmax here: 2-5% of every call's time, whichever way.)
+        const int row0 = u.t0 * kChTile, row1 = min((u.t0 + tiles) * kChTile, u.n), pages = row1 > row0 ? (row1 - 1) / c.page_rows + 1 : 0;
+        bool bad = false;
+#pragma unroll 4
+        for (int x = row0 / c.page_rows + lane; x < pages; x += 32)
+          bad |= (unsigned int)c.table[(long long)u.b * c.table_width + x] >= (unsigned int)c.n_pages;
+        if (bad) bad_pages[u.t0 > 0] = 1;
+        __syncwarp();
+      }
       if (warp == kSoftmaxWarps + kFetchWarps && tiles > 0 && elect_one()) {
         constexpr uint32_t idesc_s = kInt4 ? make_idesc_f16(128, 64, false) : make_idesc_bf16(128, 64, false);
         constexpr uint32_t idesc_o = kInt4 ? make_idesc_f16(128, kD, true) : make_idesc_bf16(128, kD, true);
@@ -768,26 +780,89 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
     });
   }
   __syncthreads();
+  if (threadIdx.x == 0 && (bad_pages[0] | bad_pages[1]) != 0) {
+    a.begins[blockIdx.x].z = bad_pages[0];
+    a.begins[blockIdx.x].w = bad_pages[1];
+  }
   if (warp == kSoftmaxWarps + kFetchWarps) tmem_dealloc(tmem, 512);
 }
 
+// Query row rho of a KV head by one warp in fp32, without the rows of bad pages: for units that have some, a call that reports an error.
+template <int kD, bool kInt4>
+__device__ __noinline__ void row_past_bad_pages(const PagedMmaArgs& a, int unit, int row) {
+  const PagedCache& c = a.c;
+  const int bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv, rho = (unit - bh * a.row_tiles) * kChRows + row;
+  if (rho >= c.n_tokens * c.G) return;
+  constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes;      // 8 dims of a cache row per lane
+  const int lane = threadIdx.x & 31, chunk = lane % kLanes, i = rho / c.G, g = rho - i * c.G, count = paged_count(c, b);
+  const int sees = i < count ? paged_length(c, b, h) - (count - 1 - i) : 0;
+  float q[8], k[8], v[8], m = -INFINITY, l = 0.f, o[8] = {};
+  Pack8<__nv_bfloat16> raw;
+  raw.load(reinterpret_cast<const __nv_bfloat16*>(a.Q.data) + b * a.Q.sb + (long long)(h * c.G + g) * a.Q.sh + i * a.Q.sn + chunk * 8);
+  raw.get(q);
+  for (int r0 = 0; r0 < sees; r0 += kAtOnce) {               // (a block's 16 rows are a multiple of kAtOnce)
+    const long long at = paged_block(c, b, h, r0 / kBlockRows);
+    if (at < 0) continue;
+    const int r = r0 + lane / kLanes;
+    load_chunk<__nv_bfloat16, kInt4>(c, c.K + at, r % kBlockRows, chunk, true, k);
+    load_chunk<__nv_bfloat16, kInt4>(c, c.V + at, r % kBlockRows, chunk, false, v);
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(q[e], k[e], s);
+#pragma unroll
+    for (int off = 1; off < kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+    if (r >= sees) continue;                                 // (its row of the page may hold anything)
+    s *= c.scale;
+    if (c.softcap > 0.f) s = c.softcap * tanhf(s / c.softcap);
+    s *= kLog2e;
+    const float top = fmaxf(m, s), down = m == -INFINITY ? 0.f : ex2_approx(m - top), p = top == -INFINITY ? 0.f : ex2_approx(s - top);
+    m = top;
+    l = fmaf(l, down, p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = fmaf(o[e], down, p * v[e]);
+  }
+  __syncwarp();
+#pragma unroll
+  for (int off = kLanes; off < 32; off <<= 1) {
+    const float mo = __shfl_xor_sync(0xffffffffu, m, off), lo = __shfl_xor_sync(0xffffffffu, l, off), top = fmaxf(m, mo);
+    const float fa = m == -INFINITY ? 0.f : ex2_approx(m - top), fb = mo == -INFINITY ? 0.f : ex2_approx(mo - top);
+    l = l * fa + lo * fb;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = o[e] * fa + __shfl_xor_sync(0xffffffffu, o[e], off) * fb;
+    m = top;
+  }
+  if (lane >= kLanes) return;
+  const float x[2][4] = {{o[0], o[1], o[2], o[3]}, {o[4], o[5], o[6], o[7]}};
+  write_row<kD, 4>(a, b, h, rho, count, 2 * chunk, x[0], m, l);
+  write_row<kD, 4>(a, b, h, rho, count, 2 * chunk + 1, x[1], m, l);
+}
+
 // grid (CTAs of the kernel before, 32), block 256: merges what several of them left of a unit, a row per warp.  A unit is merged by the
-// blocks of the first CTA that began inside it.
-template <int kD>
+// blocks of the first CTA that began inside it.  Units with bad pages are made anew: those of several CTAs there, others by the blocks of theirs.
+template <int kD, bool kInt4>
 __global__ void __launch_bounds__(256) paged_chunk_combine_kernel(const __grid_constant__ PagedMmaArgs a) {
   grid_dependency_wait();
   grid_dependency_launch();
   const PagedCache& c = a.c;
   const int x = blockIdx.x, ctas = gridDim.x, lane = threadIdx.x & 31;
-  const int2 mine = __ldcg(a.begins + x);
+  const int4 mine = __ldcg(a.begins + x);
+  const int row = (int)blockIdx.y * 8 + (threadIdx.x >> 5);
+  if (mine.z != 0) {
+    const int next = x + 1 < ctas ? __ldcg(a.begins + x + 1).x : -1;
+    for (int u = mine.y == 0 ? mine.x : mine.x + 1; u < (next < 0 ? c.batch * c.Hkv * a.row_tiles : next); ++u) row_past_bad_pages<kD, kInt4>(a, u, row);
+  }
   if (mine.x < 0 || mine.y == 0) return;                // (the first CTA begins a unit: x > 0 from here on)
+  int bad = 0;                                          // of the pieces that this lane looks at
   auto inside = [&](int y) {
-    const int2 o = __ldcg(a.begins + y);
-    return o.x == mine.x && o.y > 0;
+    const int4 o = __ldcg(a.begins + y);
+    const bool is = o.x == mine.x && o.y > 0;
+    if (is) bad |= o.w;
+    return is;
   };
   if (inside(x - 1)) return;
+  if (lane == 0) bad |= __ldcg(a.begins + x - 1).z;     // (or of another unit that it begins)
   const int unit = mine.x, bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv, count = paged_count(c, b);
-  const int row = (int)blockIdx.y * 8 + (threadIdx.x >> 5), rho = (unit - bh * a.row_tiles) * kChRows + row;
+  const int rho = (unit - bh * a.row_tiles) * kChRows + row;
   if (rho >= c.n_tokens * c.G) return;
   constexpr long long kSlot = kChRows * (kD + 2);
   constexpr int kPer = kD / 32;
@@ -828,6 +903,10 @@ __global__ void __launch_bounds__(256) paged_chunk_combine_kernel(const __grid_c
     }
     if (n < 32) break;
   }
+  if (__any_sync(0xffffffffu, bad)) {
+    row_past_bad_pages<kD, kInt4>(a, unit, row);
+    return;
+  }
   write_row<kD, kPer>(a, b, h, rho, count, lane, acc, mm, ll);
 }
 
@@ -837,7 +916,7 @@ struct ChunkVariant {
   size_t smem;
 };
 template <int kD, int kGroups> ChunkVariant chunk_variant(bool cap) {
-  return ChunkVariant{cap ? paged_chunk_kernel<kD, kGroups, true> : paged_chunk_kernel<kD, kGroups, false>, paged_chunk_combine_kernel<kD>, ChunkConfig<kD, kGroups>::kSmem};
+  return ChunkVariant{cap ? paged_chunk_kernel<kD, kGroups, true> : paged_chunk_kernel<kD, kGroups, false>, paged_chunk_combine_kernel<kD, (kGroups > 0)>, ChunkConfig<kD, kGroups>::kSmem};
 }
 bool pick_chunk(const PagedCache& c, ChunkVariant* v) {
   const int groups = c.format == RESTKV_PAGES_INT4 ? c.d / c.group : 0;
@@ -880,7 +959,7 @@ bool paged_chunk_supported(const PagedCache& c) {
 }
 
 size_t paged_chunk_bytes(const PagedCache& c, int sm_count) {
-  return (size_t)chunk_ctas(sm_count) * (2 * kChRows * (c.d + 2) * sizeof(float) + sizeof(int2));
+  return (size_t)chunk_ctas(sm_count) * (2 * kChRows * (c.d + 2) * sizeof(float) + sizeof(int4));
 }
 
 cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count, long long wait_limit,
@@ -891,7 +970,7 @@ cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out
   a.c = c; a.Q = Q; a.out = (__nv_bfloat16*)out; a.lse = lse; a.part = part; a.wait_limit = wait_limit;
   a.row_tiles = (int)(((long long)c.n_tokens * c.G + kChRows - 1) / kChRows);
   const int ctas = chunk_ctas(sm_count);
-  a.begins = reinterpret_cast<int2*>(part + (size_t)2 * ctas * kChRows * (c.d + 2));
+  a.begins = reinterpret_cast<int4*>(part + (size_t)2 * ctas * kChRows * (c.d + 2));
   const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), kChThreads, v.smem, st, a);
   if (e != cudaSuccess) return e;
   return launch_chained(v.combine, dim3((unsigned int)ctas, kChRows / 8), 256, 0, st, a);

@@ -15,7 +15,7 @@ struct PagedMmaArgs {
   __nv_bfloat16* out;
   float* lse;        // or null
   float* part;       // per CTA two of: o [rows, d], (m, l) [rows]; without clusters
-  int2* begins;      // per CTA: unit and tile of it that it begins with; chunks
+  int4* begins;      // per CTA, chunks: unit and tile of it that it begins with; whether pages were bad in units that it begins, in one that it goes on with
   int row_tiles;     // units per KV head
   int cluster;       // CTAs per unit, 0: tiles of all units end to end
   long long wait_limit;

@@ -23,30 +23,6 @@ int lanes_per_row(int d) {
   return lanes;
 }
 
-// 8 dims of a row of K or V, as fp32.
-template <typename T, bool kInt4>
-__device__ __forceinline__ void load_chunk(const PagedCache& c, const uint8_t* block, int r, int chunk, bool is_key, float* x) {
-  if constexpr (!kInt4) {
-    Pack8<T> p;
-    p.load(reinterpret_cast<const T*>(block + (long long)r * c.row_bytes) + chunk * 8);
-    p.get(x);
-  } else {
-    const int m = chunk >> 2, q = chunk & 3, words = c.d >> 5;
-    const uint8_t* codes = block + r * c.row_bytes;
-    unsigned int w;
-    if (is_key) {
-      w = reinterpret_cast<const unsigned int*>(codes)[q * words + m];
-    } else {
-      const unsigned short* v = reinterpret_cast<const unsigned short*>(codes);
-      w = v[2 * q * words + m] | (unsigned int)v[(2 * q + 1) * words + m] << 16;
-    }
-    const unsigned short* p = reinterpret_cast<const unsigned short*>(block + int4_params(c.d, chunk * 8 / c.group, r));
-    const float step = __uint_as_float((unsigned int)p[0] << 16), lo = __uint_as_float((unsigned int)p[4] << 16);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = fmaf(step, (float)(w >> (4 * e) & 15u), lo);
-  }
-}
-
 // grid (splits, query rows / 4, batch * Hkv).  A slot of `kLanes` threads takes a cache row, 8 dims per thread; every slot keeps its
 // own running (m, l, o) of the four query rows.
 template <typename T, bool kInt4, int kLanes>

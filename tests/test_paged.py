@@ -1046,3 +1046,34 @@ def test_attend_under_caps_of_any_size(handle, fmt, group, kernel, t, cap):
         q = rng.standard_normal((1, 8, t, 128))
         q[:, :1 if scale == cap else 8] *= scale        # or one head's logits reach the cap, in the same tiles as those of the others
         attend_closely(handle, cache, [340], to_dev(q, cache.t), kernel, tokens=[0, t // 2, t - 1], note="%s, q %g" % (kernel, scale))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("int4", 32), ("int4", 128)])
+@pytest.mark.parametrize("kernel,t", CLOSELY)
+@pytest.mark.parametrize("page_rows", [16, 48])
+@pytest.mark.parametrize("cap", [0.0, 5.0])
+def test_rows_of_bad_pages_are_not_seen(handle, fmt, group, kernel, t, page_rows, cap):
+    """Rows whose page number is outside the pool carry no weight, in every kernel alike; queries that see no others get 0 and -inf."""
+    rng = np.random.default_rng(23)
+    cache = Cache(rng, 2, 8, 2, 128, fmt, page_rows, -(-340 // page_rows), group, softcap=cap)
+    lengths = [340, 210]
+    cache.fill(handle, rng, lengths)
+    hidden = {(0, 1), (0, 2), (0, 6), (0, 339 // page_rows), (1, 0), (1, 3), (1, 4)} | ({(1, s) for s in range(5)} if page_rows == 16 else set())
+    tokens = sorted({0, 5, t // 3, t // 2, t - 1} & set(range(t)))
+    attend_closely(handle, cache, lengths, to_dev(rng.standard_normal((2, 8, t, 128)), cache.t), kernel, hidden, tokens)
+    only = [min(lengths[0], 3 * page_rows), lengths[1]]      # a sequence that ends with its bad pages
+    attend_closely(handle, cache, only, to_dev(rng.standard_normal((2, 8, t, 128)), cache.t), kernel, {(0, 0), (0, 1), (0, 2), (1, 4)}, tokens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "int4"])
+def test_rows_of_bad_pages_among_many_sequences(handle, fmt):
+    """Chunks of more tiles than the device has SMs: units that one block takes whole, several in a row, and units that blocks share."""
+    rng = np.random.default_rng(24)
+    b = 40
+    cache = Cache(rng, b, 4, 2, 64, fmt, 16, 30, 32 if fmt == "int4" else 0)
+    lengths = [131 + (97 * i) % 340 for i in range(b)]
+    cache.fill(handle, rng, lengths)
+    hidden = {(i, int(s)) for i in range(1, b, 3) for s in rng.integers(0, lengths[i] // 16, 2)}
+    attend_closely(handle, cache, lengths, to_dev(rng.standard_normal((b, 4, 131, 64)), cache.t), "chunk", hidden, [0, 17, 100, 130])
