@@ -449,6 +449,7 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
       }
     });
   } else if (warp >= kSoftmaxWarps + kFetchWarps) {
+    uint32_t drains = 0;
     each_piece([&](const Unit& u) {
       // ---------------- the products, by one thread ----------------
       const int tiles = u.tiles, done = u.done, nth = u.nth;
@@ -512,10 +513,10 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
             if ((y & 3) == 3) umma_commit(&B.k_empty[at1 & 1]);
           }
         }
-        if (!ok) {   // nothing may still write tensor memory, or arrive, when the CTA goes
-          umma_commit(&B.drained);
-          wait_issued(&B.drained, 0);
-        }
+        // Nothing may still write tensor memory, or arrive, when the CTA goes, which it does at the end of a piece in which any role's wait
+        // ran out, the softmax's for the last products among them.
+        umma_commit(&B.drained);
+        wait_issued(&B.drained, drains++);
       }
     });
   } else {

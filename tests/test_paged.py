@@ -1077,3 +1077,37 @@ def test_rows_of_bad_pages_among_many_sequences(handle, fmt):
     cache.fill(handle, rng, lengths)
     hidden = {(i, int(s)) for i in range(1, b, 3) for s in rng.integers(0, lengths[i] // 16, 2)}
     attend_closely(handle, cache, lengths, to_dev(rng.standard_normal((b, 4, 131, 64)), cache.t), "chunk", hidden, [0, 17, 100, 130])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("int4", 64)])
+@pytest.mark.parametrize("b,Hq,Hkv,t,n", [(1, 8, 2, 1, 3000), (1, 32, 8, 1, 40000), (1, 8, 2, 200, 3000), (4, 8, 2, 300, 600)])
+def test_paged_waits_that_run_out(handle, fmt, group, b, Hq, Hkv, t, n):
+    """A wait limit of one SM clock in the tensor-core kernels of few tokens (in clusters, dealt out) and of many: whichever waits run out, the
+    call returns by itself, with the timeout status or with its results, and the next one has them."""
+    rng = np.random.default_rng(25)
+    cache = Cache(rng, b, Hq, Hkv, 128, fmt, 64, -(-n // 64), group)
+    lengths = [n - 100 * i for i in range(b)]
+    cache.fill(handle, rng, lengths)
+    Q = to_dev(rng.standard_normal((b, Hq, t, 128)), torch.bfloat16)
+    ws = torch.empty(handle.paged_workspace_bytes(cache.desc, t), dtype=torch.uint8, device="cuda")
+
+    def call():
+        out, lse = torch.empty_like(Q), torch.empty(b, Hq, t, device="cuda")
+        handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32(lengths), cache.table, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        return handle.poll_status(), out, lse
+
+    status, want, want_lse = call()
+    assert status == rk.RESTKV_OK
+    for _ in range(5):
+        try:
+            handle.set_wait_limit(1)
+            status, out, lse = call()
+        finally:
+            handle.set_wait_limit(2_000_000_000)
+        assert status in (rk.RESTKV_OK, rk.ERR_TIMEOUT)
+        if status == rk.RESTKV_OK:
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        status, out, lse = call()
+        assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
