@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(kChThreads, 1) paged_chunk_kernel(const __grid
         // a side of tile j as a group of copies; `page` is that of tile j
         auto fetch = [&](int j, bool v) {
           const int at = done + j, s = at & 1;
-          if (j < tiles && at >= 2 && !wait(v ? &B.v_empty[s] : &B.k_empty[s], (at >> 1) - 1)) return false;
+          // the wait's verdict is a warp's: places are exchanged by whole warps
+          if (j < tiles && at >= 2 && !__all_sync(0xffffffffu, wait(v ? &B.v_empty[s] : &B.k_empty[s], (at >> 1) - 1))) return false;
 #pragma unroll
           for (int x = 0; x < kPieces; ++x) {
             if (!has(x) || is_v(x) != v || j >= tiles) continue;

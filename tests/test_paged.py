@@ -1080,7 +1080,7 @@ def test_rows_of_bad_pages_among_many_sequences(handle, fmt):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("fmt,group", [("int4", 64)])
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("int4", 64)])
 @pytest.mark.parametrize("b,Hq,Hkv,t,n", [(1, 8, 2, 1, 3000), (1, 32, 8, 1, 40000), (1, 8, 2, 200, 3000), (4, 8, 2, 300, 600)])
 def test_paged_waits_that_run_out(handle, fmt, group, b, Hq, Hkv, t, n):
     """A wait limit of one SM clock in the tensor-core kernels of few tokens (in clusters, dealt out) and of many: whichever waits run out, the
