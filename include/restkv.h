@@ -451,7 +451,8 @@ restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, i
  *   many tokens    (head_dim 64 or 128, at least 64 query rows n_tokens * group per KV head and 1536 in the call) K's 4-bit rows as above,
  *                  but of steps below 2^-8 of the largest of their 128 rows only what is above 2^-16 of that one is kept; V's 4-bit values
  *                  are rounded to f16 in the range of their 128 rows; weights are one bf16 over bf16 rows, one f16 over 4-bit rows
- * The workspace holds the parts of sequences that several blocks work on; it does not grow with their lengths.
+ * The workspace holds the parts of sequences that several blocks work on; it does not grow with their lengths, and one for n_tokens serves
+ * every call of fewer.
  */
 restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, int n_tokens, const restkv_rows* Q,
                                   const void* K_pages, const void* V_pages, const int32_t* lengths, const int32_t* table,

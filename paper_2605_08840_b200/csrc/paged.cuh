@@ -167,11 +167,12 @@ cudaError_t launch_paged_read(const PagedCache& c, bool f32, const int* first, i
                               cudaStream_t st);
 // fp32 SIMT attention: every dtype, format and head_dim.
 int paged_simt_splits(const PagedCache& c, int sm_count);
-size_t paged_simt_bytes(const PagedCache& c, int splits);
+size_t paged_simt_bytes(const PagedCache& c, int sm_count);
 cudaError_t launch_paged_simt(const PagedCache& c, bool f32, const RowsView& Q, void* out, float* lse, float* part, int splits,
                               cudaStream_t st);
 // bf16 with head_dim 64, 128 or 256 on the tensor pipe, up to 16 query rows per pass over the cache.
 cudaError_t paged_mma_init(int (*clusters_of)[5]);
+bool paged_mma_shape(const PagedCache& c);       // by type and head_dim alone
 bool paged_mma_supported(const PagedCache& c);
 size_t paged_mma_bytes(const PagedCache& c, int sm_count);
 cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count,
@@ -182,6 +183,7 @@ cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q
 // and 54, 48 tokens 64 and 81; 8 x 4000 rows, 8 tokens 77 and 44, 16 tokens 78 and 75, 24 tokens 80 and 104.
 constexpr int kChunkRows = 64, kChunkAll = 1536;
 cudaError_t paged_chunk_init();
+bool paged_chunk_shape(const PagedCache& c);     // by type, head_dim and query rows
 bool paged_chunk_supported(const PagedCache& c);
 size_t paged_chunk_bytes(const PagedCache& c, int sm_count);
 cudaError_t launch_paged_chunk(const PagedCache& c, const RowsView& Q, void* out, float* lse, float* part, int sm_count, long long wait_limit,

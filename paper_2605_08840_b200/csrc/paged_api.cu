@@ -59,11 +59,13 @@ static bool on_tensor_pipe(const PagedCache& c, bool f32) { return !f32 && paged
 
 static bool in_chunks(const PagedCache& c, bool f32) { return !f32 && paged_chunk_supported(c); }
 
+// The most that any kernel that the shape can run on needs.  It never falls as n_tokens grows (each part rises with them and, once there,
+// stays), so that a workspace for the most tokens serves calls of fewer.
 static size_t attend_bytes(const PagedCache& c, bool f32, int sm_count) {
-  const size_t simt = paged_simt_bytes(c, paged_simt_splits(c, sm_count));   // what every call can run on
-  const size_t mma = on_tensor_pipe(c, f32) ? paged_mma_bytes(c, sm_count) : 0;
-  const size_t chunk = in_chunks(c, f32) ? paged_chunk_bytes(c, sm_count) : 0;
-  return align256(simt > mma ? (simt > chunk ? simt : chunk) : (mma > chunk ? mma : chunk));
+  size_t most = paged_simt_bytes(c, sm_count);   // what every call can run on
+  if (!f32 && paged_mma_shape(c) && paged_mma_bytes(c, sm_count) > most) most = paged_mma_bytes(c, sm_count);
+  if (!f32 && paged_chunk_shape(c) && paged_chunk_bytes(c, sm_count) > most) most = paged_chunk_bytes(c, sm_count);
+  return align256(most);
 }
 
 static restkv_status make_rows(const restkv_rows* s, int heads, int n, int d, RowsView* out) {
@@ -165,8 +167,8 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
                                    h->wait_limit, call.st, &launches), launches);
     return RESTKV_OK;
   }
-  RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
-                launch_paged_simt(c, f32, q, out, lse, (float*)workspace, paged_simt_splits(c, h->sm_count), call.st), 2);
+  const int splits = paged_simt_splits(c, h->sm_count);
+  RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_paged_simt(c, f32, q, out, lse, (float*)workspace, splits, call.st), splits == 1 ? 1 : 2);
   return RESTKV_OK;
 }
 

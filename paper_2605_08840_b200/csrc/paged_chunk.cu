@@ -952,10 +952,15 @@ cudaError_t paged_chunk_init() {
   return cudaSuccess;
 }
 
-bool paged_chunk_supported(const PagedCache& c) {
+bool paged_chunk_shape(const PagedCache& c) {
   ChunkVariant v;
   const long long rows = (long long)c.n_tokens * c.G;
-  if (rows < kChunkRows || rows * c.batch * c.Hkv < kChunkAll || !pick_chunk(c, &v)) return false;
+  return rows >= kChunkRows && rows * c.batch * c.Hkv >= kChunkAll && pick_chunk(c, &v);
+}
+
+bool paged_chunk_supported(const PagedCache& c) {
+  if (!paged_chunk_shape(c)) return false;
+  const long long rows = (long long)c.n_tokens * c.G;
   const long long units = (long long)c.batch * c.Hkv * ((rows + kChRows - 1) / kChRows);
   return (c.capacity() / kChTile + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }

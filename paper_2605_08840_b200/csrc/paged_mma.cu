@@ -948,6 +948,11 @@ cudaError_t paged_mma_init(int (*clusters_of)[5]) {
   return cudaSuccess;
 }
 
+bool paged_mma_shape(const PagedCache& c) {
+  Variant v;
+  return pick(c, &v);
+}
+
 bool paged_mma_supported(const PagedCache& c) {
   Variant v;
   if (!pick(c, &v)) return false;

@@ -23,10 +23,11 @@ int lanes_per_row(int d) {
   return lanes;
 }
 
-// grid (splits, query rows / 4, batch * Hkv).  A slot of `kLanes` threads takes a cache row, 8 dims per thread; every slot keeps its
-// own running (m, l, o) of the four query rows.
+// grid (splits, query rows / 4, batch * Hkv); a single split writes the results itself.  A slot of `kLanes` threads takes a cache row, 8 dims
+// per thread; every slot keeps its own running (m, l, o) of the four query rows.
 template <typename T, bool kInt4, int kLanes>
-__global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCache c, const RowsView Q, float* __restrict__ part) {
+__global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCache c, const RowsView Q, float* __restrict__ part, T* __restrict__ out,
+                                                                  float* __restrict__ lse) {
   ptx::grid_dependency_wait();
   constexpr int kPerWarp = 32 / kLanes, kWarps = kSimtThreads / 32;
   const int splits = gridDim.x, split = blockIdx.x, bh = blockIdx.z, b = bh / c.Hkv, h = bh - b * c.Hkv;
@@ -132,9 +133,18 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCac
       acc = fmaf(w_o[w][k][dim], f, acc);
       ll = fmaf(w_ml[w][k][1], f, ll);
     }
-    float* to = part + (((long long)bh * R + rho) * splits + split) * (c.d + 2);
-    to[2 + dim] = acc;
-    if (dim == 0) { to[0] = mm; to[1] = ll; }
+    if (splits == 1) {
+      const int i = rho / c.G, g = rho - i * c.G;
+      const long long row = ((long long)b * c.Hq + h * c.G + g) * c.n_tokens + i;
+      const float v = ll > 0.f ? acc / ll : 0.f;
+      if constexpr (sizeof(T) == 4) out[row * c.d + dim] = v;
+      else out[row * c.d + dim] = __float2bfloat16(v);
+      if (lse && dim == 0) lse[row] = ll > 0.f ? mm + logf(ll) : -INFINITY;
+    } else {
+      float* to = part + (((long long)bh * R + rho) * splits + split) * (c.d + 2);
+      to[2 + dim] = acc;
+      if (dim == 0) { to[0] = mm; to[1] = ll; }
+    }
   }
 }
 
@@ -167,7 +177,7 @@ __global__ void paged_simt_combine_kernel(const PagedCache c, int splits, const 
 }
 
 template <typename T, bool kInt4>
-void (*pick_simt(int lanes))(PagedCache, RowsView, float*) {
+void (*pick_simt(int lanes))(PagedCache, RowsView, float*, T*, float*) {
   switch (lanes) {
     case 4: return paged_simt_kernel<T, kInt4, 4>;
     case 8: return paged_simt_kernel<T, kInt4, 8>;
@@ -181,8 +191,8 @@ cudaError_t launch_t(const PagedCache& c, const RowsView& Q, T* out, float* lse,
   const int R = c.n_tokens * c.G;
   const auto kernel = c.format == RESTKV_PAGES_INT4 ? pick_simt<T, true>(lanes_per_row(c.d)) : pick_simt<T, false>(lanes_per_row(c.d));
   const dim3 grid((unsigned int)splits, (unsigned int)((R + kSimtRows - 1) / kSimtRows), (unsigned int)(c.batch * c.Hkv));
-  const cudaError_t e = launch_chained(kernel, grid, kSimtThreads, 0, st, c, Q, part);
-  if (e != cudaSuccess) return e;
+  const cudaError_t e = launch_chained(kernel, grid, kSimtThreads, 0, st, c, Q, part, out, lse);
+  if (e != cudaSuccess || splits == 1) return e;
   return launch_chained(paged_simt_combine_kernel<T>, dim3((unsigned int)R, (unsigned int)(c.batch * c.Hkv)), (c.d + 31) / 32 * 32, 0, st, c,
                         splits, part, out, lse);
 }
@@ -198,8 +208,12 @@ int paged_simt_splits(const PagedCache& c, int sm_count) {
   return splits < 1 ? 1 : (int)splits;
 }
 
-size_t paged_simt_bytes(const PagedCache& c, int splits) {
-  return (size_t)c.batch * c.Hq * c.n_tokens * splits * (c.d + 2) * sizeof(float);
+// A bound of what the splits leave that never falls as the tokens grow: there are several only while four rows each make less than 2 units
+// per SM, so that units * splits stays below 4 per SM.
+size_t paged_simt_bytes(const PagedCache& c, int sm_count) {
+  const long long by_rows = (c.capacity() + 63) / 64, most = by_rows < kSimtMaxSplits ? by_rows : kSimtMaxSplits;
+  const long long rows = (long long)c.batch * c.Hq * c.n_tokens * most, bound = 4LL * 4 * sm_count;
+  return (size_t)(rows < bound ? rows : bound) * (c.d + 2) * sizeof(float);
 }
 
 cudaError_t launch_paged_simt(const PagedCache& c, bool f32, const RowsView& Q, void* out, float* lse, float* part, int splits, cudaStream_t st) {

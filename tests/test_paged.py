@@ -1111,3 +1111,38 @@ def test_paged_waits_that_run_out(handle, fmt, group, b, Hq, Hkv, t, n):
             assert torch.equal(out, want) and torch.equal(lse, want_lse)
         status, out, lse = call()
         assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+@pytest.mark.parametrize("dtype,fmt", [(rk.BF16, rk.PAGES_BF16), (rk.BF16, rk.PAGES_INT4), (rk.F32, rk.PAGES_F32), (rk.F32, rk.PAGES_INT4)])
+@pytest.mark.parametrize("b,Hq,Hkv,d", [(1, 32, 8, 128), (1, 8, 8, 64), (3, 6, 2, 96), (8, 16, 1, 256), (1, 1, 1, 32), (70, 4, 4, 128)])
+@pytest.mark.parametrize("width", [1, 3, 2000])
+def test_workspaces_serve_calls_of_fewer_tokens(dtype, fmt, b, Hq, Hkv, d, width):
+    """Sizes never fall as the tokens grow, and never pass what the blocks of one device can leave: two parts of 256 query rows per SM."""
+    lib = rk.load_library()
+    cache = rk.make_paged(b, Hq, Hkv, d, fmt, 64, b * width, width, 32 if fmt == rk.PAGES_INT4 else 0, dtype)
+    before = 0
+    for t in list(range(1, 200)) + [2 ** k + x for k in range(8, 17) for x in (-1, 0, 1) if (2 ** k + x) * Hq // Hkv < 200000]:
+        size = lib.restkv_paged_workspace_bytes(ctypes.byref(cache), t)
+        assert size % 256 == 0 and before <= size <= 148 * (2 * 256 * (d + 2) * 4 + 16) + 256, t
+        before = size
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "int4-bf16"])
+def test_one_workspace_for_all_calls_of_a_size_and_fewer(handle, fmt):
+    rng = np.random.default_rng(26)
+    dtype = "f32" if fmt.endswith("f32") else "bf16"
+    cache = Cache(rng, 1, 8, 8, 64, fmt.split("-")[0], 16, 30, 32 if fmt.startswith("int4") else 0, dtype)
+    cache.fill(handle, rng, [470])
+    size = handle.paged_workspace_bytes(cache.desc, 50)
+    memory = torch.full((size + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+    for t in (50, 49, 17, 6, 5, 4, 3, 1):
+        Q = to_dev(rng.standard_normal((1, 8, t, 64)), cache.t)
+        out, want = torch.empty_like(Q), torch.empty_like(Q)
+        handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32([470]), cache.table, out, memory[:size])
+        own = torch.empty(handle.paged_workspace_bytes(cache.desc, t), dtype=torch.uint8, device="cuda")
+        handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32([470]), cache.table, want, own)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+    assert handle.poll_status() == rk.RESTKV_OK
+    assert bool((memory[size:] == 0xA5).all())
