@@ -444,7 +444,8 @@ restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, i
  * A query that sees no row, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32.  A
  * row that some query of the call sees has to be finite.  The result of a call does not depend on other calls, streams or the order
  * in which its parts end: the same call gives the same bits.
- * RESTKV_F32, other head_dims than 64, 128 and 256 and restkv_set_kernel_path(1) run in fp32 throughout.  Else the tensor cores do,
+ * RESTKV_F32, other head_dims than 64, 128 and 256 and restkv_set_kernel_path(1) run in fp32 throughout; the first two return
+ * RESTKV_ERR_UNSUPPORTED under restkv_set_kernel_path(2 or 3), which require the tensor cores.  Else the tensor cores do,
  * and what is rounded for them is this:
  *   few tokens     K's 4-bit rows are exact (codes meet Q as f16, scaled by a power of two per query; steps and offsets are applied in
  *                  fp32); weights over bf16 rows are two bf16 parts (16 bits), over 4-bit rows weight * step is one f16 (11 bits)

@@ -167,6 +167,7 @@ restkv_status restkv_paged_attend(restkv_handle* h, const restkv_paged* cache, i
                                    h->wait_limit, call.st, &launches), launches);
     return RESTKV_OK;
   }
+  if (h->kernel_path >= 2) return RESTKV_ERR_UNSUPPORTED;   // the tensor cores are required
   const int splits = paged_simt_splits(c, h->sm_count);
   RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_paged_simt(c, f32, q, out, lse, (float*)workspace, splits, call.st), splits == 1 ? 1 : 2);
   return RESTKV_OK;

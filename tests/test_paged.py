@@ -1146,3 +1146,30 @@ def test_one_workspace_for_all_calls_of_a_size_and_fewer(handle, fmt):
         assert torch.equal(out, want)
     assert handle.poll_status() == rk.RESTKV_OK
     assert bool((memory[size:] == 0xA5).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("path", [rk.PATH_TENSOR_CORE, 3])
+@pytest.mark.parametrize("fmt,d,t,on_tensor_cores", [("f32", 128, 1, False), ("int4-f32", 64, 70, False), ("bf16", 96, 1, False), ("int4-bf16", 32, 200, False), ("bf16", 128, 1, True),
+                                                     ("int4-bf16", 64, 1, True), ("bf16", 256, 40, True), ("int4-bf16", 128, 400, True)])
+def test_attend_where_the_tensor_cores_are_required(handle, path, fmt, d, t, on_tensor_cores):
+    rng = np.random.default_rng(27)
+    cache = Cache(rng, 1, 8, 2, d, fmt.split("-")[0], 16, 32, 32 if fmt.startswith("int4") else 0, "f32" if fmt.endswith("f32") else "bf16")
+    cache.fill(handle, rng, [500])
+    Q = to_dev(rng.standard_normal((1, 8, t, d)), cache.t)
+    out, want = torch.full_like(Q, 7.0), torch.empty_like(Q)
+    ws = torch.empty(handle.paged_workspace_bytes(cache.desc, t), dtype=torch.uint8, device="cuda")
+    handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32([500]), cache.table, want, ws)
+    launches = handle.launch_count()
+    handle.set_kernel_path(path)
+    try:
+        if on_tensor_cores:
+            handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32([500]), cache.table, out, ws)
+        else:
+            with pytest.raises(rk.RestKVError) as e:
+                handle.paged_attend(cache.desc, t, Q, cache.K, cache.V, dev_i32([500]), cache.table, out, ws)
+            assert e.value.status == rk.ERR_UNSUPPORTED and handle.launch_count() == launches
+    finally:
+        handle.set_kernel_path(0)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want) if on_tensor_cores else bool((out == 7.0).all())
