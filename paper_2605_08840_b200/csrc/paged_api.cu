@@ -49,8 +49,8 @@ static restkv_status make_cache(const restkv_paged* s, PagedCache* out) {
 
 static restkv_status check_tokens(const PagedCache& c, int n_tokens) {
   if (n_tokens < 1) return RESTKV_ERR_INVALID_ARG;
-  // one grid dimension has the tokens of a batch, another the query rows of a KV head in fours
-  if ((long long)c.batch * n_tokens > 0x7FFFFFFFll || (long long)c.G * n_tokens > 4 * 65535ll) return RESTKV_ERR_UNSUPPORTED;
+  // the tokens of a batch, and the query rows of a KV head rounded up to a tile of 256, are counted in 32 bits
+  if ((long long)c.batch * n_tokens > 0x7FFFFFFFll || (long long)c.G * n_tokens > 0x7FFFFFFFll - 256) return RESTKV_ERR_UNSUPPORTED;
   return RESTKV_OK;
 }
 

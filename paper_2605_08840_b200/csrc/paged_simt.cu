@@ -23,14 +23,14 @@ int lanes_per_row(int d) {
   return lanes;
 }
 
-// grid (splits, query rows / 4, batch * Hkv); a single split writes the results itself.  A slot of `kLanes` threads takes a cache row, 8 dims
+// grid (query rows / 4, splits, batch * Hkv); a single split writes the results itself.  A slot of `kLanes` threads takes a cache row, 8 dims
 // per thread; every slot keeps its own running (m, l, o) of the four query rows.
 template <typename T, bool kInt4, int kLanes>
 __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCache c, const RowsView Q, float* __restrict__ part, T* __restrict__ out,
                                                                   float* __restrict__ lse) {
   ptx::grid_dependency_wait();
   constexpr int kPerWarp = 32 / kLanes, kWarps = kSimtThreads / 32;
-  const int splits = gridDim.x, split = blockIdx.x, bh = blockIdx.z, b = bh / c.Hkv, h = bh - b * c.Hkv;
+  const int splits = gridDim.y, split = blockIdx.y, bh = blockIdx.z, b = bh / c.Hkv, h = bh - b * c.Hkv;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, chunk = lane % kLanes;
   const bool has = chunk * 8 < c.d;
   const int R = c.n_tokens * c.G, n = paged_length(c, b, h), count = paged_count(c, b);
@@ -40,7 +40,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCac
   int most = 0;
 #pragma unroll
   for (int k = 0; k < kSimtRows; ++k) {
-    const int rho = blockIdx.y * kSimtRows + k, i = rho / c.G, g = rho - i * c.G;
+    const int rho = blockIdx.x * kSimtRows + k, i = rho / c.G, g = rho - i * c.G;
     sees[k] = rho < R && i < count ? n - (count - 1 - i) : 0;
     most = max(most, sees[k]);
     Pack8<T> p;
@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(kSimtThreads) paged_simt_kernel(const PagedCac
   }
   __syncthreads();
   for (int e = threadIdx.x; e < kSimtRows * c.d; e += kSimtThreads) {
-    const int k = e / c.d, dim = e - k * c.d, rho = blockIdx.y * kSimtRows + k;
+    const int k = e / c.d, dim = e - k * c.d, rho = blockIdx.x * kSimtRows + k;
     if (rho >= R) continue;
     float mm = -INFINITY, acc = 0.f, ll = 0.f;
 #pragma unroll
@@ -190,7 +190,7 @@ template <typename T>
 cudaError_t launch_t(const PagedCache& c, const RowsView& Q, T* out, float* lse, float* part, int splits, cudaStream_t st) {
   const int R = c.n_tokens * c.G;
   const auto kernel = c.format == RESTKV_PAGES_INT4 ? pick_simt<T, true>(lanes_per_row(c.d)) : pick_simt<T, false>(lanes_per_row(c.d));
-  const dim3 grid((unsigned int)splits, (unsigned int)((R + kSimtRows - 1) / kSimtRows), (unsigned int)(c.batch * c.Hkv));
+  const dim3 grid((unsigned int)((R + kSimtRows - 1) / kSimtRows), (unsigned int)splits, (unsigned int)(c.batch * c.Hkv));
   const cudaError_t e = launch_chained(kernel, grid, kSimtThreads, 0, st, c, Q, part, out, lse);
   if (e != cudaSuccess || splits == 1) return e;
   return launch_chained(paged_simt_combine_kernel<T>, dim3((unsigned int)R, (unsigned int)(c.batch * c.Hkv)), (c.d + 31) / 32 * 32, 0, st, c,

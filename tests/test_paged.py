@@ -1173,3 +1173,24 @@ def test_attend_where_the_tensor_cores_are_required(handle, path, fmt, d, t, on_
         handle.set_kernel_path(0)
     torch.cuda.synchronize()
     assert torch.equal(out, want) if on_tensor_cores else bool((out == 7.0).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group,kernel", [("bf16", 0, "chunk"), ("int4", 64, "chunk"), ("bf16", 0, "fp32"), ("int4", 32, "fp32")])
+def test_more_query_rows_than_a_grid_has_in_its_second_dimension(handle, fmt, group, kernel):
+    """4100 tokens of 64 query heads over one KV head: 262 400 query rows, appended with their queries and attended over."""
+    rng = np.random.default_rng(28)
+    t, n = 4100, 4160
+    cache = Cache(rng, 1, 64, 1, 64, fmt, 64, 65, group)
+    cache.fill(handle, rng, [n])
+    Q = torch.randn(1, 64, t, 64, generator=torch.Generator("cuda").manual_seed(1), device="cuda").to(cache.t)
+    K, V, k, v = (torch.empty(1, 1, t, 64, dtype=cache.t, device="cuda") for _ in range(4))
+    handle.paged_read(cache.desc, cache.K, cache.V, dev_i32([n]), cache.table, t, K, V, first=dev_i32([n - t]))
+    other = cache.K.clone(), cache.V.clone()
+    Q_out = torch.empty_like(Q)
+    handle.paged_append(cache.desc, t, K, V, *other, dev_i32([n]), cache.table, Q=Q, Q_out=Q_out)
+    handle.paged_read(cache.desc, *other, dev_i32([n]), cache.table, t, k, v, first=dev_i32([n - t]))
+    assert torch.equal(Q_out, Q)
+    if fmt == "bf16":
+        assert torch.equal(k, K) and torch.equal(v, V)
+    attend_closely(handle, cache, [n], Q, kernel, tokens=[0, 1777, 4095, 4099])
