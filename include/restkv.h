@@ -366,8 +366,12 @@ restkv_status restkv_set_output_projection(restkv_handle* h, const void* factor,
  * The pool has n_pages pages of page_rows rows for K and as many for V (caller-owned, 16-byte aligned, restkv_paged_page_bytes()
  * each).  A page holds the rows of all n_kv_heads heads, head by head.  table [batch, table_width] (device int32) names the pages
  * of every sequence in order: row r of sequence b lies in page table[b, r / page_rows].  lengths (device int32, [batch], or
- * [batch, n_kv_heads] with lengths_per_head, as restkv_evict_budgets leaves them) are the rows of every sequence, in each of the
- * calls below with the call's own new tokens included, so that one vector serves all layers of a step.
+ * [batch, n_kv_heads] with lengths_per_head, for heads that have kept different numbers of rows) are the rows of every sequence, in each of
+ * the calls below with the call's own new tokens included, so that one vector serves all layers of a step.
+ * Counts are per sequence: an append with lengths_per_head gives every head of a sequence as many rows, its last ones.  Different numbers of
+ * rows per head, as restkv_evict_budgets leaves them (the first min(max(budget, 1), max_budget, n_kv) rows of a head), go in head by head: the
+ * pool is the same bytes as n_pages * n_kv_heads pages of one head, described with n_kv_heads 1, n_q_heads the group, batch * n_kv_heads
+ * sequences, a table of page * n_kv_heads + head, and lengths = counts = the rows kept.
  *
  * Formats (restkv_page_format)
  *   BF16, F32  rows of head_dim elements, [n_pages, n_kv_heads, page_rows, head_dim]; the dtype of the call has to be the same

@@ -1194,3 +1194,97 @@ def test_more_query_rows_than_a_grid_has_in_its_second_dimension(handle, fmt, gr
     if fmt == "bf16":
         assert torch.equal(k, K) and torch.equal(v, V)
     attend_closely(handle, cache, [n], Q, kernel, tokens=[0, 1777, 4095, 4099])
+
+
+# ---- a length per head ------------------------------------------------------------------------------------------------------------------
+
+def by_head(cache):
+    """The same pool as pages of one head, batch * n_kv_heads sequences: its description and the table for it, as the header says."""
+    d = cache.desc
+    one = rk.make_paged(d.batch * d.n_kv_heads, d.n_q_heads // d.n_kv_heads, 1, d.head_dim, d.page_format, d.page_rows, d.n_pages * d.n_kv_heads, d.table_width,
+                        d.group, d.dtype)
+    table = cache.table[:, None, :] * d.n_kv_heads + torch.arange(d.n_kv_heads, dtype=torch.int32, device="cuda")[None, :, None]
+    return one, table.reshape(-1, d.table_width).contiguous()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("int4", 64)])
+def test_rows_kept_under_budgets_of_heads_go_into_pages(handle, fmt, group):
+    """restkv_evict_budgets leaves a head's kept rows first: they go in head by head, and after that every call takes lengths per head."""
+    b, Hq, Hkv, d, n_kv, w, S = 2, 8, 4, 128, 400, 32, 90
+    rng = np.random.default_rng(29)
+    K, V = (to_dev(rng.standard_normal((b, Hkv, n_kv, d)), torch.bfloat16) for _ in range(2))
+    Q = to_dev(rng.standard_normal((b, Hq, w, d)), torch.bfloat16)
+    budgets = np.array([[90, 1, 64, 33], [17, 200, 48, 5]])
+    lengths = np.minimum(budgets, S)
+    shape = rk.make_shape(b, Hq, Hkv, d, n_kv, w)
+    ws = torch.empty(handle.workspace_bytes(shape, S), dtype=torch.uint8, device="cuda")
+    indices = torch.empty(b, Hkv, S, dtype=torch.int32, device="cuda")
+    K_out, V_out = (torch.full((b, Hkv, S, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    handle.evict_budgets(shape, Q, K, V, 0.9, rk.fixed_pool(5), dev_i32(budgets), S, indices, K_out, V_out, ws)
+
+    cache = Cache(rng, b, Hq, Hkv, d, fmt, 16, 8, group, per_head=True)
+    one, table = by_head(cache)
+    n = dev_i32(lengths)
+    handle.paged_append(one, S, K_out.view(b * Hkv, 1, S, d), V_out.view(b * Hkv, 1, S, d), cache.K, cache.V, n.view(-1), table, counts=n.view(-1))
+    assert handle.poll_status() == rk.RESTKV_OK
+    idx = indices.cpu().numpy()
+    for i in range(b):
+        for h in range(Hkv):
+            rows = np64(K[i, h])[idx[i, h, :lengths[i, h]]]
+            got, steps = cache.rows(cache.K, True, i, h, int(lengths[i, h]))
+            assert np.all(np.abs(got - rows) <= 0.5 * steps + (2.0 ** -20 * np.abs(rows).max() if group else 0.0))
+    check_attention(handle, rng, cache, lengths, None, 1)
+    # generated tokens: one row more in every head
+    new = [to_dev(rng.standard_normal((b, Hkv, 3, d)), torch.bfloat16) for _ in range(2)]
+    handle.paged_append(cache.desc, 3, *new, cache.K, cache.V, n + 3, cache.table)
+    k, v = (torch.empty(b, Hkv, 3, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    handle.paged_read(cache.desc, cache.K, cache.V, n + 3, cache.table, 3, k, v, first=n)
+    torch.cuda.synchronize()
+    for got, want in zip((k, v), new):
+        span = want.float().unflatten(-1, (-1, group or d))
+        step = (span.amax(-1) - span.amin(-1))[..., None].expand(span.shape).flatten(-2) * ((1 + 2.0 ** -6) / 15 if group else 0.0)
+        assert bool(((got.float() - want.float()).abs() <= 0.5 * step + (2.0 ** -8 * want.float().abs() + 2.0 ** -8 * 0.2 if group else 0.0)).all())
+    check_attention(handle, rng, cache, lengths + 3, None, 3)
+    assert handle.poll_status() == rk.RESTKV_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("fmt", ["bf16", "f32", "int4-bf16", "int4-f32"])
+@pytest.mark.parametrize("t", [1, 5, 70])
+def test_append_with_lengths_per_head(handle, fmt, t):
+    """Byte for byte what the same rows give head by head, rotated, with counts, and rows of a bad page or past the table left out."""
+    b, Hq, Hkv, d, R = 3, 6, 3, 64, 16
+    rng = np.random.default_rng(30)
+    dtype = "f32" if fmt.endswith("f32") else "bf16"
+    fmt = fmt.split("-")[0]
+    cache = Cache(rng, b, Hq, Hkv, d, fmt, R, 10, 32 if fmt == "int4" else 0, dtype, per_head=True)
+    one, table = by_head(cache)
+    counts = np.array([t, max(0, t - 4), t // 2])
+    lengths = np.array([[70, 160, 101], [87, 80, 159], [150, 71, 90]])
+    K, V = (to_dev(rng.standard_normal((b, Hkv, t, d)), cache.t) for _ in range(2))
+    Q = to_dev(rng.standard_normal((b, Hq, t, d)), cache.t)
+    positions = rng.integers(0, 300, (b, t)).astype(np.int32)
+    cos, sin = tables(300, d)
+    rotation = rk.make_rotation(torch.from_numpy(cos).cuda(), torch.from_numpy(sin).cuda(), d)
+    want_K, want_V, q = cache.K.clone(), cache.V.clone(), torch.empty_like(Q)
+    handle.paged_append(cache.desc, t, K, V, cache.K, cache.V, dev_i32(lengths), cache.table, counts=dev_i32(counts), positions=dev_i32(positions), rotation=rotation, Q=Q, Q_out=q)
+    handle.paged_append(one, t, K.view(b * Hkv, 1, t, d), V.view(b * Hkv, 1, t, d), want_K, want_V, dev_i32(lengths.reshape(-1)), table,
+                        counts=dev_i32(np.repeat(counts, Hkv)), positions=dev_i32(np.repeat(positions, Hkv, 0)), rotation=rotation)
+    torch.cuda.synchronize()
+    assert handle.poll_status() == rk.RESTKV_OK
+    assert torch.equal(cache.K, want_K) and torch.equal(cache.V, want_V)
+    assert bool((cache.K != 255).any())
+    for i in range(b):
+        turned = rotate(np64(Q[i]), positions[i], cos, sin, d, False)
+        assert np.all(np.abs(np64(q[i]) - turned)[:, :counts[i]] <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * np.abs(turned[:, :counts[i]]) + 2.0 ** -20 * np.abs(turned).max())
+        assert bool((q[i, :, counts[i]:] == 0).all())
+    # rows without a place: of the heads that have none, nothing; the others' as before
+    lengths[0, 1], lengths[2, 0] = 161, 2
+    cache.table[1, 4] = cache.n_pages
+    one, table = by_head(cache)
+    handle.paged_append(cache.desc, t, V, K, cache.K, cache.V, dev_i32(lengths), cache.table, counts=dev_i32(counts))
+    assert handle.poll_status() == rk.ERR_INVALID_ARG
+    handle.paged_append(one, t, V.view(b * Hkv, 1, t, d), K.view(b * Hkv, 1, t, d), want_K, want_V, dev_i32(lengths.reshape(-1)), table, counts=dev_i32(np.repeat(counts, Hkv)))
+    assert handle.poll_status() == rk.ERR_INVALID_ARG
+    assert torch.equal(cache.K, want_K) and torch.equal(cache.V, want_V)
