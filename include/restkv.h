@@ -386,9 +386,10 @@ restkv_status restkv_set_output_projection(restkv_handle* h, const void* factor,
  *              kernel needs lies side by side.
  * head_dim: a multiple of 32, at most 256 (else RESTKV_ERR_UNSUPPORTED).  page_rows: a multiple of 16.  group: 32, 64 or 128, a divisor of head_dim.
  *
- * What is only known on the device is checked there: a length below 0 counts as 0; a row past table_width * page_rows, a table
- * entry outside [0, n_pages) or a position outside the rotation tables is skipped (not written, not seen, read back as 0) and sets
- * the sticky status: restkv_poll_status() then returns RESTKV_ERR_INVALID_ARG.  No two rows of a call may lie in the same place.
+ * What is only known on the device is checked there: a length below 0 counts as 0, one past table_width * page_rows as that where rows are
+ * attended over or read; a new row past it (or before row 0), a row whose table entry is outside [0, n_pages) and a token whose position is
+ * outside the rotation tables are skipped (not written, not seen, read back as 0).  All but the first set the sticky status:
+ * restkv_poll_status() then returns RESTKV_ERR_INVALID_ARG.  No two rows of a call may lie in the same place.
  */
 typedef enum { RESTKV_PAGES_BF16 = 0, RESTKV_PAGES_F32 = 1, RESTKV_PAGES_INT4 = 2 } restkv_page_format;
 
@@ -452,7 +453,9 @@ restkv_status restkv_paged_append(restkv_handle* h, const restkv_paged* cache, i
  * RESTKV_ERR_UNSUPPORTED under restkv_set_kernel_path(2 or 3), which require the tensor cores.  Else the tensor cores do,
  * and what is rounded for them is this:
  *   few tokens     K's 4-bit rows are exact (codes meet Q as f16, scaled by a power of two per query; steps and offsets are applied in
- *                  fp32); weights over bf16 rows are two bf16 parts (16 bits), over 4-bit rows weight * step is one f16 (11 bits)
+ *                  fp32); weights over bf16 rows are two bf16 parts (16 bits), over 4-bit rows weight * step is one f16: 11 bits down to
+ *                  2^-19 of the largest weight times the largest step, of any group, that some 32 rows of the sequence have, below that
+ *                  whole multiples of 2^-29 of it (so that a group whose steps are that much smaller than another's loses its codes)
  *   many tokens    (head_dim 64 or 128, at least 64 query rows n_tokens * group per KV head and 1536 in the call) K's 4-bit rows as above,
  *                  but of steps below 2^-8 of the largest of their 128 rows only what is above 2^-16 of that one is kept; V's 4-bit values
  *                  are rounded to f16 in the range of their 128 rows; weights are one bf16 over bf16 rows, one f16 over 4-bit rows

@@ -1288,3 +1288,40 @@ def test_append_with_lengths_per_head(handle, fmt, t):
     handle.paged_append(one, t, V.view(b * Hkv, 1, t, d), K.view(b * Hkv, 1, t, d), want_K, want_V, dev_i32(lengths.reshape(-1)), table, counts=dev_i32(np.repeat(counts, Hkv)))
     assert handle.poll_status() == rk.ERR_INVALID_ARG
     assert torch.equal(cache.K, want_K) and torch.equal(cache.V, want_V)
+
+
+# ---- values, long caches and unlike groups, within the stated bits ------------------------------------------------------------------------
+
+# kernel, batch, query heads, KV heads, head_dim, page rows, lengths, tokens, the tokens looked at
+CLOSE = [("few", 1, 8, 2, 128, 64, [17000], 1, [0]), ("few", 3, 8, 2, 128, 16, [300, 1, 6001], 1, [0]), ("few", 1, 16, 1, 128, 32, [5300], 1, [0]), ("few", 2, 4, 1, 64, 16, [900, 33], 4, [0, 3]),
+         ("few", 1, 4, 2, 256, 48, [2500], 1, [0]), ("few", 1, 8, 2, 256, 16, [1100], 6, [0, 5]), ("few", 1, 12, 4, 128, 16, [700], 9, [0, 4, 8]),
+         ("chunk", 1, 8, 2, 128, 64, [6000], 200, [0, 99, 199]), ("chunk", 2, 4, 4, 64, 16, [900, 333], 333, [0, 150, 332]), ("chunk", 1, 16, 1, 128, 16, [2100], 2100, [0, 255, 1024, 2099]),
+         ("fp32", 1, 8, 2, 128, 64, [6000], 1, [0]), ("fp32", 2, 6, 2, 96, 16, [700, 65], 9, [0, 8])]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", CLOSE)
+@pytest.mark.parametrize("fmt,group", [("bf16", 0), ("int4", 32), ("int4", 64), ("int4", 128)])
+@pytest.mark.parametrize("q_scale", [0.3, 2.0])
+def test_attend_within_the_stated_bits(handle, spec, fmt, group, q_scale):
+    kernel, b, Hq, Hkv, d, R, lengths, t, tokens = spec
+    if group and d % group:
+        pytest.skip("no such group in this head_dim")
+    rng = np.random.default_rng(31)
+    cache = Cache(rng, b, Hq, Hkv, d, fmt, R, -(-max(lengths) // R), group)
+    cache.fill(handle, rng, lengths)
+    attend_closely(handle, cache, lengths, to_dev(rng.standard_normal((b, Hq, t, d)) * q_scale, cache.t), kernel, tokens=tokens)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [32, 64])
+@pytest.mark.parametrize("kernel,t", CLOSELY)
+@pytest.mark.parametrize("ratio", [2.0 ** -8, 2.0 ** -16, 2.0 ** -24])
+def test_attend_over_groups_of_unlike_steps(handle, group, kernel, t, ratio):
+    """Groups of V whose values are far smaller than the first one's keep the bits that the header promises them."""
+    rng = np.random.default_rng(32)
+    cache = Cache(rng, 1, 8, 2, 128, "int4", 16, 40, group)
+    K, V = rng.standard_normal((2, 1, 2, 600, 128))
+    V *= ratio ** (np.arange(128) // group)
+    handle.paged_append(cache.desc, 600, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([600]), cache.table)
+    attend_closely(handle, cache, [600], to_dev(rng.standard_normal((1, 8, t, 128)), cache.t), kernel, tokens=[0, t - 1])
