@@ -14,10 +14,13 @@
 //     operations make 4 operand registers of 8 codes of K.  For V, whose sums over the upper codes of bytes may as well come out of
 //     those over whole bytes (upper = (byte - lower) / 16), it is one less.  q is f16 scaled by a
 //     power of two per query row (exact down to 2^-28 of the row's largest element).  s = step * (q . code) + offset * sum(q) per
-//     group, o = sum f16(p step) code + sum p offset, all sums in fp32.
+//     group, o = sum f16(p step) code + sum p offset, all sums in fp32.  Every other row of V counts down from its group's top instead,
+//     f16(-p step) (15 - code) + p (offset + 15 step): the tensor pipe cuts each product off at the last place of the running sum, and sums of
+//     one sign, which the offsets nearly cancel in the end, would keep that (error before the output's rounding 5.3e-3 at 524288 rows of 8 KV
+//     heads and 1.7e-2 at 1048576, for 6e-4 at any length; 2% more time).
 //     (bf16 16 + code: two operations per register, and the weights' rounding weighs twice as much unless 8 is taken off the codes:
 //     60 us for 131072 rows.  e4m3 codes: m16n8k32 is carried out as conversions and f16 products here, 60 us, too.)
-// Measured, 32 query heads of 128 over 8 KV heads: 131072 rows of 4 bits 40 us (3.7 TB/s), of bf16 93 us (5.8 TB/s); 2085 rows of 4 bits 7.8 us.
+// Measured, 32 query heads of 128 over 8 KV heads: 131072 rows of 4 bits 41 us (3.7 TB/s), of bf16 93 us (5.8 TB/s); 2085 rows of 4 bits 8.1 us.
 // Work is split in one of two ways:
 //   - a cluster of CTAs per unit (sequence, KV head, up to 16 query rows), merged through distributed shared memory: one launch, for
 //     short caches, where latency counts;
@@ -504,6 +507,7 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       float most = 0.f;
       if constexpr (kInt4) {
         float top = 0x1p-40f;                  // at least: weights stay well within fp32
+        const float from_top = r & 1 ? 15.f : 0.f, sign = r & 1 ? -1.f : 1.f;   // rows 4 .. 7 and 12 .. 15 of a block count down
 #pragma unroll
         for (int k = 0; k < kBlocks; ++k)
 #pragma unroll
@@ -511,8 +515,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
             const uint4 u = lds128(stage + (kBlocks + k) * C::kBlockBytes + 8 * kD + 64 * g + 16 * (r >> 1));
             v_step[k][g][0] = __uint_as_float(__byte_perm(u.x, 0u, pick));
             v_step[k][g][1] = __uint_as_float(__byte_perm(u.y, 0u, pick));
-            v_off[k][g][0] = __uint_as_float(__byte_perm(u.z, 0u, pick));
-            v_off[k][g][1] = __uint_as_float(__byte_perm(u.w, 0u, pick));
+            v_off[k][g][0] = fmaf(v_step[k][g][0], from_top, __uint_as_float(__byte_perm(u.z, 0u, pick)));
+            v_off[k][g][1] = fmaf(v_step[k][g][1], from_top, __uint_as_float(__byte_perm(u.w, 0u, pick)));
             if constexpr (kEdge) {
               // a row past the cache holds anything: a weight of 0 is to find a number there
 #pragma unroll
@@ -520,6 +524,8 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
                 if (row0 + k * kBlockRows + own + 8 * x >= n || (gone >> k & 1u)) v_step[k][g][x] = v_off[k][g][x] = 0.f;
             }
             top = fmax3(top, v_step[k][g][0], v_step[k][g][1]);
+            v_step[k][g][0] *= sign;
+            v_step[k][g][1] *= sign;
           }
         most = lg2_approx(top);
       }
@@ -570,7 +576,13 @@ paged_mma_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         if constexpr (kInt4) {
           uint32_t w[4][(kWords + 1) / 2];     // the units of rows q4, q4 + 4, q4 + 8, q4 + 12
 #pragma unroll
-          for (int j = 0; j < 4; ++j) lds_words<kWords / 2>(vt + (uint32_t)(q4 + 4 * j) * (kD / 2) + r * (kD / 16), w[j]);
+          for (int j = 0; j < 4; ++j) {
+            lds_words<kWords / 2>(vt + (uint32_t)(q4 + 4 * j) * (kD / 2) + r * (kD / 16), w[j]);
+            if (j & 1) {                       // (15 - code)
+#pragma unroll
+              for (int x = 0; x < kWords / 2; ++x) w[j][x] = ~w[j][x];
+            }
+          }
           uint32_t pb[kNT][2];
 #pragma unroll
           for (int x = 0; x < kWords; ++x) {

@@ -1325,3 +1325,38 @@ def test_attend_over_groups_of_unlike_steps(handle, group, kernel, t, ratio):
     V *= ratio ** (np.arange(128) // group)
     handle.paged_append(cache.desc, 600, to_dev(K, cache.t), to_dev(V, cache.t), cache.K, cache.V, dev_i32([600]), cache.table)
     attend_closely(handle, cache, [600], to_dev(rng.standard_normal((1, 8, t, 128)), cache.t), kernel, tokens=[0, t - 1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_attend_keeps_its_bits_over_long_caches(handle, group):
+    """One token over 524 288 rows of 4 bits: what is rounded are the weights and the output, each on its own, so that the error of all outputs
+    together is no more than independent roundings give; nothing adds up along the rows."""
+    Hkv, G, d, n, R = 8, 2, 128, 524288, 256
+    g = torch.Generator("cuda").manual_seed(33)
+    cache = rk.make_paged(1, Hkv * G, Hkv, d, rk.PAGES_INT4, R, n // R, n // R, group)
+    pages = [torch.empty(n // R * handle.paged_page_bytes(cache), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    table, lengths = torch.randperm(n // R, generator=g, device="cuda").to(torch.int32), dev_i32([n])
+    handle.paged_append(cache, n, *(torch.randn(1, Hkv, n, d, generator=g, device="cuda", dtype=torch.bfloat16) for _ in range(2)), *pages, lengths, table)
+    Q = torch.randn(1, Hkv * G, 1, d, generator=g, device="cuda").to(torch.bfloat16)
+    out = torch.empty_like(Q)
+    ws = torch.empty(handle.paged_workspace_bytes(cache, 1), dtype=torch.uint8, device="cuda")
+    handle.paged_attend(cache, 1, Q, *pages, lengths, table, out, ws)
+    # the rows as single precision has them: offset + step * code has few bits
+    exact = rk.make_paged(1, Hkv * G, Hkv, d, rk.PAGES_INT4, R, n // R, n // R, group, rk.F32)
+    K, V = (torch.empty(1, Hkv, n, d, device="cuda") for _ in range(2))
+    handle.paged_read(exact, *pages, lengths, table, n, K, V)
+    assert handle.poll_status() == rk.RESTKV_OK
+    err, size, rounded = 0.0, 0.0, 0.0
+    for h in range(Hkv):
+        w = torch.softmax(Q[0, h * G:h * G + G, 0].double() @ K[0, h].double().T / math.sqrt(d), -1)
+        v = V[0, h].double()
+        o = w @ v
+        spread = v.unflatten(-1, (-1, group))
+        span = (spread.amax(-1) - spread.amin(-1)).repeat_interleave(group, -1)          # at most 15 steps, by which a weight is rounded
+        err += float(((out[0, h * G:h * G + G, 0].double() - o) ** 2).sum())
+        size += float((o ** 2).sum())
+        rounded += float(((w ** 2) @ (span * (15.0 / 14.0)) ** 2).sum())               # (a span of 14 steps of 15 is the least that codes have)
+    # half a place of the output's 8 bits and of the weights' 11, evenly spread: 2^-7 / sqrt(12) and 2^-10 / sqrt(12)
+    bound = 2.0 ** -14 / 12 * size + 2.0 ** -20 / 12 * rounded
+    assert err <= 1.2 * bound, (err / size) ** 0.5
