@@ -26,6 +26,13 @@ struct PagedCache {
   __host__ __device__ long long capacity() const { return (long long)table_width * page_rows; }
 };
 
+// Threads that a row takes, 8 dims each: a power of two.
+inline int lanes_per_row(int d) {
+  int lanes = 4;
+  while (lanes * 8 < d) lanes *= 2;
+  return lanes;
+}
+
 struct RowsView {   // [batch, heads, n_tokens, d] in element strides
   const void* data;
   long long sb, sh, sn;

@@ -389,12 +389,6 @@ __global__ void __launch_bounds__(kRowThreads) paged_read_kernel(const PagedCach
   }
 }
 
-int lanes_per_row(int d) {
-  int lanes = 4;
-  while (lanes * 8 < d) lanes *= 2;
-  return lanes;
-}
-
 template <typename T, bool kInt4> void (*pick_append(int lanes))(AppendArgs) {
   switch (lanes) {
     case 4: return paged_append_kernel<T, kInt4, 4>;

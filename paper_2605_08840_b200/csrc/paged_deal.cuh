@@ -42,6 +42,11 @@ __device__ __forceinline__ void tanh_any(float& t0, float& t1) {
   t1 = fabsf(t1) <= kTanhNear ? f2_hi(near) : far1;
 }
 
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
 __device__ __forceinline__ float lower(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float upper(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 

@@ -17,12 +17,6 @@ constexpr int kSimtThreads = 256;
 constexpr int kSimtRows = 4;
 constexpr int kSimtMaxSplits = 64;
 
-int lanes_per_row(int d) {
-  int lanes = 4;
-  while (lanes * 8 < d) lanes *= 2;
-  return lanes;
-}
-
 // grid (query rows / 4, splits, batch * Hkv); a single split writes the results itself.  A slot of `kLanes` threads takes a cache row, 8 dims
 // per thread; every slot keeps its own running (m, l, o) of the four query rows.
 template <typename T, bool kInt4, int kLanes>
