@@ -186,8 +186,8 @@ cudaError_t launch_paged_mma(void* state, const PagedCache& c, const RowsView& Q
                              const int (*clusters_of)[5], long long wait_limit, cudaStream_t st, int* launches);
 // bf16 with head_dim 64 or 128 on tcgen05, 256 query rows of a KV head per pass: for at least kChunkRows of them, and kChunkAll in the call.
 // A pass costs the same for few rows, and a call some 25 us before and after its passes.  Measured, 32 heads of 128 (8 KV heads), 4-bit rows,
-// this one and the kernel for few tokens: 1 x 2200 rows, 48 tokens 34.7 and 29.5 us, 128 tokens 37.4 and 55.1; 1 x 17000 rows, 32 tokens 61
-// and 54, 48 tokens 64 and 81; 8 x 4000 rows, 8 tokens 77 and 44, 16 tokens 78 and 75, 24 tokens 80 and 104.
+// this one and the kernel for few tokens: 1 x 2200 rows, 48 tokens 30.1 and 29.5 us, 128 tokens 37.4 and 55.1; 1 x 17000 rows, 32 tokens 61
+// and 55, 48 tokens 53 and 81; 8 x 4000 rows, 8 tokens 77 and 45, 16 tokens 78 and 75, 24 tokens 76 and 104.
 constexpr int kChunkRows = 64, kChunkAll = 1536;
 cudaError_t paged_chunk_init();
 bool paged_chunk_shape(const PagedCache& c);     // by type, head_dim and query rows

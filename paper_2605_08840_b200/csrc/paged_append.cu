@@ -64,10 +64,11 @@ __device__ __forceinline__ uint32_t int4_codes(const float* x, float lo, float s
 
 // grid (batch * n_tokens / warps, y): a warp takes a token, or with few tokens the y-th part of its rows, so that where the token goes and
 // its cosines and sines are found once.  A row lies in kLanes threads, 32 / kLanes heads side by side; Q's heads, then K's, then V's,
-// some rounds of them on their way before the first is needed.  What bounds it: HBM (every row is read and written once), in 4 bits
-// the instructions beside it (366 per warp and 256 values, a quarter of them the codes), or for one token the latency of lengths -> table
-// -> row.  Measured, 32 + 8 heads of 128: one token 2.8 us; 8 x up to 4093 tokens, half of the dims rotated, into bf16 112 us (4.5 TB/s);
-// 32768 rotated tokens into 4 bits 219 us (4.1 TB/s).
+// some rounds of them on their way before the first is needed.  What bounds it: in 16 bits HBM (658 MB of traffic for 8 x up to 4093 tokens,
+// 6.0 TB/s; 100 MB of it are queries past a sequence's count, read and replaced by zeros); in 4 bits no unit alone (366 instructions per warp
+// and 256 values, a quarter of them the codes: issue slots 68% and DRAM 47% busy with 40% of the warps); for one token the latency of
+// lengths -> table -> row.  Measured, 32 + 8 heads of 128: one token 2.8 us; 8 x up to 4093 tokens, half of the dims rotated, into bf16
+// 112 us; 32768 rotated tokens into 4 bits 176 us (730 MB at least: 4.1 TB/s), 2048 unrotated ones without queries 8.0 us.
 struct AppendArgs {
   PagedCache c;
   RowsView K, V, Q;         // Q.data null: no queries
@@ -77,8 +78,8 @@ struct AppendArgs {
   void* Q_out;
 };
 
-// 72 registers, 28 warps per SM: with 80 (24 warps) or 64 (32 warps, some values found again) 2048 tokens into 4 bits take as long and 10%
-// longer, 8 x 4093 tokens into bf16 2% longer and 1%.
+// 72 registers, 28 warps per SM: with 80 (24 warps) or 64 (32 warps, some values found again) 2048 tokens into 4 bits and read back take as
+// long and 10% longer, 8 x 4093 tokens into bf16 2% longer and 1%.
 template <typename T, bool kInt4, int kLanes>
 __global__ void __launch_bounds__(kRowThreads, 7) paged_append_kernel(const __grid_constant__ AppendArgs a) {
   ptx::grid_dependency_wait();
@@ -285,7 +286,7 @@ __device__ __forceinline__ void int4_read(uint32_t w, uint32_t step_hi, uint32_t
 
 // grid (runs of `run` blocks of 16 rows, batch * Hkv / warps): a warp takes such a run of a head, K and V, so that a block's page is
 // looked up once and its loads are on their way together.  Rows first .. first + n_rows of every head; first may be negative.  Bound by HBM (the rows written).
-// Measured, 4-bit rows into bf16: 8 x up to 32749 rows 223 us (5.8 TB/s), 2176 rows 4.1 us.
+// Measured, 4-bit rows into bf16: 8 x up to 32749 rows 221 us (5.8 TB/s), 2176 rows 4.1 us.
 // (4 blocks a run: the set-up is a fifth of the instructions.  With few rows 1, until there are 8 warps per SM: 2176 rows 5.0 us, 8.7 in runs
 // of 4.)
 template <typename T, bool kInt4, int kLanes>
@@ -406,7 +407,7 @@ cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K
   const AppendArgs a{c, Kn, Vn, Q, K_pages, V_pages, positions, rot, Q_out};
   const long long blocks = ((long long)c.batch * c.n_tokens + warps - 1) / warps;
   // a warp per token finds its place and its angles once; with few tokens the rows go to warps of their own until there are 16 per SM
-  // (2048 tokens into 4 bits 14.0 us; until there are 32, 64: 14.5, 15.3)
+  // (2048 tokens into 4 bits and read back 14.0 us; until there are 32, 64: 14.5, 15.3)
   const int rounds = ((Q.data ? c.Hq : 0) + at_once - 1) / at_once + 2 * ((c.Hkv + at_once - 1) / at_once);
   long long y = (4LL * sm_count + blocks - 1) / blocks;
   if (y > rounds) y = rounds;

@@ -900,7 +900,7 @@ bool pick(const PagedCache& c, Variant* v) {
 // at once; then by the time that each way takes at the longest sequences the table can name, in us: fixed 6 and 12 (the second has
 // another kernel behind it), and the bytes at what its CTAs draw.  A cluster lasts as long as its own sequence, so that sequences of
 // different lengths speak for dealing out: a batch is taken to fill 0.8 of its table.  Measured, 8 KV heads of 4 query heads, clusters
-// against dealt out: 4 bits 2176 rows 7.9 / 13.3, 16384 rows 14.1 / 15.1, 32768 rows 22.2 / 20.1, 8 x 2176 rows 11.4 / 18.9, 8 x 16384
+// against dealt out: 4 bits 2176 rows 8.1 / 13.3, 16384 rows 14.1 / 15.1, 32768 rows 22.2 / 20.1, 8 x 2176 rows 11.4 / 18.9, 8 x 16384
 // 38.6 / 44.6; bf16 2176 rows 7.4 / 12.4, 32768 rows 30.8 / 34.0, 131072 rows 103.5 / 92.0, 8 x 2176 rows 16.6 / 25.9.
 int paged_mma_cluster(const PagedCache& c, const Variant& v, long long units, const int* clusters_of) {
   int i = 4;
