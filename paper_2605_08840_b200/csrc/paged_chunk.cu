@@ -31,7 +31,7 @@
 // The tiles that a unit's last query row sees, of all units end to end, are dealt out evenly; what several CTAs share is merged by a second
 // kernel.  Measured, 2048 tokens of 32 heads of 128 (8 KV heads) over 18432 rows: bf16 671 us (870 TFLOP/s, tensor pipe 43% busy), 4 bits in
 // groups of 128 667 us, of 32 804 us (the conversion of codes, a step and an offset per row and group, bounds that one); with a cap of 30 786,
-// 839 and 1075 us, with one of 5, which the logits reach, 1148 and 1240.  2048 tokens and nothing before them 122 us; 48 tokens over 17000
+// 839 and 1075 us, with one of 5, which the logits reach, 1148 and 1250.  2048 tokens and nothing before them 122 us; 48 tokens over 17000
 // rows 53 us.  What the last merge rounds is little beside the rest; the tensor pipe's own fp32 sums cut off what is below their last place,
 // which for values of one sign adds up to 6e-4 of them over 131072 rows and 1.2e-3 over 524288 (values around 0: nothing).
 #include <math.h>
