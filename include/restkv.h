@@ -478,6 +478,108 @@ restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, con
                                 const int32_t* lengths, const int32_t* table, const int32_t* first, int n_rows, void* K_out,
                                 void* V_out, restkv_stream stream);
 
+/*
+ * Decoding with beams: several hypotheses of a request at a time.  (No counterpart in the paper: what a loop over the cache above does when it
+ * keeps more than the one most likely continuation.)  Sequences of the cache are the hypotheses, those of a request side by side.
+ */
+typedef struct {
+  int batch, beams, vocab; /* requests; hypotheses of each, at most 64; tokens */
+  int n_out;               /* continuations of each request that are wanted, at most 64 */
+  restkv_dtype dtype;      /* of the logits */
+  long long stride;        /* elements from one row of logits to the next; 0 => vocab */
+  int pad_token;           /* the token that continues a hypothesis that has ended */
+} restkv_beams;
+
+/* Bytes of workspace (256-byte aligned) that restkv_beam_select needs; 0 on invalid arguments. */
+size_t restkv_beam_workspace_bytes(const restkv_beams* beams);
+
+/*
+ * restkv_beam_select -- the n_out best continuations of every request, the best first: over its hypotheses k and tokens v the largest
+ * scores[k] + logits[k,v] - log(sum over v' of exp(logits[k,v'])).
+ *   logits      device [batch * beams, vocab] in rows `stride` apart, dtype; 16-byte aligned (the rows need not be)
+ *   scores      device float [batch, beams]: what the hypotheses have summed up so far
+ *   finished    optional device uint8 [batch, beams]: a hypothesis that has ended (not 0) has one continuation, pad_token, with the score as it is; its
+ *               logits are not read
+ *   parents, tokens, scores_out   device int32, int32, float [batch, n_out]: which hypothesis, by which token, with which score
+ * Scores are compared in 64 bits (the normalisers are sums of fp32 exponentials).  Ties go to the lower hypothesis, in one hypothesis to the larger
+ * logit and then the lower token: one order, whatever the order in which blocks end.
+ * A NaN among the logits counts as -inf, +inf as the largest finite number; a NaN among the scores counts as -inf.  A continuation by a logit of
+ * -inf, or of a hypothesis with a score of -inf (whose logits are not read), has the score -inf and comes after all others.  Where there are fewer
+ * continuations than n_out the rest are hypothesis 0 with pad_token and -inf.
+ */
+restkv_status restkv_beam_select(restkv_handle* h, const restkv_beams* beams, const void* logits, const float* scores, const uint8_t* finished,
+                                 int32_t* parents, int32_t* tokens, float* scores_out, void* workspace, size_t workspace_bytes,
+                                 restkv_stream stream);
+
+/*
+ * restkv_paged_reorder -- the tables after a selection: sequence i of a request goes on from what sequence parents[i] holds.  Once for all layers.
+ *   beams      sequences of a request, at most 64; cache->batch is a multiple of it.  The sequences of a request have the same length
+ *   parents    device int32 [batch]: for every sequence one of 0 .. beams - 1, counted within its request
+ *   lengths    device int32 [batch]: rows that are there (they stay as they are)
+ *   table_out  device int32 [batch, table_width]; may be `table` itself, else the two must not overlap
+ *   copies     device int32 [batch, 3]: for restkv_paged_copy (source page, destination page, rows), or -1, -1, 0
+ *   dropped    optional device int32 [batch, table_width]: the pages that no sequence of the request names any more, each once, in the row of a
+ *              sequence that did and in its column; else -1
+ * Pages that are full are shared: a sequence names its parent's.  The page that the next row goes into, and whatever the table names behind it,
+ * every sequence has for itself.  The first sequence to go on from a parent takes the parent's own; each further one, in order, takes those
+ * of a sequence that nobody goes on from, in order, and the rows of the parent's last page have to be copied there.  So a table whose rows
+ * share a prompt's full pages, each with pages of its own behind them, is forked by parents that are all 0.
+ * Only the tables are read and written here.  A request with a parent out of range, or sequences of different lengths or of one past the table,
+ * is left as it is (nothing to copy, nothing dropped) and sets the sticky status (RESTKV_ERR_INVALID_ARG from restkv_poll_status).
+ * lengths_per_head: RESTKV_ERR_UNSUPPORTED.  The rest of the cache's description is checked as by restkv_paged_append.
+ */
+restkv_status restkv_paged_reorder(restkv_handle* h, const restkv_paged* cache, int beams, const int32_t* parents, const int32_t* lengths,
+                                   const int32_t* table, int32_t* table_out, int32_t* copies, int32_t* dropped, restkv_stream stream);
+
+/*
+ * restkv_paged_copy -- the first rows of pages to the first rows of others, for all heads of K and V and of every layer.
+ *   copies       device int32 [n_copies, 3]: source page, destination page, rows (0 .. page_rows; INT4 pages: whole blocks of 16).  A source below 0:
+ *                nothing to do.  A page that is out of range, or rows that are, is skipped and sets the sticky status
+ *   n_layers     pools of n_pages pages that lie layer_bytes apart (a multiple of 16; 0 => one pool behind the other), from K_pages and V_pages on
+ * No page may be the destination of two copies, or of one and the source of another.
+ */
+restkv_status restkv_paged_copy(restkv_handle* h, const restkv_paged* cache, const int32_t* copies, int n_copies, void* K_pages, void* V_pages,
+                                int n_layers, long long layer_bytes, restkv_stream stream);
+
+/*
+ * Cross attention: decoder tokens over the states of an encoder, or over any rows that are there as a whole (no row of K and V belongs to a
+ * token of the call, so every token sees every row).  The hypotheses of a source share its rows, which are read once for all of them.
+ */
+typedef struct {
+  int sources, beams;      /* sources; sequences of each that attend to it, side by side */
+  int n_q_heads, n_kv_heads, head_dim;
+  int n_rows;              /* rows of K and V: as many as the longest source has */
+  restkv_dtype dtype;      /* of Q, K, V and the outputs */
+  int lengths_per_head;    /* 0: lengths [sources], 1: lengths [sources, n_kv_heads], as restkv_evict_budgets leaves them */
+  float softmax_scale;     /* 0 => 1/sqrt(head_dim) */
+} restkv_cross;
+
+/* Bytes of workspace (256-byte aligned) that restkv_cross_attend needs for n_tokens query tokens; 0 on invalid arguments.  It does not grow with
+ * n_rows beyond a bound, and one for n_tokens serves every call of fewer. */
+size_t restkv_cross_workspace_bytes(const restkv_cross* cross, int n_tokens);
+
+/*
+ * restkv_cross_attend -- softmax(scale * q K^T) V (Eq. 3) of every query token over the rows of its source.
+ *   Q         [sources * beams, n_q_heads, n_tokens, head_dim]; query head hq reads KV head hq / (n_q_heads / n_kv_heads)
+ *   K, V      [sources, n_kv_heads, n_rows, head_dim], such as K_out and V_out of restkv_evict, or a projection of an encoder's states
+ *             (strides as for restkv_rows; those of a dimension of extent 1 are not looked at)
+ *   lengths   device int32, rows that are there, the first ones (clamped to [0, n_rows]); NULL: n_rows.  What lies behind them is not
+ *             part of any result, whatever it is
+ *   counts    optional device int32 [sources * beams]: tokens of every sequence that are there, the first ones (clamped to [0, n_tokens])
+ *   out       device [sources * beams, n_q_heads, n_tokens, head_dim] contiguous, dtype
+ *   lse       optional device float [sources * beams, n_q_heads, n_tokens]: natural-log sum of exp of the scaled logits; with out it is what
+ *             restkv_evict_from_lse takes (causal_tail 0, beams 1, the last w tokens, out as float)
+ * A token of a source without rows, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32.  The same
+ * call gives the same bits.
+ * head_dim: a multiple of 8, at most 256 (else RESTKV_ERR_UNSUPPORTED).  RESTKV_BF16 with head_dim 64 or 128 runs on the tensor cores (K and V
+ * with no stride of 0): few query rows beams * n_tokens * group of a KV head with weights of two bf16 parts (16 bits), many with weights of one
+ * bf16 (as an output has, too).  Everything else, and restkv_set_kernel_path(1), runs in fp32 throughout, and returns RESTKV_ERR_UNSUPPORTED under
+ * restkv_set_kernel_path(2 or 3).
+ */
+restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, int n_tokens, const restkv_rows* Q, const restkv_rows* K,
+                                  const restkv_rows* V, const int32_t* lengths, const int32_t* counts, void* out, float* lse, void* workspace,
+                                  size_t workspace_bytes, restkv_stream stream);
+
 #ifdef __cplusplus
 }
 #endif

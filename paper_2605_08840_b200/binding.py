@@ -28,6 +28,7 @@ EXPORTS = [
     "restkv_set_variant", "restkv_evict_budgets",
     "restkv_output_projection_bytes", "restkv_prepare_output_projection", "restkv_set_output_projection",
     "restkv_paged_page_bytes", "restkv_paged_workspace_bytes", "restkv_paged_append", "restkv_paged_attend", "restkv_paged_read",
+    "restkv_beam_workspace_bytes", "restkv_beam_select", "restkv_paged_reorder", "restkv_paged_copy", "restkv_cross_workspace_bytes", "restkv_cross_attend",
 ]
 KERNEL_NONE, KERNEL_PASS1, KERNEL_COMBINE, KERNEL_PASS2, KERNEL_POOL, KERNEL_SELECT, KERNEL_COMPACT = range(7)
 
@@ -79,6 +80,18 @@ class Rotation(ctypes.Structure):
     """restkv_rotation: position tables (kept alive by whoever made them, see make_rotation)."""
     _fields_ = [("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_positions", ctypes.c_int), ("rotary_dim", ctypes.c_int),
                 ("interleaved", ctypes.c_int)]
+
+
+class Beams(ctypes.Structure):
+    """restkv_beams: hypotheses, their logits and how many continuations are wanted."""
+    _fields_ = [("batch", ctypes.c_int), ("beams", ctypes.c_int), ("vocab", ctypes.c_int), ("n_out", ctypes.c_int), ("dtype", ctypes.c_int),
+                ("stride", ctypes.c_longlong), ("pad_token", ctypes.c_int)]
+
+
+class Cross(ctypes.Structure):
+    """restkv_cross: sources and the sequences that attend to them."""
+    _fields_ = [(name, ctypes.c_int) for name in ("sources", "beams", "n_q_heads", "n_kv_heads", "head_dim", "n_rows", "dtype", "lengths_per_head")]
+    _fields_ += [("softmax_scale", ctypes.c_float)]
 
 
 class RestKVError(RuntimeError):
@@ -143,6 +156,15 @@ def load_library() -> ctypes.CDLL:
     lib.restkv_paged_append.argtypes = [vp, cache, ci, rows, rows, vp, vp, vp, vp, vp, vp, ctypes.POINTER(Rotation), rows, vp, vp]
     lib.restkv_paged_attend.argtypes = [vp, cache, ci, rows, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.restkv_paged_read.argtypes = [vp, cache, vp, vp, vp, vp, vp, ci, vp, vp, vp]
+    beams, cross = ctypes.POINTER(Beams), ctypes.POINTER(Cross)
+    lib.restkv_beam_workspace_bytes.argtypes = [beams]
+    lib.restkv_beam_workspace_bytes.restype = sz
+    lib.restkv_beam_select.argtypes = [vp, beams, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.restkv_paged_reorder.argtypes = [vp, cache, ci, vp, vp, vp, vp, vp, vp, vp]
+    lib.restkv_paged_copy.argtypes = [vp, cache, vp, ci, vp, vp, ci, ctypes.c_longlong, vp]
+    lib.restkv_cross_workspace_bytes.argtypes = [cross, ci]
+    lib.restkv_cross_workspace_bytes.restype = sz
+    lib.restkv_cross_attend.argtypes = [vp, cross, ci, rows, rows, rows, vp, vp, vp, vp, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -169,6 +191,14 @@ def make_paged(batch, n_q_heads, n_kv_heads, head_dim, page_format, page_rows, n
                lengths_per_head=0, softmax_scale=0.0, softcap=0.0) -> Paged:
     return Paged(batch, n_q_heads, n_kv_heads, head_dim, dtype, page_format, group, page_rows, n_pages, table_width,
                  int(lengths_per_head), softmax_scale, softcap)
+
+
+def make_beams(batch, beams, vocab, n_out, dtype=BF16, stride=0, pad_token=0) -> Beams:
+    return Beams(batch, beams, vocab, n_out, dtype, stride, pad_token)
+
+
+def make_cross(sources, beams, n_q_heads, n_kv_heads, head_dim, n_rows, dtype=BF16, lengths_per_head=0, softmax_scale=0.0) -> Cross:
+    return Cross(sources, beams, n_q_heads, n_kv_heads, head_dim, n_rows, dtype, int(lengths_per_head), softmax_scale)
 
 
 def make_rotation(cos, sin, rotary_dim, interleaved=False) -> Rotation:
@@ -339,6 +369,34 @@ class Handle:
         self._check(self._lib.restkv_paged_read(
             self._h, ctypes.byref(cache), _ptr(K_pages), _ptr(V_pages), _ptr(lengths), _ptr(table), _ptr(first), int(n_rows), _ptr(K_out),
             _ptr(V_out), _stream_ptr(stream)), "restkv_paged_read")
+
+    def beam_workspace_bytes(self, beams: Beams) -> int:
+        return int(self._lib.restkv_beam_workspace_bytes(ctypes.byref(beams)))
+
+    def beam_select(self, beams, logits, scores, parents, tokens, scores_out, workspace, finished=None, stream=None):
+        self._check(self._lib.restkv_beam_select(
+            self._h, ctypes.byref(beams), _ptr(logits), _ptr(scores), _ptr(finished), _ptr(parents), _ptr(tokens), _ptr(scores_out), _ptr(workspace),
+            workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "restkv_beam_select")
+
+    def paged_reorder(self, cache, beams, parents, lengths, table, table_out, copies, dropped=None, stream=None):
+        self._check(self._lib.restkv_paged_reorder(
+            self._h, ctypes.byref(cache), int(beams), _ptr(parents), _ptr(lengths), _ptr(table), _ptr(table_out), _ptr(copies), _ptr(dropped),
+            _stream_ptr(stream)), "restkv_paged_reorder")
+
+    def paged_copy(self, cache, copies, K_pages, V_pages, n_copies=None, n_layers=1, layer_bytes=0, stream=None):
+        """copies: int32 [n_copies, 3] as paged_reorder leaves them; by default all of its rows."""
+        self._check(self._lib.restkv_paged_copy(
+            self._h, ctypes.byref(cache), _ptr(copies), int(copies.shape[0] if n_copies is None else n_copies), _ptr(K_pages), _ptr(V_pages), int(n_layers),
+            int(layer_bytes), _stream_ptr(stream)), "restkv_paged_copy")
+
+    def cross_workspace_bytes(self, cross: Cross, n_tokens: int) -> int:
+        return int(self._lib.restkv_cross_workspace_bytes(ctypes.byref(cross), int(n_tokens)))
+
+    def cross_attend(self, cross, n_tokens, Q, K, V, out, workspace, lengths=None, lse=None, counts=None, stream=None):
+        """Q, K, V: tensors [batch, heads, n, head_dim] of any row strides."""
+        self._check(self._lib.restkv_cross_attend(
+            self._h, ctypes.byref(cross), int(n_tokens), ctypes.byref(make_rows(Q)), ctypes.byref(make_rows(K)), ctypes.byref(make_rows(V)), _ptr(lengths),
+            _ptr(counts), _ptr(out), _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_ptr(stream)), "restkv_cross_attend")
 
     def poll_status(self, stream=None) -> int:
         return int(self._lib.restkv_poll_status(self._h, _stream_ptr(stream)))

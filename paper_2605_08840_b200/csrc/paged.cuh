@@ -172,6 +172,12 @@ cudaError_t launch_paged_append(const PagedCache& c, bool f32, const RowsView& K
                                 int sm_count, cudaStream_t st);
 cudaError_t launch_paged_read(const PagedCache& c, bool f32, const int* first, int n_rows, void* K_out, void* V_out, int sm_count,
                               cudaStream_t st);
+// Sequences of a request brought in order (at most kBeamsMost), and the pages that it takes.
+constexpr int kBeamsMost = 64;
+cudaError_t launch_paged_reorder(const PagedCache& c, int beams, const int* parents, const int* table, int* table_out, int* copies, int* dropped,
+                                 cudaStream_t st);
+cudaError_t launch_paged_copy(const PagedCache& c, const int* copies, int n_copies, int layers, long long layer_bytes, uint8_t* K_pages,
+                              uint8_t* V_pages, cudaStream_t st);
 // fp32 SIMT attention: every dtype, format and head_dim.
 int paged_simt_splits(const PagedCache& c, int sm_count);
 size_t paged_simt_bytes(const PagedCache& c, int sm_count);

@@ -189,4 +189,42 @@ restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, con
   return RESTKV_OK;
 }
 
+restkv_status restkv_paged_reorder(restkv_handle* h, const restkv_paged* cache, int beams, const int32_t* parents, const int32_t* lengths,
+                                   const int32_t* table, int32_t* table_out, int32_t* copies, int32_t* dropped, restkv_stream stream) {
+  if (!h || !parents || !lengths || !table || !table_out || !copies || beams < 1) return RESTKV_ERR_INVALID_ARG;
+  PagedCache c;
+  const restkv_status s = make_cache(cache, &c);
+  if (s != RESTKV_OK) return s;
+  if (c.batch % beams != 0) return RESTKV_ERR_INVALID_ARG;
+  if (c.per_head || beams > kBeamsMost) return RESTKV_ERR_UNSUPPORTED;
+  // a table that is neither the other nor apart from it would be read where it has been written
+  const size_t bytes = (size_t)c.batch * c.table_width * sizeof(int32_t);
+  const uintptr_t from = (uintptr_t)table, to = (uintptr_t)table_out;
+  if (from != to && from < to + bytes && to < from + bytes) return RESTKV_ERR_INVALID_ARG;
+  if (!on_device(h)) return RESTKV_ERR_INVALID_ARG;
+  c.lengths = lengths; c.table = table; c.dev_status = h->dev_status;
+  Call call{h, (cudaStream_t)stream};
+  RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_paged_reorder(c, beams, parents, table, table_out, copies, dropped, call.st), 1);
+  return RESTKV_OK;
+}
+
+restkv_status restkv_paged_copy(restkv_handle* h, const restkv_paged* cache, const int32_t* copies, int n_copies, void* K_pages, void* V_pages,
+                                int n_layers, long long layer_bytes, restkv_stream stream) {
+  if (!h || !copies || !K_pages || !V_pages || n_copies < 1 || n_layers < 1) return RESTKV_ERR_INVALID_ARG;
+  if (!aligned16(K_pages) || !aligned16(V_pages)) return RESTKV_ERR_INVALID_ARG;
+  PagedCache c;
+  const restkv_status s = make_cache(cache, &c);
+  if (s != RESTKV_OK) return s;
+  const long long pool = (long long)c.n_pages * c.Hkv * c.head_bytes;
+  if (layer_bytes == 0) layer_bytes = pool;
+  if (layer_bytes < 0 || layer_bytes % 16 != 0 || (n_layers > 1 && layer_bytes < pool)) return RESTKV_ERR_INVALID_ARG;
+  if ((long long)n_copies * n_layers > 0x7FFFFFFFll / (2 * c.Hkv)) return RESTKV_ERR_UNSUPPORTED;   // blocks of a grid
+  if (!on_device(h)) return RESTKV_ERR_INVALID_ARG;
+  c.dev_status = h->dev_status;
+  Call call{h, (cudaStream_t)stream};
+  RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
+                launch_paged_copy(c, copies, n_copies, n_layers, layer_bytes, (uint8_t*)K_pages, (uint8_t*)V_pages, call.st), 1);
+  return RESTKV_OK;
+}
+
 }  // extern "C"

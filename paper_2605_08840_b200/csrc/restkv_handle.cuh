@@ -29,6 +29,13 @@ struct restkv_handle {
 namespace restkv {
 
 inline size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+// Whether the handle's device is the current one, on which a launch would go.
+inline bool on_device(const restkv_handle* h) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) == cudaSuccess) return dev == h->device;
+  (void)cudaGetLastError();
+  return false;
+}
 inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 
 struct Call {
