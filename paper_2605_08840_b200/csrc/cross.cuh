@@ -43,5 +43,11 @@ __device__ __forceinline__ long long cross_out_row(const CrossProblem& c, const 
 int cross_simt_splits(const CrossProblem& c, int sm_count);
 size_t cross_simt_bytes(const CrossProblem& c, int sm_count);
 cudaError_t launch_cross_simt(const CrossProblem& c, bool f32, float* part, int splits, cudaStream_t st);
+// bf16 with head_dim 64 or 128 on the warp-level tensor instructions, up to 32 query rows per pass over K and V
+cudaError_t cross_few_init();
+bool cross_few_supported(const CrossProblem& c);
+size_t cross_few_bytes(const CrossProblem& c, int sm_count);
+cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, int sm_count, const int* clusters_of, long long wait_limit, unsigned int* dev_status,
+                             cudaStream_t st, int* launches);
 
 }  // namespace restkv

@@ -41,8 +41,11 @@ static restkv_status make_view(const restkv_rows* s, int batch, int heads, int n
   return RESTKV_OK;
 }
 
+// The most that any kernel that the call can run on needs.  It never falls as n_tokens grows (each part rises with them and, once there, stays).
 static size_t cross_bytes(const CrossProblem& c, bool f32, int sm_count) {
-  return align256(cross_simt_bytes(c, sm_count));
+  size_t most = cross_simt_bytes(c, sm_count);
+  if (!f32 && cross_few_bytes(c, sm_count) > most) most = cross_few_bytes(c, sm_count);
+  return align256(most);
 }
 
 static int current_sms() {
@@ -81,6 +84,12 @@ restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, i
   if (!on_device(h)) return RESTKV_ERR_INVALID_ARG;
   c.lengths = lengths; c.counts = counts; c.out = out; c.lse = lse;
   Call call{h, (cudaStream_t)stream};
+  if (!f32 && h->tc_state && h->kernel_path != 1 && cross_few_supported(c)) {
+    int launches = 0;
+    RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
+                  launch_cross_few(h->tc_state, c, (float*)workspace, h->sm_count, h->paged_clusters[0], h->wait_limit, h->dev_status, call.st, &launches), launches);
+    return RESTKV_OK;
+  }
   if (h->kernel_path >= 2) return RESTKV_ERR_UNSUPPORTED;   // the tensor cores are required
   const int splits = cross_simt_splits(c, h->sm_count);
   RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_cross_simt(c, f32, (float*)workspace, splits, call.st), splits == 1 ? 1 : 2);

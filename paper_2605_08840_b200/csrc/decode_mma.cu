@@ -18,6 +18,7 @@
 #include <cooperative_groups.h>
 
 #include "tc_common.cuh"
+#include "warp_mma.cuh"
 
 namespace restkv {
 
@@ -35,19 +36,6 @@ constexpr uint32_t kDmWarpBytes = kDmStages * kDmStage;
 constexpr size_t kDmSmem = (size_t)kDmWarps * kDmWarpBytes + 1024;
 constexpr int kDmMaxG = kDecodeMmaMaxG;
 
-__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t* r) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void ldsm4_t(uint32_t addr, uint32_t* r) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
-}
-__device__ __forceinline__ void mma16816(float* c, const uint32_t* a, uint32_t b0, uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 
 struct DecodeArgs {
   int G, n_rows, splits;          // splits: clusters per head (1: the cluster writes the result itself)

@@ -92,12 +92,11 @@ __device__ __forceinline__ int entry_tiles(const PagedCache& c, int e, int tile_
 struct Run {
   int tile, end, entry, first, tiles;
 };
-__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int most, int x, int grid) {
+template <class TilesOf> __device__ __forceinline__ Run find_run(int entries, int units, TilesOf&& tiles_of, int most, int x, int grid) {
   const int lane = threadIdx.x & 31;
-  const int entries = entries_of(c), units = units_of(c, row_tiles);
-  const int t0 = lane < entries ? entry_tiles(c, lane, tile_rows) : 0;
+  const int t0 = lane < entries ? tiles_of(lane) : 0;
   int sum = t0 * units;
-  for (int e = 32 + lane; e < entries; e += 32) sum += entry_tiles(c, e, tile_rows) * units;
+  for (int e = 32 + lane; e < entries; e += 32) sum += tiles_of(e) * units;
   const int all = __reduce_add_sync(0xffffffffu, sum);
   const Deal deal(all, grid, most);
   Run r{0, 0, 0, 0, 1};
@@ -106,7 +105,7 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int 
   int want = deal.start(x), before = 0;
   bool have = false;
   for (int base = 0; base < entries; base += 32) {
-    const int t = base == 0 ? t0 : base + lane < entries ? entry_tiles(c, base + lane, tile_rows) : 0;
+    const int t = base == 0 ? t0 : base + lane < entries ? tiles_of(base + lane) : 0;
     int upto = t * units;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -132,6 +131,9 @@ __device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int 
     before += __shfl_sync(0xffffffffu, upto, 31);
   }
   return r;
+}
+__device__ __forceinline__ Run find_run(const PagedCache& c, int row_tiles, int tile_rows, int most, int x, int grid) {
+  return find_run(entries_of(c), units_of(c, row_tiles), [&](int e) { return entry_tiles(c, e, tile_rows); }, most, x, grid);
 }
 
 // Dims kPer v .. of a query row's result.
