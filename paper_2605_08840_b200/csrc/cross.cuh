@@ -49,5 +49,11 @@ bool cross_few_supported(const CrossProblem& c);
 size_t cross_few_bytes(const CrossProblem& c, int sm_count);
 cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, int sm_count, const int* clusters_of, long long wait_limit, unsigned int* dev_status,
                              cudaStream_t st, int* launches);
+// the same on tcgen05, 256 query rows per pass: from kManyRows of them on
+constexpr int kManyRows = 65;
+cudaError_t cross_many_init();
+bool cross_many_supported(const CrossProblem& c);
+size_t cross_many_bytes(const CrossProblem& c, int sm_count);
+cudaError_t launch_cross_many(void* state, const CrossProblem& c, float* part, int sm_count, long long wait_limit, unsigned int* dev_status, cudaStream_t st);
 
 }  // namespace restkv

@@ -45,6 +45,7 @@ static restkv_status make_view(const restkv_rows* s, int batch, int heads, int n
 static size_t cross_bytes(const CrossProblem& c, bool f32, int sm_count) {
   size_t most = cross_simt_bytes(c, sm_count);
   if (!f32 && cross_few_bytes(c, sm_count) > most) most = cross_few_bytes(c, sm_count);
+  if (!f32 && cross_many_bytes(c, sm_count) > most) most = cross_many_bytes(c, sm_count);
   return align256(most);
 }
 
@@ -84,7 +85,12 @@ restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, i
   if (!on_device(h)) return RESTKV_ERR_INVALID_ARG;
   c.lengths = lengths; c.counts = counts; c.out = out; c.lse = lse;
   Call call{h, (cudaStream_t)stream};
-  if (!f32 && h->tc_state && h->kernel_path != 1 && cross_few_supported(c)) {
+  const bool tensor_cores = !f32 && h->tc_state && h->kernel_path != 1;
+  if (tensor_cores && cross_many_supported(c)) {
+    RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_cross_many(h->tc_state, c, (float*)workspace, h->sm_count, h->wait_limit, h->dev_status, call.st), 2);
+    return RESTKV_OK;
+  }
+  if (tensor_cores && cross_few_supported(c)) {
     int launches = 0;
     RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE,
                   launch_cross_few(h->tc_state, c, (float*)workspace, h->sm_count, h->paged_clusters[0], h->wait_limit, h->dev_status, call.st, &launches), launches);

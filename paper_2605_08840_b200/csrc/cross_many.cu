@@ -1,0 +1,590 @@
+// Cross attention of many query rows of a KV head (a decoder's prompt, or the tokens of many hypotheses) on tcgen05: bf16, head_dim 64 or 128.
+//
+// What bounds it: 4 * 128 * 128 * head_dim operations per 128 query rows and 128 rows of K and V are 1024 cycles of the tensor pipe at head_dim 128, and the
+// exponentials as many of the special-function unit.
+//   - a CTA per SM takes 256 query rows (hypotheses x tokens x heads of the group) in two tiles of 128, each with a warpgroup of its own, a thread per
+//     row; a tile of K and V serves both;
+//   - K and V come by TMA from where they lie (four dimensions with strides) into a ring of tiles, in the order in which they are used;
+//   - S (fp32) and O of both tiles fill the tensor memory's 512 columns at head_dim 128; P (bf16) takes S's place and is the A operand of P V there;
+//   - a tile of logits is taken into registers as a whole (the softmax's warps have 208 of them per thread, the others 88); its weights go out in two
+//     halves, so that the first meets V while the second is made;
+//   - the reference of the weights is moved (sums and O scaled) only where they would pass 2^8;
+//   - rows behind a source's length: their logits are replaced, and what V holds there is cleared in the last 16 rows that a product reads, for a
+//     weight of 0 is to find a number.
+// The tiles of all units (source, KV head, 256 query rows) end to end are dealt out evenly; what several CTAs share is merged by a second kernel.
+#include <math.h>
+
+#include "cross_tc.cuh"
+#include "paged_deal.cuh"
+
+namespace restkv {
+
+namespace {
+
+constexpr int kMaRows = 256;                 // query rows of a unit
+constexpr int kMaTile = 128;                 // rows of K and V of a tile
+constexpr int kMaSoftmax = 8;                // warps; then the loader's and the products'
+constexpr int kMaThreads = (kMaSoftmax + 4) * 32;   // (two warps more: registers are moved by whole warpgroups)
+// Registers per thread: of the launch, and as the warpgroups of the softmax and the other one then share them.
+constexpr int kMaRegs = 168, kMaSoftmaxRegs = 208, kMaOtherRegs = 88;
+static_assert(2 * kMaSoftmaxRegs + kMaOtherRegs == 3 * kMaRegs, "more than the launch has would be waited for");
+constexpr int kMaSnap = 4;                   // tiles that a CTA could go through while it ends one unit and begins another
+constexpr float kMaSlack = 8.f;              // log2 of what weights may grow to before O is rescaled
+
+struct CrossManyArgs {
+  CrossProblem c;
+  float* part;                               // per CTA two of: o [256, d], (m, l) [256]
+  int2* begins;                              // per CTA: unit and tile of it that it begins with; -1: none
+  unsigned int* dev_status;
+  int row_tiles;                             // units per KV head
+  long long wait_limit;
+};
+
+template <int kD> struct ManyConfig {
+  static constexpr uint32_t kTileBytesD = 128u * kD * 2u;
+  static constexpr int kSlots = kD == 128 ? 5 : 8;                       // of the ring: tiles of K and of V in turn
+  static constexpr size_t kSmem = (2 + kSlots) * (size_t)kTileBytesD + 1024;
+};
+
+struct ManyBarriers {
+  uint64_t q_full[2], s_full[2], p_full[2][2], pv_done[2], full[8], empty[8], edge, drained;
+};
+
+// Row `row`, 16-byte chunk `chunk` of a 16-bit operand tile of 128 rows: boxes of [128 rows x 64 elements], 128-byte swizzle.
+__device__ __forceinline__ uint32_t many_at(uint32_t tile, int row, int chunk) {
+  return tile + (uint32_t)(chunk >> 3) * 16384u + (uint32_t)row * 128u + (uint32_t)(((chunk & 7) ^ (row & 7)) << 4);
+}
+__device__ __forceinline__ void many_sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// Tiles of a unit: none if its source has no rows, or if none of its tokens is there.
+__device__ __forceinline__ int many_tiles(const CrossProblem& c, int row_tiles, int unit) {
+  const int bh = unit / row_tiles, rho0 = (unit - bh * row_tiles) * kMaRows, b = bh / c.Hkv, n = cross_length(c, b, bh - b * c.Hkv);
+  if (n == 0) return 0;
+  if (c.counts) {
+    const int R = (int)c.rows(), last = (min(rho0 + kMaRows, R) - 1) / c.G;
+    bool live = false;
+    for (int x = rho0 / c.G; x <= last && !live; x += c.n_tokens - x % c.n_tokens)   // the first of the unit's tokens of every hypothesis
+      live = x % c.n_tokens < c.counts[b * c.beams + x / c.n_tokens];
+    if (!live) return 0;
+  }
+  return (n + kMaTile - 1) / kMaTile;
+}
+
+template <int kD>
+__global__ void __launch_bounds__(kMaThreads, 1)
+cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossManyArgs a) {
+  using C = ManyConfig<kD>;
+  constexpr int kSlots = C::kSlots;
+  const CrossProblem& c = a.c;
+  extern __shared__ uint8_t smem_raw[];
+  __shared__ __align__(8) ManyBarriers B;
+  __shared__ Piece piece_s;
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_flag, counted[kMaThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+  const uint32_t q_at = base, ring_at = base + 2 * C::kTileBytesD;
+  auto wait = [&](uint64_t* bar, int phase) { return mbar_wait(bar, (uint32_t)phase & 1u, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit); };
+
+  if (threadIdx.x == 0) {
+    abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&B.q_full[i], 128);
+      mbar_init(&B.s_full[i], 1);
+      mbar_init(&B.p_full[i][0], 128);
+      mbar_init(&B.p_full[i][1], 128);
+      mbar_init(&B.pv_done[i], 1);
+    }
+    for (int i = 0; i < kSlots; ++i) {
+      mbar_init(&B.full[i], 1);
+      mbar_init(&B.empty[i], 1);
+    }
+    mbar_init(&B.edge, 1);
+    mbar_init(&B.drained, 1);
+    fence_mbar_init();
+  }
+  if (warp == kMaSoftmax + 1) {
+    tmem_alloc(&tmem_slot, 512);
+    tmem_relinquish();
+  }
+  if (threadIdx.x == kMaSoftmax * 32) {
+    prefetch_tensormap(&tmK);
+    prefetch_tensormap(&tmV);
+  }
+  grid_dependency_wait();
+  grid_dependency_launch();
+  auto tiles_of = [&](int unit) { return max(1, many_tiles(c, a.row_tiles, unit)); };   // a unit without rows has its outputs written, too
+  {
+    // The CTA's run of tiles: every thread counts those of some units; the threads in whose units the run begins and ends say where.
+    const int units = c.sources * c.Hkv * a.row_tiles, per = (units + kMaThreads - 1) / kMaThreads;
+    const int u0 = min((int)threadIdx.x * per, units), u1 = min(u0 + per, units);
+    int sum = 0;
+    for (int u = u0; u < u1; ++u) sum += tiles_of(u);
+    int upto = sum, all = 0, first = 0;
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) {
+      const int o = __shfl_up_sync(0xffffffffu, upto, off);
+      if (lane >= off) upto += o;
+    }
+    if (lane == 31) counted[warp] = upto;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < kMaThreads / 32; ++x) {
+      first += x < warp ? counted[x] : 0;
+      all += counted[x];
+    }
+    first += upto - sum;
+    const Deal deal(all, gridDim.x, kMaSnap);
+    const int x = blockIdx.x;
+    if (threadIdx.x == 0) {
+      if (x >= deal.ctas) piece_s.run = Run{0, 0, 0, 0, 1};
+      else if (x + 1 == deal.ctas) piece_s.run.end = all;
+    }
+    for (int k = 0; k < 2; ++k) {
+      if (x + k >= deal.ctas) break;
+      const int want = deal.start(x + k);
+      if (want < first || want >= first + sum) continue;
+      int u = u0, f = first, t = tiles_of(u);
+      while (want >= f + t) {
+        f += t;
+        t = tiles_of(++u);
+      }
+      const int boundary = f + deal.moved(want - f, t);
+      if (k == 1) {
+        piece_s.run.end = boundary;
+      } else {
+        piece_s.run.tile = boundary;
+        piece_s.run.entry = u;
+        piece_s.run.first = f;
+        piece_s.run.tiles = t;
+      }
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      const Run run = piece_s.run;
+      if (run.tile < run.end) piece_s.cut(1, tiles_of);
+      a.begins[blockIdx.x] = run.tile < run.end ? make_int2(piece_s.unit, piece_s.t0) : make_int2(-1, 0);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  constexpr uint32_t kO = 256;                          // O of tile w: columns kO + w * kD; S and P: w * 128
+  const volatile Piece& piece = piece_s;
+
+  struct Unit {
+    int b, h, rho0, n, t0, tiles, done, nth;            // done: tiles of the pieces before, phases of the barriers; nth: pieces before
+  };
+  // A role's part of every piece.  All roles go from piece to piece together.
+  auto each_piece = [&](auto&& part) {
+    int done = 0;
+    for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
+      const int unit = piece.unit, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kMaRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
+      const int t0 = piece.t0, tiles = min(piece.t1, many_tiles(c, a.row_tiles, unit)) - t0;
+      part(Unit{b, h, rho0, cross_length(c, b, h), t0, tiles, done, nth});
+      __syncwarp();
+      // all go on to the next piece, or none
+      const bool stop = __syncthreads_or(abort_flag) != 0;
+      tc_fence_after();
+      done += tiles;
+      if (threadIdx.x == 0) {
+        piece_s.run.tile += piece_s.t1 - piece_s.t0;
+        if (stop) piece_s.run.tile = piece_s.run.end;
+        if (piece_s.run.tile < piece_s.run.end) piece_s.cut(1, tiles_of);
+      }
+      __syncthreads();
+    }
+  };
+
+  // Each side's code sits behind its own register-budget change.
+  if (warp >= kMaSoftmax) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMaOtherRegs));
+    if (warp >= kMaSoftmax + 2) {
+      each_piece([](const Unit&) {});
+    } else if (warp == kMaSoftmax) {
+      int edges = 0;
+      each_piece([&](const Unit& u) {
+        // ---------------- loading K and V, in turn ----------------
+        bool ok = true;
+        int x = 2 * u.done;
+        const int end = x + 2 * u.tiles;
+        for (; x < end; ++x) {
+          const int s = x % kSlots, row = (u.t0 + ((x - 2 * u.done) >> 1)) * kMaTile;
+          // the verdict is the warp's: it clears rows together
+          ok = x < kSlots || __all_sync(0xffffffffu, wait(&B.empty[s], x / kSlots - 1));
+          if (!ok) break;
+          const bool is_v = x & 1, clear = is_v && u.n < row + kMaTile && (u.n & 15) != 0;
+          uint8_t* const to = smem_raw + (ring_at - smem_u32(smem_raw)) + (uint32_t)s * C::kTileBytesD;
+          uint64_t* const bar = clear ? &B.edge : &B.full[s];
+          if (elect_one()) {
+            mbar_arrive_expect_tx(bar, C::kTileBytesD);
+#pragma unroll
+            for (int y = 0; y < kD / 64; ++y) tma_load_4d(to + y * 16384, is_v ? &tmV : &tmK, bar, y * 64, row, u.h, u.b);
+          }
+          __syncwarp();
+          if (clear) {
+            wait_issued(&B.edge, (uint32_t)edges++);      // (a copy that has been asked for comes)
+            const int r0 = u.n - row, r1 = (r0 + 15) & ~15;
+            for (int y = lane; y < (r1 - r0) * (kD / 8); y += 32) many_sts128(many_at(ring_at + (uint32_t)s * C::kTileBytesD, r0 + y / (kD / 8), y % (kD / 8)), 0u, 0u, 0u, 0u);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&B.full[s]);
+          }
+        }
+        if (!ok) {                                        // nothing may still be on its way into shared memory when the CTA returns
+          for (int y = x > kSlots ? x - kSlots : 0; y < x; ++y) wait_issued(&B.full[y % kSlots], (uint32_t)(y / kSlots));
+        }
+      });
+    } else {
+      uint32_t drains = 0;
+      each_piece([&](const Unit& u) {
+        // ---------------- the products, by one thread ----------------
+        const int tiles = u.tiles, done = u.done;
+        if (tiles > 0 && elect_one()) {
+          constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, false), idesc_o = make_idesc_bf16(128, kD, true);
+          // descriptors count 16-byte units
+          const uint64_t q0 = kmajor_desc(q_at), k0 = kmajor_desc(ring_at), v0 = make_smem_desc(ring_at, 16384u, 1024u);
+          auto qk = [&](int w, int s) {
+            const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4));
+#pragma unroll
+            for (int k = 0; k < kD / 16; ++k) {
+              const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
+              umma_ss(tmem + (uint32_t)w * 128u, a0 + step, b0 + step, idesc_s, k > 0);
+            }
+            umma_commit(&B.s_full[w]);
+          };
+          auto slot = [&](int x) { return x % kSlots; };
+          auto there = [&](int x) { return wait(&B.full[x % kSlots], x / kSlots); };
+          bool ok = there(2 * done);
+          for (int w = 0; w < 2 && ok; ++w) {
+            ok = wait(&B.q_full[w], u.nth);
+            if (!ok) break;
+            tc_fence_after();
+            qk(w, slot(2 * done));
+          }
+          if (ok) umma_commit(&B.empty[slot(2 * done)]);
+          for (int j = 0; j < tiles && ok; ++j) {
+            const int at = done + j, xv = 2 * at + 1, xk = 2 * at + 2;
+            const int left = u.n - (u.t0 + j) * kMaTile, steps = left >= kMaTile ? 8 : (left + 15) / 16;   // of 16 rows that are there
+            ok = there(xv);
+            for (int w = 0; w < 2 && ok; ++w) {
+              const uint64_t b0 = v0 + (uint64_t)(slot(xv) * (C::kTileBytesD >> 4));
+#pragma unroll
+              for (int half = 0; half < 2; ++half) {
+                ok = ok && wait(&B.p_full[w][half], at);
+                if (!ok) break;
+                tc_fence_after();
+#pragma unroll
+                for (int k = 4 * half; k < 4 * half + 4; ++k)   // 16 rows: 8 columns of P, 2048 bytes of V
+                  if (k < steps) umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)(w * 128 + k * 8), b0 + (uint64_t)(k * 128), idesc_o, j > 0 || k > 0);
+              }
+              if (!ok) break;
+              umma_commit(&B.pv_done[w]);
+              if (w == 1) umma_commit(&B.empty[slot(xv)]);
+              if (j + 1 < tiles) {                        // the next logits, in whose place are the weights that the product before reads
+                ok = (w > 0 || there(xk)) && wait(&B.pv_done[w], at);
+                if (!ok) break;
+                tc_fence_after();
+                qk(w, slot(xk));
+                if (w == 1) umma_commit(&B.empty[slot(xk)]);
+              }
+            }
+          }
+          // Nothing may still write tensor memory, or arrive, when the CTA goes, which it does at the end of a piece in which any role's wait ran out.
+          umma_commit(&B.drained);
+          wait_issued(&B.drained, drains++);
+        }
+      });
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMaSoftmaxRegs));
+    each_piece([&](const Unit& u) {
+      // ---------------- softmax: a query row per thread ----------------
+      const int tiles = u.tiles, done = u.done, R = (int)c.rows();
+      const int w = warp >> 2, r = threadIdx.x & 127, rho = u.rho0 + w * 128 + r;
+      const uint32_t row_lane = (uint32_t)(warp & 3) << 21;          // lanes 32 (warp % 4) .. of tensor memory, in bits 16 up
+      const uint32_t s_tm = tmem + row_lane + (uint32_t)w * 128u, o_tm = tmem + row_lane + kO + (uint32_t)w * kD;
+      const CrossRow mine = cross_row(c, u.b, rho < R ? rho : 0);
+      const bool live = rho < R && cross_live(c, mine);
+      if (tiles > 0) {
+        // the warp's rows into shared memory, a row in kD / 8 lanes side by side, four rows per lane together
+        constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes;
+        const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
+        const int x = lane % kLanes, row0 = (warp & 3) * 32 + lane / kLanes;
+#pragma unroll 1
+        for (int z0 = 0; z0 < 32; z0 += 4 * kAtOnce) {
+          uint4 raw[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) {
+            const int rho_z = u.rho0 + w * 128 + row0 + z0 + y * kAtOnce;
+            raw[y] = make_uint4(0u, 0u, 0u, 0u);
+            if (rho_z < R) {
+              const CrossRow q = cross_row(c, u.b, rho_z);
+              if (cross_live(c, q)) raw[y] = reinterpret_cast<const uint4*>(cross_query<__nv_bfloat16>(c, q, u.h))[x];
+            }
+          }
+#pragma unroll
+          for (int y = 0; y < 4; ++y) many_sts128(many_at(tile, row0 + z0 + y * kAtOnce, x), raw[y].x, raw[y].y, raw[y].z, raw[y].w);
+        }
+        fence_proxy_async_smem();
+      }
+      mbar_arrive(&B.q_full[w]);                        // (once per piece, whether it has tiles or not)
+      const float f = c.scale * kLog2e;
+      float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
+      bool ok = true;
+      for (int j = 0; j < tiles; ++j) {
+        const int at = done + j, left = u.n - (u.t0 + j) * kMaTile;
+        // the waits' verdict is a warp's: tensor memory is read by whole warps
+        ok = __all_sync(0xffffffffu, wait(&B.s_full[w], at));
+        if (!ok) break;
+        tc_fence_after();
+        float v[kMaTile];
+#pragma unroll
+        for (int x = 0; x < kMaTile; x += 32) tmem_ld32(s_tm + x, v + x);
+        tmem_wait_ld();
+        if (left < kMaTile) {
+#pragma unroll
+          for (int x = 0; x < kMaTile; ++x)
+            if (x >= left) v[x] = -INFINITY;
+        }
+        float m[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int x = 4; x + 8 <= kMaTile; x += 8)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) m[z] = fmax3(m[z], v[x + 2 * z], v[x + 2 * z + 1]);
+        m[0] = fmax3(m[0], v[kMaTile - 4], v[kMaTile - 3]);
+        m[1] = fmax3(m[1], v[kMaTile - 2], v[kMaTile - 1]);
+        const float mx = fmaxf(fmax3(m[0], m[1], m[2]), m[3]) * f;      // (the factor is positive)
+        if (__any_sync(0xffffffffu, mx > ref + kMaSlack)) {
+          float down = 1.f;
+          if (mx > ref + kMaSlack) {
+            down = ex2_approx(ref - mx);                // ref = -inf gives 0
+            ref = mx;
+          }
+          l *= down;
+          if (j > 0) {                                  // the products of the tile before may still be adding to O
+            ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], at - 1));
+            if (!ok) break;
+            tc_fence_after();
+#pragma unroll 1
+            for (int x = 0; x < kD; x += 16) {
+              float o[16];
+              tmem_ld16(o_tm + x, o);
+              tmem_wait_ld();
+              uint32_t y[16];
+#pragma unroll
+              for (int z = 0; z < 16; ++z) y[z] = __float_as_uint(o[z] * down);
+              tmem_st16(o_tm + x, y);
+            }
+          }
+        }
+        const float m_use = ref == -INFINITY ? 0.f : ref;               // only logits of -inf so far: they weigh nothing
+        const f32x2 ff = f2_make(f, f), minus_m = f2_make(-m_use, -m_use);
+        f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+#pragma unroll
+          for (int x = 64 * half; x < 64 * half + 64; x += 32) {
+            uint32_t p[16];
+#pragma unroll
+            for (int y = 0; y < 32; y += 4) {
+              const f32x2 a0 = f2_fma(f2_make(v[x + y], v[x + y + 1]), ff, minus_m), a1 = f2_fma(f2_make(v[x + y + 2], v[x + y + 3]), ff, minus_m);
+              const float e0 = ex2_approx(f2_lo(a0)), e1 = ex2_approx(f2_hi(a0)), e2 = ex2_approx(f2_lo(a1)), e3 = ex2_approx(f2_hi(a1));
+              sum0 = f2_add(sum0, f2_make(e0, e1));
+              sum1 = f2_add(sum1, f2_make(e2, e3));
+              p[y / 2] = pack_bf16x2(e0, e1);
+              p[y / 2 + 1] = pack_bf16x2(e2, e3);
+            }
+            tmem_st16(s_tm + x / 2, p);                 // P where S has been read already
+          }
+          tmem_wait_st();
+          tc_fence_before();
+          mbar_arrive(&B.p_full[w][half]);
+        }
+        sum0 = f2_add(sum0, sum1);
+        l += f2_lo(sum0) + f2_hi(sum0);
+      }
+      // ---- the row's result ----
+      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], done + tiles - 1));
+      if (ok) {
+        tc_fence_after();
+        const bool whole = piece.whole != 0, some = l > 0.f && live;
+        const float norm = whole ? (some ? 1.f / l : 0.f) : 1.f;
+        const bool nothing = tiles <= 0 || (whole && !some);
+        float* const part = a.part + (long long)(2 * blockIdx.x + (u.t0 == 0)) * kMaRows * (kD + 2);
+        const long long row = cross_out_row(c, mine, u.h);
+        // By way of the warp's rows of Q's tile, which no product reads any more, for stores of whole rows: kD values of 16 bits at once, or
+        // fp32 ones in two turns.  16-byte chunk k of row r is at k ^ r.
+        constexpr int kChunks = kD / 8;
+        const uint32_t staged = q_at + (uint32_t)w * C::kTileBytesD + (uint32_t)(warp & 3) * (32u * 2u * kD);
+        const uint32_t to_row = staged + (uint32_t)lane * (2u * kD);
+        __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(c.out);
+        for (int turn = 0; turn < (whole ? 1 : 2); ++turn) {
+#pragma unroll
+          for (int x = 0; x < kD / 32; ++x) {
+            if (!whole && x / (kD / 64) != turn) continue;
+            float o[32];
+            if (tiles > 0) {
+              tmem_ld32(o_tm + x * 32, o);
+              tmem_wait_ld();
+            }
+#pragma unroll
+            for (int y = 0; y < 32; ++y) o[y] = nothing ? 0.f : o[y] * norm;
+            if (whole) {
+#pragma unroll
+              for (int y = 0; y < 32; y += 8)
+                many_sts128(to_row + (uint32_t)((((32 * x + y) / 8) ^ (lane & (kChunks - 1))) * 16), pack_bf16x2(o[y], o[y + 1]), pack_bf16x2(o[y + 2], o[y + 3]),
+                            pack_bf16x2(o[y + 4], o[y + 5]), pack_bf16x2(o[y + 6], o[y + 7]));
+            } else {
+#pragma unroll
+              for (int y = 0; y < 32; y += 4)
+                many_sts128(to_row + (uint32_t)(((((32 * x + y) % (kD / 2)) / 4) ^ (lane & (kChunks - 1))) * 16), __float_as_uint(o[y]), __float_as_uint(o[y + 1]),
+                            __float_as_uint(o[y + 2]), __float_as_uint(o[y + 3]));
+            }
+          }
+          __syncwarp();
+          const int k = lane % kChunks, in_tile = w * 128 + (warp & 3) * 32;
+#pragma unroll 4
+          for (int z = 0; z < 32; z += 32 / kChunks) {
+            const int at = z + lane / kChunks;
+            const long long to = __shfl_sync(0xffffffffu, row, at);
+            if (u.rho0 + in_tile + at >= R) continue;
+            const uint4 y = lds128(staged + (uint32_t)at * (2u * kD) + (uint32_t)((k ^ (at & (kChunks - 1))) * 16));
+            if (whole) reinterpret_cast<uint4*>(out + to * kD)[k] = y;
+            else reinterpret_cast<uint4*>(part + (in_tile + at) * kD + turn * (kD / 2))[k] = y;
+          }
+          __syncwarp();
+        }
+        if (rho < R) {
+          if (whole) {
+            if (c.lse) c.lse[row] = some ? fmaf(ref, 0.6931471805599453f, logf(l)) : -INFINITY;
+          } else {
+            reinterpret_cast<float2*>(part + kMaRows * kD)[w * 128 + r] = make_float2(ref, l);
+          }
+        }
+        tc_fence_before();
+      }
+    });
+  }
+  __syncthreads();
+  if (warp == kMaSoftmax + 1) tmem_dealloc(tmem, 512);
+}
+
+// grid (CTAs of the kernel before, 32), block 256: merges what several of them left of a unit, a row per warp.  A unit is merged by the blocks of the
+// first CTA that began inside it.
+template <int kD>
+__global__ void __launch_bounds__(256) cross_many_combine_kernel(const __grid_constant__ CrossManyArgs a) {
+  grid_dependency_wait();
+  grid_dependency_launch();
+  const CrossProblem& c = a.c;
+  const int x = blockIdx.x, ctas = gridDim.x, lane = threadIdx.x & 31;
+  const int2 mine = __ldcg(a.begins + x);
+  if (mine.x < 0 || mine.y == 0) return;                // (the first CTA begins a unit: x > 0 from here on)
+  auto inside = [&](int y) {
+    const int2 o = __ldcg(a.begins + y);
+    return o.x == mine.x && o.y > 0;
+  };
+  if (inside(x - 1)) return;
+  const int unit = mine.x, row = (int)blockIdx.y * 8 + (threadIdx.x >> 5), bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
+  const int rho = (unit - bh * a.row_tiles) * kMaRows + row;
+  if (rho >= (int)c.rows()) return;
+  constexpr long long kSlot = kMaRows * (kD + 2);
+  constexpr int kPer = kD / 32;
+  auto piece = [&](int k) { return a.part + (2ll * (x - 1 + k) + (k == 0)) * kSlot; };   // the CTA before began the unit
+  // 32 pieces at a time, a lane's (reference, sum) each
+  float mm = -INFINITY, ll = 0.f, acc[kPer] = {};
+  for (int base = 0;; base += 32) {
+    const int k = base + lane;
+    const bool some = k == 0 || (x - 1 + k < ctas && inside(x - 1 + k));
+    const int n = __popc(__ballot_sync(0xffffffffu, some));
+    const float2 ml = some ? __ldcg(reinterpret_cast<const float2*>(piece(k) + kMaRows * kD) + row) : make_float2(-INFINITY, 0.f);
+    float top = ml.x;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    top = fmaxf(top, mm);
+    const float down = mm == -INFINITY ? 0.f : ex2_approx(mm - top), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
+    mm = top;
+    float sum = ml.y * f;
+#pragma unroll
+    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+    ll = fmaf(ll, down, sum);
+#pragma unroll
+    for (int y = 0; y < kPer; ++y) acc[y] *= down;
+#pragma unroll 8
+    for (int y = 0; y < n; ++y) {
+      const float g = __shfl_sync(0xffffffffu, f, y);
+      const float* o = piece(base + y) + row * kD + kPer * lane;
+      float w[kPer];
+      if constexpr (kPer == 4) {
+        const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
+        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+      } else {
+        const float2 u = __ldcg(reinterpret_cast<const float2*>(o));
+        w[0] = u.x; w[1] = u.y;
+      }
+#pragma unroll
+      for (int z = 0; z < kPer; ++z) acc[z] = g > 0.f ? fmaf(w[z], g, acc[z]) : acc[z];
+    }
+    if (n < 32) break;
+  }
+  const CrossRow r = cross_row(c, b, rho);
+  const bool some = ll > 0.f && cross_live(c, r);
+  const long long at = cross_out_row(c, r, h);
+  const float norm = some ? 1.f / ll : 0.f;
+  uint32_t y[kPer / 2];
+#pragma unroll
+  for (int z = 0; z < kPer / 2; ++z) y[z] = some ? pack_bf16x2(acc[2 * z] * norm, acc[2 * z + 1] * norm) : 0u;
+  __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD + kPer * lane;
+  if constexpr (kPer == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
+  else *reinterpret_cast<uint32_t*>(to) = y[0];
+  if (lane == 0 && c.lse) c.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+}
+
+int many_ctas(int sm_count) { return sm_count < kMaxCtas ? sm_count : kMaxCtas; }
+
+}  // namespace
+
+template <int kD> cudaError_t many_init() {
+  cudaFuncAttributes has;
+  const cudaError_t e = cudaFuncGetAttributes(&has, cross_many_kernel<kD>);
+  if (e != cudaSuccess) return e;
+  if (has.numRegs != kMaRegs) return cudaErrorInvalidDeviceFunction;   // its warpgroups would wait for registers that are not there
+  return cudaFuncSetAttribute(cross_many_kernel<kD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)ManyConfig<kD>::kSmem);
+}
+cudaError_t cross_many_init() {
+  const cudaError_t e = many_init<64>();
+  return e != cudaSuccess ? e : many_init<128>();
+}
+
+bool cross_many_shape(const CrossProblem& c) { return (c.d == 64 || c.d == 128) && c.rows() >= kManyRows; }
+
+bool cross_many_supported(const CrossProblem& c) {
+  if (!cross_many_shape(c) || !cross_map_fits(c, c.K) || !cross_map_fits(c, c.V)) return false;
+  const long long units = (long long)c.sources * c.Hkv * ((c.rows() + kMaRows - 1) / kMaRows);
+  return ((long long)c.n_rows / kMaTile + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
+}
+
+size_t cross_many_bytes(const CrossProblem& c, int sm_count) {
+  if (!cross_many_shape(c)) return 0;
+  return (size_t)many_ctas(sm_count) * (2 * kMaRows * (c.d + 2) * sizeof(float) + sizeof(int2));
+}
+
+cudaError_t launch_cross_many(void* state, const CrossProblem& c, float* part, int sm_count, long long wait_limit, unsigned int* dev_status, cudaStream_t st) {
+  CUtensorMap tmK, tmV;
+  if (!make_cross_map((TcState*)state, &tmK, c, c.K, kMaTile) || !make_cross_map((TcState*)state, &tmV, c, c.V, kMaTile)) return cudaErrorInvalidValue;
+  const int ctas = many_ctas(sm_count);
+  CrossManyArgs a{};
+  a.c = c; a.part = part; a.dev_status = dev_status; a.wait_limit = wait_limit;
+  a.row_tiles = (int)((c.rows() + kMaRows - 1) / kMaRows);
+  a.begins = reinterpret_cast<int2*>(part + (size_t)2 * ctas * kMaRows * (c.d + 2));
+  const cudaError_t e = c.d == 64 ? launch_chained(cross_many_kernel<64>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<64>::kSmem, st, tmK, tmV, a)
+                                  : launch_chained(cross_many_kernel<128>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<128>::kSmem, st, tmK, tmV, a);
+  if (e != cudaSuccess) return e;
+  const dim3 grid((unsigned int)ctas, kMaRows / 8);
+  return c.d == 64 ? launch_chained(cross_many_combine_kernel<64>, grid, 256, 0, st, a) : launch_chained(cross_many_combine_kernel<128>, grid, 256, 0, st, a);
+}
+
+}  // namespace restkv

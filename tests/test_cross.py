@@ -265,6 +265,37 @@ def test_cross_in_fp32_throughout_and_where_the_tensor_cores_are_required(handle
         handle.set_kernel_path(rk.PATH_AUTO)
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("S,beams,Hq,Hkv,d,t,m", [(1, 4, 32, 8, 128, 1, 3000), (1, 4, 32, 8, 128, 1, 40000), (1, 1, 8, 2, 128, 300, 3001), (3, 1, 8, 2, 64, 500, 700), (1, 8, 8, 2, 64, 1, 9000)])
+def test_cross_waits_that_run_out(handle, S, beams, Hq, Hkv, d, t, m):
+    """A wait limit of one SM clock in the tensor-core kernels of few query rows (in clusters, dealt out) and of many: whichever waits run out, the
+    call returns by itself, with the timeout status or with its results, and the next one has them."""
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, torch.bfloat16, 14)
+    desc = rk.make_cross(S, beams, Hq, Hkv, d, m)
+    ws = torch.empty(handle.cross_workspace_bytes(desc, t), dtype=torch.uint8, device="cuda")
+    lengths = dev_i32([m - 100 * i for i in range(S)])
+
+    def call():
+        out, lse = torch.empty(S * beams, Hq, t, d, dtype=torch.bfloat16, device="cuda"), torch.empty(S * beams, Hq, t, device="cuda")
+        handle.cross_attend(desc, t, Q, K, V, out, ws, lengths=lengths, lse=lse)
+        torch.cuda.synchronize()
+        return handle.poll_status(), out, lse
+
+    status, want, want_lse = call()
+    assert status == rk.RESTKV_OK
+    for _ in range(5):
+        try:
+            handle.set_wait_limit(1)
+            status, out, lse = call()
+        finally:
+            handle.set_wait_limit(2_000_000_000)
+        assert status in (rk.RESTKV_OK, rk.ERR_TIMEOUT)
+        if status == rk.RESTKV_OK:
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
+        status, out, lse = call()
+        assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
 # ---- refusals -------------------------------------------------------------------------------------------------------------------------
 
 def good(**kw):
