@@ -1,18 +1,24 @@
 // Cross attention of many query rows of a KV head (a decoder's prompt, or the tokens of many hypotheses) on tcgen05: bf16, head_dim 64 or 128.
 //
 // What bounds it: 4 * 128 * 128 * head_dim operations per 128 query rows and 128 rows of K and V are 1024 cycles of the tensor pipe at head_dim 128, and the
-// exponentials as many of the special-function unit.
+// exponentials as many of the special-function unit; between the two the chain logits -> maximum -> exponentials -> weights -> products -> next
+// logits, each arrow some 200 cycles of barriers besides.  So
 //   - a CTA per SM takes 256 query rows (hypotheses x tokens x heads of the group) in two tiles of 128, each with a warpgroup of its own, a thread per
 //     row; a tile of K and V serves both;
 //   - K and V come by TMA from where they lie (four dimensions with strides) into a ring of tiles, in the order in which they are used;
+//   - a tile of logits is two halves of 64 columns in turn: while a row's thread is at one, the other's weights meet V and its next logits are made (whole
+//     tiles in turn, in registers as a whole: 296 us for 283);
+//   - the two warpgroups take turns at the exponentials: both at them together would wait for their products together (291 us);
 //   - S (fp32) and O of both tiles fill the tensor memory's 512 columns at head_dim 128; P (bf16) takes S's place and is the A operand of P V there;
-//   - a tile of logits is taken into registers as a whole (the softmax's warps have 208 of them per thread, the others 88); its weights go out in two
-//     halves, so that the first meets V while the second is made;
+//   - a thread issues the logits' products, one for each tile the others, so that none waits for what it need not;
+//   - every role goes through the pieces of the CTA's run by itself;
 //   - the reference of the weights is moved (sums and O scaled) only where they would pass 2^8;
 //   - rows behind a source's length: their logits are replaced, and what V holds there is cleared in the last 16 rows that a product reads, for a
 //     weight of 0 is to find a number.
 // The tiles of all units (source, KV head, 256 query rows) end to end are dealt out evenly; what several CTAs share is merged by a second kernel.
 #include <math.h>
+
+#include <type_traits>
 
 #include "cross_tc.cuh"
 #include "paged_deal.cuh"
@@ -26,9 +32,11 @@ constexpr int kMaTile = 128;                 // rows of K and V of a tile
 constexpr int kMaSoftmax = 8;                // warps; then the loader's and the products'
 constexpr int kMaThreads = (kMaSoftmax + 4) * 32;   // (two warps more: registers are moved by whole warpgroups)
 // Registers per thread: of the launch, and as the warpgroups of the softmax and the other one then share them.
-constexpr int kMaRegs = 168, kMaSoftmaxRegs = 208, kMaOtherRegs = 88;
+constexpr int kMaRegs = 168, kMaSoftmaxRegs = 176, kMaOtherRegs = 152;
 static_assert(2 * kMaSoftmaxRegs + kMaOtherRegs == 3 * kMaRegs, "more than the launch has would be waited for");
-constexpr int kMaSnap = 4;                   // tiles that a CTA could go through while it ends one unit and begins another
+// Tiles that a CTA could go through while it ends one unit and begins another: each unit counts for as many more, ahead of its own, and a boundary that
+// lies nearer to a unit's end moves there.
+constexpr int kMaAhead = 4, kMaSnap = 8;
 constexpr float kMaSlack = 8.f;              // log2 of what weights may grow to before O is rescaled
 
 struct CrossManyArgs {
@@ -47,7 +55,7 @@ template <int kD> struct ManyConfig {
 };
 
 struct ManyBarriers {
-  uint64_t q_full[2], s_full[2], p_full[2][2], pv_done[2], full[8], empty[8], edge, drained;
+  uint64_t q_full[2], q_free[2], s_full[2][2], p_full[2][2], pv_done[2][2], full[8], empty[8], turn[2], edge, drained[3];
 };
 
 // Row `row`, 16-byte chunk `chunk` of a 16-bit operand tile of 128 rows: boxes of [128 rows x 64 elements], 128-byte swizzle.
@@ -56,6 +64,11 @@ __device__ __forceinline__ uint32_t many_at(uint32_t tile, int row, int chunk) {
 }
 __device__ __forceinline__ void many_sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
 }
 
 // Tiles of a unit: none if its source has no rows, or if none of its tokens is there.
@@ -91,18 +104,21 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&B.q_full[i], 128);
-      mbar_init(&B.s_full[i], 1);
-      mbar_init(&B.p_full[i][0], 128);
-      mbar_init(&B.p_full[i][1], 128);
-      mbar_init(&B.pv_done[i], 1);
+      mbar_init(&B.q_full[i], 4);                       // an arrival per warp: those of 128 threads take hundreds of cycles
+      mbar_init(&B.q_free[i], 4);
+      mbar_init(&B.turn[i], 4);
+      for (int half = 0; half < 2; ++half) {
+        mbar_init(&B.s_full[i][half], 1);
+        mbar_init(&B.p_full[i][half], 4);
+        mbar_init(&B.pv_done[i][half], 1);
+      }
     }
     for (int i = 0; i < kSlots; ++i) {
       mbar_init(&B.full[i], 1);
-      mbar_init(&B.empty[i], 1);
+      mbar_init(&B.empty[i], 2);                        // the products of both tiles
     }
     mbar_init(&B.edge, 1);
-    mbar_init(&B.drained, 1);
+    for (int i = 0; i < 3; ++i) mbar_init(&B.drained[i], 1);
     fence_mbar_init();
   }
   if (warp == kMaSoftmax + 1) {
@@ -115,7 +131,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
   grid_dependency_wait();
   grid_dependency_launch();
-  auto tiles_of = [&](int unit) { return max(1, many_tiles(c, a.row_tiles, unit)); };   // a unit without rows has its outputs written, too
+  auto tiles_of = [&](int unit) { return kMaAhead + max(1, many_tiles(c, a.row_tiles, unit)); };   // a unit without rows has its outputs written, too
   {
     // The CTA's run of tiles: every thread counts those of some units; the threads in whose units the run begins and ends say where.
     const int units = c.sources * c.Hkv * a.row_tiles, per = (units + kMaThreads - 1) / kMaThreads;
@@ -161,51 +177,122 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         piece_s.run.tiles = t;
       }
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      const Run run = piece_s.run;
-      if (run.tile < run.end) piece_s.cut(1, tiles_of);
-      a.begins[blockIdx.x] = run.tile < run.end ? make_int2(piece_s.unit, piece_s.t0) : make_int2(-1, 0);
-    }
   }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   constexpr uint32_t kO = 256;                          // O of tile w: columns kO + w * kD; S and P: w * 128
-  const volatile Piece& piece = piece_s;
 
   struct Unit {
     int b, h, rho0, n, t0, tiles, done, nth;            // done: tiles of the pieces before, phases of the barriers; nth: pieces before
+    bool whole;                                         // no other CTA has tiles of the unit
   };
-  // A role's part of every piece.  All roles go from piece to piece together.
+  // A role's part of every piece, as long as its waits do not run out.  Every role goes through the pieces by itself: what one needs of another
+  // it waits for at a barrier, so that K, V and the first logits of a piece are under way while the results of the one before are written.
+  const Run run = piece_s.run;
   auto each_piece = [&](auto&& part) {
-    int done = 0;
-    for (int nth = 0; piece.run.tile < piece.run.end; ++nth) {
-      const int unit = piece.unit, bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kMaRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
-      const int t0 = piece.t0, tiles = min(piece.t1, many_tiles(c, a.row_tiles, unit)) - t0;
-      part(Unit{b, h, rho0, cross_length(c, b, h), t0, tiles, done, nth});
-      __syncwarp();
-      // all go on to the next piece, or none
-      const bool stop = __syncthreads_or(abort_flag) != 0;
-      tc_fence_after();
-      done += tiles;
-      if (threadIdx.x == 0) {
-        piece_s.run.tile += piece_s.t1 - piece_s.t0;
-        if (stop) piece_s.run.tile = piece_s.run.end;
-        if (piece_s.run.tile < piece_s.run.end) piece_s.cut(1, tiles_of);
-      }
-      __syncthreads();
+    int done = 0, nth = 0, unit = run.entry, counted = run.tiles, from = run.tile - run.first, left = run.end - run.tile;
+    if (left > 0 && from >= counted) {                  // (the run begins with the unit after)
+      from = 0;
+      counted = tiles_of(++unit);
     }
+    if (threadIdx.x == 0) a.begins[blockIdx.x] = left > 0 && from + left > kMaAhead ? make_int2(unit, max(0, from - kMaAhead)) : make_int2(-1, 0);
+    while (left > 0) {
+      const int to = min(from + left, counted), bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
+      const int t0 = max(0, from - kMaAhead), t1 = to - kMaAhead;
+      if (t1 > 0) {                                     // (a run that ends ahead of a unit's tiles leaves it to the next CTA)
+        const Unit u{b, h, (unit - bh * a.row_tiles) * kMaRows, cross_length(c, b, h), t0, min(t1, many_tiles(c, a.row_tiles, unit)) - t0, done, nth, t0 == 0 && to == counted};
+        if (!part(u)) break;
+        done += u.tiles;
+        ++nth;
+      }
+      left -= to - from;
+      from = 0;
+      if (left > 0) counted = tiles_of(++unit);
+    }
+  };
+
+  // descriptors count 16-byte units
+  auto there = [&](int x) { return wait(&B.full[x % kSlots], x / kSlots); };
+  // ---------------- the logits S = Q K^T, by one thread ----------------
+  auto logits = [&]() {
+    constexpr uint32_t idesc = make_idesc_bf16(128, 64, false);
+    const uint64_t q0 = kmajor_desc(q_at), k0 = kmajor_desc(ring_at);
+    auto qk = [&](int s, int w, int half) {
+      const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4) + half * (8192 >> 4));
+#pragma unroll
+      for (int k = 0; k < kD / 16; ++k) {
+        const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
+        umma_ss(tmem + (uint32_t)(w * 128 + half * 64), a0 + step, b0 + step, idesc, k > 0);
+      }
+      umma_commit(&B.s_full[w][half]);
+    };
+    each_piece([&](const Unit& u) {
+      bool ok = true;
+      for (int j = 0; j <= u.tiles && ok; ++j) {
+        const int at = u.done + j, s = 2 * at % kSlots;
+        // (no phase of a barrier may be passed over: a piece without tiles has its queries waited for, too)
+        if (j == u.tiles && j > 0) break;
+        ok = u.tiles <= 0 || there(2 * at);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int w = x & 1, half = x >> 1;
+          if (j == 0) {
+            if (half == 0) ok = ok && wait(&B.q_full[w], u.nth);
+          } else {                                      // in the place of the logits are the weights that the product before reads
+            ok = ok && wait(&B.pv_done[w][half], at - 1);
+          }
+          if (!ok) break;
+          if (u.tiles <= 0) continue;
+          tc_fence_after();
+          qk(s, w, half);
+        }
+        if (!ok || u.tiles <= 0) break;
+        umma_commit(&B.empty[s]);
+        umma_commit(&B.empty[s]);                       // (V's tiles have two readers)
+      }
+      return ok;
+    });
+    umma_commit(&B.drained[0]);                         // nothing may still write tensor memory, or arrive, when the CTA goes
+    wait_issued(&B.drained[0], 0u);
+  };
+  // ---------------- O += P V of one tile of query rows, by one thread ----------------
+  auto outputs = [&](auto tile) {
+    constexpr int w = decltype(tile)::value;
+    constexpr uint32_t idesc = make_idesc_bf16(128, kD, true);
+    const uint64_t v0 = make_smem_desc(ring_at, 16384u, 1024u);
+    each_piece([&](const Unit& u) {
+      bool ok = true;
+      for (int j = 0; j < u.tiles && ok; ++j) {
+        const int at = u.done + j, s = (2 * at + 1) % kSlots;
+        const int left = u.n - (u.t0 + j) * kMaTile, steps = left >= kMaTile ? 8 : (left + 15) / 16;   // of 16 rows that are there
+        const uint64_t b0 = v0 + (uint64_t)(s * (C::kTileBytesD >> 4));
+        ok = there(2 * at + 1);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          ok = ok && wait(&B.p_full[w][half], at);
+          if (!ok) break;
+          tc_fence_after();
+#pragma unroll
+          for (int k = 4 * half; k < 4 * half + 4; ++k)   // 16 rows: 8 columns of P, 2048 bytes of V
+            if (k < steps)
+              umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)(w * 128 + half * 64 + (k & 3) * 8), b0 + (uint64_t)(k * 128), idesc, j > 0 || k > 0);
+          umma_commit(&B.pv_done[w][half]);
+        }
+        if (ok) umma_commit(&B.empty[s]);
+      }
+      return ok;
+    });
+    umma_commit(&B.drained[1 + w]);
+    wait_issued(&B.drained[1 + w], 0u);
   };
 
   // Each side's code sits behind its own register-budget change.
   if (warp >= kMaSoftmax) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMaOtherRegs));
-    if (warp >= kMaSoftmax + 2) {
-      each_piece([](const Unit&) {});
-    } else if (warp == kMaSoftmax) {
-      int edges = 0;
+    if (warp == kMaSoftmax) {
+      int edges = 0, asked = 0;                         // tiles asked for
       each_piece([&](const Unit& u) {
         // ---------------- loading K and V, in turn ----------------
         bool ok = true;
@@ -234,70 +321,17 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             if (lane == 0) mbar_arrive(&B.full[s]);
           }
         }
-        if (!ok) {                                        // nothing may still be on its way into shared memory when the CTA returns
-          for (int y = x > kSlots ? x - kSlots : 0; y < x; ++y) wait_issued(&B.full[y % kSlots], (uint32_t)(y / kSlots));
-        }
+        asked = x;
+        return ok;
       });
+      // nothing may still be on its way into shared memory when the CTA returns
+      for (int y = asked > kSlots ? asked - kSlots : 0; y < asked; ++y) wait_issued(&B.full[y % kSlots], (uint32_t)(y / kSlots));
+    } else if (warp == kMaSoftmax + 1) {
+      if (elect_one()) logits();
+    } else if (warp == kMaSoftmax + 2) {
+      if (elect_one()) outputs(std::integral_constant<int, 0>{});
     } else {
-      uint32_t drains = 0;
-      each_piece([&](const Unit& u) {
-        // ---------------- the products, by one thread ----------------
-        const int tiles = u.tiles, done = u.done;
-        if (tiles > 0 && elect_one()) {
-          constexpr uint32_t idesc_s = make_idesc_bf16(128, 128, false), idesc_o = make_idesc_bf16(128, kD, true);
-          // descriptors count 16-byte units
-          const uint64_t q0 = kmajor_desc(q_at), k0 = kmajor_desc(ring_at), v0 = make_smem_desc(ring_at, 16384u, 1024u);
-          auto qk = [&](int w, int s) {
-            const uint64_t a0 = q0 + (uint64_t)(w * (C::kTileBytesD >> 4)), b0 = k0 + (uint64_t)(s * (C::kTileBytesD >> 4));
-#pragma unroll
-            for (int k = 0; k < kD / 16; ++k) {
-              const uint64_t step = (uint64_t)(((uint32_t)(k >> 2) * 16384u + (uint32_t)(k & 3) * 32u) >> 4);
-              umma_ss(tmem + (uint32_t)w * 128u, a0 + step, b0 + step, idesc_s, k > 0);
-            }
-            umma_commit(&B.s_full[w]);
-          };
-          auto slot = [&](int x) { return x % kSlots; };
-          auto there = [&](int x) { return wait(&B.full[x % kSlots], x / kSlots); };
-          bool ok = there(2 * done);
-          for (int w = 0; w < 2 && ok; ++w) {
-            ok = wait(&B.q_full[w], u.nth);
-            if (!ok) break;
-            tc_fence_after();
-            qk(w, slot(2 * done));
-          }
-          if (ok) umma_commit(&B.empty[slot(2 * done)]);
-          for (int j = 0; j < tiles && ok; ++j) {
-            const int at = done + j, xv = 2 * at + 1, xk = 2 * at + 2;
-            const int left = u.n - (u.t0 + j) * kMaTile, steps = left >= kMaTile ? 8 : (left + 15) / 16;   // of 16 rows that are there
-            ok = there(xv);
-            for (int w = 0; w < 2 && ok; ++w) {
-              const uint64_t b0 = v0 + (uint64_t)(slot(xv) * (C::kTileBytesD >> 4));
-#pragma unroll
-              for (int half = 0; half < 2; ++half) {
-                ok = ok && wait(&B.p_full[w][half], at);
-                if (!ok) break;
-                tc_fence_after();
-#pragma unroll
-                for (int k = 4 * half; k < 4 * half + 4; ++k)   // 16 rows: 8 columns of P, 2048 bytes of V
-                  if (k < steps) umma_ts(tmem + kO + (uint32_t)w * kD, tmem + (uint32_t)(w * 128 + k * 8), b0 + (uint64_t)(k * 128), idesc_o, j > 0 || k > 0);
-              }
-              if (!ok) break;
-              umma_commit(&B.pv_done[w]);
-              if (w == 1) umma_commit(&B.empty[slot(xv)]);
-              if (j + 1 < tiles) {                        // the next logits, in whose place are the weights that the product before reads
-                ok = (w > 0 || there(xk)) && wait(&B.pv_done[w], at);
-                if (!ok) break;
-                tc_fence_after();
-                qk(w, slot(xk));
-                if (w == 1) umma_commit(&B.empty[slot(xk)]);
-              }
-            }
-          }
-          // Nothing may still write tensor memory, or arrive, when the CTA goes, which it does at the end of a piece in which any role's wait ran out.
-          umma_commit(&B.drained);
-          wait_issued(&B.drained, drains++);
-        }
-      });
+      if (elect_one()) outputs(std::integral_constant<int, 1>{});
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMaSoftmaxRegs));
@@ -309,54 +343,58 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const uint32_t s_tm = tmem + row_lane + (uint32_t)w * 128u, o_tm = tmem + row_lane + kO + (uint32_t)w * kD;
       const CrossRow mine = cross_row(c, u.b, rho < R ? rho : 0);
       const bool live = rho < R && cross_live(c, mine);
+      // the rows' place in shared memory, by way of which the other warps may still be writing their results of the piece before
+      if (u.nth > 0 && !__all_sync(0xffffffffu, wait(&B.q_free[w], u.nth - 1))) return false;
       if (tiles > 0) {
-        // the warp's rows into shared memory, a row in kD / 8 lanes side by side, four rows per lane together
-        constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes;
+        // the warp's rows into shared memory, a row in kD / 8 lanes side by side, all of a lane's on their way together
+        constexpr int kLanes = kD / 8, kAtOnce = 32 / kLanes, kAhead = 16;
         const uint32_t tile = q_at + (uint32_t)w * C::kTileBytesD;
-        const int x = lane % kLanes, row0 = (warp & 3) * 32 + lane / kLanes;
+        const int x = lane % kLanes;
+        const long long own = live ? reinterpret_cast<const uint4*>(cross_query<__nv_bfloat16>(c, mine, u.h)) - reinterpret_cast<const uint4*>(c.Q.data) : -1;
 #pragma unroll 1
-        for (int z0 = 0; z0 < 32; z0 += 4 * kAtOnce) {
-          uint4 raw[4];
+        for (int z0 = 0; z0 < 32; z0 += kAhead * kAtOnce) {
+          uint4 raw[kAhead];
 #pragma unroll
-          for (int y = 0; y < 4; ++y) {
-            const int rho_z = u.rho0 + w * 128 + row0 + z0 + y * kAtOnce;
-            raw[y] = make_uint4(0u, 0u, 0u, 0u);
-            if (rho_z < R) {
-              const CrossRow q = cross_row(c, u.b, rho_z);
-              if (cross_live(c, q)) raw[y] = reinterpret_cast<const uint4*>(cross_query<__nv_bfloat16>(c, q, u.h))[x];
-            }
+          for (int y = 0; y < kAhead; ++y) {
+            if (z0 + y * kAtOnce >= 32) break;
+            const long long from = __shfl_sync(0xffffffffu, own, z0 + y * kAtOnce + lane / kLanes);
+            raw[y] = from >= 0 ? reinterpret_cast<const uint4*>(c.Q.data)[from + x] : make_uint4(0u, 0u, 0u, 0u);
           }
 #pragma unroll
-          for (int y = 0; y < 4; ++y) many_sts128(many_at(tile, row0 + z0 + y * kAtOnce, x), raw[y].x, raw[y].y, raw[y].z, raw[y].w);
+          for (int y = 0; y < kAhead; ++y) {
+            if (z0 + y * kAtOnce >= 32) break;
+            many_sts128(many_at(tile, (warp & 3) * 32 + z0 + y * kAtOnce + lane / kLanes, x), raw[y].x, raw[y].y, raw[y].z, raw[y].w);
+          }
         }
         fence_proxy_async_smem();
       }
-      mbar_arrive(&B.q_full[w]);                        // (once per piece, whether it has tiles or not)
+      warp_arrive(&B.q_full[w]);                        // (once per piece, whether it has tiles or not)
       const float f = c.scale * kLog2e;
       float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
       bool ok = true;
-      for (int j = 0; j < tiles; ++j) {
-        const int at = done + j, left = u.n - (u.t0 + j) * kMaTile;
+      for (int j2 = 0; j2 < 2 * tiles; ++j2) {
+        const int j = j2 >> 1, half = j2 & 1, at = done + j, left = u.n - (u.t0 + j) * kMaTile - 64 * half;
         // the waits' verdict is a warp's: tensor memory is read by whole warps
-        ok = __all_sync(0xffffffffu, wait(&B.s_full[w], at));
+        ok = __all_sync(0xffffffffu, wait(&B.s_full[w][half], at));
         if (!ok) break;
         tc_fence_after();
-        float v[kMaTile];
-#pragma unroll
-        for (int x = 0; x < kMaTile; x += 32) tmem_ld32(s_tm + x, v + x);
+        const uint32_t s_half = s_tm + (uint32_t)half * 64u;
+        float v[64];
+        tmem_ld32(s_half, v);
+        tmem_ld32(s_half + 32u, v + 32);
         tmem_wait_ld();
-        if (left < kMaTile) {
+        if (left < 64) {
 #pragma unroll
-          for (int x = 0; x < kMaTile; ++x)
+          for (int x = 0; x < 64; ++x)
             if (x >= left) v[x] = -INFINITY;
         }
         float m[4] = {v[0], v[1], v[2], v[3]};
 #pragma unroll
-        for (int x = 4; x + 8 <= kMaTile; x += 8)
+        for (int x = 4; x + 8 <= 64; x += 8)
 #pragma unroll
           for (int z = 0; z < 4; ++z) m[z] = fmax3(m[z], v[x + 2 * z], v[x + 2 * z + 1]);
-        m[0] = fmax3(m[0], v[kMaTile - 4], v[kMaTile - 3]);
-        m[1] = fmax3(m[1], v[kMaTile - 2], v[kMaTile - 1]);
+        m[0] = fmax3(m[0], v[60], v[61]);
+        m[1] = fmax3(m[1], v[62], v[63]);
         const float mx = fmaxf(fmax3(m[0], m[1], m[2]), m[3]) * f;      // (the factor is positive)
         if (__any_sync(0xffffffffu, mx > ref + kMaSlack)) {
           float down = 1.f;
@@ -365,8 +403,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             ref = mx;
           }
           l *= down;
-          if (j > 0) {                                  // the products of the tile before may still be adding to O
-            ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], at - 1));
+          if (j2 > 0) {                                 // the products of the half before may still be adding to O
+            ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][half ^ 1], half ? at : at - 1));
             if (!ok) break;
             tc_fence_after();
 #pragma unroll 1
@@ -381,37 +419,38 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             }
           }
         }
+        // The tiles' warpgroups take turns at the exponentials: while one is at them, the other loads and looks for the maximum.
+        if (w == 1 || 2 * at + half > 0) ok = __all_sync(0xffffffffu, wait(&B.turn[w], 2 * at + half - (w == 0)));
+        if (!ok) break;
         const float m_use = ref == -INFINITY ? 0.f : ref;               // only logits of -inf so far: they weigh nothing
         const f32x2 ff = f2_make(f, f), minus_m = f2_make(-m_use, -m_use);
         f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
+        for (int x = 0; x < 64; x += 32) {
+          uint32_t p[16];
 #pragma unroll
-          for (int x = 64 * half; x < 64 * half + 64; x += 32) {
-            uint32_t p[16];
-#pragma unroll
-            for (int y = 0; y < 32; y += 4) {
-              const f32x2 a0 = f2_fma(f2_make(v[x + y], v[x + y + 1]), ff, minus_m), a1 = f2_fma(f2_make(v[x + y + 2], v[x + y + 3]), ff, minus_m);
-              const float e0 = ex2_approx(f2_lo(a0)), e1 = ex2_approx(f2_hi(a0)), e2 = ex2_approx(f2_lo(a1)), e3 = ex2_approx(f2_hi(a1));
-              sum0 = f2_add(sum0, f2_make(e0, e1));
-              sum1 = f2_add(sum1, f2_make(e2, e3));
-              p[y / 2] = pack_bf16x2(e0, e1);
-              p[y / 2 + 1] = pack_bf16x2(e2, e3);
-            }
-            tmem_st16(s_tm + x / 2, p);                 // P where S has been read already
+          for (int y = 0; y < 32; y += 4) {
+            const f32x2 a0 = f2_fma(f2_make(v[x + y], v[x + y + 1]), ff, minus_m), a1 = f2_fma(f2_make(v[x + y + 2], v[x + y + 3]), ff, minus_m);
+            const float e0 = ex2_approx(f2_lo(a0)), e1 = ex2_approx(f2_hi(a0)), e2 = ex2_approx(f2_lo(a1)), e3 = ex2_approx(f2_hi(a1));
+            sum0 = f2_add(sum0, f2_make(e0, e1));
+            sum1 = f2_add(sum1, f2_make(e2, e3));
+            p[y / 2] = pack_bf16x2(e0, e1);
+            p[y / 2 + 1] = pack_bf16x2(e2, e3);
           }
-          tmem_wait_st();
-          tc_fence_before();
-          mbar_arrive(&B.p_full[w][half]);
+          tmem_st16(s_half + x / 2, p);                 // P where S has been read already
+          if (x == 0) warp_arrive(&B.turn[1 - w]);
         }
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&B.p_full[w][half]);
         sum0 = f2_add(sum0, sum1);
         l += f2_lo(sum0) + f2_hi(sum0);
       }
       // ---- the row's result ----
-      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w], done + tiles - 1));
+      if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][1], done + tiles - 1));
       if (ok) {
         tc_fence_after();
-        const bool whole = piece.whole != 0, some = l > 0.f && live;
+        const bool whole = u.whole, some = l > 0.f && live;
         const float norm = whole ? (some ? 1.f / l : 0.f) : 1.f;
         const bool nothing = tiles <= 0 || (whole && !some);
         float* const part = a.part + (long long)(2 * blockIdx.x + (u.t0 == 0)) * kMaRows * (kD + 2);
@@ -447,7 +486,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
           __syncwarp();
           const int k = lane % kChunks, in_tile = w * 128 + (warp & 3) * 32;
-#pragma unroll 4
+#pragma unroll 8
           for (int z = 0; z < 32; z += 32 / kChunks) {
             const int at = z + lane / kChunks;
             const long long to = __shfl_sync(0xffffffffu, row, at);
@@ -467,6 +506,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         tc_fence_before();
       }
+      warp_arrive(&B.q_free[w]);
+      return ok;
     });
   }
   __syncthreads();
@@ -564,7 +605,7 @@ bool cross_many_shape(const CrossProblem& c) { return (c.d == 64 || c.d == 128) 
 bool cross_many_supported(const CrossProblem& c) {
   if (!cross_many_shape(c) || !cross_map_fits(c, c.K) || !cross_map_fits(c, c.V)) return false;
   const long long units = (long long)c.sources * c.Hkv * ((c.rows() + kMaRows - 1) / kMaRows);
-  return ((long long)c.n_rows / kMaTile + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
+  return ((long long)c.n_rows / kMaTile + 1 + kMaAhead) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }
 
 size_t cross_many_bytes(const CrossProblem& c, int sm_count) {
