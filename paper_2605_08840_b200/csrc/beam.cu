@@ -1,13 +1,14 @@
 // The best continuations of a request's hypotheses: scores[k] + logits[k,v] - log sum exp(logits[k,:]), over hypotheses and tokens.
 //
-// One pass over the logits.  A block has a slice of a row in registers: its maximum and sum of exponentials, and its n_out largest logits.  A
-// second kernel joins a request's slices: normalisers, scores in 64 bits, the n_out best.
-// Largest of a block: groups of four threads name their largest logit; the n_out-th of those bounds the n_out-th of the slice from below, and
-// what reaches it, a few more than n_out as a rule, goes to shared memory and is ranked by counting.  Where it is more than the list holds
-// (a slice of equal logits, say) the largest are taken one by one instead.  The second kernel does the same with scores.
+// One pass over the logits.  A block goes through a slice of a row: its maximum and sum of exponentials, and its n_out largest logits.  A second kernel
+// joins a request's slices: normalisers, scores in 64 bits, the n_out best.
+// Largest of a block: groups of four threads name their largest logit; the n_out-th of those bounds the n_out-th of the slice from below, and what
+// reaches it, a few more than n_out as a rule, is read once more (by the threads whose batch of pieces has some), collected in shared memory and
+// ranked by counting.  Where that is more than the list holds (a slice of equal logits, say) the bound is found anew among logits with their tokens,
+// of which no two are equal, and where that does not do either the largest are taken one by one.  The second kernel does the same with scores.
 // Logits of -inf are no candidates in either; requests that run out of others look for them in the rows at the end.
-// What bounds it: HBM for large calls, beside it the special-function unit (an exponential per logit: 16 per clock and SM, 14 us for the
-// 67 million logits of 512 rows of 131072 whose bytes take 21); for small ones two launches, each a chain of loads and a few barriers.
+// What bounds it: HBM for large calls, beside it the special-function unit (an exponential per logit: 16 per clock and SM, 14 us for the 67 million
+// logits of 512 rows of 131072 whose bytes take 21); for small ones two launches, each a chain of loads and a few barriers.
 #include <math.h>
 
 #include "beam.cuh"
@@ -21,7 +22,7 @@ using namespace ptx;
 
 constexpr int kBeThreads = 256, kBeWarps = kBeThreads / 32;
 constexpr int kGroups = kBeThreads / 4;         // at least kBeamOut
-constexpr int kList = 1024;
+constexpr int kList = 2048, kJoinList = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 static_assert(kGroups >= kBeamOut, "a threshold needs as many groups as continuations");
 
@@ -44,20 +45,20 @@ __device__ __forceinline__ int row_kind(const BeamProblem& p, int row) {
 }
 
 // The n-th largest of the groups' values, of kGroups by their first threads; ends with a barrier.
-__device__ __forceinline__ float nth_of_groups(float mine, int n, float (&group_s)[kGroups], float& limit_s) {
+template <typename K> __device__ __forceinline__ K nth_of_groups(K mine, int n, K (&group_s)[kGroups], K& limit_s) {
   const int t = threadIdx.x;
-  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 1));
-  mine = fmaxf(mine, __shfl_xor_sync(0xffffffffu, mine, 2));
+#pragma unroll
+  for (int x = 1; x <= 2; x <<= 1) {
+    const K o = __shfl_xor_sync(0xffffffffu, mine, x);
+    mine = o > mine ? o : mine;
+  }
   if ((t & 3) == 0) group_s[t >> 2] = mine;
   __syncthreads();
   if (t < kGroups) {
-    const float x = group_s[t];
+    const K x = group_s[t];
     int before = 0;
-#pragma unroll
-    for (int i = 0; i < kGroups; i += 4) {
-      const float4 y = *reinterpret_cast<const float4*>(&group_s[i]);
-      before += (y.x > x || (y.x == x && i < t)) + (y.y > x || (y.y == x && i + 1 < t)) + (y.z > x || (y.z == x && i + 2 < t)) + (y.w > x || (y.w == x && i + 3 < t));
-    }
+#pragma unroll 16
+    for (int i = 0; i < kGroups; ++i) before += group_s[i] > x || (group_s[i] == x && i < t);
     if (before == n - 1) limit_s = x;
   }
   __syncthreads();
@@ -103,16 +104,18 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, unsigned int off) {
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-struct SliceStats { float top, sum; };   // of a slice: its maximum and the sum of exp(x - top); no finite logit: -inf, 0
+struct __align__(8) SliceStats { float top, sum; };   // of a slice: its maximum and the sum of exp(x - top); no finite logit: -inf, 0
 
-// grid: rows x slices, slices running fastest.  A slice is kVec * kBeThreads pieces of 16 bytes of a row.
-template <typename T, int kVec>
-__global__ void __launch_bounds__(kBeThreads) beam_slice_kernel(const BeamProblem p, int slices, SliceStats* __restrict__ stats, u64* __restrict__ lists) {
+// grid: rows x slices, slices running fastest.  A slice is kBatches batches of kBatch * kBeThreads pieces of 16 bytes of a row.
+template <typename T, int kBatch, int kBatches>
+__global__ void __launch_bounds__(kBeThreads, 5) beam_slice_kernel(const BeamProblem p, int slices, SliceStats* __restrict__ stats, u64* __restrict__ lists) {
   using V = Vec<T>;
-  constexpr int kPer = V::kPer;
+  constexpr int kPer = V::kPer, kMine = kBatch * kPer;      // logits of a thread in a batch
   __shared__ __align__(16) float group_s[kGroups];
+  __shared__ u64 group_key_s[kGroups], limit_key_s;
   __shared__ float limit_s, top_s[kBeWarps], sum_s[kBeWarps];
-  __shared__ int count_s;
+  __shared__ int count_s, hits_s;
+  __shared__ unsigned short hit_s[kBatches * kBeThreads];
   __shared__ u64 list_s[kList], best_s[kBeWarps];
   const int row = blockIdx.x / slices, slice = blockIdx.x - row * slices, t = threadIdx.x, lane = t & 31, warp = t >> 5;
   grid_dependency_wait();
@@ -122,55 +125,73 @@ __global__ void __launch_bounds__(kBeThreads) beam_slice_kernel(const BeamProble
   // A thread's tokens do not depend on where in its 16-byte pieces the row begins: equal rows have equal sums, bit for bit.
   const unsigned int off = (unsigned int)(reinterpret_cast<uintptr_t>(from) & 15u);   // bytes of the row before in the row's first piece
   const uint4* const pieces = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
-  const int piece0 = slice * (kVec * kBeThreads) + t, in_row = (int)(((long long)p.vocab * (int)sizeof(T) + off + 15) / 16);
-  auto token_of = [&](int y, int i) { return (piece0 + y * kBeThreads) * kPer + i; };
-  V v[kVec];
+  const int piece0 = slice * (kBatches * kBatch * kBeThreads) + t, in_row = (int)(((long long)p.vocab * (int)sizeof(T) + off + 15) / 16);
+  auto piece_of = [&](int b, int y) { return piece0 + (b * kBatch + y) * kBeThreads; };
+  auto token_of = [&](int b, int e) { return piece_of(b, e / kPer) * kPer + e % kPer; };     // of the thread's e-th logit of batch b
+  if (t == 0) count_s = hits_s = 0;
+  float top = -INFINITY, sum = 0.f, most[kBatches];         // of the thread, and of its batches
 #pragma unroll
-  for (int y = 0; y < kVec; ++y) v[y].u = piece0 + y * kBeThreads < in_row ? __ldcs(pieces + piece0 + y * kBeThreads) : make_uint4(0u, 0u, 0u, 0u);
-  if (off) {
+  for (int b = 0; b < kBatches; ++b) {
+    V v[kBatch];
 #pragma unroll
-    for (int y = 0; y < kVec; ++y) {
-      uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, v[y].u.x, 1), __shfl_down_sync(0xffffffffu, v[y].u.y, 1), __shfl_down_sync(0xffffffffu, v[y].u.z, 1),
-                              __shfl_down_sync(0xffffffffu, v[y].u.w, 1));
-      if (lane == 31) next = piece0 + y * kBeThreads + 1 < in_row ? __ldcs(pieces + piece0 + y * kBeThreads + 1) : make_uint4(0u, 0u, 0u, 0u);
-      v[y].u = shifted(v[y].u, next, off);
+    for (int y = 0; y < kBatch; ++y) v[y].u = piece_of(b, y) < in_row ? __ldcs(pieces + piece_of(b, y)) : make_uint4(0u, 0u, 0u, 0u);
+    if (off) {
+#pragma unroll
+      for (int y = 0; y < kBatch; ++y) {
+        uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, v[y].u.x, 1), __shfl_down_sync(0xffffffffu, v[y].u.y, 1), __shfl_down_sync(0xffffffffu, v[y].u.z, 1),
+                                __shfl_down_sync(0xffffffffu, v[y].u.w, 1));
+        if (lane == 31) next = piece_of(b, y) + 1 < in_row ? __ldg(pieces + piece_of(b, y) + 1) : make_uint4(0u, 0u, 0u, 0u);
+        v[y].u = shifted(v[y].u, next, off);
+      }
     }
-  }
 #pragma unroll
-  for (int y = 0; y < kVec; ++y) {
-    if (token_of(y, kPer) <= p.vocab) continue;
+    for (int y = 0; y < kBatch; ++y) {
+      if (token_of(b, y * kPer + kPer - 1) < p.vocab) continue;
 #pragma unroll
-    for (int i = 0; i < kPer; ++i)
-      if (token_of(y, i) >= p.vocab) v[y].set(i, -INFINITY);
-  }
-  if (t == 0) count_s = 0;
-  float top = -INFINITY;                                                // (a NaN is passed over)
+      for (int i = 0; i < kPer; ++i)
+        if (token_of(b, y * kPer + i) >= p.vocab) v[y].set(i, -INFINITY);
+    }
+    float m0 = -INFINITY, m1 = -INFINITY;                   // (a NaN is passed over)
 #pragma unroll
-  for (int y = 0; y < kVec; ++y)
-#pragma unroll
-    for (int i = 0; i < kPer; i += 2) top = fmax3(top, v[y].at(i), v[y].at(i + 1));
-  auto sum_by = [&](float of, auto&& value) {
+    for (int e = 0; e < kMine; e += 4) {
+      m0 = fmax3(m0, v[e / kPer].at(e % kPer), v[e / kPer].at(e % kPer + 1));
+      m1 = fmax3(m1, v[e / kPer].at(e % kPer + 2), v[e / kPer].at(e % kPer + 3));
+    }
+    most[b] = fmaxf(m0, m1);
+    const float next = fmaxf(top, most[b]), of = next == -INFINITY ? 0.f : next;
+    sum *= ex2_approx((top - of) * kLog2e);
+    top = next;
     f32x2 s0 = f2_make(0.f, 0.f), s1 = s0;
     const f32x2 minus = f2_make(-of, -of), scale = f2_make(kLog2e, kLog2e);
 #pragma unroll
-    for (int y = 0; y < kVec; ++y)
-#pragma unroll
-      for (int i = 0; i < kPer; i += 4) {
-        // the difference first: large terms have small ones, whose rounding is small
-        const f32x2 a = f2_mul(f2_add(f2_make(value(v[y].at(i)), value(v[y].at(i + 1))), minus), scale);
-        const f32x2 b = f2_mul(f2_add(f2_make(value(v[y].at(i + 2)), value(v[y].at(i + 3))), minus), scale);
-        s0 = f2_add(s0, f2_make(ex2_approx(f2_lo(a)), ex2_approx(f2_hi(a))));
-        s1 = f2_add(s1, f2_make(ex2_approx(f2_lo(b)), ex2_approx(f2_hi(b))));
-      }
+    for (int e = 0; e < kMine; e += 4) {
+      const V& w = v[e / kPer];
+      const int i = e % kPer;
+      // the difference first: large terms have small ones, whose rounding is small
+      const f32x2 x = f2_mul(f2_add(f2_make(w.at(i), w.at(i + 1)), minus), scale), y = f2_mul(f2_add(f2_make(w.at(i + 2), w.at(i + 3)), minus), scale);
+      s0 = f2_add(s0, f2_make(ex2_approx(f2_lo(x)), ex2_approx(f2_hi(x))));
+      s1 = f2_add(s1, f2_make(ex2_approx(f2_lo(y)), ex2_approx(f2_hi(y))));
+    }
     s0 = f2_add(s0, s1);
-    return f2_lo(s0) + f2_hi(s0);
+    sum += f2_lo(s0) + f2_hi(s0);
+  }
+  // the thread's e-th logit of batch b once more, as it counts
+  auto again = [&](int b, int e) {
+    const int token = token_of(b, e);
+    return token < p.vocab ? usable(to_f32<T>(from[token])) : -INFINITY;
   };
-  float sum = sum_by(top == -INFINITY ? 0.f : top, [](float x) { return x; });
-  // A NaN or +inf among the logits shows in the sum, and all is made again of what counts in their place.
-  const bool odd = !(sum < INFINITY);
-  if (odd) {
-    top = usable(top);
-    sum = sum_by(top == -INFINITY ? 0.f : top, [](float x) { return usable(x); });
+  if (!(sum < INFINITY)) {   // a NaN or +inf among the logits shows in the sum: all anew of what counts in their place
+    top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < kBatches; ++b) {
+      most[b] = -INFINITY;
+#pragma unroll 1
+      for (int e = 0; e < kMine; ++e) most[b] = fmaxf(most[b], again(b, e));
+      top = fmaxf(top, most[b]);
+    }
+    sum = 0.f;
+#pragma unroll 1
+    for (int e = 0; e < kBatches * kMine; ++e) sum += top == -INFINITY ? 0.f : ex2_approx((again(e / kMine, e % kMine) - top) * kLog2e);
   }
   const float limit = nth_of_groups(top, p.n_out, group_s, limit_s);
   // ---- the slice's statistics ----
@@ -183,22 +204,48 @@ __global__ void __launch_bounds__(kBeThreads) beam_slice_kernel(const BeamProble
     for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
     if (lane == 0) { top_s[warp] = m; sum_s[warp] = s; }
   }
-  // ---- what reaches the limit ----
+  // ---- what reaches the limit: the batches that have some are read once more, by all threads side by side ----
   if (top >= limit && top > -INFINITY) {
 #pragma unroll
-    for (int y = 0; y < kVec; ++y)
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) {
-        const float x = v[y].at(i);
-        // (a NaN compares false; +inf is above every limit)
-        if (x >= limit && x > -INFINITY) {
-          const int at = atomicAdd(&count_s, 1);
-          if (at < kList) list_s[at] = make_key(usable(x), token_of(y, i));
-        }
-      }
+    for (int b = 0; b < kBatches; ++b)
+      if (most[b] >= limit) hit_s[atomicAdd(&hits_s, 1)] = (unsigned short)(b * kBeThreads + t);
   }
   __syncthreads();
-  const int count = count_s;
+  for (int x = t, all = hits_s * kMine; x < all; x += kBeThreads) {
+    const int hit = hit_s[x / kMine], e = x % kMine, token = token_of(hit / kBeThreads, e) + (hit % kBeThreads - t) * kPer;
+    const float z = token < p.vocab ? usable(to_f32<T>(from[token])) : -INFINITY;
+    if (z >= limit && z > -INFINITY) {
+      const int at = atomicAdd(&count_s, 1);
+      if (at < kList) list_s[at] = make_key(z, token);
+    }
+  }
+  __syncthreads();
+  int count = count_s;
+  if (count > kList) {
+    // too many of one size: a limit among logits with their tokens
+    u64 best = 0;
+#pragma unroll 1
+    for (int e = 0; e < kBatches * kMine; ++e) {
+      const float x = again(e / kMine, e % kMine);
+      const u64 key = x > -INFINITY ? make_key(x, token_of(e / kMine, e % kMine)) : 0;
+      best = key > best ? key : best;
+    }
+    if (t == 0) count_s = 0;
+    const u64 limit_key = nth_of_groups(best, p.n_out, group_key_s, limit_key_s);
+    if (best >= limit_key && best > 0) {
+#pragma unroll 1
+      for (int e = 0; e < kBatches * kMine; ++e) {
+        const float x = again(e / kMine, e % kMine);
+        const u64 key = x > -INFINITY ? make_key(x, token_of(e / kMine, e % kMine)) : 0;
+        if (key >= limit_key && key > 0) {
+          const int at = atomicAdd(&count_s, 1);
+          if (at < kList) list_s[at] = key;
+        }
+      }
+    }
+    __syncthreads();
+    count = count_s;
+  }
   u64* const list = lists + (long long)blockIdx.x * p.n_out;
   if (count <= kList) {
     for (int x = t; x < count; x += kBeThreads) {
@@ -212,15 +259,12 @@ __global__ void __launch_bounds__(kBeThreads) beam_slice_kernel(const BeamProble
     u64 last = ~0ull;
     for (int k = 0; k < p.n_out; ++k) {
       u64 best = 0;
-#pragma unroll
-      for (int y = 0; y < kVec; ++y)
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-          const float x = v[y].at(i);
-          if (!(x > -INFINITY)) continue;
-          const u64 key = make_key(usable(x), token_of(y, i));
-          if (key < last && key > best) best = key;
-        }
+#pragma unroll 1
+      for (int e = 0; e < kBatches * kMine; ++e) {
+        const float x = again(e / kMine, e % kMine);
+        const u64 key = x > -INFINITY ? make_key(x, token_of(e / kMine, e % kMine)) : 0;
+        if (key < last && key > best) best = key;
+      }
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) {
         const u64 o = __shfl_xor_sync(0xffffffffu, best, x);
@@ -260,23 +304,45 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
   __shared__ float limit_s;
   __shared__ int count_s, kind_s[kBeamsPerRequest];
   __shared__ double score_s[kBeamsPerRequest], total_s[kBeamsPerRequest];   // hypotheses' scores and normalisers
-  __shared__ Candidate list_s[kList / 2], best_s[kBeWarps];
+  __shared__ Candidate list_s[kJoinList], best_s[kBeWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, row0 = (int)blockIdx.x * p.beams, n_out = p.n_out;
   grid_dependency_wait();
   grid_dependency_launch();
   if (t == 0) count_s = 0;
+  // Candidate x of the request: hypotheses one after the other, each with the lists of its slices.  A thread has kHeld of 256 kHeld at a time, the
+  // first on their way before the normalisers are known.
+  constexpr int kHeld = 8;
+  const int per_row = slices * n_out, all = p.beams * per_row;
+  u64 key[kHeld];
+  auto hold = [&](int base) {
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int x = base + i * kBeThreads + t;
+      key[i] = x < all ? __ldcg(lists + (long long)row0 * per_row + x) : 0;
+    }
+  };
+  hold(0);
   for (int k = warp; k < p.beams; k += kBeWarps) {
     const int row = row0 + k, kind = row_kind(p, row);
     double total = 0.0;
+    float m = -INFINITY, tops[2], sums[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const SliceStats* const of = stats + (long long)row * slices + lane + 32 * i;
+      const float2 z = lane + 32 * i < slices ? __ldcg(reinterpret_cast<const float2*>(of)) : make_float2(-INFINITY, 0.f);
+      tops[i] = z.x;
+      sums[i] = z.y;
+    }
     if (kind == 0) {
-      float m = -INFINITY;
-      for (int x = lane; x < slices; x += 32) m = fmaxf(m, __ldcg(&stats[(long long)row * slices + x].top));
+      m = fmaxf(tops[0], tops[1]);
+      for (int x = lane + 64; x < slices; x += 32) m = fmaxf(m, __ldcg(&stats[(long long)row * slices + x].top));
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-      double s = 0.0;
-      for (int x = lane; x < slices; x += 32) {
-        const float top = __ldcg(&stats[(long long)row * slices + x].top), sum = __ldcg(&stats[(long long)row * slices + x].sum);
-        if (top > -INFINITY) s += (double)sum * (double)ex2_approx((top - m) * kLog2e);
+      auto part = [&](float top, float sum) { return top > -INFINITY ? (double)sum * (double)ex2_approx((top - m) * kLog2e) : 0.0; };
+      double s = part(tops[0], sums[0]) + part(tops[1], sums[1]);
+      for (int x = lane + 64; x < slices; x += 32) {
+        const float2 z = __ldcg(reinterpret_cast<const float2*>(&stats[(long long)row * slices + x]));
+        s += part(z.x, z.y);
       }
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
@@ -285,32 +351,37 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
     if (lane == 0) { kind_s[k] = kind; score_s[k] = (double)p.scores[row]; total_s[k] = total; }
   }
   __syncthreads();
-  // candidate x of the request: hypotheses one after the other, each with the lists of its slices
-  const int per_row = slices * n_out, all = p.beams * per_row;
-  auto candidate = [&](int x) {
-    const int k = x / per_row, y = x - k * per_row, kind = kind_s[k];
+  auto candidate = [&](int x, u64 key) {
+    const int k = x / per_row, kind = kind_s[k];
     Candidate c{0.0, 0, k};
     if (kind == 0) {
-      c.key = __ldcg(lists + (long long)(row0 + k) * per_row + y);
-      c.score = score_s[k] + ((double)key_logit(c.key) - total_s[k]);
-    } else if (kind == 1 && y == 0) {
+      c.key = key;
+      c.score = score_s[k] + ((double)key_logit(key) - total_s[k]);
+    } else if (kind == 1 && x == k * per_row) {
       c.key = make_key(0.f, p.pad_token);
       c.score = score_s[k];
     }
     return c;
   };
+  auto each = [&](auto&& use) {                   // over what is held
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int x = i * kBeThreads + t;
+      if (x < all) use(candidate(x, key[i]));
+    }
+    if (all <= kHeld * kBeThreads) return;
+    for (int x = kHeld * kBeThreads + t; x < all; x += kBeThreads) use(candidate(x, __ldcg(lists + (long long)row0 * per_row + x)));
+  };
   float top = -INFINITY;
-  for (int x = t; x < all; x += kBeThreads) {
-    const Candidate c = candidate(x);
+  each([&](const Candidate& c) {
     if (c.key) top = fmaxf(top, (float)c.score);
-  }
+  });
   const float limit = nth_of_groups(top, n_out, group_s, limit_s);
-  for (int x = t; x < all; x += kBeThreads) {
-    const Candidate c = candidate(x);
-    if (!c.key || !((float)c.score >= limit)) continue;
+  each([&](const Candidate& c) {
+    if (!c.key || !((float)c.score >= limit)) return;
     const int at = atomicAdd(&count_s, 1);
-    if (at < kList / 2) list_s[at] = c;
-  }
+    if (at < kJoinList) list_s[at] = c;
+  });
   __syncthreads();
   const int count = count_s;
   auto put = [&](int at, const Candidate& c) {
@@ -319,7 +390,7 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
     p.tokens[to] = key_token(c.key);
     p.scores_out[to] = (float)c.score;
   };
-  if (count <= kList / 2) {
+  if (count <= kJoinList) {
     for (int x = t; x < count; x += kBeThreads) {
       const Candidate mine = list_s[x];
       int before = 0;
@@ -330,10 +401,9 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
     Candidate last{INFINITY, ~0ull, -1};
     for (int k = 0; k < n_out; ++k) {
       Candidate best{0.0, 0, 0};                  // key 0: none
-      for (int x = t; x < all; x += kBeThreads) {
-        const Candidate c = candidate(x);
+      each([&](const Candidate& c) {
         if (c.key && last.before(c) && (!best.key || c.before(best))) best = c;
-      }
+      });
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) {
         const Candidate o{__shfl_xor_sync(0xffffffffu, best.score, x), __shfl_xor_sync(0xffffffffu, best.key, x), __shfl_xor_sync(0xffffffffu, best.beam, x)};
@@ -370,23 +440,23 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
   for (int at = have + lane; at < n_out; at += 32) put(at, Candidate{-INFINITY, make_key(0.f, p.pad_token), 0});
 }
 
-// 16-byte pieces of a row for a thread: many where there are blocks enough, else few, for more blocks.
-int vectors(const BeamProblem& p, int sm_count) {
-  const long long rows = (long long)p.batch * p.beams, pieces = ((long long)p.vocab * (p.f32 ? 4 : 2) + 15) / 16;
-  return rows * ((pieces + 8 * kBeThreads - 1) / (8 * kBeThreads)) < 2 * sm_count ? 2 : 8;
-}
-int slices_of(const BeamProblem& p, int vec) {
+// 16-byte pieces of a slice for a thread: many where there are blocks enough, else few, for more blocks.
+constexpr int kFew = 2, kManyBatch = 4, kManyBatches = 4;
+int slices_of(const BeamProblem& p, int each) {
   const long long pieces = ((long long)p.vocab * (p.f32 ? 4 : 2) + 15) / 16;
-  return (int)((pieces + (long long)vec * kBeThreads - 1) / ((long long)vec * kBeThreads));
+  return (int)((pieces + (long long)each * kBeThreads - 1) / ((long long)each * kBeThreads));
 }
+bool in_few(const BeamProblem& p, int sm_count) { return (long long)p.batch * p.beams * slices_of(p, kManyBatch * kManyBatches) < 4 * sm_count; }
+int slices_of(const BeamProblem& p, bool few) { return slices_of(p, few ? kFew : kManyBatch * kManyBatches); }
 
 template <typename T>
 cudaError_t launch_t(const BeamProblem& p, int sm_count, void* workspace, cudaStream_t st) {
-  const int vec = vectors(p, sm_count), slices = slices_of(p, vec);
+  const bool few = in_few(p, sm_count);
+  const int slices = slices_of(p, few);
   const long long blocks = (long long)p.batch * p.beams * slices;
   u64* const lists = (u64*)workspace;
   SliceStats* const stats = (SliceStats*)(lists + blocks * p.n_out);
-  const auto kernel = vec == 2 ? beam_slice_kernel<T, 2> : beam_slice_kernel<T, 8>;
+  const auto kernel = few ? beam_slice_kernel<T, kFew, 1> : beam_slice_kernel<T, kManyBatch, kManyBatches>;
   const cudaError_t e = launch_chained(kernel, dim3((unsigned int)blocks), kBeThreads, 0, st, p, slices, stats, lists);
   if (e != cudaSuccess) return e;
   return launch_chained(beam_join_kernel<T>, dim3((unsigned int)p.batch), kBeThreads, 0, st, p, slices, stats, lists);
@@ -395,7 +465,7 @@ cudaError_t launch_t(const BeamProblem& p, int sm_count, void* workspace, cudaSt
 }  // namespace
 
 size_t beam_bytes(const BeamProblem& p, int sm_count) {
-  return (size_t)p.batch * p.beams * slices_of(p, vectors(p, sm_count)) * (p.n_out * sizeof(u64) + sizeof(SliceStats));
+  return (size_t)p.batch * p.beams * slices_of(p, in_few(p, sm_count)) * (p.n_out * sizeof(u64) + sizeof(SliceStats));
 }
 
 cudaError_t launch_beam_select(const BeamProblem& p, int sm_count, void* workspace, cudaStream_t st) {
