@@ -44,25 +44,43 @@ __device__ __forceinline__ int row_kind(const BeamProblem& p, int row) {
   return p.finished && p.finished[row] ? 1 : 0;
 }
 
-// The n-th largest of the groups' values, of kGroups by their first threads; ends with a barrier.
+// The n-th largest of the groups' values; ends with a barrier.  A group ranks its own value, a quarter of the others per thread.
 template <typename K> __device__ __forceinline__ K nth_of_groups(K mine, int n, K (&group_s)[kGroups], K& limit_s) {
-  const int t = threadIdx.x;
+  const int t = threadIdx.x, group = t >> 2;
 #pragma unroll
   for (int x = 1; x <= 2; x <<= 1) {
     const K o = __shfl_xor_sync(0xffffffffu, mine, x);
     mine = o > mine ? o : mine;
   }
-  if ((t & 3) == 0) group_s[t >> 2] = mine;
+  if ((t & 3) == 0) group_s[group] = mine;
   __syncthreads();
-  if (t < kGroups) {
-    const K x = group_s[t];
-    int before = 0;
-#pragma unroll 16
-    for (int i = 0; i < kGroups; ++i) before += group_s[i] > x || (group_s[i] == x && i < t);
-    if (before == n - 1) limit_s = x;
+  int before = 0;
+#pragma unroll
+  for (int i = 0; i < kGroups / 4; ++i) {
+    const int g = 4 * i + (t & 3);
+    const K o = group_s[g];
+    before += o > mine || (o == mine && g < group);
   }
+  before += __shfl_xor_sync(0xffffffffu, before, 1);
+  before += __shfl_xor_sync(0xffffffffu, before, 2);
+  if (before == n - 1 && (t & 3) == 0) limit_s = mine;
   __syncthreads();
   return limit_s;
+}
+
+// How many of `count` come before each of them, four threads to one.
+template <class Before, class Use> __device__ __forceinline__ void rank(int count, Before&& comes_before, Use&& use) {
+  for (int x0 = 0; x0 < count; x0 += kBeThreads / 4) {
+    const int x = x0 + ((int)threadIdx.x >> 2);
+    int before = 0;
+    if (x < count) {
+#pragma unroll 4
+      for (int y = threadIdx.x & 3; y < count; y += 4) before += comes_before(x, y);
+    }
+    before += __shfl_xor_sync(0xffffffffu, before, 1);
+    before += __shfl_xor_sync(0xffffffffu, before, 2);
+    if (x < count && (threadIdx.x & 3) == 0) use(x, before);
+  }
 }
 
 template <typename T> struct Vec;      // 16 bytes of logits
@@ -211,12 +229,22 @@ __global__ void __launch_bounds__(kBeThreads, 5) beam_slice_kernel(const BeamPro
       if (most[b] >= limit) hit_s[atomicAdd(&hits_s, 1)] = (unsigned short)(b * kBeThreads + t);
   }
   __syncthreads();
-  for (int x = t, all = hits_s * kMine; x < all; x += kBeThreads) {
-    const int hit = hit_s[x / kMine], e = x % kMine, token = token_of(hit / kBeThreads, e) + (hit % kBeThreads - t) * kPer;
-    const float z = token < p.vocab ? usable(to_f32<T>(from[token])) : -INFINITY;
-    if (z >= limit && z > -INFINITY) {
+  constexpr int kAhead = 4;
+  for (int x0 = t, all = hits_s * kMine; x0 < all; x0 += kAhead * kBeThreads) {
+    float z[kAhead];
+    int token[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int x = x0 + i * kBeThreads, hit = x < all ? hit_s[x / kMine] : 0, e = x % kMine;
+      token[i] = token_of(hit / kBeThreads, e) + (hit % kBeThreads - t) * kPer;
+      z[i] = x < all && token[i] < p.vocab ? to_f32<T>(from[token[i]]) : -INFINITY;
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      z[i] = usable(z[i]);
+      if (!(z[i] >= limit) || z[i] == -INFINITY) continue;
       const int at = atomicAdd(&count_s, 1);
-      if (at < kList) list_s[at] = make_key(z, token);
+      if (at < kList) list_s[at] = make_key(z[i], token[i]);
     }
   }
   __syncthreads();
@@ -248,12 +276,9 @@ __global__ void __launch_bounds__(kBeThreads, 5) beam_slice_kernel(const BeamPro
   }
   u64* const list = lists + (long long)blockIdx.x * p.n_out;
   if (count <= kList) {
-    for (int x = t; x < count; x += kBeThreads) {
-      const u64 mine = list_s[x];
-      int before = 0;
-      for (int y = 0; y < count; ++y) before += list_s[y] > mine;
-      if (before < p.n_out) list[before] = mine;
-    }
+    rank(count, [&](int x, int y) { return list_s[y] > list_s[x]; }, [&](int x, int before) {
+      if (before < p.n_out) list[before] = list_s[x];
+    });
     for (int x = count + t; x < p.n_out; x += kBeThreads) list[x] = 0;
   } else {
     u64 last = ~0ull;
@@ -289,13 +314,18 @@ __global__ void __launch_bounds__(kBeThreads, 5) beam_slice_kernel(const BeamPro
   }
 }
 
-// A continuation by its score, hypothesis and key.
+// A continuation by its score, hypothesis and key.  Scores are compared by their bits in an order of integers.
 struct Candidate {
-  double score;
-  u64 key;
+  u64 score, key;
   int beam;
-  __device__ bool before(const Candidate& o) const { return score > o.score || (score == o.score && (beam < o.beam || (beam == o.beam && key > o.key))); }
+  // (without branches: lanes that take different ones of them cost 240 cycles a comparison)
+  __device__ bool before(const Candidate& o) const { return (score > o.score) | ((score == o.score) & ((beam < o.beam) | ((beam == o.beam) & (key > o.key)))); }
 };
+__device__ __forceinline__ u64 score_bits(double x) {
+  const long long u = __double_as_longlong(x + 0.0);      // (-0 is 0)
+  return (u64)(u ^ (u >> 63 | (long long)(1ull << 63)));
+}
+__device__ __forceinline__ double score_of(u64 bits) { return __longlong_as_double((long long)(bits >> 63 ? bits ^ 1ull << 63 : ~bits)); }
 
 // grid: requests
 template <typename T>
@@ -303,7 +333,8 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
   __shared__ __align__(16) float group_s[kGroups];
   __shared__ float limit_s;
   __shared__ int count_s, kind_s[kBeamsPerRequest];
-  __shared__ double score_s[kBeamsPerRequest], total_s[kBeamsPerRequest];   // hypotheses' scores and normalisers
+  __shared__ double total_s[kBeamsPerRequest];    // normalisers ...
+  __shared__ float score_s[kBeamsPerRequest], near_s[kBeamsPerRequest];   // ... and rounded
   __shared__ Candidate list_s[kJoinList], best_s[kBeWarps];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, row0 = (int)blockIdx.x * p.beams, n_out = p.n_out;
   grid_dependency_wait();
@@ -348,39 +379,49 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
       for (int x = 16; x > 0; x >>= 1) s += __shfl_xor_sync(0xffffffffu, s, x);
       total = (double)m + log(s);                 // (a row without candidates has none that would use it)
     }
-    if (lane == 0) { kind_s[k] = kind; score_s[k] = (double)p.scores[row]; total_s[k] = total; }
+    if (lane == 0) { kind_s[k] = kind; score_s[k] = p.scores[row]; total_s[k] = total; near_s[k] = (float)total; }
   }
   __syncthreads();
-  auto candidate = [&](int x, u64 key) {
-    const int k = x / per_row, kind = kind_s[k];
-    Candidate c{0.0, 0, k};
-    if (kind == 0) {
-      c.key = key;
-      c.score = score_s[k] + ((double)key_logit(key) - total_s[k]);
-    } else if (kind == 1 && x == k * per_row) {
-      c.key = make_key(0.f, p.pad_token);
-      c.score = score_s[k];
-    }
-    return c;
+  // Scores in fp32 first, with bounds of what they are off by: the n_out-th largest lower bound bounds the n_out-th largest score, and what may
+  // reach it is scored in 64 bits (an operation in 64 bits takes as long as a dozen others).
+  struct Bounds {
+    float least, most;
+  };
+  auto bounds = [&](int k, u64 key) {
+    const float x = kind_s[k] == 0 ? key_logit(key) : 0.f, before = score_s[k], total = near_s[k];
+    const float near = before + (x - total), off = 0x1p-21f * (fabsf(before) + fabsf(x) + fabsf(total));
+    return Bounds{near - off, near + off};
+  };
+  auto key_at = [&](int k, int x, u64 key) {      // 0: no candidate
+    const int kind = kind_s[k];
+    return kind == 0 ? key : kind == 1 && x == k * per_row ? make_key(0.f, p.pad_token) : 0;
+  };
+  auto candidate = [&](int k, u64 key) {
+    return Candidate{score_bits(kind_s[k] == 0 ? (double)score_s[k] + ((double)key_logit(key) - total_s[k]) : (double)score_s[k]), key, k};
   };
   auto each = [&](auto&& use) {                   // over what is held
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
       const int x = i * kBeThreads + t;
-      if (x < all) use(candidate(x, key[i]));
+      if (x >= all) break;
+      const int k = x / per_row;
+      const u64 own = key_at(k, x, key[i]);
+      if (own) use(k, own);
     }
     if (all <= kHeld * kBeThreads) return;
-    for (int x = kHeld * kBeThreads + t; x < all; x += kBeThreads) use(candidate(x, __ldcg(lists + (long long)row0 * per_row + x)));
+    for (int x = kHeld * kBeThreads + t; x < all; x += kBeThreads) {
+      const int k = x / per_row;
+      const u64 own = key_at(k, x, __ldcg(lists + (long long)row0 * per_row + x));
+      if (own) use(k, own);
+    }
   };
   float top = -INFINITY;
-  each([&](const Candidate& c) {
-    if (c.key) top = fmaxf(top, (float)c.score);
-  });
+  each([&](int k, u64 key) { top = fmaxf(top, bounds(k, key).least); });      // (a NaN, of infinities, bounds nothing)
   const float limit = nth_of_groups(top, n_out, group_s, limit_s);
-  each([&](const Candidate& c) {
-    if (!c.key || !((float)c.score >= limit)) return;
+  each([&](int k, u64 key) {
+    if (bounds(k, key).most < limit) return;
     const int at = atomicAdd(&count_s, 1);
-    if (at < kJoinList) list_s[at] = c;
+    if (at < kJoinList) list_s[at] = candidate(k, key);
   });
   __syncthreads();
   const int count = count_s;
@@ -388,21 +429,19 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
     const long long to = (long long)blockIdx.x * n_out + at;
     p.parents[to] = c.beam;
     p.tokens[to] = key_token(c.key);
-    p.scores_out[to] = (float)c.score;
+    p.scores_out[to] = (float)score_of(c.score);
   };
   if (count <= kJoinList) {
-    for (int x = t; x < count; x += kBeThreads) {
-      const Candidate mine = list_s[x];
-      int before = 0;
-      for (int y = 0; y < count; ++y) before += list_s[y].before(mine);
-      if (before < n_out) put(before, mine);
-    }
+    rank(count, [&](int x, int y) { return list_s[y].before(list_s[x]); }, [&](int x, int before) {
+      if (before < n_out) put(before, list_s[x]);
+    });
   } else {
-    Candidate last{INFINITY, ~0ull, -1};
+    Candidate last{~0ull, ~0ull, -1};
     for (int k = 0; k < n_out; ++k) {
-      Candidate best{0.0, 0, 0};                  // key 0: none
-      each([&](const Candidate& c) {
-        if (c.key && last.before(c) && (!best.key || c.before(best))) best = c;
+      Candidate best{0, 0, 0};                    // key 0: none
+      each([&](int k, u64 key) {
+        const Candidate c = candidate(k, key);
+        if (last.before(c) && (!best.key || c.before(best))) best = c;
       });
 #pragma unroll
       for (int x = 16; x > 0; x >>= 1) {
@@ -433,11 +472,11 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
       const bool is = v < tokens && (kind_s[k] == 2 || !(to_f32<T>(from[v]) > -INFINITY));
       const unsigned int found = __ballot_sync(0xffffffffu, is);
       const int at = have + __popc(found & ((1u << lane) - 1u));
-      if (is && at < n_out) put(at, Candidate{-INFINITY, make_key(0.f, ended ? p.pad_token : v), k});
+      if (is && at < n_out) put(at, Candidate{score_bits(-INFINITY), make_key(0.f, ended ? p.pad_token : v), k});
       have += __popc(found);
     }
   }
-  for (int at = have + lane; at < n_out; at += 32) put(at, Candidate{-INFINITY, make_key(0.f, p.pad_token), 0});
+  for (int at = have + lane; at < n_out; at += 32) put(at, Candidate{score_bits(-INFINITY), make_key(0.f, p.pad_token), 0});
 }
 
 // 16-byte pieces of a slice for a thread: many where there are blocks enough, else few, for more blocks.
