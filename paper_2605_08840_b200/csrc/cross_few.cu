@@ -2,7 +2,7 @@
 // head_dim 64 or 128.
 //
 // What bounds it: K and V are read once, for all hypotheses of a source, and meet up to 32 query rows per pass: the step streams HBM.
-//   - a warp owns every eighth tile of its CTA's run and a ring of tile slots that its own lane fills by TMA from K and V as they lie (four
+//   - a warp owns every eighth (fourth) tile of its CTA's run and a ring of tile slots that its own lane fills by TMA from K and V as they lie (four
 //     dimensions with strides; 128-byte swizzle for ldmatrix), so that warps never wait for one another while they stream;
 //   - mma.sync m16n8k16 with rows of the cache as rows, query rows as columns: S^T = K Q^T, O^T = V^T P^T.  Tiles of 8 query rows, 1, 2 or 4
 //     of them, so that few rows are not padded and 32 read K and V once; of 32 the queries are read from shared memory, where O has the registers;
@@ -26,7 +26,6 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kFewWarps = 8, kFewThreads = kFewWarps * 32;
 constexpr int kFewSnap = 24;                    // tiles that a CTA could go through while it ends one unit and begins another
 constexpr float kFewSlack = 8.f;                // log2 of what weights may grow to before O is rescaled
 
@@ -39,21 +38,22 @@ struct CrossFewArgs {
   long long wait_limit;
 };
 
-template <int kD, int kNT> struct FewConfig {
+template <int kD, int kNT, bool kCluster> struct FewConfig {
+  // Dealt out, two CTAs of four warps share an SM: one streams while the other ends a unit and begins the next.
+  static constexpr int kWarps = kCluster ? 8 : 4, kThreads = kWarps * 32, kPerSm = kCluster ? 1 : 2;
   static constexpr int kRows = 8 * kNT;
   static constexpr int kBlocks = kD == 64 ? 2 : 1;                        // blocks of 16 rows of a tile
   static constexpr int kTileRows = 16 * kBlocks;
   static constexpr uint32_t kBox = kTileRows * 128;                       // [rows x 64 dims]
   static constexpr uint32_t kSide = kTileRows * kD * 2;                   // K's, or V's
   static constexpr uint32_t kStageBytes = 2 * kSide;
-  static constexpr int kStages = 3, kClusterStages = 2;
+  static constexpr int kStages = kCluster ? 2 : 3;
   static constexpr bool kQInShared = kNT > 2;
   static constexpr uint32_t kQBytes = kQInShared ? kRows * kD * 2u : 0u;
   static constexpr uint32_t kPartBytes = kRows * kD * 4u;                 // a warp's o in the merge
-  static constexpr size_t kSmem = (size_t)kFewWarps * kStages * kStageBytes + kQBytes + 1024;
-  static constexpr uint32_t kPushBytes = kPartBytes + 256u + 16u * kRows * 8u;
-  static constexpr size_t kClusterSmem = (size_t)kFewWarps * kClusterStages * kStageBytes + kQBytes + kPushBytes + 1024;
-  static_assert(kClusterStages * kStageBytes >= kPartBytes, "the merge needs the ring's space");
+  static constexpr uint32_t kPushBytes = kCluster ? kPartBytes + 256u + 16u * kRows * 8u : 0u;   // what the peers push
+  static constexpr size_t kSmem = (size_t)kWarps * kStages * kStageBytes + kQBytes + kPushBytes + 1024;
+  static_assert(kStages * kStageBytes >= kPartBytes, "the merge needs the ring's space");
 };
 
 __device__ __forceinline__ int few_entries(const CrossProblem& c) { return c.per_head ? c.sources * c.Hkv : c.sources; }
@@ -76,15 +76,14 @@ template <int kD> __device__ __forceinline__ void few_write(const CrossProblem& 
 }
 
 template <int kD, int kNT, bool kCluster>
-__global__ void __launch_bounds__(kFewThreads, 1)
+__global__ void __launch_bounds__(FewConfig<kD, kNT, kCluster>::kThreads, FewConfig<kD, kNT, kCluster>::kPerSm)
 cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CrossFewArgs a) {
-  using C = FewConfig<kD, kNT>;
-  constexpr int kRows = C::kRows, kBlocks = C::kBlocks, kW = kFewWarps;
-  constexpr int kStages = kCluster ? C::kClusterStages : C::kStages;
+  using C = FewConfig<kD, kNT, kCluster>;
+  constexpr int kRows = C::kRows, kBlocks = C::kBlocks, kW = C::kWarps, kStages = C::kStages, kThreads = C::kThreads;
   constexpr uint32_t ring_bytes = (uint32_t)kStages * C::kStageBytes;
   const CrossProblem& c = a.c;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ __align__(8) uint64_t full[kW][C::kStages];
+  __shared__ __align__(8) uint64_t full[kW][kStages];
   __shared__ float w_ml[kW][kRows][2];
   __shared__ float w_factor[kW][kRows];
   __shared__ float2 c_ml[kRows];
@@ -158,7 +157,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     uint32_t qb[C::kQInShared ? 1 : kD / 16][C::kQInShared ? 1 : kNT][2];
     if constexpr (C::kQInShared) {
       constexpr int kChunks = kD / 8;
-      for (int x = threadIdx.x; x < kRows * kChunks; x += kFewThreads) {
+      for (int x = threadIdx.x; x < kRows * kChunks; x += kThreads) {
         const int row = x / kChunks, chunk = x % kChunks, rho = rho0 + row;
         uint4 u = make_uint4(0u, 0u, 0u, 0u);
         if (rho < R) u = reinterpret_cast<const uint4*>(cross_query<__nv_bfloat16>(c, cross_row(c, b, rho), h))[chunk];
@@ -335,7 +334,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     }
     __syncthreads();
     const int rows = R - rho0 < kRows ? R - rho0 : kRows;
-    for (int x = threadIdx.x; x < kRows * kW; x += kFewThreads) {   // a warp's factor for each row, and the CTA's (reference, sum)
+    for (int x = threadIdx.x; x < kRows * kW; x += kThreads) {   // a warp's factor for each row, and the CTA's (reference, sum)
       const int row = x / kW, w = x % kW;
       const float mw = w_ml[w][row][0];
       float mm = mw;
@@ -358,7 +357,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     const int per_cta = kCluster ? (items + a.cluster - 1) / a.cluster : 0;
     const int whole = kCluster ? 0 : piece.whole;
     if (kCluster) cluster_wait();
-    for (int x = threadIdx.x; x < items; x += kFewThreads) {
+    for (int x = threadIdx.x; x < items; x += kThreads) {
       const int row = x / (kD / 4), v = x % (kD / 4);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -377,7 +376,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       }
     }
     if constexpr (kCluster) {
-      for (int x = threadIdx.x; x < rows * a.cluster; x += kFewThreads) {
+      for (int x = threadIdx.x; x < rows * a.cluster; x += kThreads) {
         const int to = x / rows, row = x - to * rows;
         *cg::this_cluster().map_shared_rank(push_ml + cluster_rank * kRows + row, to) = c_ml[row];
       }
@@ -386,7 +385,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       cluster_wait();
       // a.cluster threads side by side hold an item's parts
       const int from = threadIdx.x & (a.cluster - 1);
-      for (int y = threadIdx.x / a.cluster; y - (int)((threadIdx.x & 31) / a.cluster) < per_cta; y += kFewThreads / a.cluster) {   // whole warps stay
+      for (int y = threadIdx.x / a.cluster; y - (int)((threadIdx.x & 31) / a.cluster) < per_cta; y += kThreads / a.cluster) {   // whole warps stay
         const int x = y * a.cluster + cluster_rank;
         const bool there = y < per_cta && x < items;
         const int row = there ? x / (kD / 4) : 0, v = x % (kD / 4);
@@ -488,13 +487,16 @@ struct FewVariant {
   void (*kernel)(CUtensorMap, CUtensorMap, CrossFewArgs);
   void (*in_clusters)(CUtensorMap, CUtensorMap, CrossFewArgs);
   void (*combine)(CrossFewArgs, int, int);
-  int d, rows, tile_rows;
+  int d, rows, tile_rows, threads, cluster_threads, per_sm;
   size_t smem, cluster_smem;
 };
 template <int kD, int kNT> FewVariant few_variant() {
-  using C = FewConfig<kD, kNT>;
-  return FewVariant{cross_few_kernel<kD, kNT, false>, cross_few_kernel<kD, kNT, true>, cross_few_combine_kernel<kD, C::kRows>, kD, C::kRows, C::kTileRows, C::kSmem, C::kClusterSmem};
+  using C = FewConfig<kD, kNT, false>;
+  using K = FewConfig<kD, kNT, true>;
+  return FewVariant{cross_few_kernel<kD, kNT, false>, cross_few_kernel<kD, kNT, true>, cross_few_combine_kernel<kD, C::kRows>, kD, C::kRows, C::kTileRows, C::kThreads, K::kThreads,
+                    C::kPerSm, C::kSmem, K::kSmem};
 }
+int few_ctas(const FewVariant& v, int sm_count) { return v.per_sm * sm_count < kMaxCtas ? v.per_sm * sm_count : kMaxCtas; }
 // Up to 8 query rows in one tile of 8, up to 16 in two; more in four, 32 of them per pass over K and V.
 template <int kD> FewVariant few_of(long long rows) { return rows <= 8 ? few_variant<kD, 1>() : rows <= 16 ? few_variant<kD, 2>() : few_variant<kD, 4>(); }
 bool pick_few(const CrossProblem& c, long long rows, FewVariant* v) {
@@ -543,7 +545,7 @@ bool cross_few_supported(const CrossProblem& c) {
 size_t cross_few_bytes(const CrossProblem& c, int sm_count) {
   FewVariant v;
   if (!pick_few(c, c.rows(), &v)) return 0;
-  return (size_t)2 * sm_count * v.rows * (v.d + 2) * sizeof(float);
+  return (size_t)2 * few_ctas(v, sm_count) * v.rows * (v.d + 2) * sizeof(float);
 }
 
 cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, int sm_count, const int* clusters_of, long long wait_limit, unsigned int* dev_status,
@@ -561,7 +563,7 @@ cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, in
   if (a.cluster) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned int)(units * a.cluster));
-    cfg.blockDim = dim3((unsigned int)kFewThreads);
+    cfg.blockDim = dim3((unsigned int)v.cluster_threads);
     cfg.dynamicSmemBytes = v.cluster_smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -574,8 +576,8 @@ cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, in
     cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, v.in_clusters, tmK, tmV, a);
   }
-  const int ctas = sm_count < kMaxCtas ? sm_count : kMaxCtas;
-  const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), kFewThreads, v.smem, st, tmK, tmV, a);
+  const int ctas = few_ctas(v, sm_count);
+  const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
   *launches = 2;
   return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), 2 * v.d, 0, st, a, ctas, v.tile_rows);
