@@ -26,7 +26,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kFewSnap = 24;                    // tiles that a CTA could go through while it ends one unit and begins another
+constexpr int kFewSnap = 8;                     // tiles that a CTA could go through while it ends one unit and begins another
 constexpr float kFewSlack = 8.f;                // log2 of what weights may grow to before O is rescaled
 
 struct CrossFewArgs {
@@ -87,6 +87,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   __shared__ float w_ml[kW][kRows][2];
   __shared__ float w_factor[kW][kRows];
   __shared__ float2 c_ml[kRows];
+  __shared__ float push_factor[kCluster ? 16 : 1][kRows];
   __shared__ int abort_flag;
   __shared__ Piece piece_s;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, r = lane >> 2, q4 = lane & 3, mat = lane >> 3, mr = lane & 7;
@@ -131,12 +132,10 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     const volatile Piece& piece = piece_s;
     const int unit = kCluster ? (int)(blockIdx.x / (unsigned int)a.cluster) : piece.unit;
     const int bh = unit / a.row_tiles, rho0 = (unit - bh * a.row_tiles) * kRows, b = bh / c.Hkv, h = bh - b * c.Hkv;
-    const int n = cross_length(c, b, h);
     // the warp's tiles: `stride` apart from `next` on, below t1
     const int cluster_rank = kCluster ? (int)(blockIdx.x % (unsigned int)a.cluster) : 0, stride = kCluster ? a.cluster * kW : kW;
     const int next = (kCluster ? cluster_rank * kW : piece.t0) + warp;
-    const int t1 = kCluster ? (n + C::kTileRows - 1) / C::kTileRows : min(piece.t1, (n + C::kTileRows - 1) / C::kTileRows);
-    const int mine = t1 > next ? (t1 - next + stride - 1) / stride : 0;
+    auto tiles_below = [&](int t1) { return t1 > next ? (t1 - next + stride - 1) / stride : 0; };
     auto request = [&](int i, int s) {          // tile i into slot s, by one lane
       uint8_t* dst = ring + (uint32_t)s * C::kStageBytes;
       uint64_t* bar = &full[warp][s];
@@ -148,7 +147,17 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
         tma_load_4d(dst + C::kSide + x * C::kBox, &tmV, bar, x * 64, row, h, b);
       }
     };
-    if (elect_one()) {
+    // in clusters the first tiles are asked for before the source's length is known: as many as K and V have
+    int asked = 0;
+    if (kCluster) {
+      asked = min(tiles_below((c.n_rows + C::kTileRows - 1) / C::kTileRows), kStages);
+      if (elect_one()) {
+        for (int i = 0; i < asked; ++i) request(i, i);
+      }
+    }
+    const int n = cross_length(c, b, h), n_tiles = (n + C::kTileRows - 1) / C::kTileRows;
+    const int mine = tiles_below(kCluster ? n_tiles : min(piece.t1, n_tiles));
+    if (!kCluster && elect_one()) {
       for (int i = 0; i < kStages && i < mine; ++i) request(i, slot + i < kStages ? slot + i : slot + i - kStages);
     }
     __syncwarp();
@@ -295,7 +304,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit));
       if (!ok) {
         if (lane == 0)                          // nothing may still be on its way into shared memory when the CTA returns
-          for (int j = 0; j < kStages && i + j < mine; ++j) {
+          for (int j = 0; j < kStages && i + j < max(mine, asked); ++j) {
             const int s = slot + j < kStages ? slot + j : slot + j - kStages;
             wait_issued(&full[warp][s], s < slot ? parity ^ 1u : parity);
           }
@@ -310,6 +319,10 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       __syncwarp();
       if (++slot == kStages) { slot = 0; parity ^= 1u; }
     }
+
+    // (tiles past the source's rows: they have to be there before their places serve for something else)
+    if (kCluster && ok)
+      for (int i = mine; i < asked; ++i) wait_issued(&full[warp][i % kStages], (uint32_t)(i / kStages));
 
     // ---- merge, in a fixed order: the warps of the CTA through their (idle) rings ----
     __syncwarp();
@@ -383,27 +396,29 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       __syncwarp();
       cluster_arrive();
       cluster_wait();
-      // a.cluster threads side by side hold an item's parts
-      const int from = threadIdx.x & (a.cluster - 1);
-      for (int y = threadIdx.x / a.cluster; y - (int)((threadIdx.x & 31) / a.cluster) < per_cta; y += kThreads / a.cluster) {   // whole warps stay
-        const int x = y * a.cluster + cluster_rank;
-        const bool there = y < per_cta && x < items;
-        const int row = there ? x / (kD / 4) : 0, v = x % (kD / 4);
-        const float2 ml = push_ml[from * kRows + row];
-        float4 acc = there ? push_o[from * per_cta + y] : make_float4(0.f, 0.f, 0.f, 0.f);
+      // the CTAs' factors for each row, a.cluster threads side by side to a row
+      for (int x = threadIdx.x; x - (int)(threadIdx.x & 31) < rows * a.cluster; x += kThreads) {   // whole warps stay
+        const int row = x / a.cluster, from = x & (a.cluster - 1);
+        const float2 ml = row < rows ? push_ml[from * kRows + row] : make_float2(-INFINITY, 0.f);
         float mm = ml.x;
         for (int off = a.cluster / 2; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
         const float f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - mm);
         float ll = ml.y * f;
-        acc.x *= f; acc.y *= f; acc.z *= f; acc.w *= f;
-        for (int off = a.cluster / 2; off > 0; off >>= 1) {
-          ll += __shfl_xor_sync(0xffffffffu, ll, off);
-          acc.x += __shfl_xor_sync(0xffffffffu, acc.x, off);
-          acc.y += __shfl_xor_sync(0xffffffffu, acc.y, off);
-          acc.z += __shfl_xor_sync(0xffffffffu, acc.z, off);
-          acc.w += __shfl_xor_sync(0xffffffffu, acc.w, off);
+        for (int off = a.cluster / 2; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
+        if (row < rows) {
+          push_factor[from][row] = f;
+          if (from == 0) c_ml[row] = make_float2(mm, ll);
         }
-        if (there && from == 0) few_write<kD>(c, b, h, rho0 + row, v, acc, mm, ll);
+      }
+      __syncthreads();
+      for (int y = threadIdx.x; y < per_cta; y += kThreads) {
+        const int x = y * a.cluster + cluster_rank;
+        if (x >= items) continue;
+        const int row = x / (kD / 4);
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int from = 0; from < a.cluster; ++from) fma4(acc, push_o[from * per_cta + y], push_factor[from][row]);
+        few_write<kD>(c, b, h, rho0 + row, x % (kD / 4), acc, c_ml[row].x, c_ml[row].y);
       }
       return;
     }

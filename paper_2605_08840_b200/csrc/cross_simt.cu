@@ -13,7 +13,7 @@ namespace restkv {
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
-constexpr int kRows = 4;
+constexpr int kRows = 4, kAtOnce = 2;
 constexpr int kMaxSplits = 64;
 
 // grid (query rows / 4, splits, sources * Hkv); a single split writes the results itself.  A slot of `kLanes` threads takes a row of K and V, 8
@@ -51,39 +51,66 @@ __global__ void __launch_bounds__(kThreads) cross_simt_kernel(const CrossProblem
   const int r0 = (int)(blocks * split / splits) * 16, end = (int)(blocks * (split + 1) / splits) * 16, r1 = end < n ? end : n;
   const T* const K = reinterpret_cast<const T*>(c.K.data) + b * c.K.sb + h * c.K.sh + chunk * 8;
   const T* const V = reinterpret_cast<const T*>(c.V.data) + b * c.V.sb + h * c.V.sh + chunk * 8;
-  for (int base = r0; base < r1; base += kWarps * kPerWarp) {
-    const int row = base + warp * kPerWarp + lane / kLanes;
-    const bool in = row < r1;
-    float kf[8], vf[8];
-    Pack8<T> kp, vp;
-    kp.zero();
-    vp.zero();
-    if (in && has) {
-      kp.load(K + row * c.K.sn);
-      vp.load(V + row * c.V.sn);
+  // kAtOnce rows per slot together: their loads, sums and exponentials do not wait for one another, and the maximum is looked at once for all
+  constexpr int kStep = kWarps * kPerWarp;
+  for (int base = r0; base < r1; base += kAtOnce * kStep) {
+    const int row0 = base + warp * kPerWarp + lane / kLanes;
+    Pack8<T> kp[kAtOnce], vp[kAtOnce];
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      kp[x].zero();
+      vp[x].zero();
+      if (has && row0 + x * kStep < r1) {
+        kp[x].load(K + (row0 + x * kStep) * c.K.sn);
+        vp[x].load(V + (row0 + x * kStep) * c.V.sn);
+      }
     }
-    kp.get(kf);
-    vp.get(vf);
+    float s[kRows][kAtOnce];
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      float kf[8];
+      kp[x].get(kf);
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        s[k][x] = 0.f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[k][x] = fmaf(q[k][e], kf[e], s[k][x]);
+      }
+    }
+#pragma unroll
+    for (int off = kLanes / 2; off > 0; off >>= 1)
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+#pragma unroll
+        for (int x = 0; x < kAtOnce; ++x) s[k][x] += __shfl_xor_sync(0xffffffffu, s[k][x], off);
 #pragma unroll
     for (int k = 0; k < kRows; ++k) {
-      float s = 0.f;
+      float top = m[k];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(q[k][e], kf[e], s);
-#pragma unroll
-      for (int off = kLanes / 2; off > 0; off >>= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-      if (!in) continue;
-      s *= c.scale;
-      if (s > m[k]) {
-        const float f = __expf(m[k] - s);                                // m = -inf gives 0
-        l[k] *= f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) o[k][e] *= f;
-        m[k] = s;
+      for (int x = 0; x < kAtOnce; ++x) {
+        s[k][x] = row0 + x * kStep < r1 ? s[k][x] * c.scale : -INFINITY;
+        top = fmaxf(top, s[k][x]);
       }
-      const float p = m[k] == -INFINITY ? 0.f : __expf(s - m[k]);       // only logits of -inf so far: they weigh nothing
-      l[k] += p;
+      const float of = top == -INFINITY ? 0.f : top;                       // only logits of -inf so far: they weigh nothing
+      const float f = __expf(m[k] - of);                                   // m = -inf gives 0
+      m[k] = top;
+      l[k] *= f;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[k][e] = fmaf(p, vf[e], o[k][e]);
+      for (int e = 0; e < 8; ++e) o[k][e] *= f;
+#pragma unroll
+      for (int x = 0; x < kAtOnce; ++x) {
+        s[k][x] = __expf(s[k][x] - of);
+        l[k] += s[k][x];
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kAtOnce; ++x) {
+      float vf[8];
+      vp[x].get(vf);
+#pragma unroll
+      for (int k = 0; k < kRows; ++k)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[k][e] = fmaf(s[k][x], vf[e], o[k][e]);
     }
   }
   // merge: the slots of a warp by butterfly exchange, the warps through shared memory
