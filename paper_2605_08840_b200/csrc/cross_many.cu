@@ -514,74 +514,96 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if (warp == kMaSoftmax + 1) tmem_dealloc(tmem, 512);
 }
 
-// grid (CTAs of the kernel before, 32), block 256: merges what several of them left of a unit, a row per warp.  A unit is merged by the blocks of the
-// first CTA that began inside it.
+// grid (CTAs of the kernel before, 8), block 256: merges what several of them left of a unit, four rows per warp (one: 4700 blocks in four waves,
+// each as long as its chain of loads).  A unit is merged by the blocks of the first CTA that began inside it.
 template <int kD>
 __global__ void __launch_bounds__(256) cross_many_combine_kernel(const __grid_constant__ CrossManyArgs a) {
   grid_dependency_wait();
   grid_dependency_launch();
   const CrossProblem& c = a.c;
   const int x = blockIdx.x, ctas = gridDim.x, lane = threadIdx.x & 31;
-  const int2 mine = __ldcg(a.begins + x);
+  const int2 mine = __ldcg(a.begins + x), before = x > 0 ? __ldcg(a.begins + x - 1) : make_int2(-1, 0);
   if (mine.x < 0 || mine.y == 0) return;                // (the first CTA begins a unit: x > 0 from here on)
-  auto inside = [&](int y) {
-    const int2 o = __ldcg(a.begins + y);
-    return o.x == mine.x && o.y > 0;
-  };
-  if (inside(x - 1)) return;
-  const int unit = mine.x, row = (int)blockIdx.y * 8 + (threadIdx.x >> 5), bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
-  const int rho = (unit - bh * a.row_tiles) * kMaRows + row;
-  if (rho >= (int)c.rows()) return;
+  if (before.x == mine.x && before.y > 0) return;
+  constexpr int kAtOnce = 4, kPer = kD / 32;
+  const int unit = mine.x, row0 = (int)blockIdx.y * 8 * kAtOnce + (int)(threadIdx.x >> 5) * kAtOnce, bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
+  const int rho0 = (unit - bh * a.row_tiles) * kMaRows + row0, left = (int)c.rows() - rho0;
+  if (left <= 0) return;
   constexpr long long kSlot = kMaRows * (kD + 2);
-  constexpr int kPer = kD / 32;
   auto piece = [&](int k) { return a.part + (2ll * (x - 1 + k) + (k == 0)) * kSlot; };   // the CTA before began the unit
   // 32 pieces at a time, a lane's (reference, sum) each
-  float mm = -INFINITY, ll = 0.f, acc[kPer] = {};
+  float mm[kAtOnce], ll[kAtOnce], acc[kAtOnce][kPer];
+#pragma unroll
+  for (int i = 0; i < kAtOnce; ++i) {
+    mm[i] = -INFINITY;
+    ll[i] = 0.f;
+#pragma unroll
+    for (int z = 0; z < kPer; ++z) acc[i][z] = 0.f;
+  }
   for (int base = 0;; base += 32) {
     const int k = base + lane;
-    const bool some = k == 0 || (x - 1 + k < ctas && inside(x - 1 + k));
-    const int n = __popc(__ballot_sync(0xffffffffu, some));
-    const float2 ml = some ? __ldcg(reinterpret_cast<const float2*>(piece(k) + kMaRows * kD) + row) : make_float2(-INFINITY, 0.f);
-    float top = ml.x;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    top = fmaxf(top, mm);
-    const float down = mm == -INFINITY ? 0.f : ex2_approx(mm - top), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
-    mm = top;
-    float sum = ml.y * f;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-    ll = fmaf(ll, down, sum);
-#pragma unroll
-    for (int y = 0; y < kPer; ++y) acc[y] *= down;
-#pragma unroll 8
-    for (int y = 0; y < n; ++y) {
-      const float g = __shfl_sync(0xffffffffu, f, y);
-      const float* o = piece(base + y) + row * kD + kPer * lane;
-      float w[kPer];
-      if constexpr (kPer == 4) {
-        const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
-        w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-      } else {
-        const float2 u = __ldcg(reinterpret_cast<const float2*>(o));
-        w[0] = u.x; w[1] = u.y;
-      }
-#pragma unroll
-      for (int z = 0; z < kPer; ++z) acc[z] = g > 0.f ? fmaf(w[z], g, acc[z]) : acc[z];
+    bool some = k == 0;
+    if (k > 0 && x - 1 + k < ctas) {
+      const int2 o = __ldcg(a.begins + x - 1 + k);
+      some = o.x == mine.x && o.y > 0;
     }
+    const int n = __popc(__ballot_sync(0xffffffffu, some));
+    float f[kAtOnce];
+    float2 ml[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i)                   // (a slot has all 256 rows)
+      ml[i] = some ? __ldcg(reinterpret_cast<const float2*>(piece(k) + kMaRows * kD) + row0 + i) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (i >= left) ml[i] = make_float2(-INFINITY, 0.f);   // rows that there are not: nobody wrote them
+      float top = ml[i].x;
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      top = fmaxf(top, mm[i]);
+      const float down = mm[i] == -INFINITY ? 0.f : ex2_approx(mm[i] - top);
+      f[i] = ml[i].x == -INFINITY ? 0.f : ex2_approx(ml[i].x - top);
+      mm[i] = top;
+      float sum = ml[i].y * f[i];
+#pragma unroll
+      for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+      ll[i] = fmaf(ll[i], down, sum);
+#pragma unroll
+      for (int z = 0; z < kPer; ++z) acc[i][z] *= down;
+    }
+#pragma unroll 2
+    for (int y = 0; y < n; ++y)
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float g = __shfl_sync(0xffffffffu, f[i], y);
+        const float* o = piece(base + y) + (row0 + i) * kD + kPer * lane;
+        float w[kPer];
+        if constexpr (kPer == 4) {
+          const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
+          w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
+        } else {
+          const float2 u = __ldcg(reinterpret_cast<const float2*>(o));
+          w[0] = u.x; w[1] = u.y;
+        }
+#pragma unroll
+        for (int z = 0; z < kPer; ++z) acc[i][z] = g > 0.f ? fmaf(w[z], g, acc[i][z]) : acc[i][z];
+      }
     if (n < 32) break;
   }
-  const CrossRow r = cross_row(c, b, rho);
-  const bool some = ll > 0.f && cross_live(c, r);
-  const long long at = cross_out_row(c, r, h);
-  const float norm = some ? 1.f / ll : 0.f;
-  uint32_t y[kPer / 2];
 #pragma unroll
-  for (int z = 0; z < kPer / 2; ++z) y[z] = some ? pack_bf16x2(acc[2 * z] * norm, acc[2 * z + 1] * norm) : 0u;
-  __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD + kPer * lane;
-  if constexpr (kPer == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
-  else *reinterpret_cast<uint32_t*>(to) = y[0];
-  if (lane == 0 && c.lse) c.lse[at] = some ? fmaf(mm, 0.6931471805599453f, logf(ll)) : -INFINITY;
+  for (int i = 0; i < kAtOnce; ++i) {
+    if (i >= left) break;
+    const CrossRow r = cross_row(c, b, rho0 + i);
+    const bool some = ll[i] > 0.f && cross_live(c, r);
+    const long long at = cross_out_row(c, r, h);
+    const float norm = some ? 1.f / ll[i] : 0.f;
+    uint32_t y[kPer / 2];
+#pragma unroll
+    for (int z = 0; z < kPer / 2; ++z) y[z] = some ? pack_bf16x2(acc[i][2 * z] * norm, acc[i][2 * z + 1] * norm) : 0u;
+    __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD + kPer * lane;
+    if constexpr (kPer == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
+    else *reinterpret_cast<uint32_t*>(to) = y[0];
+    if (lane == 0 && c.lse) c.lse[at] = some ? fmaf(mm[i], 0.6931471805599453f, logf(ll[i])) : -INFINITY;
+  }
 }
 
 int many_ctas(int sm_count) { return sm_count < kMaxCtas ? sm_count : kMaxCtas; }
@@ -624,7 +646,7 @@ cudaError_t launch_cross_many(void* state, const CrossProblem& c, float* part, i
   const cudaError_t e = c.d == 64 ? launch_chained(cross_many_kernel<64>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<64>::kSmem, st, tmK, tmV, a)
                                   : launch_chained(cross_many_kernel<128>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<128>::kSmem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned int)ctas, kMaRows / 8);
+  const dim3 grid((unsigned int)ctas, kMaRows / 32);
   return c.d == 64 ? launch_chained(cross_many_combine_kernel<64>, grid, 256, 0, st, a) : launch_chained(cross_many_combine_kernel<128>, grid, 256, 0, st, a);
 }
 
