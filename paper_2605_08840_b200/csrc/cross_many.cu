@@ -35,13 +35,14 @@ constexpr int kMaThreads = (kMaSoftmax + 4) * 32;   // (two warps more: register
 constexpr int kMaRegs = 168, kMaSoftmaxRegs = 176, kMaOtherRegs = 152;
 static_assert(2 * kMaSoftmaxRegs + kMaOtherRegs == 3 * kMaRegs, "more than the launch has would be waited for");
 // Tiles that a CTA could go through while it ends one unit and begins another: each unit counts for as many more, ahead of its own, and a boundary that
-// lies nearer to a unit's end moves there.
-constexpr int kMaAhead = 4, kMaSnap = 8;
+// lies nearer to a unit's end moves there.  (8 sources of up to 509 tokens: 4 and 2 108 us, 4 and 8 113, 4 and 1 109, 2 and 2 111.)
+constexpr int kMaAhead = 4, kMaSnap = 2;
+constexpr int kMaEmpty = 2;                  // what a unit without tiles counts for: zeros are written
 constexpr float kMaSlack = 8.f;              // log2 of what weights may grow to before O is rescaled
 
 struct CrossManyArgs {
   CrossProblem c;
-  float* part;                               // per CTA two of: o [256, d], (m, l) [256]
+  float* part;                               // per CTA two of: o [d / 4, 256, 4], (m, l) [256]
   int2* begins;                              // per CTA: unit and tile of it that it begins with; -1: none
   unsigned int* dev_status;
   int row_tiles;                             // units per KV head
@@ -131,7 +132,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   }
   grid_dependency_wait();
   grid_dependency_launch();
-  auto tiles_of = [&](int unit) { return kMaAhead + max(1, many_tiles(c, a.row_tiles, unit)); };   // a unit without rows has its outputs written, too
+  auto counted_of = [&](int tiles) { return tiles > 0 ? kMaAhead + tiles : kMaEmpty; };
+  auto tiles_of = [&](int unit) { return counted_of(many_tiles(c, a.row_tiles, unit)); };
   {
     // The CTA's run of tiles: every thread counts those of some units; the threads in whose units the run begins and ends say where.
     const int units = c.sources * c.Hkv * a.row_tiles, per = (units + kMaThreads - 1) / kMaThreads;
@@ -162,7 +164,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (x + k >= deal.ctas) break;
       const int want = deal.start(x + k);
       if (want < first || want >= first + sum) continue;
-      int u = u0, f = first, t = tiles_of(u);
+      int u = u0, f = first, t = per == 1 ? sum : tiles_of(u);
       while (want >= f + t) {
         f += t;
         t = tiles_of(++u);
@@ -192,24 +194,25 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   // it waits for at a barrier, so that K, V and the first logits of a piece are under way while the results of the one before are written.
   const Run run = piece_s.run;
   auto each_piece = [&](auto&& part) {
-    int done = 0, nth = 0, unit = run.entry, counted = run.tiles, from = run.tile - run.first, left = run.end - run.tile;
-    if (left > 0 && from >= counted) {                  // (the run begins with the unit after)
+    int done = 0, nth = 0, unit = run.entry, from = run.tile - run.first, left = run.end - run.tile;
+    if (left > 0 && from >= run.tiles) {                // (the run begins with the unit after)
       from = 0;
-      counted = tiles_of(++unit);
+      ++unit;
     }
-    if (threadIdx.x == 0) a.begins[blockIdx.x] = left > 0 && from + left > kMaAhead ? make_int2(unit, max(0, from - kMaAhead)) : make_int2(-1, 0);
+    int tiles = left > 0 ? many_tiles(c, a.row_tiles, unit) : 0;
+    if (threadIdx.x == 0) a.begins[blockIdx.x] = tiles > 0 && from + left > kMaAhead ? make_int2(unit, max(0, from - kMaAhead)) : make_int2(-1, 0);
     while (left > 0) {
-      const int to = min(from + left, counted), bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
-      const int t0 = max(0, from - kMaAhead), t1 = to - kMaAhead;
-      if (t1 > 0) {                                     // (a run that ends ahead of a unit's tiles leaves it to the next CTA)
-        const Unit u{b, h, (unit - bh * a.row_tiles) * kMaRows, cross_length(c, b, h), t0, min(t1, many_tiles(c, a.row_tiles, unit)) - t0, done, nth, t0 == 0 && to == counted};
-        if (!part(u)) break;
-        done += u.tiles;
+      const int to = min(from + left, counted_of(tiles)), bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
+      const int t0 = tiles > 0 ? max(0, from - kMaAhead) : 0, t1 = tiles > 0 ? to - kMaAhead : 0;
+      // (a run that ends ahead of a unit's tiles leaves it to the next CTA; one without tiles is its who has its beginning)
+      if (tiles > 0 ? t1 > 0 : from == 0) {
+        if (!part(Unit{b, h, (unit - bh * a.row_tiles) * kMaRows, cross_length(c, b, h), t0, t1 - t0, done, nth, t0 == 0 && t1 == tiles})) break;
+        done += t1 - t0;
         ++nth;
       }
       left -= to - from;
       from = 0;
-      if (left > 0) counted = tiles_of(++unit);
+      if (left > 0) tiles = many_tiles(c, a.row_tiles, ++unit);
     }
   };
 
@@ -300,6 +303,9 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         const int end = x + 2 * u.tiles;
         for (; x < end; ++x) {
           const int s = x % kSlots, row = (u.t0 + ((x - 2 * u.done) >> 1)) * kMaTile;
+          // at first no more than a tile of each, ahead of the queries, which all wait for
+          if (x == 2) ok = __all_sync(0xffffffffu, wait(&B.q_full[0], u.nth) && wait(&B.q_full[1], u.nth));
+          if (!ok) break;
           // the verdict is the warp's: it clears rows together
           ok = x < kSlots || __all_sync(0xffffffffu, wait(&B.empty[s], x / kSlots - 1));
           if (!ok) break;
@@ -451,37 +457,38 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (ok) {
         tc_fence_after();
         const bool whole = u.whole, some = l > 0.f && live;
-        const float norm = whole ? (some ? 1.f / l : 0.f) : 1.f;
-        const bool nothing = tiles <= 0 || (whole && !some);
         float* const part = a.part + (long long)(2 * blockIdx.x + (u.t0 == 0)) * kMaRows * (kD + 2);
         const long long row = cross_out_row(c, mine, u.h);
-        // By way of the warp's rows of Q's tile, which no product reads any more, for stores of whole rows: kD values of 16 bits at once, or
-        // fp32 ones in two turns.  16-byte chunk k of row r is at k ^ r.
-        constexpr int kChunks = kD / 8;
-        const uint32_t staged = q_at + (uint32_t)w * C::kTileBytesD + (uint32_t)(warp & 3) * (32u * 2u * kD);
-        const uint32_t to_row = staged + (uint32_t)lane * (2u * kD);
         __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(c.out);
-        for (int turn = 0; turn < (whole ? 1 : 2); ++turn) {
+        constexpr int kChunks = kD / 8;
+        if (!whole) {
+          // four dims of all 256 rows after the other: a thread's stores lie beside those of the next row's
+          float4* const to = reinterpret_cast<float4*>(part) + w * 128 + r;
 #pragma unroll
           for (int x = 0; x < kD / 32; ++x) {
-            if (!whole && x / (kD / 64) != turn) continue;
             float o[32];
-            if (tiles > 0) {
+            tmem_ld32(o_tm + x * 32, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int y = 0; y < 32; y += 4) to[(32 * x + y) / 4 * kMaRows] = make_float4(o[y], o[y + 1], o[y + 2], o[y + 3]);
+          }
+        } else {
+          // By way of the warp's rows of Q's tile, which no product reads any more, for stores of whole rows.  16-byte chunk k of row r is at k ^ r.
+          const uint32_t staged = q_at + (uint32_t)w * C::kTileBytesD + (uint32_t)(warp & 3) * (32u * 2u * kD);
+          const uint32_t to_row = staged + (uint32_t)lane * (2u * kD);
+          const float norm = some ? 1.f / l : 0.f;
+          if (tiles > 0) {
+#pragma unroll
+            for (int x = 0; x < kD / 32; ++x) {
+              float o[32];
               tmem_ld32(o_tm + x * 32, o);
               tmem_wait_ld();
-            }
 #pragma unroll
-            for (int y = 0; y < 32; ++y) o[y] = nothing ? 0.f : o[y] * norm;
-            if (whole) {
+              for (int y = 0; y < 32; ++y) o[y] = some ? o[y] * norm : 0.f;
 #pragma unroll
               for (int y = 0; y < 32; y += 8)
                 many_sts128(to_row + (uint32_t)((((32 * x + y) / 8) ^ (lane & (kChunks - 1))) * 16), pack_bf16x2(o[y], o[y + 1]), pack_bf16x2(o[y + 2], o[y + 3]),
                             pack_bf16x2(o[y + 4], o[y + 5]), pack_bf16x2(o[y + 6], o[y + 7]));
-            } else {
-#pragma unroll
-              for (int y = 0; y < 32; y += 4)
-                many_sts128(to_row + (uint32_t)(((((32 * x + y) % (kD / 2)) / 4) ^ (lane & (kChunks - 1))) * 16), __float_as_uint(o[y]), __float_as_uint(o[y + 1]),
-                            __float_as_uint(o[y + 2]), __float_as_uint(o[y + 3]));
             }
           }
           __syncwarp();
@@ -491,11 +498,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             const int at = z + lane / kChunks;
             const long long to = __shfl_sync(0xffffffffu, row, at);
             if (u.rho0 + in_tile + at >= R) continue;
-            const uint4 y = lds128(staged + (uint32_t)at * (2u * kD) + (uint32_t)((k ^ (at & (kChunks - 1))) * 16));
-            if (whole) reinterpret_cast<uint4*>(out + to * kD)[k] = y;
-            else reinterpret_cast<uint4*>(part + (in_tile + at) * kD + turn * (kD / 2))[k] = y;
+            reinterpret_cast<uint4*>(out + to * kD)[k] = tiles > 0 ? lds128(staged + (uint32_t)at * (2u * kD) + (uint32_t)((k ^ (at & (kChunks - 1))) * 16)) : make_uint4(0u, 0u, 0u, 0u);
           }
-          __syncwarp();
         }
         if (rho < R) {
           if (whole) {
@@ -575,7 +579,7 @@ __global__ void __launch_bounds__(256) cross_many_combine_kernel(const __grid_co
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         const float g = __shfl_sync(0xffffffffu, f[i], y);
-        const float* o = piece(base + y) + (row0 + i) * kD + kPer * lane;
+        const float* o = piece(base + y) + (kPer * lane / 4 * kMaRows + row0 + i) * 4 + kPer * lane % 4;
         float w[kPer];
         if constexpr (kPer == 4) {
           const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
