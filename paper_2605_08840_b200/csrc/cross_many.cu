@@ -37,6 +37,7 @@ static_assert(2 * kMaSoftmaxRegs + kMaOtherRegs == 3 * kMaRegs, "more than the l
 // Tiles that a CTA could go through while it ends one unit and begins another: each unit counts for as many more, ahead of its own, and a boundary that
 // lies nearer to a unit's end moves there.  (8 sources of up to 509 tokens: 4 and 2 108 us, 4 and 8 113, 4 and 1 109, 2 and 2 111.)
 constexpr int kMaAhead = 4, kMaSnap = 2;
+constexpr int kMaLeast = 8;                  // of these a CTA has at least: what more CTAs left would take longer to merge
 constexpr int kMaEmpty = 2;                  // what a unit without tiles counts for: zeros are written
 constexpr float kMaSlack = 8.f;              // log2 of what weights may grow to before O is rescaled
 
@@ -154,7 +155,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       all += counted[x];
     }
     first += upto - sum;
-    const Deal deal(all, gridDim.x, kMaSnap);
+    const Deal deal(all, min((int)gridDim.x, max(1, all / kMaLeast)), kMaSnap);
     const int x = blockIdx.x;
     if (threadIdx.x == 0) {
       if (x >= deal.ctas) piece_s.run = Run{0, 0, 0, 0, 1};
@@ -187,14 +188,18 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   constexpr uint32_t kO = 256;                          // O of tile w: columns kO + w * kD; S and P: w * 128
 
   struct Unit {
-    int b, h, rho0, n, t0, tiles, done, nth;            // done: tiles of the pieces before, phases of the barriers; nth: pieces before
-    bool whole;                                         // no other CTA has tiles of the unit
+    int b, h, rho0, n, t0, tiles, nth;                  // nth: pieces before
+    // tiles of the pieces before and how many of these have some, and of those of them with a second tile of query rows: the barriers' phases
+    int done, begun, done2, begun2;
+    bool two, whole;                                    // more than 128 query rows; no other CTA has tiles of the unit
+    __device__ int done_of(int w) const { return w ? done2 : done; }
+    __device__ int begun_of(int w) const { return w ? begun2 : begun; }
   };
   // A role's part of every piece, as long as its waits do not run out.  Every role goes through the pieces by itself: what one needs of another
   // it waits for at a barrier, so that K, V and the first logits of a piece are under way while the results of the one before are written.
   const Run run = piece_s.run;
   auto each_piece = [&](auto&& part) {
-    int done = 0, nth = 0, unit = run.entry, from = run.tile - run.first, left = run.end - run.tile;
+    int done = 0, begun = 0, done2 = 0, begun2 = 0, nth = 0, unit = run.entry, from = run.tile - run.first, left = run.end - run.tile;
     if (left > 0 && from >= run.tiles) {                // (the run begins with the unit after)
       from = 0;
       ++unit;
@@ -206,8 +211,13 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       const int t0 = tiles > 0 ? max(0, from - kMaAhead) : 0, t1 = tiles > 0 ? to - kMaAhead : 0;
       // (a run that ends ahead of a unit's tiles leaves it to the next CTA; one without tiles is its who has its beginning)
       if (tiles > 0 ? t1 > 0 : from == 0) {
-        if (!part(Unit{b, h, (unit - bh * a.row_tiles) * kMaRows, cross_length(c, b, h), t0, t1 - t0, done, nth, t0 == 0 && t1 == tiles})) break;
+        const int rho0 = (unit - bh * a.row_tiles) * kMaRows;
+        const bool two = rho0 + 128 < (int)c.rows();
+        if (!part(Unit{b, h, rho0, cross_length(c, b, h), t0, t1 - t0, nth, done, begun, done2, begun2, two, t0 == 0 && t1 == tiles})) break;
         done += t1 - t0;
+        begun += t1 > t0;
+        done2 += two ? t1 - t0 : 0;
+        begun2 += two && t1 > t0;
         ++nth;
       }
       left -= to - from;
@@ -233,25 +243,20 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     };
     each_piece([&](const Unit& u) {
       bool ok = true;
-      for (int j = 0; j <= u.tiles && ok; ++j) {
+      for (int j = 0; j < u.tiles && ok; ++j) {
         const int at = u.done + j, s = 2 * at % kSlots;
-        // (no phase of a barrier may be passed over: a piece without tiles has its queries waited for, too)
-        if (j == u.tiles && j > 0) break;
-        ok = u.tiles <= 0 || there(2 * at);
+        ok = there(2 * at);
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int w = x & 1, half = x >> 1;
-          if (j == 0) {
-            if (half == 0) ok = ok && wait(&B.q_full[w], u.nth);
-          } else {                                      // in the place of the logits are the weights that the product before reads
-            ok = ok && wait(&B.pv_done[w][half], at - 1);
-          }
+          if (w == 1 && !u.two) continue;
+          if (j > 0) ok = ok && wait(&B.pv_done[w][half], u.done_of(w) + j - 1);   // in the place of the logits are the weights that the product before reads
+          else if (half == 0) ok = ok && wait(&B.q_full[w], u.begun_of(w));
           if (!ok) break;
-          if (u.tiles <= 0) continue;
           tc_fence_after();
           qk(s, w, half);
         }
-        if (!ok || u.tiles <= 0) break;
+        if (!ok) break;
         umma_commit(&B.empty[s]);
         umma_commit(&B.empty[s]);                       // (V's tiles have two readers)
       }
@@ -267,14 +272,15 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     const uint64_t v0 = make_smem_desc(ring_at, 16384u, 1024u);
     each_piece([&](const Unit& u) {
       bool ok = true;
+      if (w == 1 && !u.two) return true;
       for (int j = 0; j < u.tiles && ok; ++j) {
         const int at = u.done + j, s = (2 * at + 1) % kSlots;
         const int left = u.n - (u.t0 + j) * kMaTile, steps = left >= kMaTile ? 8 : (left + 15) / 16;   // of 16 rows that are there
         const uint64_t b0 = v0 + (uint64_t)(s * (C::kTileBytesD >> 4));
-        ok = there(2 * at + 1);
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-          ok = ok && wait(&B.p_full[w][half], at);
+          // (V's barrier is looked at behind the weights', when the phase before this tile's is known to be over)
+          ok = ok && wait(&B.p_full[w][half], u.done_of(w) + j) && (half > 0 || there(2 * at + 1));
           if (!ok) break;
           tc_fence_after();
 #pragma unroll
@@ -284,6 +290,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           umma_commit(&B.pv_done[w][half]);
         }
         if (ok) umma_commit(&B.empty[s]);
+        if (ok && !u.two) umma_commit(&B.empty[s]);     // (for the other tile, which has no rows)
       }
       return ok;
     });
@@ -304,7 +311,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         for (; x < end; ++x) {
           const int s = x % kSlots, row = (u.t0 + ((x - 2 * u.done) >> 1)) * kMaTile;
           // at first no more than a tile of each, ahead of the queries, which all wait for
-          if (x == 2) ok = __all_sync(0xffffffffu, wait(&B.q_full[0], u.nth) && wait(&B.q_full[1], u.nth));
+          if (x == 2) ok = __all_sync(0xffffffffu, wait(&B.q_full[0], u.begun) && (!u.two || wait(&B.q_full[1], u.begun2)));
           if (!ok) break;
           // the verdict is the warp's: it clears rows together
           ok = x < kSlots || __all_sync(0xffffffffu, wait(&B.empty[s], x / kSlots - 1));
@@ -343,8 +350,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kMaSoftmaxRegs));
     each_piece([&](const Unit& u) {
       // ---------------- softmax: a query row per thread ----------------
-      const int tiles = u.tiles, done = u.done, R = (int)c.rows();
-      const int w = warp >> 2, r = threadIdx.x & 127, rho = u.rho0 + w * 128 + r;
+      const int w = warp >> 2, done = u.done_of(w), tiles = w == 0 || u.two ? u.tiles : 0, R = (int)c.rows();
+      const int r = threadIdx.x & 127, rho = u.rho0 + w * 128 + r;
       const uint32_t row_lane = (uint32_t)(warp & 3) << 21;          // lanes 32 (warp % 4) .. of tensor memory, in bits 16 up
       const uint32_t s_tm = tmem + row_lane + (uint32_t)w * 128u, o_tm = tmem + row_lane + kO + (uint32_t)w * kD;
       const CrossRow mine = cross_row(c, u.b, rho < R ? rho : 0);
@@ -374,7 +381,8 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         fence_proxy_async_smem();
       }
-      warp_arrive(&B.q_full[w]);                        // (once per piece, whether it has tiles or not)
+      // (Only where somebody waits for it: nobody may be two phases ahead of who waits for one.)
+      if (tiles > 0) warp_arrive(&B.q_full[w]);
       const float f = c.scale * kLog2e;
       float ref = -INFINITY, l = 0.f;                   // weights are 2^(logit - ref)
       bool ok = true;
@@ -426,7 +434,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           }
         }
         // The tiles' warpgroups take turns at the exponentials: while one is at them, the other loads and looks for the maximum.
-        if (w == 1 || 2 * at + half > 0) ok = __all_sync(0xffffffffu, wait(&B.turn[w], 2 * at + half - (w == 0)));
+        if (u.two && (w == 1 || u.done2 + j2 > 0)) ok = __all_sync(0xffffffffu, wait(&B.turn[w], 2 * u.done2 + j2 - (w == 0)));
         if (!ok) break;
         const float m_use = ref == -INFINITY ? 0.f : ref;               // only logits of -inf so far: they weigh nothing
         const f32x2 ff = f2_make(f, f), minus_m = f2_make(-m_use, -m_use);
@@ -444,7 +452,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
             p[y / 2 + 1] = pack_bf16x2(e2, e3);
           }
           tmem_st16(s_half + x / 2, p);                 // P where S has been read already
-          if (x == 0) warp_arrive(&B.turn[1 - w]);
+          if (x == 0 && u.two) warp_arrive(&B.turn[1 - w]);
         }
         tmem_wait_st();
         tc_fence_before();
@@ -466,6 +474,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
           float4* const to = reinterpret_cast<float4*>(part) + w * 128 + r;
 #pragma unroll
           for (int x = 0; x < kD / 32; ++x) {
+            if (tiles <= 0) break;                      // (none of its rows is there)
             float o[32];
             tmem_ld32(o_tm + x * 32, o);
             tmem_wait_ld();
