@@ -47,13 +47,15 @@ cudaError_t launch_cross_simt(const CrossProblem& c, bool f32, float* part, int 
 cudaError_t cross_few_init();
 bool cross_few_supported(const CrossProblem& c);
 size_t cross_few_bytes(const CrossProblem& c, int sm_count);
+double cross_few_us(const CrossProblem& c, const int* clusters_of);   // about how long it would take
 cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, int sm_count, const int* clusters_of, long long wait_limit, unsigned int* dev_status,
                              cudaStream_t st, int* launches);
-// the same on tcgen05, 256 query rows per pass: from kManyRows of them on
-constexpr int kManyRows = 65;
+// the same on tcgen05, 256 query rows per pass: from kManyRows of them on, where it takes less time
+constexpr int kManyRows = 33;
 cudaError_t cross_many_init();
 bool cross_many_supported(const CrossProblem& c);
 size_t cross_many_bytes(const CrossProblem& c, int sm_count);
+double cross_many_us(const CrossProblem& c, int sm_count);
 cudaError_t launch_cross_many(void* state, const CrossProblem& c, float* part, int sm_count, long long wait_limit, unsigned int* dev_status, cudaStream_t st);
 
 }  // namespace restkv

@@ -32,6 +32,7 @@ constexpr float kFewSlack = 8.f;                // log2 of what weights may grow
 struct CrossFewArgs {
   CrossProblem c;
   float* part;                                  // per CTA two of: o [rows, d], (m, l) [rows]; without clusters
+  int2* begins;                                 // per CTA: unit and tile of it that it begins with; -1: none
   unsigned int* dev_status;
   int row_tiles;                                // units per KV head
   int cluster;                                  // CTAs per unit, 0: tiles of all units end to end
@@ -117,6 +118,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
       if (lane == 0) {
         piece_s.run = run;
         if (run.tile < run.end) piece_s.cut(few_units(c, a.row_tiles), tiles_of);
+        a.begins[blockIdx.x] = run.tile < run.end ? make_int2(piece_s.unit, piece_s.t0) : make_int2(-1, 0);
       }
     }
     __syncthreads();
@@ -434,81 +436,18 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
   }
 }
 
-// grid (units, rows), block 2 kD: joins what several CTAs left of a unit, 8 pieces at a time (kD / 4 threads each).
-template <int kD, int kRows>
-__global__ void __launch_bounds__(2 * kD) cross_few_combine_kernel(const __grid_constant__ CrossFewArgs a, int grid, int tile_rows) {
-  grid_dependency_wait();
-  grid_dependency_launch();
-  __shared__ int run_s[2];
-  __shared__ float2 ml_s[kMaxCtas];
-  __shared__ float4 acc_s[8][kD / 4];
-  const CrossProblem& c = a.c;
-  const int unit = blockIdx.x, row = blockIdx.y, bh = unit / a.row_tiles, rho = (unit - bh * a.row_tiles) * kRows + row;
-  if (rho >= (int)c.rows()) return;
-  const int units = few_units(c, a.row_tiles), entry = unit / units;
-  const int b = bh / c.Hkv, h = bh - b * c.Hkv, lane = threadIdx.x & 31;
-  if (threadIdx.x < 32) {
-    // where the unit's entry begins, by the same sums as in the kernel before
-    int before = 0, all = 0;
-    const int entries = few_entries(c);
-    for (int e = threadIdx.x; e < entries; e += 32) {
-      const int t = few_tiles(c, e, tile_rows) * units;
-      all += t;
-      if (e < entry) before += t;
-    }
-    all = __reduce_add_sync(0xffffffffu, all);
-    before = __reduce_add_sync(0xffffffffu, before);
-    if (threadIdx.x == 0) { run_s[0] = all; run_s[1] = before; }
-  }
-  const int tiles = few_tiles(c, entry, tile_rows);
-  __syncthreads();
-  const Deal deal(run_s[0], grid, kFewSnap);
-  const int u0 = run_s[1] + (unit - entry * units) * tiles;
-  const int x0 = deal.first_of(u0, tiles), pieces = deal.last_of(u0, tiles) - x0 + 1;
-  if (pieces == 1) return;                      // it was one CTA's: written
-  constexpr int kSlot = kRows * (kD + 2);
-  auto piece = [&](int x) { return a.part + (2ll * (x0 + x) + (x == 0)) * kSlot; };
-  const int sub = threadIdx.x / (kD / 4), v = threadIdx.x % (kD / 4);
-  constexpr int kAhead = 5;                     // requested before the factors are known
-  float4 o[kAhead];
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k)
-    if (sub + 8 * k < pieces) o[k] = __ldcg(reinterpret_cast<const float4*>(piece(sub + 8 * k) + row * kD) + v);
-  for (int x = threadIdx.x; x < pieces; x += 2 * kD) ml_s[x] = __ldcg(reinterpret_cast<const float2*>(piece(x) + kRows * kD) + row);
-  __syncthreads();
-  float mm = -INFINITY, ll = 0.f;
-  for (int x = lane; x < pieces; x += 32) mm = fmaxf(mm, ml_s[x].x);
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor_sync(0xffffffffu, mm, off));
-  auto factor = [&](int x) { return ml_s[x].x == -INFINITY ? 0.f : ex2_approx(ml_s[x].x - mm); };
-  for (int x = lane; x < pieces; x += 32) ll = fmaf(ml_s[x].y, factor(x), ll);
-#pragma unroll
-  for (int off = 16; off > 0; off >>= 1) ll += __shfl_xor_sync(0xffffffffu, ll, off);
-  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-  for (int k = 0; k < kAhead; ++k)
-    if (sub + 8 * k < pieces) fma4(acc, o[k], factor(sub + 8 * k));
-  for (int x = sub + 8 * kAhead; x < pieces; x += 8) fma4(acc, __ldcg(reinterpret_cast<const float4*>(piece(x) + row * kD) + v), factor(x));
-  acc_s[sub][v] = acc;
-  __syncthreads();
-  if (sub != 0) return;
-#pragma unroll
-  for (int k = 1; k < 8; ++k) fma4(acc, acc_s[k][v], 1.f);
-  few_write<kD>(c, b, h, rho, v, acc, mm, ll);
-}
-
 // ---- host ----
 struct FewVariant {
   void (*kernel)(CUtensorMap, CUtensorMap, CrossFewArgs);
   void (*in_clusters)(CUtensorMap, CUtensorMap, CrossFewArgs);
-  void (*combine)(CrossFewArgs, int, int);
+  cudaError_t (*merge)(const CrossProblem&, const float*, const int2*, int, int, cudaStream_t);
   int d, rows, tile_rows, threads, cluster_threads, per_sm;
   size_t smem, cluster_smem;
 };
 template <int kD, int kNT> FewVariant few_variant() {
   using C = FewConfig<kD, kNT, false>;
   using K = FewConfig<kD, kNT, true>;
-  return FewVariant{cross_few_kernel<kD, kNT, false>, cross_few_kernel<kD, kNT, true>, cross_few_combine_kernel<kD, C::kRows>, kD, C::kRows, C::kTileRows, C::kThreads, K::kThreads,
+  return FewVariant{cross_few_kernel<kD, kNT, false>, cross_few_kernel<kD, kNT, true>, launch_merge<kD, C::kRows>, kD, C::kRows, C::kTileRows, C::kThreads, K::kThreads,
                     C::kPerSm, C::kSmem, K::kSmem};
 }
 int few_ctas(const FewVariant& v, int sm_count) { return v.per_sm * sm_count < kMaxCtas ? v.per_sm * sm_count : kMaxCtas; }
@@ -520,17 +459,24 @@ bool pick_few(const CrossProblem& c, long long rows, FewVariant* v) {
   return true;
 }
 
-// CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units.  The largest cluster that lets all units run at once;
-// then by the time that each way takes at the longest sources that there may be, in us: fixed 6 and 12 (the second has another kernel behind
-// it), and the bytes at what its CTAs draw.  A cluster lasts as long as its own source, so that sources of different lengths speak for dealing out.
-int few_cluster(const CrossProblem& c, const FewVariant& v, long long units, const int* clusters_of) {
-  int i = 4;
-  while (i >= 0 && units > clusters_of[i]) --i;
-  if (i < 1) return 0;
-  const double mb = 4e-6 * (double)units * c.n_rows * c.d;
+// How a call would run: CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units, and about how long, in us.  Fixed 6, and 12 or 16
+// (these have another kernel behind them), and the bytes at what HBM and the CTAs draw: by the tiles of query rows, 0.09, 0.07 or 0.044 TB/s each.
+// A cluster lasts as long as its own source, so that sources of different lengths speak for dealing out.  Measured, 8 KV heads of 128 with 32 query rows,
+// 30000 rows: clusters of 4 90.0 us, of 8 50.9, dealt out 36.0; 4000 rows 18.8, 13.9, 17.4; 16 query rows over 1500 rows 8.9, 8.3, 13.0.
+struct FewWay {
+  int cluster;
+  double us;
+};
+FewWay few_way(const CrossProblem& c, const FewVariant& v, long long units, const int* clusters_of) {
+  const double mb = 4e-6 * (double)units * c.n_rows * c.d, each = v.rows == 8 ? 0.09 : v.rows == 16 ? 0.07 : 0.044;
   const double fill = c.lengths && (c.sources > 1 || c.per_head) ? 0.8 : 1.0;
-  const double in_clusters = 6.0 + mb / fmin(0.085 * (double)(units << i), 5.5), dealt = 12.0 + fill * mb / 6.1;
-  return in_clusters < dealt ? 1 << i : 0;
+  FewWay best{0, (v.rows == 32 ? 16.0 : 12.0) + fill * mb / fmin(118.0 * each, 6.1)};
+  for (int i = 1; i < 5; ++i) {
+    if (units > clusters_of[i]) break;
+    const double us = 6.0 + mb / fmin(each * (double)(units << i), 5.5);
+    if (us < best.us) best = FewWay{1 << i, us};
+  }
+  return best;
 }
 
 }  // namespace
@@ -557,10 +503,16 @@ bool cross_few_supported(const CrossProblem& c) {
   return ((long long)c.n_rows / v.tile_rows + 1) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }
 
+double cross_few_us(const CrossProblem& c, const int* clusters_of) {
+  FewVariant v;
+  if (!pick_few(c, c.rows(), &v)) return INFINITY;
+  return few_way(c, v, (long long)c.sources * c.Hkv * ((c.rows() + v.rows - 1) / v.rows), clusters_of).us;
+}
+
 size_t cross_few_bytes(const CrossProblem& c, int sm_count) {
   FewVariant v;
   if (!pick_few(c, c.rows(), &v)) return 0;
-  return (size_t)2 * few_ctas(v, sm_count) * v.rows * (v.d + 2) * sizeof(float);
+  return (size_t)few_ctas(v, sm_count) * (2 * v.rows * (v.d + 2) * sizeof(float) + sizeof(int2));
 }
 
 cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, int sm_count, const int* clusters_of, long long wait_limit, unsigned int* dev_status,
@@ -573,7 +525,7 @@ cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, in
   a.c = c; a.part = part; a.dev_status = dev_status; a.wait_limit = wait_limit;
   a.row_tiles = (int)((c.rows() + v.rows - 1) / v.rows);
   const long long units = (long long)c.sources * c.Hkv * a.row_tiles;
-  a.cluster = few_cluster(c, v, units, clusters_of);
+  a.cluster = few_way(c, v, units, clusters_of).cluster;
   *launches = 1;
   if (a.cluster) {
     cudaLaunchConfig_t cfg = {};
@@ -592,10 +544,11 @@ cudaError_t launch_cross_few(void* state, const CrossProblem& c, float* part, in
     return cudaLaunchKernelEx(&cfg, v.in_clusters, tmK, tmV, a);
   }
   const int ctas = few_ctas(v, sm_count);
+  a.begins = reinterpret_cast<int2*>(part + (size_t)2 * ctas * v.rows * (v.d + 2));
   const cudaError_t e = launch_chained(v.kernel, dim3((unsigned int)ctas), v.threads, v.smem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
   *launches = 2;
-  return launch_chained(v.combine, dim3((unsigned int)units, (unsigned int)v.rows), 2 * v.d, 0, st, a, ctas, v.tile_rows);
+  return v.merge(c, part, a.begins, a.row_tiles, ctas, st);
 }
 
 }  // namespace restkv

@@ -527,98 +527,6 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   if (warp == kMaSoftmax + 1) tmem_dealloc(tmem, 512);
 }
 
-// grid (CTAs of the kernel before, 8), block 256: merges what several of them left of a unit, four rows per warp (one: 4700 blocks in four waves,
-// each as long as its chain of loads).  A unit is merged by the blocks of the first CTA that began inside it.
-template <int kD>
-__global__ void __launch_bounds__(256) cross_many_combine_kernel(const __grid_constant__ CrossManyArgs a) {
-  grid_dependency_wait();
-  grid_dependency_launch();
-  const CrossProblem& c = a.c;
-  const int x = blockIdx.x, ctas = gridDim.x, lane = threadIdx.x & 31;
-  const int2 mine = __ldcg(a.begins + x), before = x > 0 ? __ldcg(a.begins + x - 1) : make_int2(-1, 0);
-  if (mine.x < 0 || mine.y == 0) return;                // (the first CTA begins a unit: x > 0 from here on)
-  if (before.x == mine.x && before.y > 0) return;
-  constexpr int kAtOnce = 4, kPer = kD / 32;
-  const int unit = mine.x, row0 = (int)blockIdx.y * 8 * kAtOnce + (int)(threadIdx.x >> 5) * kAtOnce, bh = unit / a.row_tiles, b = bh / c.Hkv, h = bh - b * c.Hkv;
-  const int rho0 = (unit - bh * a.row_tiles) * kMaRows + row0, left = (int)c.rows() - rho0;
-  if (left <= 0) return;
-  constexpr long long kSlot = kMaRows * (kD + 2);
-  auto piece = [&](int k) { return a.part + (2ll * (x - 1 + k) + (k == 0)) * kSlot; };   // the CTA before began the unit
-  // 32 pieces at a time, a lane's (reference, sum) each
-  float mm[kAtOnce], ll[kAtOnce], acc[kAtOnce][kPer];
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) {
-    mm[i] = -INFINITY;
-    ll[i] = 0.f;
-#pragma unroll
-    for (int z = 0; z < kPer; ++z) acc[i][z] = 0.f;
-  }
-  for (int base = 0;; base += 32) {
-    const int k = base + lane;
-    bool some = k == 0;
-    if (k > 0 && x - 1 + k < ctas) {
-      const int2 o = __ldcg(a.begins + x - 1 + k);
-      some = o.x == mine.x && o.y > 0;
-    }
-    const int n = __popc(__ballot_sync(0xffffffffu, some));
-    float f[kAtOnce];
-    float2 ml[kAtOnce];
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i)                   // (a slot has all 256 rows)
-      ml[i] = some ? __ldcg(reinterpret_cast<const float2*>(piece(k) + kMaRows * kD) + row0 + i) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-    for (int i = 0; i < kAtOnce; ++i) {
-      if (i >= left) ml[i] = make_float2(-INFINITY, 0.f);   // rows that there are not: nobody wrote them
-      float top = ml[i].x;
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-      top = fmaxf(top, mm[i]);
-      const float down = mm[i] == -INFINITY ? 0.f : ex2_approx(mm[i] - top);
-      f[i] = ml[i].x == -INFINITY ? 0.f : ex2_approx(ml[i].x - top);
-      mm[i] = top;
-      float sum = ml[i].y * f[i];
-#pragma unroll
-      for (int off = 16; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-      ll[i] = fmaf(ll[i], down, sum);
-#pragma unroll
-      for (int z = 0; z < kPer; ++z) acc[i][z] *= down;
-    }
-#pragma unroll 2
-    for (int y = 0; y < n; ++y)
-#pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
-        const float g = __shfl_sync(0xffffffffu, f[i], y);
-        const float* o = piece(base + y) + (kPer * lane / 4 * kMaRows + row0 + i) * 4 + kPer * lane % 4;
-        float w[kPer];
-        if constexpr (kPer == 4) {
-          const float4 u = __ldcg(reinterpret_cast<const float4*>(o));
-          w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w;
-        } else {
-          const float2 u = __ldcg(reinterpret_cast<const float2*>(o));
-          w[0] = u.x; w[1] = u.y;
-        }
-#pragma unroll
-        for (int z = 0; z < kPer; ++z) acc[i][z] = g > 0.f ? fmaf(w[z], g, acc[i][z]) : acc[i][z];
-      }
-    if (n < 32) break;
-  }
-#pragma unroll
-  for (int i = 0; i < kAtOnce; ++i) {
-    if (i >= left) break;
-    const CrossRow r = cross_row(c, b, rho0 + i);
-    const bool some = ll[i] > 0.f && cross_live(c, r);
-    const long long at = cross_out_row(c, r, h);
-    const float norm = some ? 1.f / ll[i] : 0.f;
-    uint32_t y[kPer / 2];
-#pragma unroll
-    for (int z = 0; z < kPer / 2; ++z) y[z] = some ? pack_bf16x2(acc[i][2 * z] * norm, acc[i][2 * z + 1] * norm) : 0u;
-    __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD + kPer * lane;
-    if constexpr (kPer == 4) *reinterpret_cast<uint2*>(to) = make_uint2(y[0], y[1]);
-    else *reinterpret_cast<uint32_t*>(to) = y[0];
-    if (lane == 0 && c.lse) c.lse[at] = some ? fmaf(mm[i], 0.6931471805599453f, logf(ll[i])) : -INFINITY;
-  }
-}
-
 int many_ctas(int sm_count) { return sm_count < kMaxCtas ? sm_count : kMaxCtas; }
 
 }  // namespace
@@ -643,6 +551,13 @@ bool cross_many_supported(const CrossProblem& c) {
   return ((long long)c.n_rows / kMaTile + 1 + kMaAhead) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }
 
+// About how long a call takes: 6 us, and 2.95 (head_dim 64: 1.9) per tile of a CTA, of which it has four at least, and two for ends and beginnings of units.  Measured, 8 sources x 8
+// KV heads of 128, 128 query rows: 500 rows 18 us, 4000 rows 53 (in passes of 32 rows 66 and 145); one source: 4000 rows 36, 30000 71 (20 and 100).
+double cross_many_us(const CrossProblem& c, int sm_count) {
+  const double units = (double)c.sources * c.Hkv * (double)((c.rows() + kMaRows - 1) / kMaRows), tiles = units * ((c.n_rows + kMaTile - 1) / kMaTile) / sm_count + 2.0;
+  return 6.0 + (c.d == 64 ? 1.9 : 2.95) * (tiles > 4.0 ? tiles : 4.0);
+}
+
 size_t cross_many_bytes(const CrossProblem& c, int sm_count) {
   if (!cross_many_shape(c)) return 0;
   return (size_t)many_ctas(sm_count) * (2 * kMaRows * (c.d + 2) * sizeof(float) + sizeof(int2));
@@ -659,8 +574,7 @@ cudaError_t launch_cross_many(void* state, const CrossProblem& c, float* part, i
   const cudaError_t e = c.d == 64 ? launch_chained(cross_many_kernel<64>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<64>::kSmem, st, tmK, tmV, a)
                                   : launch_chained(cross_many_kernel<128>, dim3((unsigned int)ctas), kMaThreads, ManyConfig<128>::kSmem, st, tmK, tmV, a);
   if (e != cudaSuccess) return e;
-  const dim3 grid((unsigned int)ctas, kMaRows / 32);
-  return c.d == 64 ? launch_chained(cross_many_combine_kernel<64>, grid, 256, 0, st, a) : launch_chained(cross_many_combine_kernel<128>, grid, 256, 0, st, a);
+  return c.d == 64 ? launch_merge<64, kMaRows>(c, part, a.begins, a.row_tiles, ctas, st) : launch_merge<128, kMaRows>(c, part, a.begins, a.row_tiles, ctas, st);
 }
 
 }  // namespace restkv
