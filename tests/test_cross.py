@@ -265,6 +265,48 @@ def test_cross_in_fp32_throughout_and_where_the_tensor_cores_are_required(handle
         handle.set_kernel_path(rk.PATH_AUTO)
 
 
+# sources, beams, query heads, KV heads, head_dim, tokens, rows
+SHARED = [(1, 1, 32, 8, 128, 9, 9000), (1, 3, 16, 16, 64, 11, 5000), (1, 1, 12, 4, 128, 11, 30000), (1, 33, 8, 8, 64, 1, 12345), (4, 2, 12, 4, 128, 11, 1200), (8, 1, 32, 8, 128, 10, 600),
+          (1, 1, 8, 2, 128, 60, 20000), (2, 1, 4, 4, 64, 256, 4100), (2, 1, 4, 4, 128, 257, 4100), (1, 1, 3, 1, 64, 43, 40000), (5, 7, 4, 2, 128, 17, 2000), (1, 1, 1, 1, 64, 33, 1)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", SHARED)
+def test_cross_units_shared_by_few_and_many_ctas(handle, spec):
+    S, beams, Hq, Hkv, d, t, m = spec
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, torch.bfloat16, 15, 1.5)
+    try:
+        handle.set_kernel_path(rk.PATH_TENSOR_CORE)
+        check(handle, Q, K, V)
+        check(handle, Q, K, V, [m - m // (3 + i) * (i > 0) for i in range(S)], [(5 * i + t) % (t + 1) if i else t for i in range(S * beams)])
+    finally:
+        handle.set_kernel_path(rk.PATH_AUTO)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("d,t,most", [(128, 300, 1500), (64, 150, 700), (128, 1, 4000), (64, 6, 9000), (128, 40, 500)])
+@pytest.mark.parametrize("kept", [0, 1, 3, 20])
+def test_cross_of_sources_that_are_mostly_empty(handle, d, t, most, kept):
+    """30 sources, of which some have rows, and sequences without tokens: units without work ahead of, between and behind those with it."""
+    r = np.random.default_rng(100 * kept + t)
+    lengths, counts = np.zeros((30, 2), int), np.zeros(60, int)
+    for i in r.choice(30, kept, replace=False):
+        lengths[i] = r.integers(0, most + 1, 2)
+        counts[2 * i:2 * i + 2] = r.choice([0, 1, t // 2, t], 2)
+    Q, K, V = make(30, 2, 4, 2, d, t, most, torch.bfloat16, 16, 1.0)
+    check(handle, Q, K, V, lengths, counts)
+    check(handle, Q, K, V, lengths[:, 0], counts)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", [(1, 4, 8, 2, 128, 1, 1000), (2, 8, 4, 4, 64, 1, 3000), (1, 4, 32, 8, 128, 1, 40000), (1, 2, 8, 1, 64, 2, 20000), (3, 1, 4, 4, 128, 30, 700)])
+def test_cross_weights_of_few_query_rows_have_two_parts(handle, spec):
+    S, beams, Hq, Hkv, d, t, m = spec
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, torch.bfloat16, 17, 2.0)
+    V.abs_()                                     # nothing cancels: the output's rounding and the weights' are all there is
+    check(handle, Q, K, V, closely=True)
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("S,beams,Hq,Hkv,d,t,m", [(1, 4, 32, 8, 128, 1, 3000), (1, 4, 32, 8, 128, 1, 40000), (1, 1, 8, 2, 128, 300, 3001), (3, 1, 8, 2, 64, 500, 700), (1, 8, 8, 2, 64, 1, 9000)])
 def test_cross_waits_that_run_out(handle, S, beams, Hq, Hkv, d, t, m):
