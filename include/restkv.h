@@ -481,6 +481,7 @@ restkv_status restkv_paged_read(restkv_handle* h, const restkv_paged* cache, con
 /*
  * Decoding with beams: several hypotheses of a request at a time.  (No counterpart in the paper: what a loop over the cache above does when it
  * keeps more than the one most likely continuation.)  Sequences of the cache are the hypotheses, those of a request side by side.
+ * These calls, and restkv_cross_attend, return RESTKV_ERR_INVALID_ARG where the handle's device is not the current one.
  */
 typedef struct {
   int batch, beams, vocab; /* requests; hypotheses of each, at most 64; tokens */
@@ -500,7 +501,8 @@ size_t restkv_beam_workspace_bytes(const restkv_beams* beams);
  *   scores      device float [batch, beams]: what the hypotheses have summed up so far
  *   finished    optional device uint8 [batch, beams]: a hypothesis that has ended (not 0) has one continuation, pad_token, with the score as it is; its
  *               logits are not read
- *   parents, tokens, scores_out   device int32, int32, float [batch, n_out]: which hypothesis, by which token, with which score
+ *   parents, tokens, scores_out   device int32, int32, float [batch, n_out]: which hypothesis, by which token, with which score; scores_out may be
+ *               `scores` where n_out == beams
  * Scores are compared in 64 bits (the normalisers are sums of fp32 exponentials).  Ties go to the lower hypothesis, in one hypothesis to the larger
  * logit and then the lower token: one order, whatever the order in which blocks end.
  * A NaN among the logits counts as -inf, +inf as the largest finite number; a NaN among the scores counts as -inf.  A continuation by a logit of
@@ -572,9 +574,9 @@ size_t restkv_cross_workspace_bytes(const restkv_cross* cross, int n_tokens);
  * A token of a source without rows, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32.  The same
  * call gives the same bits.
  * head_dim: a multiple of 8, at most 256 (else RESTKV_ERR_UNSUPPORTED).  RESTKV_BF16 with head_dim 64 or 128 runs on the tensor cores (K and V
- * with no stride of 0): few query rows beams * n_tokens * group of a KV head with weights of two bf16 parts (16 bits), many with weights of one
- * bf16 (as an output has, too).  Everything else, and restkv_set_kernel_path(1), runs in fp32 throughout, and returns RESTKV_ERR_UNSUPPORTED under
- * restkv_set_kernel_path(2 or 3).
+ * with no stride of 0): up to 32 query rows beams * n_tokens * group of a KV head with weights of two bf16 parts (16 bits); more with weights of
+ * one bf16 (as an output has, too) where that takes less time, which goes by the sizes alone.  Everything else, and restkv_set_kernel_path(1),
+ * runs in fp32 throughout, and returns RESTKV_ERR_UNSUPPORTED under restkv_set_kernel_path(2 or 3).
  */
 restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, int n_tokens, const restkv_rows* Q, const restkv_rows* K,
                                   const restkv_rows* V, const int32_t* lengths, const int32_t* counts, void* out, float* lse, void* workspace,

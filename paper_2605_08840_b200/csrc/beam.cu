@@ -24,6 +24,7 @@ constexpr int kBeThreads = 256, kBeWarps = kBeThreads / 32, kBePerSm = 5;
 constexpr int kGroups = kBeThreads / 4;         // at least kBeamOut
 constexpr int kList = 2048, kJoinList = 512;
 constexpr float kLog2e = 1.4426950408889634f;
+static_assert((kGroups & (kGroups - 1)) == 0, "places turn round");
 static_assert(kGroups >= kBeamOut, "a threshold needs as many groups as continuations");
 
 typedef unsigned long long u64;
@@ -274,12 +275,14 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
     __syncthreads();
     count = count_s;
   }
-  u64* const list = lists + (long long)blockIdx.x * p.n_out;
+  // a request's lists side by side: place k of all of them, then place k + 1
+  const int request = row / p.beams, side = p.beams * slices;
+  u64* const list = lists + (long long)request * side * p.n_out + ((int)blockIdx.x - request * side);
   if (count <= kList) {
     rank(count, [&](int x, int y) { return list_s[y] > list_s[x]; }, [&](int x, int before) {
-      if (before < p.n_out) list[before] = list_s[x];
+      if (before < p.n_out) list[before * side] = list_s[x];
     });
-    for (int x = count + t; x < p.n_out; x += kBeThreads) list[x] = 0;
+    for (int x = count + t; x < p.n_out; x += kBeThreads) list[x * side] = 0;
   } else {
     u64 last = ~0ull;
     for (int k = 0; k < p.n_out; ++k) {
@@ -301,7 +304,7 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
       last = best_s[0];
 #pragma unroll
       for (int w = 1; w < kBeWarps; ++w) last = best_s[w] > last ? best_s[w] : last;
-      if (t == 0) list[k] = last;             // (more than kList candidates: never 0)
+      if (t == 0) list[k * side] = last;             // (more than kList candidates: never 0)
     }
   }
   if (t == 0) {
@@ -329,7 +332,7 @@ __device__ __forceinline__ double score_of(u64 bits) { return __longlong_as_doub
 
 // grid: requests
 template <typename T>
-__global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem p, int slices, const SliceStats* __restrict__ stats, const u64* __restrict__ lists) {
+__global__ void __launch_bounds__(kBeThreads, 4) beam_join_kernel(const BeamProblem p, int slices, const SliceStats* __restrict__ stats, const u64* __restrict__ lists) {
   __shared__ __align__(16) float group_s[kGroups];
   __shared__ float limit_s;
   __shared__ int count_s, kind_s[kBeamsPerRequest];
@@ -340,16 +343,19 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
   grid_dependency_wait();
   grid_dependency_launch();
   if (t == 0) count_s = 0;
-  // Candidate x of the request: hypotheses one after the other, each with the lists of its slices.  A thread has kHeld of 256 kHeld at a time, the
-  // first on their way before the normalisers are known.
+  // Candidate x of the request: the firsts of all slices of all hypotheses, then the seconds ...; so the groups whose largest make the limit have the
+  // same share of the firsts (by lists one after the other, the 64th of 64 groups had lasts of lists only: 2300 us for 64 of 64 hypotheses).
+  // A thread holds kHeld of the first 256 kHeld, on their way before the normalisers are known.
   constexpr int kHeld = 8;
-  const int per_row = slices * n_out, all = p.beams * per_row;
-  u64 key[kHeld];
+  const int side = p.beams * slices, all = side * n_out;
+  // 64 in turn to the 64 groups, each time 16 groups on: the four of a group come from different slices wherever there are several
+  const int place = (t & 3) * kGroups + (((t >> 2) + kGroups / 4 * (t & 3)) & (kGroups - 1));
+  u64 held[kHeld];
   auto hold = [&](int base) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-      const int x = base + i * kBeThreads + t;
-      key[i] = x < all ? __ldcg(lists + (long long)row0 * per_row + x) : 0;
+      const int x = base + i * kBeThreads + place;
+      held[i] = x < all ? __ldcg(lists + (long long)blockIdx.x * all + x) : 0;
     }
   };
   hold(0);
@@ -394,25 +400,31 @@ __global__ void __launch_bounds__(kBeThreads) beam_join_kernel(const BeamProblem
   };
   auto key_at = [&](int k, int x, u64 key) {      // 0: no candidate
     const int kind = kind_s[k];
-    return kind == 0 ? key : kind == 1 && x == k * per_row ? make_key(0.f, p.pad_token) : 0;
+    return kind == 0 ? key : kind == 1 && x == k * slices ? make_key(0.f, p.pad_token) : 0;
   };
   auto candidate = [&](int k, u64 key) {
     return Candidate{score_bits(kind_s[k] == 0 ? (double)score_s[k] + ((double)key_logit(key) - total_s[k]) : (double)score_s[k]), key, k};
   };
-  auto each = [&](auto&& use) {                   // over what is held
+  // a / b, b > 0, for which 1 / b is given: a below 2^21 by a product that is off by less than half of 1 / b
+  auto quotient = [&](int a, int b, float inverse) { return all <= 1 << 21 ? (int)(((float)a + 0.5f) * inverse) : a / b; };
+  const float per_side = 1.f / (float)side, per_slice = 1.f / (float)slices;
+  auto some = [&](int base, auto&& use) {
 #pragma unroll
     for (int i = 0; i < kHeld; ++i) {
-      const int x = i * kBeThreads + t;
+      const int x = base + i * kBeThreads + place;
       if (x >= all) break;
-      const int k = x / per_row;
-      const u64 own = key_at(k, x, key[i]);
+      const int k = quotient(x - quotient(x, side, per_side) * side, slices, per_slice);
+      const u64 own = key_at(k, x, held[i]);
       if (own) use(k, own);
     }
-    if (all <= kHeld * kBeThreads) return;
-    for (int x = kHeld * kBeThreads + t; x < all; x += kBeThreads) {
-      const int k = x / per_row;
-      const u64 own = key_at(k, x, __ldcg(lists + (long long)row0 * per_row + x));
-      if (own) use(k, own);
+  };
+  bool first = true;                              // what is held is where `each` begins
+  auto each = [&](auto&& use) {
+#pragma unroll 1
+    for (int base = 0; base < all; base += kHeld * kBeThreads) {
+      if (!first) hold(base);
+      some(base, use);
+      first = all <= kHeld * kBeThreads;
     }
   };
   float top = -INFINITY;

@@ -16,7 +16,7 @@ static restkv_status make_beams(const restkv_beams* s, BeamProblem* out) {
   p.f32 = s->dtype == RESTKV_F32;
   p.stride = s->stride ? s->stride : s->vocab;
   p.pad_token = s->pad_token;
-  // a block per 4096 tokens of a row at most, all in one grid
+  // a block per 2048 tokens of a row at most, all in one grid
   if ((long long)p.batch * p.beams > 0x7FFFFFFFll / (p.vocab / 2048 + 2)) return RESTKV_ERR_UNSUPPORTED;
   *out = p;
   return RESTKV_OK;
