@@ -116,6 +116,20 @@ def test_select(handle, spec, dtype, stride_pad):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("spec", [(1, 64, 20000, 64), (2, 33, 9001, 40), (3, 16, 4096, 64), (1, 1, 262144, 64), (2, 64, 4096, 63)])
+@pytest.mark.parametrize("spread", [0.0, 1.0, 30.0])
+def test_select_many_of_many(handle, spec, spread):
+    """More candidates than a block holds at a time, hypotheses of like scores and of such that one of them has nearly all."""
+    batch, beams, vocab, n_out = spec
+    rng = np.random.default_rng(vocab + int(spread))
+    logits = torch.from_numpy((rng.standard_normal((batch, beams, vocab)) * 2).astype(np.float32)).cuda().bfloat16()
+    finished = np.zeros((batch, beams), bool)
+    if beams > 2:
+        finished[:, 2::7] = True
+    check_select(handle, logits, -spread * rng.random((batch, beams)), n_out, finished)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("vocab,n_out", [(777, 12), (20001, 8), (40, 64)])
 def test_select_with_ended_and_absent_hypotheses(handle, dtype, vocab, n_out):
