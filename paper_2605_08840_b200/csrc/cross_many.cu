@@ -578,11 +578,13 @@ bool cross_many_supported(const CrossProblem& c) {
   return ((long long)c.n_rows / kMaTile + 1 + kMaAhead) * units <= 0x7FFFFFFFll;   // tiles are counted in 32 bits
 }
 
-// About how long a call takes: 6 us, and 2.95 (head_dim 64: 1.9) per tile of a CTA, of which it has four at least, and two for ends and beginnings of units.  Measured, 8 sources x 8
-// KV heads of 128, 128 query rows: 500 rows 18 us, 4000 rows 53 (in passes of 32 rows 66 and 145); one source: 4000 rows 36, 30000 71 (20 and 100).
+// About how long a call takes: 6 us, and 2.95 (head_dim 64: 1.9) per tile of a CTA, of which it has four at least or all of a unit's, and two for ends and
+// beginnings of units.  Measured, 8 sources x 8 KV heads of 128, 128 query rows: 500 rows 17 us, 4000 rows 54 (in passes of 32 rows 66 and 145); one
+// source: 4000 rows 21, 30000 44 (20 and 100); 4 sources of 100 rows, 80 query rows 14 (20).
 double cross_many_us(const CrossProblem& c, int sm_count) {
-  const double units = (double)c.sources * c.Hkv * (double)((c.rows() + kMaRows - 1) / kMaRows), tiles = units * ((c.n_rows + kMaTile - 1) / kMaTile) / sm_count + 2.0;
-  return 6.0 + (c.d == 64 ? 1.9 : 2.95) * (tiles > 4.0 ? tiles : 4.0);
+  const double units = (double)c.sources * c.Hkv * (double)((c.rows() + kMaRows - 1) / kMaRows), of_unit = (double)((c.n_rows + kMaTile - 1) / kMaTile);
+  const double tiles = units * of_unit / sm_count + 2.0, least = of_unit < 2.0 ? 3.0 : 4.0;
+  return 6.0 + (c.d == 64 ? 1.9 : 2.95) * (tiles > least ? tiles : least);
 }
 
 size_t cross_many_bytes(const CrossProblem& c, int sm_count) {
