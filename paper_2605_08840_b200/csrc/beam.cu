@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
   __shared__ __align__(16) float group_s[kGroups];
   __shared__ u64 group_key_s[kGroups], limit_key_s;
   __shared__ float limit_s, top_s[kBeWarps], sum_s[kBeWarps];
-  __shared__ int count_s, hits_s;
+  __shared__ int count_s, anew_s, hits_s;   // of the list, of the list as it is found anew: no counter is set back, for a warp may be late to read it
   __shared__ unsigned short hit_s[kBatches * kBeThreads];
   __shared__ u64 list_s[kList], best_s[kBeWarps];
   const int row = blockIdx.x / slices, slice = blockIdx.x - row * slices, t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
   const int piece0 = slice * (kBatches * kBatch * kBeThreads) + t, in_row = (int)(((long long)p.vocab * (int)sizeof(T) + off + 15) / 16);
   auto piece_of = [&](int b, int y) { return piece0 + (b * kBatch + y) * kBeThreads; };
   auto token_of = [&](int b, int e) { return piece_of(b, e / kPer) * kPer + e % kPer; };     // of the thread's e-th logit of batch b
-  if (t == 0) count_s = hits_s = 0;
+  if (t == 0) count_s = anew_s = hits_s = 0;
   float top = -INFINITY, sum = 0.f, most[kBatches];         // of the thread, and of its batches
 #pragma unroll
   for (int b = 0; b < kBatches; ++b) {
@@ -259,7 +259,6 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
       const u64 key = x > -INFINITY ? make_key(x, token_of(e / kMine, e % kMine)) : 0;
       best = key > best ? key : best;
     }
-    if (t == 0) count_s = 0;
     const u64 limit_key = nth_of_groups(best, p.n_out, group_key_s, limit_key_s);
     if (best >= limit_key && best > 0) {
 #pragma unroll 1
@@ -267,13 +266,13 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
         const float x = again(e / kMine, e % kMine);
         const u64 key = x > -INFINITY ? make_key(x, token_of(e / kMine, e % kMine)) : 0;
         if (key >= limit_key && key > 0) {
-          const int at = atomicAdd(&count_s, 1);
+          const int at = atomicAdd(&anew_s, 1);
           if (at < kList) list_s[at] = key;
         }
       }
     }
     __syncthreads();
-    count = count_s;
+    count = anew_s;
   }
   // a request's lists side by side: place k of all of them, then place k + 1
   const int request = row / p.beams, side = p.beams * slices;

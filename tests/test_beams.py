@@ -178,6 +178,28 @@ def test_select_ties(handle, dtype, vocab, n_out):
 
 @pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("batch,vocab", [(1, 9000), (40, 30000)])
+@pytest.mark.parametrize("low", [False, True])
+def test_select_of_more_equal_logits_than_a_list_holds_every_time(handle, dtype, batch, vocab, low):
+    """Slices of more than 2048 equal logits (the bound is found anew among logits with their tokens), and of such that one group of threads has only
+    lower ones (so that this bound holds back nothing either), call after call: the same continuations, by the order that the header states."""
+    beams, n_out = 3, 64
+    at = torch.arange(vocab, device="cuda") // (16 // torch.empty(0, dtype=dtype).element_size()) % 256
+    x = torch.where(at < 4, 0.0, 1.0).to(dtype) if low else torch.ones(vocab, dtype=dtype, device="cuda")
+    logits = x.expand(batch, beams, vocab)
+    want = check_select(handle, logits, np.zeros((batch, beams)), n_out, exact_ties=True)
+    desc = rk.make_beams(batch, beams, vocab, n_out, rk.F32 if dtype == torch.float32 else rk.BF16)
+    held, scores = logits.reshape(-1, vocab).contiguous(), torch.zeros(batch, beams, device="cuda")
+    ws = torch.empty(handle.beam_workspace_bytes(desc), dtype=torch.uint8, device="cuda")
+    for _ in range(50):
+        got = [torch.full_like(x, -7) for x in want]
+        handle.beam_select(desc, held, scores, *got, ws)
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+    assert handle.poll_status() == rk.RESTKV_OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("order", ["up", "down", "strided", "steps"])
 def test_select_where_the_largest_lie_close_together(handle, dtype, order):
     vocab = 33000
