@@ -571,8 +571,9 @@ size_t restkv_cross_workspace_bytes(const restkv_cross* cross, int n_tokens);
  *   out       device [sources * beams, n_q_heads, n_tokens, head_dim] contiguous, dtype
  *   lse       optional device float [sources * beams, n_q_heads, n_tokens]: natural-log sum of exp of the scaled logits; with out it is what
  *             restkv_evict_from_lse takes (causal_tail 0, beams 1, the last w tokens, out as float)
- * A token of a source without rows, and one past its sequence's count, gets 0 and -inf.  Logits, softmax statistics and sums are fp32.  The same
- * call gives the same bits.
+ * A token of a source without rows, and one past its sequence's count, gets 0 and -inf, as does one whose logits are all -inf.  A NaN or +inf among
+ * the logits of a token makes its outputs and its lse NaN; a value that is not finite makes the outputs that it enters not finite (of +-inf: NaN or
+ * inf).  Logits, softmax statistics and sums are fp32.  The same call gives the same bits.
  * head_dim: a multiple of 8, at most 256 (else RESTKV_ERR_UNSUPPORTED).  RESTKV_BF16 with head_dim 64 or 128 runs on the tensor cores (K and V
  * with no stride of 0): up to 32 query rows beams * n_tokens * group of a KV head with weights of two bf16 parts (16 bits); more with weights of
  * one bf16 (as an output has, too) where that takes less time, which goes by the sizes alone.  Everything else, and restkv_set_kernel_path(1),

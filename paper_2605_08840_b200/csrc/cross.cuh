@@ -27,6 +27,9 @@ __device__ __forceinline__ CrossRow cross_row(const CrossProblem& c, int source,
   return CrossRow{source * c.beams + beam, x - beam * c.n_tokens, rho - x * c.G};
 }
 __device__ __forceinline__ bool cross_live(const CrossProblem& c, const CrossRow& r) { return !c.counts || r.i < c.counts[r.seq]; }
+// Whether a query row has a result: rows of K that weigh something, or logits that are no numbers, which make the sum of the weights none (a logit of
+// +inf does, too: its weight is 2^(inf - inf)) and with it the row's outputs and log-sum-exp.
+__device__ __forceinline__ bool cross_some(const CrossProblem& c, const CrossRow& r, float l) { return l != 0.f && cross_live(c, r); }
 __device__ __forceinline__ int cross_length(const CrossProblem& c, int source, int h) {
   if (!c.lengths) return c.n_rows;
   const int n = c.lengths[c.per_head ? source * c.Hkv + h : source];

@@ -68,7 +68,7 @@ __device__ __forceinline__ int few_tiles(const CrossProblem& c, int entry, int t
 // Dims 4 v .. of a query row's result.
 template <int kD> __device__ __forceinline__ void few_write(const CrossProblem& c, int source, int h, int rho, int v, float4 acc, float mm, float ll) {
   const CrossRow r = cross_row(c, source, rho);
-  const bool some = ll > 0.f && cross_live(c, r);
+  const bool some = cross_some(c, r, ll);
   const long long at = cross_out_row(c, r, h);
   const float f = some ? 1.f / ll : 0.f;
   reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD)[v] =

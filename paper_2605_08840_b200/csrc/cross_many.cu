@@ -491,7 +491,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
       if (ok && tiles > 0) ok = __all_sync(0xffffffffu, wait(&B.pv_done[w][1], done + tiles - 1));
       if (ok) {
         tc_fence_after();
-        const bool whole = u.whole, some = l > 0.f && live;
+        const bool whole = u.whole, some = l != 0.f && live;   // (as cross_some)
         float* const part = a.part + (long long)(2 * blockIdx.x + (u.t0 == 0)) * kMaRows * (kD + 2);
         const long long row = cross_out_row(c, mine, u.h);
         __nv_bfloat16* const out = reinterpret_cast<__nv_bfloat16*>(c.out);

@@ -153,7 +153,7 @@ __global__ void __launch_bounds__(kThreads) cross_simt_kernel(const CrossProblem
     }
     if (splits == 1) {
       const CrossRow r = cross_row(c, b, rho);
-      const bool some = ll > 0.f && cross_live(c, r);
+      const bool some = cross_some(c, r, ll);
       const long long row = cross_out_row(c, r, h);
       const float v = some ? acc / ll : 0.f;
       if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(c.out)[row * c.d + dim] = v;
@@ -179,9 +179,9 @@ __global__ void cross_simt_combine_kernel(const CrossProblem c, int splits, cons
   for (int s = 0; s < splits; ++s) mm = fmaxf(mm, from[s * (c.d + 2)]);
   for (int s = 0; s < splits; ++s) {
     const float ms = from[s * (c.d + 2)];
-    if (ms != -INFINITY) ll += from[s * (c.d + 2) + 1] * __expf(ms - mm);
+    ll += ms == -INFINITY ? from[s * (c.d + 2) + 1] : from[s * (c.d + 2) + 1] * __expf(ms - mm);   // (0, or a sum that is no number)
   }
-  const bool some = ll > 0.f && cross_live(c, r);
+  const bool some = cross_some(c, r, ll);
   const long long row = cross_out_row(c, r, h);
   for (int k = threadIdx.x; k < c.d; k += blockDim.x) {
     float acc = 0.f;

@@ -111,7 +111,10 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossProblem c, 
     }
   };
   auto join = [&](int i, float2 ml, const float (&o)[kPer]) {
-    if (ml.x == -INFINITY) return;
+    if (ml.x == -INFINITY) {               // nothing of weight; but a sum that is no number stays none
+      ll[i] += ml.y;
+      return;
+    }
     const float top = fmaxf(mm[i], ml.x), down = mm[i] == -INFINITY ? 0.f : ex2_approx(mm[i] - top), f = ex2_approx(ml.x - top);
     mm[i] = top;
     ll[i] = fmaf(ll[i], down, ml.y * f);
@@ -158,7 +161,7 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossProblem c, 
   for (int i = 0; i < kAtOnce; ++i) {
     if (i >= left || (kByUnit && i != warp)) continue;
     const CrossRow r = cross_row(c, u.b, u.rho0 + row0 + i);
-    const bool some = ll[i] > 0.f && cross_live(c, r);
+    const bool some = cross_some(c, r, ll[i]);
     const long long at = cross_out_row(c, r, u.h);
     const float norm = some ? 1.f / ll[i] : 0.f;
     __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(c.out) + at * kD + kPer * lane;

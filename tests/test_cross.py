@@ -169,6 +169,70 @@ def test_cross_one_row_for_all(handle, dtype, t):
     check(handle, Q, K[:, :, :1].expand(1, 2, 60, 128), V[:, :, :1].expand(1, 2, 60, 128))
 
 
+# one token in clusters, dealt out, of several heads; many rows alone, by few CTAs, by many; fp32 with splits and without
+NOT_FINITE = [(1, 4, 8, 2, 128, 1, 1500), (1, 4, 32, 8, 128, 1, 40000), (12, 5, 16, 16, 64, 1, 2000), (2, 1, 4, 2, 128, 300, 200), (1, 1, 8, 2, 64, 300, 9000), (1, 2, 2, 1, 128, 40, 30000),
+              (3, 2, 4, 2, 96, 2, 700), (80, 2, 4, 4, 40, 2, 90)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", NOT_FINITE)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("what", ["key", "keys", "query", "large", "value"])
+def test_cross_of_what_is_not_finite(handle, spec, dtype, what):
+    """A NaN among the logits that count, or one of +inf, is seen in the token's outputs and log-sum-exp, and nowhere else: no token of other sources,
+    heads or sequences has it, and what lies behind a length or a count has no part in it."""
+    S, beams, Hq, Hkv, d, t, m = spec
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, dtype, 18, 1.0, "dense")
+    G, n = Hq // Hkv, m - 17
+    K[:, :, n:], V[:, :, n:] = float("nan"), float("nan")
+    bad = torch.zeros(S * beams, Hq, t, dtype=torch.bool, device="cuda")      # whose logits are not numbers
+    if what == "key":
+        K[0, 0, n // 2, 3] = float("nan")
+        bad[:beams, :G] = True
+    elif what == "keys":                        # every one of them
+        K[0, -1, :n] = float("nan")
+        bad[:beams, -G:] = True
+    elif what == "query":
+        Q[-1, 1, t // 2, 5] = float("nan")
+        bad[-1, 1, t // 2] = True
+    elif what == "large":                       # logits of +inf for tokens that are above 0 there, of -inf for the others
+        K[0, 0, n - 1, 0] = float("inf")
+        bad[:beams, :G] = Q[:beams, :G, :, 0] > 0
+    else:
+        V[0, 0, n // 3, 2] = float("nan")
+    desc = rk.make_cross(S, beams, Hq, Hkv, d, m, rk.F32 if dtype == torch.float32 else rk.BF16)
+    ws = torch.full((handle.cross_workspace_bytes(desc, t),), 255, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full((S * beams, Hq, t, d), 7.0, dtype=dtype, device="cuda"), torch.full((S * beams, Hq, t), 7.0, device="cuda")
+    handle.cross_attend(desc, t, Q, K, V, out, ws, lengths=dev_i32([n] * S), lse=lse)
+    torch.cuda.synchronize()
+    assert handle.poll_status() == rk.RESTKV_OK
+    assert torch.equal(lse.isnan(), bad)
+    want = bad[..., None].expand_as(out).clone()
+    if what == "value":
+        want[:beams, :G, :, 2] = True
+    assert torch.equal(out.isnan(), want)
+    assert bool(out[~want].isfinite().all()) and bool(lse[~bad].isfinite().all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("spec", NOT_FINITE)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_cross_of_logits_that_are_all_infinite(handle, spec, dtype):
+    """Keys of -inf in one channel: tokens that are above 0 there have weights of nothing and get 0 and -inf, the others are no numbers."""
+    S, beams, Hq, Hkv, d, t, m = spec
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, dtype, 19, 1.0, "dense")
+    K[..., 1] = NEG_INF
+    desc = rk.make_cross(S, beams, Hq, Hkv, d, m, rk.F32 if dtype == torch.float32 else rk.BF16)
+    ws = torch.full((handle.cross_workspace_bytes(desc, t),), 255, dtype=torch.uint8, device="cuda")
+    out, lse = torch.full((S * beams, Hq, t, d), 7.0, dtype=dtype, device="cuda"), torch.full((S * beams, Hq, t), 7.0, device="cuda")
+    handle.cross_attend(desc, t, Q, K, V, out, ws, lse=lse)
+    torch.cuda.synchronize()
+    assert handle.poll_status() == rk.RESTKV_OK
+    empty = Q[..., 1] > 0
+    assert torch.equal(lse.isneginf(), empty) and torch.equal(lse.isnan(), ~empty)
+    assert bool((out[empty] == 0).all()) and bool(out[~empty].isnan().all())
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("spec", [(1, 4, 32, 8, 128, 1, 20000), (8, 5, 16, 16, 64, 1, 3000), (1, 1, 32, 8, 128, 600, 5000), (4, 2, 8, 2, 64, 40, 500), (2, 3, 8, 2, 64, 4, 1024)])
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
