@@ -12,6 +12,7 @@
 #include <math.h>
 
 #include "beam.cuh"
+#include "row_pieces.cuh"
 #include "sm100_ptx.cuh"
 
 namespace restkv {
@@ -126,7 +127,9 @@ __device__ __forceinline__ uint4 shifted(uint4 a, uint4 b, unsigned int off) {
 struct __align__(8) SliceStats { float top, sum; };   // of a slice: its maximum and the sum of exp(x - top); no finite logit: -inf, 0
 
 // grid: rows x slices, slices running fastest.  A slice is kBatches batches of kBatch * kBeThreads pieces of 16 bytes of a row.
-template <typename T, int kBatch, int kBatches>
+// kRagged: the rows end inside a piece, behind which is nobody's memory.  (A kernel of its own, for the others have no register to spare.  The ends of
+// rows token by token take longer: 255 rows of 50257 of 16 bits 17.2 us, 256, which end with a piece, 16.6; 512 of 131072 as before, 35.8.)
+template <typename T, int kBatch, int kBatches, bool kRagged>
 __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const BeamProblem p, int slices, SliceStats* __restrict__ stats, u64* __restrict__ lists) {
   using V = Vec<T>;
   constexpr int kPer = V::kPer, kMine = kBatch * kPer;      // logits of a thread in a batch
@@ -144,7 +147,8 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
   // A thread's tokens do not depend on where in its 16-byte pieces the row begins: equal rows have equal sums, bit for bit.
   const unsigned int off = (unsigned int)(reinterpret_cast<uintptr_t>(from) & 15u);   // bytes of the row before in the row's first piece
   const uint4* const pieces = reinterpret_cast<const uint4*>(reinterpret_cast<uintptr_t>(from) & ~(uintptr_t)15);
-  const int piece0 = slice * (kBatches * kBatch * kBeThreads) + t, in_row = (int)(((long long)p.vocab * (int)sizeof(T) + off + 15) / 16);
+  const RowPieces<kRagged> in_row(off, p.vocab, (int)sizeof(T));
+  const int piece0 = slice * (kBatches * kBatch * kBeThreads) + t;
   auto piece_of = [&](int b, int y) { return piece0 + (b * kBatch + y) * kBeThreads; };
   auto token_of = [&](int b, int e) { return piece_of(b, e / kPer) * kPer + e % kPer; };     // of the thread's e-th logit of batch b
   if (t == 0) count_s = anew_s = hits_s = 0;
@@ -153,22 +157,27 @@ __global__ void __launch_bounds__(kBeThreads, kBePerSm) beam_slice_kernel(const 
   for (int b = 0; b < kBatches; ++b) {
     V v[kBatch];
 #pragma unroll
-    for (int y = 0; y < kBatch; ++y) v[y].u = piece_of(b, y) < in_row ? __ldcs(pieces + piece_of(b, y)) : make_uint4(0u, 0u, 0u, 0u);
+    for (int y = 0; y < kBatch; ++y) v[y].u = piece_of(b, y) < in_row.loaded ? __ldcs(pieces + piece_of(b, y)) : make_uint4(0u, 0u, 0u, 0u);
     if (off) {
 #pragma unroll
       for (int y = 0; y < kBatch; ++y) {
         uint4 next = make_uint4(__shfl_down_sync(0xffffffffu, v[y].u.x, 1), __shfl_down_sync(0xffffffffu, v[y].u.y, 1), __shfl_down_sync(0xffffffffu, v[y].u.z, 1),
                                 __shfl_down_sync(0xffffffffu, v[y].u.w, 1));
-        if (lane == 31) next = piece_of(b, y) + 1 < in_row ? __ldg(pieces + piece_of(b, y) + 1) : make_uint4(0u, 0u, 0u, 0u);
+        if (lane == 31) next = piece_of(b, y) + 1 < in_row.loaded ? __ldg(pieces + piece_of(b, y) + 1) : make_uint4(0u, 0u, 0u, 0u);
         v[y].u = shifted(v[y].u, next, off);
       }
     }
+    if (!kRagged || (slice + 1) * (kBatches * kBatch * kBeThreads) > in_row.inside) {
 #pragma unroll
-    for (int y = 0; y < kBatch; ++y) {
-      if (token_of(b, y * kPer + kPer - 1) < p.vocab) continue;
+      for (int y = 0; y < kBatch; ++y) {
+        if (kRagged ? piece_of(b, y) < in_row.inside : token_of(b, y * kPer + kPer - 1) < p.vocab) continue;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i)
-        if (token_of(b, y * kPer + i) >= p.vocab) v[y].set(i, -INFINITY);
+        for (int i = 0; i < kPer; ++i) {
+          const int token = token_of(b, y * kPer + i);
+          if (token >= p.vocab) v[y].set(i, -INFINITY);
+          else if (kRagged) v[y].set(i, to_f32<T>(from[token]));
+        }
+      }
     }
     float m0 = -INFINITY, m1 = -INFINITY;                   // (a NaN is passed over)
 #pragma unroll
@@ -505,13 +514,13 @@ Slicing slicing(const BeamProblem& p, int sm_count) {
   return Slicing{4, 8};
 }
 
-template <typename T> void (*pick(const Slicing& s))(BeamProblem, int, SliceStats*, u64*) {
-  if (s.batch == 2) return beam_slice_kernel<T, 2, 1>;
+template <typename T, bool kRagged> void (*pick(const Slicing& s))(BeamProblem, int, SliceStats*, u64*) {
+  if (s.batch == 2) return beam_slice_kernel<T, 2, 1, kRagged>;
   switch (s.batches) {
-    case 1: return beam_slice_kernel<T, 4, 1>;
-    case 2: return beam_slice_kernel<T, 4, 2>;
-    case 4: return beam_slice_kernel<T, 4, 4>;
-    default: return beam_slice_kernel<T, 4, 8>;
+    case 1: return beam_slice_kernel<T, 4, 1, kRagged>;
+    case 2: return beam_slice_kernel<T, 4, 2, kRagged>;
+    case 4: return beam_slice_kernel<T, 4, 4, kRagged>;
+    default: return beam_slice_kernel<T, 4, 8, kRagged>;
   }
 }
 
@@ -522,7 +531,8 @@ cudaError_t launch_t(const BeamProblem& p, int sm_count, void* workspace, cudaSt
   const long long blocks = (long long)p.batch * p.beams * slices;
   u64* const lists = (u64*)workspace;
   SliceStats* const stats = (SliceStats*)(lists + blocks * p.n_out);
-  const cudaError_t e = launch_chained(pick<T>(s), dim3((unsigned int)blocks), kBeThreads, 0, st, p, slices, stats, lists);
+  const bool ragged = rows_end_inside_a_piece((long long)p.batch * p.beams, p.stride, p.vocab, (int)sizeof(T));
+  const cudaError_t e = launch_chained(ragged ? pick<T, true>(s) : pick<T, false>(s), dim3((unsigned int)blocks), kBeThreads, 0, st, p, slices, stats, lists);
   if (e != cudaSuccess) return e;
   return launch_chained(beam_join_kernel<T>, dim3((unsigned int)p.batch), kBeThreads, 0, st, p, slices, stats, lists);
 }

@@ -1,12 +1,14 @@
 """Decoding with beams: the best continuations of every request's hypotheses, the paged cache brought in the order of their parents, against plain
 implementations in 64 bits that are written from the header's definitions."""
 import ctypes
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2605_08840_b200 import binding as rk
+from paper_2605_08840_b200 import build as rk_build
 
 NEG_INF = float("-inf")
 
@@ -264,6 +266,62 @@ def test_select_same_bits_in_a_graph_on_another_stream_and_over_its_scores(handl
     handle.beam_select(desc, logits, scores, got[0], got[1], scores, ws)      # the scores are brought up to date in place
     torch.cuda.synchronize()
     assert torch.equal(scores, want[2]) and torch.equal(got[1], want[1])
+
+
+def test_nothing_behind_the_rows_of_logits_is_read(tmp_path):
+    """The 16-byte pieces that are loaded of rows of any length and stride: none reaches behind the last row's end; what is taken from them lies in pieces that
+    are loaded; and no more than two runs of 16 bytes of a row are left, which are loaded token by token."""
+    source = tmp_path / "pieces.cc"
+    source.write_text("""
+#include <cstdio>
+#include <initializer_list>
+#include "row_pieces.cuh"
+template <bool kRagged> void print(int off, int n, int size) {
+  const restkv::RowPieces<kRagged> r((unsigned int)off, n, size);
+  std::printf(" %d %d", r.loaded, r.inside);
+}
+int main() {
+  for (int size : {2, 4})
+    for (int n : {1, 2, 3, 4, 5, 6, 7, 8, 9, 15, 16, 17, 31, 100, 257, 50257, 131072, 0x40000000})
+      for (int pad : {0, 1, 2, 3, 5, 8})
+        for (int rows : {1, 2, 3, 4, 8, 81}) {
+          const bool ragged = restkv::rows_end_inside_a_piece(rows, (long long)n + pad, n, size);
+          for (int row = 0; row < rows; ++row) {
+            std::printf("%d %d %d %d %d %d", size, n, pad, rows, row, (int)ragged);
+            const int off = (int)(row * ((long long)n + pad) * size % 16);
+            ragged ? print<true>(off, n, size) : print<false>(off, n, size);
+            std::printf("\\n");
+          }
+        }
+}
+""")
+    program = tmp_path / "pieces"
+    subprocess.run(["g++", "-std=c++17", "-I", rk_build.CSRC, "-o", str(program), str(source)], check=True)
+    lines = subprocess.run([str(program)], check=True, capture_output=True, text=True).stdout.split("\n")[:-1]
+    assert len(lines) == 2 * 18 * 6 * (1 + 2 + 3 + 4 + 8 + 81)
+    for line in lines:
+        size, n, pad, rows, row, ragged, loaded, inside = (int(x) for x in line.split())
+        begin = row * (n + pad) * size
+        off, end, last = begin % 16, begin + n * size, ((rows - 1) * (n + pad) + n) * size
+        assert begin - off + 16 * loaded <= last, line
+        if ragged:                              # from piece `inside` on token by token
+            assert begin + 16 * max(0, inside) <= end and (inside <= 0 or off + 16 * inside <= 16 * loaded), line
+            assert -(-(end - begin) // 16) - max(0, inside) <= 2, line
+        else:
+            assert begin - off + 16 * loaded >= end, line
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("stride_pad", [0, 1, 5])
+def test_select_by_the_last_tokens_of_rows_of_any_length(handle, dtype, stride_pad):
+    """The largest logits are a row's last ones, in whatever part of 16 bytes it ends, alone in their slice or not."""
+    rng = np.random.default_rng(stride_pad)
+    for vocab in [*range(1, 20), *range(2040, 2060), *range(4090, 4106), 8193, 50257]:
+        x = rng.standard_normal((3, 2, vocab)).astype(np.float32)
+        x[:, :, -3:] = 20 + np.arange(min(3, vocab))
+        x[1, 0, -1] = np.nan
+        check_select(handle, torch.from_numpy(x).cuda().to(dtype), -rng.random((3, 2)), 5, stride_pad=stride_pad)
 
 
 def good_beams(**kw):
