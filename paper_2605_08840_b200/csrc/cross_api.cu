@@ -86,8 +86,8 @@ restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, i
   c.lengths = lengths; c.counts = counts; c.out = out; c.lse = lse;
   Call call{h, (cudaStream_t)stream};
   const bool tensor_cores = !f32 && h->tc_state && h->kernel_path != 1;
-  const bool few = cross_few_supported(c);
-  if (tensor_cores && cross_many_supported(c) && (!few || cross_many_us(c, h->sm_count) < cross_few_us(c, h->paged_clusters[0]))) {
+  const bool few = h->cross_few && cross_few_supported(c), many = h->cross_many && cross_many_supported(c);
+  if (tensor_cores && many && (!few || cross_many_us(c, h->sm_count) < cross_few_us(c, h->paged_clusters[0]))) {
     RESTKV_LAUNCH(call, RESTKV_KERNEL_NONE, launch_cross_many(h->tc_state, c, (float*)workspace, h->sm_count, h->wait_limit, h->dev_status, call.st), 2);
     return RESTKV_OK;
   }

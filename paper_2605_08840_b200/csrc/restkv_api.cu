@@ -269,9 +269,10 @@ restkv_status restkv_create(restkv_handle** out) {
   h->counter_turn[0] = h->counter_turn[1] = 0u;
   h->tc_state = nullptr;
   if (tc_init(&h->tc_state) != cudaSuccess || tc_fused_init() != cudaSuccess ||
-      decode_mma_init(h->decode_clusters) != cudaSuccess || paged_mma_init(h->paged_clusters) != cudaSuccess || paged_chunk_init() != cudaSuccess ||
-      cross_few_init() != cudaSuccess || cross_many_init() != cudaSuccess)
+      decode_mma_init(h->decode_clusters) != cudaSuccess || paged_mma_init(h->paged_clusters) != cudaSuccess || paged_chunk_init() != cudaSuccess)
     h->tc_state = nullptr;
+  h->cross_few = cross_few_init() == cudaSuccess;
+  h->cross_many = cross_many_init() == cudaSuccess;
   h->wait_limit = 2000000000ll;
   h->fused_select = true;
   h->last_evict_fused = false;

@@ -11,6 +11,7 @@ struct restkv_handle {
   unsigned int* dev_status;   // device block of kDevWords: word 0 = sticky status bits, then the sets of barrier counters
   std::atomic<unsigned int> counter_turn[2];   // launches so far that took a set: called, recorded into graphs
   void* tc_state;
+  bool cross_few, cross_many; // whether these kernels of the cross attention can run (tc_state says so for all others on the tensor cores)
   int select_clusters[4];     // clusters of 1, 2, 4, 8 CTAs of the select kernel that the device holds at once
   int decode_clusters[5];     // clusters of 1, 2, 4, 8, 16 CTAs of the decode kernel that the device holds at once
   int paged_clusters[2][5];   // the same of the paged attention kernels with one and with two CTAs per SM

@@ -1,12 +1,16 @@
 """Cross attention: decoder tokens over an encoder's rows, shared by the hypotheses of a source, against a plain implementation in 64 bits."""
 import ctypes
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2605_08840_b200 import binding as rk
+from paper_2605_08840_b200 import build as rk_build
 
 NEG_INF = float("-inf")
 
@@ -400,6 +404,64 @@ def test_cross_waits_that_run_out(handle, S, beams, Hq, Hkv, d, t, m):
             assert torch.equal(out, want) and torch.equal(lse, want_lse)
         status, out, lse = call()
         assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
+
+
+STUBS = {"cross_many": """
+cudaError_t cross_many_init() { return cudaErrorInvalidDeviceFunction; }
+bool cross_many_supported(const CrossProblem&) { return true; }
+double cross_many_us(const CrossProblem&, int) { return 0.0; }
+size_t cross_many_bytes(const CrossProblem&, int) { return 0; }
+cudaError_t launch_cross_many(void*, const CrossProblem&, float*, int, long long, unsigned int*, cudaStream_t) { return cudaErrorUnknown; }
+""", "cross_few": """
+cudaError_t cross_few_init() { return cudaErrorInvalidDeviceFunction; }
+bool cross_few_supported(const CrossProblem&) { return true; }
+double cross_few_us(const CrossProblem&, const int*) { return 0.0; }
+size_t cross_few_bytes(const CrossProblem&, int) { return 0; }
+cudaError_t launch_cross_few(void*, const CrossProblem&, float*, int, const int*, long long, unsigned int*, cudaStream_t, int*) { return cudaErrorUnknown; }
+"""}
+
+WITHOUT_IT = """
+import sys
+import torch
+from paper_2605_08840_b200 import binding as rk
+rk.LIB_PATH = sys.argv[1]
+import test_cross as here
+from helpers import DeviceRun
+from paper_2605_08840_b200.inputs import Case, make_inputs
+handle = rk.Handle()
+handle.set_kernel_path(rk.PATH_TENSOR_CORE)
+DeviceRun(handle, make_inputs(Case("here", 1, 8, 2, 128, 2000, 32, 100, 5, 0, 0.9, "bf16", 0, "normal", 1))).evict()
+assert handle.poll_status() == rk.RESTKV_OK
+refused = 0
+for path in (rk.PATH_TENSOR_CORE, rk.PATH_AUTO):
+    handle.set_kernel_path(path)
+    for t in (1, 200):
+        try:
+            here.check(handle, *here.make(2, 2, 8, 2, 128, t, 333, torch.bfloat16, 1))
+        except rk.RestKVError as e:
+            assert e.status == rk.ERR_UNSUPPORTED and path == rk.PATH_TENSOR_CORE, e
+            refused += 1
+print("refused", refused)
+"""
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("name,refused", [("cross_many", 0), ("cross_few", 1)])
+def test_a_kernel_that_cannot_run_takes_no_other_with_it(tmp_path, name, refused):
+    """A library in which one of the tensor-core kernels of the cross attention finds at the handle's creation that it cannot run: scores are made on the
+    tensor cores all the same, and cross attention by the kernels that are left."""
+    stub, obj, lib = tmp_path / "stub.cu", tmp_path / "stub.o", tmp_path / "without.so"
+    stub.write_text('#include "cross.cuh"\nnamespace restkv {\n%s\n}\n' % STUBS[name])
+    nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
+    subprocess.run([nvcc] + rk_build.COMPILE_FLAGS + ["-I", rk_build.CSRC, "-o", str(obj), str(stub)], check=True, capture_output=True)
+    objs = [os.path.join(rk_build.OBJ, os.path.basename(s)[:-3] + ".o") for s in rk_build.sources()]
+    objs = [str(obj) if os.path.basename(o) == name + ".o" else o for o in objs]
+    subprocess.run([nvcc] + rk_build.LINK_FLAGS + ["-o", str(lib)] + objs, check=True, capture_output=True)
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    env = dict(os.environ, PYTHONPATH=os.pathsep.join([root, os.path.join(root, "tests")]))
+    res = subprocess.run([sys.executable, "-c", WITHOUT_IT, str(lib)], cwd=root, env=env, capture_output=True, text=True, timeout=300)
+    assert res.returncode == 0, res.stdout + res.stderr
+    assert res.stdout.split() == ["refused", str(refused)]
 
 
 # ---- refusals -------------------------------------------------------------------------------------------------------------------------
