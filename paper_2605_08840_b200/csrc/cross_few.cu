@@ -303,7 +303,7 @@ cross_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant_
     };
 
     for (int i = 0; i < mine; ++i) {
-      ok = __all_sync(0xffffffffu, mbar_wait(&full[warp][slot], parity, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit));
+      ok = __all_sync(0xffffffffu, mbar_wait_within(&full[warp][slot], parity, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit));
       if (!ok) {
         if (lane == 0)                          // nothing may still be on its way into shared memory when the CTA returns
           for (int j = 0; j < kStages && i + j < max(mine, asked); ++j) {

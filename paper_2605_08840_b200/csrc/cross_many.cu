@@ -104,7 +104,7 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
   const uint32_t q_at = base, ring_at = base + 2 * C::kTileBytesD;
-  auto wait = [&](uint64_t* bar, int phase) { return mbar_wait(bar, (uint32_t)phase & 1u, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit); };
+  auto wait = [&](uint64_t* bar, int phase) { return mbar_wait<0>(bar, (uint32_t)phase & 1u, &abort_flag, a.dev_status, kDevTimeout, a.wait_limit); };
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
@@ -462,7 +462,10 @@ cross_many_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant
         }
         // The tiles' warpgroups take turns at the exponentials: while one is at them, the other loads and looks for the maximum.
         if (u.two && (w == 1 || u.done2 + j2 > 0)) ok = __all_sync(0xffffffffu, wait(&B.turn[w], 2 * u.done2 + j2 - (w == 0)));
-        if (!ok) break;
+        if (!ok) {
+          tmem_wait_st();                               // (O may have been scaled: nothing is on its way when the CTA gives up its tensor memory)
+          break;
+        }
         const float m_use = ref == -INFINITY ? 0.f : ref;               // only logits of -inf so far: they weigh nothing
         const f32x2 ff = f2_make(f, f), minus_m = f2_make(-m_use, -m_use);
         f32x2 sum0 = f2_make(0.f, 0.f), sum1 = sum0;

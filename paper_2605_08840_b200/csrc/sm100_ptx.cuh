@@ -57,7 +57,9 @@ __device__ __forceinline__ bool mbar_try_wait(uint64_t* bar, uint32_t parity) {
 
 // Bounded wait: gives up after `max_cycles` SM clocks or as soon as *abort_flag is set, records the
 // failure in *abort_flag and the device status word, and returns false.  Never spins for ever.  Every lane has a verdict of its own:
-// what takes the whole warp (tensor-memory loads, votes, __syncwarp) must not depend on it.
+// what takes the whole warp (tensor-memory loads, votes, __syncwarp) must not depend on it.  kFirst: the first poll that looks at the clock, of
+// 64; each 64th after it does, too.
+template <int kFirst = 63>
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                           unsigned int* dev_status, unsigned int status_bit,
                                           long long max_cycles = 2000000000ll) {
@@ -65,13 +67,37 @@ __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity, volati
   const long long t0 = clock64();
   for (int it = 0;; ++it) {
     if (mbar_try_wait(bar, parity)) return true;
-    if ((it & 63) == 63) {
+    if ((it & 63) == kFirst) {
       if (*abort_flag) return false;
       if (clock64() - t0 > max_cycles) {
         *abort_flag = 1;
         atomicOr(dev_status, status_bit);
         return false;
       }
+    }
+  }
+}
+
+// The same for any limit.  The hardware suspends a try_wait for longer than a copy takes to arrive, so that limits of less would never run out: below 20000
+// clocks the polls are of the kind that returns at once, and each looks at the clock.
+__device__ __forceinline__ bool mbar_wait_within(uint64_t* bar, uint32_t parity, volatile int* abort_flag, unsigned int* dev_status, unsigned int status_bit, long long max_cycles) {
+  if (max_cycles >= 20000) return mbar_wait(bar, parity, abort_flag, dev_status, status_bit, max_cycles);
+  const long long t0 = clock64();
+  for (;;) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_u32(bar)), "r"(parity)
+        : "memory");
+    if (ok) return true;
+    if (*abort_flag) return false;
+    if (clock64() - t0 > max_cycles) {
+      *abort_flag = 1;
+      atomicOr(dev_status, status_bit);
+      return false;
     }
   }
 }

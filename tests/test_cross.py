@@ -406,6 +406,38 @@ def test_cross_waits_that_run_out(handle, S, beams, Hq, Hkv, d, t, m):
         assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
 
 
+# in clusters, dealt out, many query rows of either head_dim
+@pytest.mark.gpu
+@pytest.mark.parametrize("S,beams,Hq,Hkv,d,t,m", [(1, 4, 32, 8, 128, 1, 8000), (1, 4, 32, 8, 128, 1, 40000), (1, 1, 8, 2, 128, 300, 3001), (3, 1, 8, 2, 64, 500, 700)])
+def test_cross_waits_run_out_indeed(handle, S, beams, Hq, Hkv, d, t, m):
+    """With K and V in none of the caches a wait limit of one SM clock does run out, in every kernel that waits: the call returns by itself and says so, and
+    the next one has its results."""
+    Q, K, V = make(S, beams, Hq, Hkv, d, t, m, torch.bfloat16, 20)
+    desc = rk.make_cross(S, beams, Hq, Hkv, d, m)
+    ws = torch.empty(handle.cross_workspace_bytes(desc, t), dtype=torch.uint8, device="cuda")
+    cold = torch.empty(1 << 28, dtype=torch.uint8, device="cuda")
+
+    def call():
+        out, lse = torch.empty(S * beams, Hq, t, d, dtype=torch.bfloat16, device="cuda"), torch.empty(S * beams, Hq, t, device="cuda")
+        cold.fill_(1)
+        handle.cross_attend(desc, t, Q, K, V, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        return handle.poll_status(), out, lse
+
+    status, want, want_lse = call()
+    assert status == rk.RESTKV_OK
+    seen = []
+    for _ in range(5):
+        try:
+            handle.set_wait_limit(1)
+            seen.append(call()[0])
+        finally:
+            handle.set_wait_limit(2_000_000_000)
+        status, out, lse = call()
+        assert status == rk.RESTKV_OK and torch.equal(out, want) and torch.equal(lse, want_lse)
+    assert set(seen) <= {rk.RESTKV_OK, rk.ERR_TIMEOUT} and rk.ERR_TIMEOUT in seen
+
+
 STUBS = {"cross_many": """
 cudaError_t cross_many_init() { return cudaErrorInvalidDeviceFunction; }
 bool cross_many_supported(const CrossProblem&) { return true; }
