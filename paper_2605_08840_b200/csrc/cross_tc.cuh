@@ -111,11 +111,8 @@ __global__ void __launch_bounds__(256) cross_merge_kernel(const CrossProblem c, 
     }
   };
   auto join = [&](int i, float2 ml, const float (&o)[kPer]) {
-    if (ml.x == -INFINITY) {               // nothing of weight; but a sum that is no number stays none
-      ll[i] += ml.y;
-      return;
-    }
-    const float top = fmaxf(mm[i], ml.x), down = mm[i] == -INFINITY ? 0.f : ex2_approx(mm[i] - top), f = ex2_approx(ml.x - top);
+    // (no branch: a sum that is no number stays none, whatever its reference)
+    const float top = fmaxf(mm[i], ml.x), down = mm[i] == -INFINITY ? 0.f : ex2_approx(mm[i] - top), f = ml.x == -INFINITY ? 0.f : ex2_approx(ml.x - top);
     mm[i] = top;
     ll[i] = fmaf(ll[i], down, ml.y * f);
 #pragma unroll
