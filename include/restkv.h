@@ -576,8 +576,8 @@ size_t restkv_cross_workspace_bytes(const restkv_cross* cross, int n_tokens);
  * inf).  Logits, softmax statistics and sums are fp32.  The same call gives the same bits.
  * head_dim: a multiple of 8, at most 256 (else RESTKV_ERR_UNSUPPORTED).  RESTKV_BF16 with head_dim 64 or 128 runs on the tensor cores (K and V
  * with no stride of 0): up to 32 query rows beams * n_tokens * group of a KV head with weights of two bf16 parts (16 bits); more with weights of
- * one bf16 (as an output has, too) where that takes less time, which goes by the sizes alone.  Everything else, and restkv_set_kernel_path(1),
- * runs in fp32 throughout, and returns RESTKV_ERR_UNSUPPORTED under restkv_set_kernel_path(2 or 3).
+ * one bf16 (as an output has, too) where that takes less time, which goes by the sizes and by whether there are lengths, never by what a tensor holds.
+ * Everything else, and restkv_set_kernel_path(1), runs in fp32 throughout, and returns RESTKV_ERR_UNSUPPORTED under restkv_set_kernel_path(2 or 3).
  */
 restkv_status restkv_cross_attend(restkv_handle* h, const restkv_cross* cross, int n_tokens, const restkv_rows* Q, const restkv_rows* K,
                                   const restkv_rows* V, const int32_t* lengths, const int32_t* counts, void* out, float* lse, void* workspace,

@@ -461,7 +461,8 @@ bool pick_few(const CrossProblem& c, long long rows, FewVariant* v) {
 
 // How a call would run: CTAs per unit of a launch in clusters, 0 for one that deals out the tiles of all units, and about how long, in us.  Fixed 6, and 12 or 16
 // (these have another kernel behind them), and the bytes at what HBM and the CTAs draw: by the tiles of query rows, 0.09, 0.07 or 0.044 TB/s each.
-// A cluster lasts as long as its own source, so that sources of different lengths speak for dealing out.  Measured, 8 KV heads of 128 with 32 query rows,
+// Fitted to the times below and their like, on 148 SMs: dealt out, as much as 118 CTAs draw, 6.1 TB/s at most; in clusters 5.5.  A cluster lasts as long as its own source, so that
+// sources of different lengths, which only the device knows, speak for dealing out: 0.8 of the rows are taken to be there.  Measured, 8 KV heads of 128 with 32 query rows,
 // 30000 rows: clusters of 4 90.0 us, of 8 50.9, dealt out 36.0; 4000 rows 18.8, 13.9, 17.4; 16 query rows over 1500 rows 8.9, 8.3, 13.0.
 struct FewWay {
   int cluster;

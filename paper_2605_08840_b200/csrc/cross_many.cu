@@ -13,6 +13,8 @@
 //   - a thread issues the logits' products, one for each tile the others, so that none waits for what it need not;
 //   - every role goes through the pieces of the CTA's run by itself;
 //   - the reference of the weights is moved (sums and O scaled) only where they would pass 2^8;
+//   - weights are rounded to one bf16, by 2^-8 of each at most, for the product with V (their sum is that of the unrounded ones): outputs are off by 2.3e-3 of
+//     their size, 1.65e-3 of which is their own rounding.  A second part, as the kernel of few query rows has, would be half as many products again;
 //   - rows behind a source's length: their logits are replaced, and what V holds there is cleared in the last 16 rows that a product reads, for a
 //     weight of 0 is to find a number.
 // The tiles of all units (source, KV head, 256 query rows) end to end are dealt out evenly; what several CTAs share is merged by a second kernel.
@@ -29,8 +31,8 @@ namespace {
 
 constexpr int kMaRows = 256;                 // query rows of a unit
 constexpr int kMaTile = 128;                 // rows of K and V of a tile
-constexpr int kMaSoftmax = 8;                // warps; then the loader's and the products'
-constexpr int kMaThreads = (kMaSoftmax + 4) * 32;   // (two warps more: registers are moved by whole warpgroups)
+constexpr int kMaSoftmax = 8;                // warps
+constexpr int kMaThreads = (kMaSoftmax + 4) * 32;   // the loader, the logits' products, and a warp for each tile's other products
 // Registers per thread: of the launch, and as the warpgroups of the softmax and the other one then share them.
 constexpr int kMaRegs = 168, kMaSoftmaxRegs = 176, kMaOtherRegs = 152;
 static_assert(2 * kMaSoftmaxRegs + kMaOtherRegs == 3 * kMaRegs, "more than the launch has would be waited for");
@@ -583,7 +585,7 @@ bool cross_many_supported(const CrossProblem& c) {
 
 // About how long a call takes: 6 us, and 2.95 (head_dim 64: 1.9) per tile of a CTA, of which it has four at least or all of a unit's, and two for ends and
 // beginnings of units.  Measured, 8 sources x 8 KV heads of 128, 128 query rows: 500 rows 17 us, 4000 rows 54 (in passes of 32 rows 66 and 145); one
-// source: 4000 rows 21, 30000 44 (20 and 100); 4 sources of 100 rows, 80 query rows 14 (20).
+// source: 4000 rows 21, 30000 46 (20 and 100); 4 sources of 100 rows, 80 query rows 12.3 (20).
 double cross_many_us(const CrossProblem& c, int sm_count) {
   const double units = (double)c.sources * c.Hkv * (double)((c.rows() + kMaRows - 1) / kMaRows), of_unit = (double)((c.n_rows + kMaTile - 1) / kMaTile);
   const double tiles = units * of_unit / sm_count + 2.0, least = of_unit < 2.0 ? 3.0 : 4.0;

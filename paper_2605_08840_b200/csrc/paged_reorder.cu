@@ -7,9 +7,10 @@
 // The tables: a thread per column takes it from all sequences of the request before it writes any (a table may be brought in order in
 // place); who takes whose pages is found anew by every block, from `beams` parents in shared memory.  Bound by the table's bytes, and for
 // one request by the launch.
-// The pages: a block per copy, layer, K or V, and head, whose rows lie in one piece; blocks of sequences that copy nothing end at once.  Bound by HBM
-// for many layers: 40 last pages of 8 layers, 92 MB, 17 us behind 4 for the tables.  (A few larger blocks per page instead: the same there, 1 us more
-// for one request.)
+// The pages: a block per copy, layer, K or V, and head, whose rows lie in one piece; blocks of sequences that copy nothing end at once.  40
+// last pages of 8 layers, 46 MB read and as many written, take 17 us behind 4 for the tables, 5.4 TB/s; no unit is at its limit (issue slots 49%, L2 29%, DRAM
+// 17%: copies of one page read it from L2 after the first, and what is written stays there), the blocks are short and begin with a load that the others wait
+// for.  (A few larger blocks per page instead: the same there, 1 us more for one request.)
 #include "paged.cuh"
 #include "sm100_ptx.cuh"
 

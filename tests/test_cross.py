@@ -181,7 +181,7 @@ NOT_FINITE = [(1, 4, 8, 2, 128, 1, 1500), (1, 4, 32, 8, 128, 1, 40000), (12, 5, 
 @pytest.mark.gpu
 @pytest.mark.parametrize("spec", NOT_FINITE)
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
-@pytest.mark.parametrize("what", ["key", "keys", "query", "large", "value"])
+@pytest.mark.parametrize("what", ["key", "keys", "query", "large", "value", "infinite"])
 def test_cross_of_what_is_not_finite(handle, spec, dtype, what):
     """A NaN among the logits that count, or one of +inf, is seen in the token's outputs and log-sum-exp, and nowhere else: no token of other sources,
     heads or sequences has it, and what lies behind a length or a count has no part in it."""
@@ -203,7 +203,7 @@ def test_cross_of_what_is_not_finite(handle, spec, dtype, what):
         K[0, 0, n - 1, 0] = float("inf")
         bad[:beams, :G] = Q[:beams, :G, :, 0] > 0
     else:
-        V[0, 0, n // 3, 2] = float("nan")
+        V[0, 0, n // 3, 2] = float("nan" if what == "value" else "inf")
     desc = rk.make_cross(S, beams, Hq, Hkv, d, m, rk.F32 if dtype == torch.float32 else rk.BF16)
     ws = torch.full((handle.cross_workspace_bytes(desc, t),), 255, dtype=torch.uint8, device="cuda")
     out, lse = torch.full((S * beams, Hq, t, d), 7.0, dtype=dtype, device="cuda"), torch.full((S * beams, Hq, t), 7.0, device="cuda")
@@ -212,9 +212,9 @@ def test_cross_of_what_is_not_finite(handle, spec, dtype, what):
     assert handle.poll_status() == rk.RESTKV_OK
     assert torch.equal(lse.isnan(), bad)
     want = bad[..., None].expand_as(out).clone()
-    if what == "value":
+    if what in ("value", "infinite"):
         want[:beams, :G, :, 2] = True
-    assert torch.equal(out.isnan(), want)
+    assert torch.equal(~out.isfinite() if what == "infinite" else out.isnan(), want)
     assert bool(out[~want].isfinite().all()) and bool(lse[~bad].isfinite().all())
 
 
