@@ -273,6 +273,7 @@ restkv_status restkv_create(restkv_handle** out) {
     h->tc_state = nullptr;
   h->cross_few = cross_few_init() == cudaSuccess;
   h->cross_many = cross_many_init() == cudaSuccess;
+  if (!h->cross_few || !h->cross_many) (void)cudaGetLastError();   // it is no later launch's error
   h->wait_limit = 2000000000ll;
   h->fused_select = true;
   h->last_evict_fused = false;
